@@ -387,6 +387,139 @@ WZ_API size_t wz_project_workspace_size(int64_t B, int C);
 WZ_API int wz_project(const wz_project_args *a);
 
 /* ------------------------------------------------------------------------ */
+/* Decoder cache: keys and values of projected tokens, and attention to them  */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * What the LLM of Eq. 2 does with condensed tokens: their keys and values are
+ * appended to a paged cache, at positions that may follow from the index map's
+ * (t, i, j), and queries attend to it.  The cache holds 8 bits a number: e4m3
+ * codes (4 exponent, 3 mantissa bits, largest 448) and, for each page and KV
+ * head, one scale for the keys and one for the values; number = code * scale.
+ * Scales are powers of two in [2^-60, 2^60], so that a code expressed in a
+ * larger scale is the code that the larger scale would have given it, but for
+ * a second rounding of subnormal codes.  Memory that no token was written to
+ * may hold anything.
+ */
+typedef struct {
+    void *k, *v;             /* [pages][heads][page_tokens][D] e4m3, 16-B aligned */
+    float *k_scale, *v_scale; /* [pages][heads]                               */
+    int64_t pages;           /* 1 .. 2^31 - 1                                */
+    int heads;               /* KV heads, at most 1024                       */
+    int page_tokens;         /* 16, 32, 64 or 128                            */
+    int D;                   /* channels of a head: 16, 32, .. 128           */
+} wz_kv_cache;
+
+/* device_status bits of the two calls below, OR-ed in by the device (the
+ * caller clears the word): a page number outside the cache, a sequence past
+ * its row of the page table, a position outside the rotation table, lengths
+ * that contradict each other.  What such an entry concerns is skipped and
+ * nothing outside the arrays is touched. */
+#define WZ_STATUS_CACHE 0x400
+
+/*
+ * Append the keys and values of T new tokens, and rotate keys and queries by
+ * position on the way.  Sequence b's tokens are rows cu[b] .. cu[b+1]-1 of q,
+ * k and v (cu[0] = 0, cu[B] = T, a sequence may have none); its i-th goes to
+ * slot p = start[b] + i, that is row p % page_tokens of page
+ * page_table[b][p / page_tokens].
+ *   Rotation (rotation != NULL): channels 0 .. rot-1 of a head are rot/2
+ *   pairs, (f, f + rot/2) or, interleaved, (2f, 2f + 1); pair f turns by the
+ *   angle whose cosine and sine are rotation[pos][f] and
+ *   rotation[pos][rot/2 + f].  pos is the token's slot (positions NULL), or
+ *   positions[x] (axes 1), or with axes 3 the axis of positions[x][3] whose
+ *   section frequency f falls in: the first section[0] frequencies take axis
+ *   0, the next section[1] axis 1, the rest axis 2.  x1' = x1 c - x2 s and
+ *   x2' = x2 c + x1 s, each product and the sum rounded to f32.
+ *   Scales: a page and head needs the smallest power of two s with |x| <= 448 s
+ *   for the call's finite numbers.  A call that writes a page's row 0 sets the
+ *   page's scale to that; otherwise the scale becomes the larger of it and the
+ *   old one, and the codes of the rows before are rounded to it anew.
+ *   Infinities saturate at +-448 s, NaN stays NaN.
+ * Pages that the call writes to belong to one sequence each.  Calls on one
+ * stream are ordered; overlapping calls must not share a page.
+ * Errors: WZ_ERR_INVALID_ARG (null, misaligned, bad size or enum),
+ * WZ_ERR_UNSUPPORTED, WZ_ERR_CUDA; nothing is launched on an argument error.
+ */
+typedef struct {
+    wz_kv_cache cache;
+    const void *k, *v;       /* [T] rows of [heads][D], dtype                */
+    const void *q;           /* [T] rows of [Hq][D], dtype; nullable         */
+    void *q_out;             /* the rotated queries (may be q itself)        */
+    int64_t k_stride, v_stride, q_stride, q_out_stride; /* elements from one */
+                             /* token's row to the next's: multiples of 8    */
+    int dtype;               /* WZ_DTYPE_BF16 or WZ_DTYPE_F32                */
+    int64_t T;
+    int B;                   /* sequences                                    */
+    int max_new;             /* the most new tokens of a sequence; 0: T      */
+    int Hq;                  /* query heads (0 with q NULL)                  */
+    const int32_t *cu;       /* [B+1]                                        */
+    const int32_t *start;    /* [B] tokens that the cache holds already      */
+    const int32_t *page_table; /* [B][max_pages]                             */
+    int max_pages;
+    const float *rotation;   /* [rotation_rows][rot], 16-B aligned; nullable */
+    int64_t rotation_rows;
+    int rot;                 /* rotated channels: 16, 32, .. D               */
+    int interleaved;
+    const int32_t *positions; /* [T][axes]; nullable with axes 1             */
+    int axes;                /* 1 or 3                                       */
+    int section[3];          /* axes 3: frequencies per axis, sum rot / 2    */
+    int32_t *device_status;  /* [1]; nullable                                */
+    wz_stream_t stream;
+} wz_kv_append_args;
+
+/* Zero `a`, with axes = 1. */
+WZ_API void wz_kv_append_args_init(wz_kv_append_args *a);
+WZ_API int wz_kv_append(const wz_kv_append_args *a);
+
+/*
+ * Attention over the cache: row (x, h) of q, head h of token x, attends to the
+ * keys and values of KV head h / (Hq / heads) of its sequence b:
+ *   out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale <q, k_t> - m),
+ *   lse = m + ln sum_t p_t,           m = max_t scale <q, k_t>
+ * over the slots t < kv_len[b] or, causal, over t <= kv_len[b] - n_b + i for
+ * the i-th of the sequence's n_b = cu[b+1] - cu[b] tokens (the new tokens are
+ * the cache's last ones).  A row that no slot is left for has out 0 and lse
+ * -infinity.  Slots that a row does not see may hold anything, NaN included.
+ * Products and sums run on the tensor cores with fp32 accumulation: the codes
+ * as they are, a query as two e4m3 numbers of a row scale of its own (bf16
+ * exactly, but for channels below 2^-14 of the row's largest), weights with 8
+ * (up to 16 rows a sequence and KV head) or 11 bits; maxima and sums in fp32.
+ * The result does not depend on how other calls or streams run.
+ * Errors: WZ_ERR_INVALID_ARG, WZ_ERR_UNSUPPORTED, WZ_ERR_WORKSPACE,
+ * WZ_ERR_NO_MEMORY, WZ_ERR_CUDA; nothing is launched on an argument error.
+ */
+typedef struct {
+    wz_kv_cache cache;
+    const void *q;           /* [T] rows of [Hq][D] bf16                     */
+    int64_t q_stride;        /* elements from row to row: a multiple of 8    */
+    void *out;               /* [T] rows of [Hq][D] bf16                     */
+    int64_t out_stride;
+    float *lse;              /* [T][Hq]; nullable                            */
+    int64_t T;
+    int B;                   /* sequences                                    */
+    int max_new;             /* the most tokens of q of a sequence; 0: T     */
+    int Hq;                  /* a multiple of the cache's heads              */
+    const int32_t *cu;       /* [B+1] rows of q of each sequence             */
+    const int32_t *kv_len;   /* [B] slots in use                             */
+    const int32_t *page_table; /* [B][max_pages]                             */
+    int max_pages;
+    int causal;
+    float scale;             /* 0: 1 / sqrt(D)                               */
+    void *workspace;         /* >= wz_attend_workspace_size() bytes, 256-B   */
+    size_t workspace_bytes;  /* aligned; NULL = cudaMallocAsync on stream    */
+    int32_t *device_status;  /* [1] WZ_STATUS_CACHE, or nonzero where a      */
+                             /* bounded wait gave up; nullable               */
+    wz_stream_t stream;
+} wz_attend_args;
+
+/* Zero `a`, with causal = 1. */
+WZ_API void wz_attend_args_init(wz_attend_args *a);
+/* Bytes that a call with T tokens of Hq heads of D channels needs at most. */
+WZ_API size_t wz_attend_workspace_size(int64_t T, int Hq, int D);
+WZ_API int wz_attend(const wz_attend_args *a);
+
+/* ------------------------------------------------------------------------ */
 /* Single-level DWT (Eq. 8, 10, 11, 14)                                      */
 /* ------------------------------------------------------------------------ */
 

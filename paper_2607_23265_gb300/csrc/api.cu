@@ -874,6 +874,101 @@ int wz_project(const wz_project_args *a) {
     return WZ_OK;
 }
 
+// What both calls ask of a cache.
+static int check_cache(const wz_kv_cache &c) {
+    if (!c.k || !c.v || !c.k_scale || !c.v_scale || !aligned(c.k, 16) || !aligned(c.v, 16) || !aligned(c.k_scale, 4) ||
+        !aligned(c.v_scale, 4))
+        return WZ_ERR_INVALID_ARG;
+    if (c.pages < 1 || c.heads < 1 || c.D < 1) return WZ_ERR_INVALID_ARG;
+    if (c.page_tokens != 16 && c.page_tokens != 32 && c.page_tokens != 64 && c.page_tokens != 128)
+        return WZ_ERR_INVALID_ARG;
+    if (c.D % 16 != 0 || c.D > 128 || c.heads > 1024 || c.pages > INT32_MAX || c.pages * c.heads > INT32_MAX)
+        return WZ_ERR_UNSUPPORTED;
+    return WZ_OK;
+}
+
+// Rows of `width` elements at p, `stride` elements apart.
+static bool rows_ok(const void *p, int64_t stride, int64_t width) {
+    return p && aligned(p, 16) && stride >= width && stride % 8 == 0;
+}
+
+void wz_kv_append_args_init(wz_kv_append_args *a) {
+    if (!a) return;
+    memset(a, 0, sizeof(*a));
+    a->axes = 1;
+}
+
+int wz_kv_append(const wz_kv_append_args *a) {
+    if (!a) return WZ_ERR_INVALID_ARG;
+    const int st = check_cache(a->cache);
+    if (st != WZ_OK) return st;
+    const wz_kv_cache &c = a->cache;
+    if (a->dtype != WZ_DTYPE_BF16 && a->dtype != WZ_DTYPE_F32) return WZ_ERR_INVALID_ARG;
+    if (a->T < 0 || a->T > INT32_MAX || a->B < 0 || a->max_new < 0 || a->max_pages < 1) return WZ_ERR_INVALID_ARG;
+    if (a->q ? a->Hq < 1 || a->Hq % c.heads != 0 : a->Hq != 0) return WZ_ERR_INVALID_ARG;
+    if (a->rotation) {
+        if (!aligned(a->rotation, 16) || a->rotation_rows < 1 || a->rotation_rows > INT32_MAX || a->rot < 16 ||
+            a->rot > c.D || a->rot % 16 != 0 || (a->axes != 1 && a->axes != 3) || !aligned(a->positions, 4))
+            return WZ_ERR_INVALID_ARG;
+        if (a->axes == 3) {
+            int64_t sum = 0;
+            for (int i = 0; i < 3; ++i) {
+                if (a->section[i] < 0) return WZ_ERR_INVALID_ARG;
+                sum += a->section[i];
+            }
+            if (!a->positions || sum != a->rot / 2) return WZ_ERR_INVALID_ARG;
+        }
+    }
+    if (a->B > (1 << 24)) return WZ_ERR_UNSUPPORTED;
+    if (a->T == 0 || a->B == 0) return a->T == 0 ? WZ_OK : WZ_ERR_INVALID_ARG;
+    const int64_t width = (int64_t)c.heads * c.D;
+    if (!rows_ok(a->k, a->k_stride, width) || !rows_ok(a->v, a->v_stride, width)) return WZ_ERR_INVALID_ARG;
+    if (a->q && (!rows_ok(a->q, a->q_stride, (int64_t)a->Hq * c.D) ||
+                 !rows_ok(a->q_out, a->q_out_stride, (int64_t)a->Hq * c.D)))
+        return WZ_ERR_INVALID_ARG;
+    if (!a->cu || !a->start || !a->page_table || !aligned(a->cu, 4) || !aligned(a->start, 4) ||
+        !aligned(a->page_table, 4) || !aligned(a->device_status, 4))
+        return WZ_ERR_INVALID_ARG;
+    Nvtx range("wz::kv_append");
+    WZ_CUDA(launch_kv_append(*a, (cudaStream_t)a->stream));
+    return WZ_OK;
+}
+
+void wz_attend_args_init(wz_attend_args *a) {
+    if (!a) return;
+    memset(a, 0, sizeof(*a));
+    a->causal = 1;
+}
+
+size_t wz_attend_workspace_size(int64_t T, int Hq, int D) {
+    if (T < 0 || T > INT32_MAX || Hq < 1 || D < 1) return 0;
+    return align_up(attend_workspace_bytes(T, Hq));
+}
+
+int wz_attend(const wz_attend_args *a) {
+    if (!a) return WZ_ERR_INVALID_ARG;
+    int st = check_cache(a->cache);
+    if (st != WZ_OK) return st;
+    const wz_kv_cache &c = a->cache;
+    if (a->T < 0 || a->T > INT32_MAX || a->B < 0 || a->max_new < 0 || a->max_pages < 1 || a->Hq < 1 ||
+        a->Hq % c.heads != 0 || !std::isfinite(a->scale))
+        return WZ_ERR_INVALID_ARG;
+    if (a->Hq > 65536 || (int64_t)a->B * c.heads > INT32_MAX || a->B > (1 << 24)) return WZ_ERR_UNSUPPORTED;
+    if (a->T == 0 || a->B == 0) return a->T == 0 ? WZ_OK : WZ_ERR_INVALID_ARG;
+    if (!rows_ok(a->q, a->q_stride, (int64_t)a->Hq * c.D) || !rows_ok(a->out, a->out_stride, (int64_t)a->Hq * c.D))
+        return WZ_ERR_INVALID_ARG;
+    if (!a->cu || !a->kv_len || !a->page_table || !aligned(a->cu, 4) || !aligned(a->kv_len, 4) ||
+        !aligned(a->page_table, 4) || !aligned(a->lse, 4) || !aligned(a->device_status, 4))
+        return WZ_ERR_INVALID_ARG;
+    const cudaStream_t s = (cudaStream_t)a->stream;
+    Scratch ws;
+    st = ws.acquire(a->workspace, a->workspace_bytes, wz_attend_workspace_size(a->T, a->Hq, c.D), s);
+    if (st != WZ_OK) return st;
+    Nvtx range("wz::attend");
+    WZ_CUDA(launch_attend(*a, ws.ptr, s));
+    return WZ_OK;
+}
+
 int wz_dwt_len(int n, int wavelet) {
     const int F = wavelet_taps(wavelet);
     if (n < 1 || F == 0) return -1;

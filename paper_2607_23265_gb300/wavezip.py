@@ -91,6 +91,35 @@ class ProjectArgs(C.Structure):
     ]
 
 
+class KvCacheStruct(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+        ("pages", C.c_int64), ("heads", C.c_int), ("page_tokens", C.c_int), ("D", C.c_int),
+    ]
+
+
+class KvAppendArgs(C.Structure):
+    _fields_ = [
+        ("cache", KvCacheStruct), ("k", C.c_void_p), ("v", C.c_void_p), ("q", C.c_void_p), ("q_out", C.c_void_p),
+        ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("q_stride", C.c_int64), ("q_out_stride", C.c_int64),
+        ("dtype", C.c_int), ("T", C.c_int64), ("B", C.c_int), ("max_new", C.c_int), ("Hq", C.c_int),
+        ("cu", C.c_void_p), ("start", C.c_void_p), ("page_table", C.c_void_p), ("max_pages", C.c_int),
+        ("rotation", C.c_void_p), ("rotation_rows", C.c_int64), ("rot", C.c_int), ("interleaved", C.c_int),
+        ("positions", C.c_void_p), ("axes", C.c_int), ("section", C.c_int * 3),
+        ("device_status", C.c_void_p), ("stream", C.c_void_p),
+    ]
+
+
+class AttendArgs(C.Structure):
+    _fields_ = [
+        ("cache", KvCacheStruct), ("q", C.c_void_p), ("q_stride", C.c_int64), ("out", C.c_void_p),
+        ("out_stride", C.c_int64), ("lse", C.c_void_p), ("T", C.c_int64), ("B", C.c_int), ("max_new", C.c_int),
+        ("Hq", C.c_int), ("cu", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p),
+        ("max_pages", C.c_int), ("causal", C.c_int), ("scale", C.c_float), ("workspace", C.c_void_p),
+        ("workspace_bytes", C.c_size_t), ("device_status", C.c_void_p), ("stream", C.c_void_p),
+    ]
+
+
 NUM_KERNELS = 6
 KERNEL_NAMES = ("query_pool", "relevance", "frame_stats", "temporal", "spatial", "condense")
 
@@ -117,6 +146,11 @@ def _load(path: str = LIB_PATH):
         "wz_relevance_static": (i, [vp, i, i, i, i, i, vp, i, vp, vp, vp, vp, vp]),
         "wz_project_workspace_size": (sz, [i64, i]),
         "wz_project": (i, [C.POINTER(ProjectArgs)]),
+        "wz_kv_append_args_init": (None, [C.POINTER(KvAppendArgs)]),
+        "wz_kv_append": (i, [C.POINTER(KvAppendArgs)]),
+        "wz_attend_args_init": (None, [C.POINTER(AttendArgs)]),
+        "wz_attend_workspace_size": (sz, [i64, i, i]),
+        "wz_attend": (i, [C.POINTER(AttendArgs)]),
         "wz_dwt_len": (i, [i, i]),
         "wz_wavelet_filters": (i, [i] + [C.POINTER(C.c_double)] * 4),
         "wz_dwt1d": (i, [vp, i, i, i, i, vp, vp, vp]),
@@ -482,6 +516,7 @@ def wz_graph_cache(capacity: int = -1) -> dict:
 
 STATUS_WAIT_TIMEOUT = 0x100
 STATUS_BOUNDS = 0x200
+STATUS_CACHE = 0x400
 
 
 @contextlib.contextmanager
@@ -544,3 +579,146 @@ def wz_project(tokens: torch.Tensor, w1: torch.Tensor, b1, w2: torch.Tensor, b2,
     a.stream = _stream(stream, tokens.device)
     _check(_lib.wz_project(C.byref(a)), "wz_project")
     return res
+
+
+# --------------------------------------------------------------------------
+# Decoder cache
+# --------------------------------------------------------------------------
+
+class KvCache:
+    """A paged cache in 8 bits: k, v [pages, heads, page_tokens, D] float8_e4m3fn and their
+    scales [pages, heads] float32, all contiguous on one CUDA device and kept by the caller."""
+
+    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "heads", "page_tokens", "D", "device", "_struct")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != torch.float8_e4m3fn or v.dtype != k.dtype:
+            raise ValueError("k and v must be float8_e4m3fn of one shape [pages, heads, page_tokens, D]")
+        for s in (k_scale, v_scale):
+            if s.dtype != torch.float32 or s.shape != k.shape[:2]:
+                raise ValueError(f"scales must be float32 of shape {tuple(k.shape[:2])}")
+        for x in (k, v, k_scale, v_scale):
+            if not x.is_cuda or x.device != k.device or not x.is_contiguous():
+                raise ValueError("a cache's tensors must be contiguous on one CUDA device")
+        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, k.device
+        self.pages, self.heads, self.page_tokens, self.D = k.shape
+        self._struct = KvCacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                                     self.pages, self.heads, self.page_tokens, self.D)
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page_tokens: int, D: int, device="cuda"):
+        codes = [torch.zeros((pages, heads, page_tokens, D), dtype=torch.uint8, device=device)
+                 .view(torch.float8_e4m3fn) for _ in range(2)]
+        scales = [torch.ones((pages, heads), dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(*codes, *scales)
+
+
+def rotation_table(positions: int, rot: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """[positions, rot] float32 for wz_kv_append: the cosines of pos * base^(-2f / rot), f < rot / 2,
+    then their sines, formed in 64 bits."""
+    f = torch.arange(rot // 2, dtype=torch.float64, device=device)
+    angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * base ** (-2 * f / rot)
+    return torch.cat([angle.cos(), angle.sin()], 1).float()
+
+
+def _rows(t: torch.Tensor, T: int, D: int, dtype, device, name: str) -> int:
+    """Checks a [T, heads, D] tensor whose heads are contiguous; elements from row to row."""
+    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be {dtype} of shape [{T}, heads, {D}] on {device}")
+    s = t.stride()
+    if s[2] != 1 or (t.shape[1] > 1 and s[1] != D):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    return s[0] if T > 1 else -(-t.shape[1] * D // 8) * 8
+
+
+def _ints(t: torch.Tensor, device, name: str, dim: int = 1) -> int:
+    if t.dtype != torch.int32 or t.device != device or t.dim() != dim or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {dim} dimension(s) on {device}")
+    return t.data_ptr()
+
+
+def _sequences(a, cu, lens, page_table, device, name: str):
+    B = lens.numel()
+    a.cu, a.page_table = _ints(cu, device, "cu"), _ints(page_table, device, "page_table", 2)
+    if cu.numel() != B + 1 or page_table.shape[0] != B:
+        raise ValueError(f"shapes: cu [B + 1], {name} [B], page_table [B, max_pages]")
+    a.B, a.max_pages = B, page_table.shape[1]
+    return _ints(lens, device, name)
+
+
+def wz_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KvCache, page_table: torch.Tensor, cu: torch.Tensor,
+                 start: torch.Tensor, *, max_new: int = 0, q: torch.Tensor | None = None,
+                 q_out: torch.Tensor | None = None, rotation: torch.Tensor | None = None,
+                 positions: torch.Tensor | None = None, sections=None, interleaved: bool = False,
+                 device_status: torch.Tensor | None = None, stream=None):
+    """wz_kv_append: k, v [T, heads, D] into the cache, keys (and queries q [T, Hq, D]) rotated on the way.
+    Rows may be slices of a wider projection.  Returns the rotated queries (q_out), or None without q."""
+    dev, T, D = cache.device, k.shape[0], cache.D
+    a = KvAppendArgs()
+    a.cache, a.T, a.max_new, a.dtype, a.axes = cache._struct, T, max_new, _dtype_code(k), 1
+    if k.shape[1] != cache.heads or v.shape != k.shape:
+        raise ValueError(f"k and v must have the cache's {cache.heads} heads")
+    a.k_stride = _rows(k, T, D, k.dtype, dev, "k")
+    a.v_stride = _rows(v, T, D, k.dtype, dev, "v")
+    a.k, a.v = k.data_ptr(), v.data_ptr()
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have the shape of q")
+        a.q_stride = _rows(q, T, D, k.dtype, dev, "q")
+        a.q_out_stride = _rows(q_out, T, D, k.dtype, dev, "q_out")
+        a.q, a.q_out, a.Hq = q.data_ptr(), q_out.data_ptr(), q.shape[1]
+    a.start = _sequences(a, cu, start, page_table, dev, "start")
+    if rotation is not None:
+        if rotation.dtype != torch.float32 or rotation.dim() != 2 or rotation.device != dev or \
+                not rotation.is_contiguous():
+            raise ValueError("rotation must be a contiguous float32 tensor [positions, rot] on the cache's device")
+        a.rotation, (a.rotation_rows, a.rot) = rotation.data_ptr(), rotation.shape
+        a.interleaved = int(interleaved)
+        if positions is not None:
+            a.positions = _ints(positions, dev, "positions", positions.dim())
+            if tuple(positions.shape) not in ((T,), (T, 3)):
+                raise ValueError("positions must be [T] or [T, 3]")
+            if positions.dim() == 2:
+                a.axes = 3
+                a.section[:] = sections
+    if device_status is not None:
+        a.device_status = _ints(device_status, dev, "device_status")
+    a.stream = _stream(stream, dev)
+    _check(_lib.wz_kv_append(C.byref(a)), "wz_kv_append")
+    return q_out if q is not None else None
+
+
+def wz_attend_workspace_size(T: int, Hq: int, D: int) -> int:
+    return int(_lib.wz_attend_workspace_size(int(T), int(Hq), int(D)))
+
+
+def wz_attend(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, cu: torch.Tensor, kv_len: torch.Tensor, *,
+              max_new: int = 0, causal: bool = True, scale: float | None = None, out: torch.Tensor | None = None,
+              lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+              device_status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """wz_attend: q [T, Hq, D] bf16 attends to the first kv_len[b] slots of its sequence.  Returns the
+    output [T, Hq, D] bf16; lse [T, Hq] float32 is written where given."""
+    dev, (T, Hq, _) = cache.device, q.shape
+    a = AttendArgs()
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+    if out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    a.cache, a.T, a.Hq, a.max_new, a.causal, a.scale = cache._struct, T, Hq, max_new, int(causal), scale or 0.0
+    a.q_stride = _rows(q, T, cache.D, torch.bfloat16, dev, "q")
+    a.out_stride = _rows(out, T, cache.D, torch.bfloat16, dev, "out")
+    a.q, a.out = q.data_ptr(), out.data_ptr()
+    if lse is not None:
+        if lse.dtype != torch.float32 or lse.shape != (T, Hq) or lse.device != dev or not lse.is_contiguous():
+            raise ValueError(f"lse must be a contiguous float32 tensor [{T}, {Hq}] on {dev}")
+        a.lse = lse.data_ptr()
+    a.kv_len = _sequences(a, cu, kv_len, page_table, dev, "kv_len")
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if device_status is not None:
+        a.device_status = _ints(device_status, dev, "device_status")
+    a.stream = _stream(stream, dev)
+    _check(_lib.wz_attend(C.byref(a)), "wz_attend")
+    return out
