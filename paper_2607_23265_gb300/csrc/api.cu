@@ -961,9 +961,9 @@ int wz_attend(const wz_attend_args *a) {
         !aligned(a->page_table, 4) || !aligned(a->lse, 4) || !aligned(a->device_status, 4))
         return WZ_ERR_INVALID_ARG;
     const cudaStream_t s = (cudaStream_t)a->stream;
+    const size_t need = a->workspace ? wz_attend_workspace_size(a->T, a->Hq, c.D) : attend_workspace_need(*a);
     Scratch ws;
-    st = ws.acquire(a->workspace, a->workspace_bytes, wz_attend_workspace_size(a->T, a->Hq, c.D), s);
-    if (st != WZ_OK) return st;
+    if (need && (st = ws.acquire(a->workspace, a->workspace_bytes, need, s)) != WZ_OK) return st;
     Nvtx range("wz::attend");
     WZ_CUDA(launch_attend(*a, ws.ptr, s));
     return WZ_OK;

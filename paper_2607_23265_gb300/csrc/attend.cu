@@ -1,0 +1,98 @@
+// Attention over the paged 8-bit cache (wz_attend): which kernel a call takes, its
+// workspace, its tensor maps.
+//   attend_few.cu   at most 16 query rows (new tokens x heads of a group): decoding
+//   attend_many.cu  more: questions and prompts
+#include <algorithm>
+#include <cstring>
+
+#include "wz_attend.cuh"
+
+namespace wz {
+
+namespace {
+
+bool encode_cache(PFN_cuTensorMapEncodeTiled_v12000 enc, CUtensorMap *m, const wz_kv_cache &c, const void *codes) {
+    cuuint64_t dims[3] = {(cuuint64_t)c.D, (cuuint64_t)c.page_tokens, (cuuint64_t)c.pages * c.heads};
+    cuuint64_t strides[2] = {(cuuint64_t)c.D, (cuuint64_t)c.D * c.page_tokens};
+    cuuint32_t box[3] = {128, (cuuint32_t)c.page_tokens, 1};   // channels past D are filled with zeros
+    cuuint32_t es[3] = {1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(codes), dims, strides, box, es,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct AttendPlan {
+    bool few;
+    int max_new;
+    int splits;              // attend_many: CTAs that share the slots of a row tile
+    size_t workspace;
+};
+
+AttendPlan attend_plan(const wz_attend_args &a, int sms) {
+    AttendPlan pl;
+    pl.max_new = (int)(a.max_new ? std::min<int64_t>(a.max_new, a.T) : a.T);
+    const int64_t rows = (int64_t)pl.max_new * (a.Hq / a.cache.heads);
+    pl.few = rows <= 16;
+    pl.splits = 1;
+    if (pl.few) {
+        pl.workspace = (size_t)kFewSlots * 16 * (128 * sizeof(float) + sizeof(float2));
+        return pl;
+    }
+    // Few row tiles leave SMs idle: their slots are cut into pieces.  A split costs a
+    // CTA's start and end and the pieces' way through memory, about kSplitTiles tiles.
+    const int64_t items = (rows + kManyRows - 1) / kManyRows * a.cache.heads * a.B;
+    const int64_t tiles = ((int64_t)a.max_pages * a.cache.page_tokens + kATile - 1) / kATile;
+    double best = 0;
+    for (int s = 1; s <= 32 && (s == 1 || (items * s <= kManySlots && s <= tiles)); ++s) {
+        const int64_t waves = (items * s + sms - 1) / sms;
+        const double cost = (double)waves * ((double)tiles / s + (s > 1 ? 2 * kSplitTiles : kSplitTiles));
+        if (s == 1 || cost < best) {
+            best = cost;
+            pl.splits = s;
+        }
+    }
+    pl.workspace = pl.splits > 1
+                       ? (size_t)(items * pl.splits) * kManyRows * (128 * sizeof(float) + sizeof(float2)) : 0;
+    return pl;
+}
+
+}  // namespace
+
+size_t attend_workspace_bytes(int64_t T, int Hq) {
+    const size_t few = (size_t)kFewSlots * 16 * (128 * sizeof(float) + sizeof(float2));
+    const size_t many = (size_t)kManySlots * kManyRows * (128 * sizeof(float) + sizeof(float2));
+    return T * Hq <= 16 ? few : std::max(few, many);
+}
+
+size_t attend_workspace_need(const wz_attend_args &a) { return attend_plan(a, std::max(sm_count(), 1)).workspace; }
+
+cudaError_t launch_attend(const wz_attend_args &a, void *workspace, cudaStream_t s) {
+    auto enc = tmap_encode_fn();
+    if (!enc) return cudaErrorNotSupported;
+    const int sms = sm_count();
+    if (sms < 1) return cudaErrorInvalidDevice;
+    AttendMaps maps;
+    memset(&maps, 0, sizeof(maps));
+    if (!encode_cache(enc, &maps.k, a.cache, a.cache.k) || !encode_cache(enc, &maps.v, a.cache, a.cache.v))
+        return cudaErrorInvalidValue;
+    const AttendPlan pl = attend_plan(a, sms);
+    AttendParams p;
+    memset(&p, 0, sizeof(p));
+    p.q = static_cast<const __nv_bfloat16 *>(a.q);
+    p.out = static_cast<__nv_bfloat16 *>(a.out);
+    p.q_stride = a.q_stride; p.out_stride = a.out_stride; p.lse = a.lse;
+    p.cu = a.cu; p.kv_len = a.kv_len; p.table = a.page_table;
+    p.k_scale = a.cache.k_scale; p.v_scale = a.cache.v_scale;
+    p.part = static_cast<float *>(workspace);
+    const size_t rows = pl.workspace / (128 * sizeof(float) + sizeof(float2));
+    p.ml = workspace ? reinterpret_cast<float2 *>(p.part + rows * 128) : nullptr;
+    p.pages = a.cache.pages;
+    p.T = (int)a.T; p.B = a.B; p.Hq = a.Hq; p.heads = a.cache.heads; p.G = a.Hq / a.cache.heads;
+    p.D = a.cache.D; p.P = a.cache.page_tokens; p.max_pages = a.max_pages; p.causal = a.causal != 0;
+    p.scale2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)p.D)) * kLog2e;
+    p.status = a.device_status;
+    return pl.few ? launch_attend_few(maps, p, pl.max_new, sms, s)
+                  : launch_attend_many(maps, p, pl.max_new, pl.splits, s);
+}
+
+}  // namespace wz

@@ -36,10 +36,6 @@ namespace {
 constexpr int kFThreads = 192;
 constexpr int kFMaxStages = 6;
 constexpr float kPScale = 256.f;   // a tile's largest weight
-// The second number of a pair stands for what the first leaves, at most 1/32 of the
-// largest (half a step at 256 is 8): it is kept 32 times as large, which keeps 8
-// bits of weights down to 2^-15 of the largest.
-constexpr float kRest = 32.f;
 
 template <int R>
 struct FewShared {
@@ -154,11 +150,6 @@ struct Walk {
     }
 };
 
-__device__ __forceinline__ void few_fail(const AttendParams &p, volatile int *abort_flag) {
-    *abort_flag = 1;
-    if (p.status) atomicOr(p.status, WZ_STATUS_WAIT_TIMEOUT);
-}
-
 }  // namespace
 
 template <int R>
@@ -255,7 +246,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                     ok = ptx::mbar_wait(&S->empty[st], ((uint32_t)(seq / Sh::kStages) & 1u) ^ 1u, kATimeoutNs);
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     if (!ok) {
-                        few_fail(p, abort_flag);
+                        attend_fail(p, abort_flag);
                         break;
                     }
                     if (lane == 0) ptx::mbar_arrive_expect_tx(&S->full[st], kATileBytes);
@@ -283,7 +274,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
             bool ok = true;
             auto wait = [&](uint64_t *bar, uint32_t parity) {
                 if (ok && !ptx::mbar_wait(bar, parity, kATimeoutNs)) {
-                    few_fail(p, abort_flag);
+                    attend_fail(p, abort_flag);
                     ok = false;
                 }
                 return ok;
@@ -341,41 +332,13 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
             const int ntok = rows / p.G;   // tokens that are answered
             // the item's queries: row c = token c / G, head c % G of the group
             for (int c = warp; c < R; c += 4) {
-                float v[4] = {0.f, 0.f, 0.f, 0.f};
                 const int i = c / p.G, g = c - i * p.G;
-                if (c < rows && 4 * lane < p.D) {
-                    const uint2 raw = *reinterpret_cast<const uint2 *>(
-                        p.q + (size_t)(x0 + i) * p.q_stride + (size_t)(h * p.G + g) * p.D + 4 * lane);
-                    v[0] = __uint_as_float(raw.x << 16);
-                    v[1] = __uint_as_float(raw.x & 0xFFFF0000u);
-                    v[2] = __uint_as_float(raw.y << 16);
-                    v[3] = __uint_as_float(raw.y & 0xFFFF0000u);
-                }
-                float m = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
-                const bool finite = __all_sync(0xFFFFFFFFu, fabsf(v[0]) + fabsf(v[1]) + fabsf(v[2]) + fabsf(v[3]) <
-                                                                INFINITY);
-                const uint32_t mb = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m));
-                // power of two that takes the largest channel to [128, 256)
-                int e = 134 - (int)(mb >> 23);
-                e = mb == 0 || !finite ? 0 : min(max(e, -126), 126);
-                const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-                const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-                uint32_t hi = 0, lo = 0;
-#pragma unroll
-                for (int j = 0; j < 4; j += 2) {
-                    const float a = v[j] * up, d = v[j + 1] * up;
-                    const uint32_t q1 = e4m3x2(a, d);
-                    const float2 f = __half22float2(half2_of_e4m3((uint16_t)q1));
-                    hi |= q1 << (8 * j);
-                    lo |= e4m3x2((a - f.x) * kRest, (d - f.y) * kRest) << (8 * j);
-                }
-                if (!finite) hi = lo = 0;
-                const int at1 = c * 128 + ((4 * lane) ^ ((c & 7) << 4));
-                const int at2 = (R + c) * 128 + ((4 * lane) ^ (((R + c) & 7) << 4));
-                *reinterpret_cast<uint32_t *>(qs + at1) = hi;
-                *reinterpret_cast<uint32_t *>(qs + at2) = lo;
+                const QueryPiece v = query_piece<true>(query_load(
+                    p, c < rows ? p.q + (size_t)(x0 + i) * p.q_stride + (size_t)(h * p.G + g) * p.D : nullptr));
+                *reinterpret_cast<uint32_t *>(qs + c * 128 + ((4 * lane) ^ ((c & 7) << 4))) = v.hi;
+                *reinterpret_cast<uint32_t *>(qs + (R + c) * 128 + ((4 * lane) ^ (((R + c) & 7) << 4))) = v.lo;
                 if (lane == 0) {
-                    S->rowf[c] = finite ? down * p.scale2 : NAN;
+                    S->rowf[c] = v.factor * p.scale2;
                     S->lim[c] = c < rows ? min(kv, attend_visible(p, i, len.x, kv)) : 0;
                 }
             }
@@ -563,7 +526,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                 }
             }
         }
-        if (!ok) few_fail(p, abort_flag);
+        if (!ok) attend_fail(p, abort_flag);
     }
     __syncthreads();
     if (warp == 5) {
@@ -667,51 +630,11 @@ cudaError_t launch_few(const AttendMaps &maps, AttendParams p, int max_new, int 
                          jargs, true);
 }
 
-bool encode_cache(PFN_cuTensorMapEncodeTiled_v12000 enc, CUtensorMap *m, const wz_kv_cache &c, const void *codes) {
-    cuuint64_t dims[3] = {(cuuint64_t)c.D, (cuuint64_t)c.page_tokens, (cuuint64_t)c.pages * c.heads};
-    cuuint64_t strides[2] = {(cuuint64_t)c.D, (cuuint64_t)c.D * c.page_tokens};
-    cuuint32_t box[3] = {128, (cuuint32_t)c.page_tokens, 1};   // channels past D are filled with zeros
-    cuuint32_t es[3] = {1, 1, 1};
-    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(codes), dims, strides, box, es,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 }  // namespace
 
-size_t attend_workspace_bytes(int64_t T, int Hq) {
-    (void)T;
-    (void)Hq;
-    return (size_t)kFewSlots * 16 * (128 * sizeof(float) + sizeof(float2));
-}
-
-cudaError_t launch_attend(const wz_attend_args &a, void *workspace, cudaStream_t s) {
-    auto enc = tmap_encode_fn();
-    if (!enc) return cudaErrorNotSupported;
-    const int sms = sm_count();
-    if (sms < 1) return cudaErrorInvalidDevice;
-    AttendMaps maps;
-    memset(&maps, 0, sizeof(maps));
-    if (!encode_cache(enc, &maps.k, a.cache, a.cache.k) || !encode_cache(enc, &maps.v, a.cache, a.cache.v))
-        return cudaErrorInvalidValue;
-    AttendParams p;
-    memset(&p, 0, sizeof(p));
-    p.q = static_cast<const __nv_bfloat16 *>(a.q);
-    p.out = static_cast<__nv_bfloat16 *>(a.out);
-    p.q_stride = a.q_stride; p.out_stride = a.out_stride; p.lse = a.lse;
-    p.cu = a.cu; p.kv_len = a.kv_len; p.table = a.page_table;
-    p.k_scale = a.cache.k_scale; p.v_scale = a.cache.v_scale;
-    p.part = static_cast<float *>(workspace);
-    p.ml = reinterpret_cast<float2 *>(p.part + (size_t)kFewSlots * 16 * 128);
-    p.pages = a.cache.pages;
-    p.T = (int)a.T; p.B = a.B; p.Hq = a.Hq; p.heads = a.cache.heads; p.G = a.Hq / a.cache.heads;
-    p.D = a.cache.D; p.P = a.cache.page_tokens; p.max_pages = a.max_pages; p.causal = a.causal != 0;
-    p.scale2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)p.D)) * kLog2e;
-    p.status = a.device_status;
-    const int max_new = a.max_new ? std::min(a.max_new, p.T) : p.T;
-    const int64_t rows = (int64_t)max_new * p.G;
-    if (rows > 16) return cudaErrorNotSupported;
-    return rows <= 8 ? launch_few<8>(maps, p, max_new, sms, s) : launch_few<16>(maps, p, max_new, sms, s);
+cudaError_t launch_attend_few(const AttendMaps &maps, const AttendParams &p, int max_new, int sms, cudaStream_t s) {
+    return (int64_t)max_new * p.G <= 8 ? launch_few<8>(maps, p, max_new, sms, s)
+                                       : launch_few<16>(maps, p, max_new, sms, s);
 }
 
 }  // namespace wz

@@ -1,0 +1,546 @@
+// Attention over the paged 8-bit cache for many query rows (wz_attend): prompts,
+// questions, anything beyond 16 rows (tokens x heads of the group) a sequence and
+// KV head.
+//
+// Bound by the tensor cores.  A CTA takes 256 rows of one sequence and KV head as two
+// row tiles of 128 that take turns: while one tile's weights are formed, the other's
+// products run.
+//   S [128 rows x 128 tokens] = (q1 + q2) K^T    e4m3: a query is two codes a channel,
+//                                                both into one accumulator
+//   O [128 rows x D]         += W V              f16: weights from tensor memory (they
+//                                                take the place of S), V from shared memory
+// The codes of K go to the tensor cores as they are.  Those of V are converted to
+// f16 once for both row tiles, because weights in f16 need no second number: 11
+// bits, and relative to the running maximum a range of 2^-32, so that the many small
+// weights of a long context are not lost beside one large one.  The scales of V's
+// pages multiply the weights, those of K's the logits, one of each for 16 tokens.
+// A thread of warps 0-7 has one row: maximum, weights and sum need no other lane.
+// The maximum that weights are relative to follows the true one only when that is
+// 2^8 above it; O is rescaled in tensor memory then.
+//   warps 0-3, 4-7  weights of row tile 0, 1
+//   warps 8-11      V to f16
+//   warp 12         TMA producer: rings of K and V tiles
+//   warp 13         TMEM allocation, MMA issuer (one thread)
+// Tensor memory: S (then W) of the tiles in columns 0 and 128, O in 256 and 384.
+// Every wait is bounded; where one gives up the kernel sets a status bit, ends its
+// copies, frees tensor memory and returns.
+#include <cstring>
+
+#include "wz_attend.cuh"
+
+namespace wz {
+
+namespace {
+
+constexpr int kMThreads = 14 * 32;
+constexpr int kMKStages = 3, kMVStages = 2;
+constexpr int kMTmem = 512;
+constexpr float kMTop = 7.f;     // a row's largest weight is about 2^7 ..
+constexpr float kMSlack = 8.f;   // .. and at most 2^15, below f16's largest
+
+struct ManyShared {
+    uint64_t k_full[kMKStages], k_empty[kMKStages], v_full[kMVStages], v_empty[kMVStages];
+    uint64_t w_full[2], w_empty[2];              // V in f16
+    uint64_t s_full[2], p_ready[2], o_full[2];   // by row tile
+    uint64_t q_ready, drain;
+    uint32_t tmem_base;
+    int abort;
+    int nan_min[128];                            // per channel: first token that some rows see and whose V is NaN
+};
+
+constexpr int kMQBytes = 4 * 128 * 128;          // row tiles x (codes, rests)
+constexpr size_t kMSmem =
+    1024 + kMQBytes + (size_t)(kMKStages + kMVStages) * kATileBytes + 2 * 2 * (size_t)kATileBytes + sizeof(ManyShared);
+static_assert(kMSmem <= 227 * 1024, "shared memory of the CTA");
+
+// What a CTA does: rows r0 .. r1-1 of (b, h), tiles t0 .. t1-1 of 128 slots.
+struct ManyItem {
+    int b, h, r0, r1, n, kv, x0;   // n: the sequence's tokens of q
+    int t0, t1;
+};
+
+__device__ __forceinline__ bool many_item(const AttendParams &p, int row_tiles, int splits, int idx, ManyItem *it) {
+    const int s = idx % splits;
+    idx /= splits;
+    it->h = idx % p.heads;
+    idx /= p.heads;
+    it->b = idx % p.B;
+    const int rt = row_tiles - 1 - idx / p.B;   // the longest rows of causal calls first
+    const int2 len = attend_lengths(p, it->b);
+    const int64_t rows = (int64_t)len.x * p.G;
+    if ((int64_t)rt * kManyRows >= rows) return false;
+    it->n = len.x;
+    it->kv = len.y;
+    it->x0 = p.cu[it->b];
+    it->r0 = rt * kManyRows;
+    it->r1 = (int)min(rows, (int64_t)it->r0 + kManyRows);
+    const int most = min(it->kv, attend_visible(p, (it->r1 - 1) / p.G, it->n, it->kv));
+    const int64_t tiles = (most + kATile - 1) / kATile;
+    it->t0 = (int)(tiles * s / splits);
+    it->t1 = (int)(tiles * (s + 1) / splits);
+    return true;
+}
+
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+}  // namespace
+
+__global__ void __launch_bounds__(kMThreads, 1)
+attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant__ AttendParams p, int row_tiles,
+                   int splits) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *qs = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t *kring = qs + kMQBytes;
+    uint8_t *vring = kring + (size_t)kMKStages * kATileBytes;
+    uint8_t *wring = vring + (size_t)kMVStages * kATileBytes;      // V in f16: two buffers of 32 KB
+    ManyShared *S = reinterpret_cast<ManyShared *>(wring + 4 * (size_t)kATileBytes);
+    volatile int *abort_flag = &S->abort;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    pdl_wait();
+    pdl_trigger();
+    ManyItem it;
+    if (!many_item(p, row_tiles, splits, (int)blockIdx.x, &it)) {
+        if (tid == 0 && !attend_lengths_sound(p, it.b)) kv_report(p.status);
+        return;
+    }
+    if (tid == 0 && !attend_lengths_sound(p, it.b)) kv_report(p.status);
+    if (tid == 0) {
+        for (int s = 0; s < kMKStages; ++s) {
+            ptx::mbar_init(&S->k_full[s], 1);
+            ptx::mbar_init(&S->k_empty[s], 1);
+        }
+        for (int s = 0; s < kMVStages; ++s) {
+            ptx::mbar_init(&S->v_full[s], 1);
+            ptx::mbar_init(&S->v_empty[s], 4);
+        }
+        for (int i = 0; i < 2; ++i) {
+            ptx::mbar_init(&S->w_full[i], 4);
+            ptx::mbar_init(&S->w_empty[i], 1);
+            ptx::mbar_init(&S->s_full[i], 1);
+            ptx::mbar_init(&S->p_ready[i], 4);
+            ptx::mbar_init(&S->o_full[i], 1);
+        }
+        ptx::mbar_init(&S->q_ready, 8);
+        ptx::mbar_init(&S->drain, 1);
+        S->abort = 0;
+        ptx::fence_barrier_init();
+        ptx::fence_proxy_async_smem();
+    }
+    if (tid < 128) S->nan_min[tid] = INT32_MAX;
+    if (warp == 13) {
+        ptx::tmem_alloc(&S->tmem_base, kMTmem);
+        ptx::tmem_relinquish();
+    }
+    if (warp == 12 && lane == 0) {
+        ptx::prefetch_tmap(&maps.k);
+        ptx::prefetch_tmap(&maps.v);
+    }
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = S->tmem_base;
+    const int n = it.t1 - it.t0;
+    const int qtiles = it.r1 - it.r0 > 128 ? 2 : 1;
+    const int minlim = max(0, min(it.kv, attend_visible(p, it.r0 / p.G, it.n, it.kv)));
+    const int maxlim = max(0, min(it.kv, attend_visible(p, (it.r1 - 1) / p.G, it.n, it.kv)));
+
+    if (warp == 12) {
+        // ---------------- TMA producer: lane = page of the tile ----------------
+        const uint64_t pol = ptx::policy_evict_last();   // other row tiles read the same slots
+        const int pages_tile = kATile / p.P, box = p.P * 128;
+        const int absent = (int)(p.pages * p.heads);     // past the cache: zeros
+        auto slab = [&](int tile) {
+            const int t = tile * kATile + lane * p.P;
+            int pg = -1;
+            if (lane < pages_tile && t < it.kv) {
+                pg = attend_page(p, it.b, t);
+                if (pg < 0) kv_report(p.status);
+            }
+            return pg < 0 ? absent : pg * p.heads + it.h;
+        };
+        int znext = n > 0 ? slab(it.t0) : absent, done = 0;
+        bool ok = true;
+        for (int i = 0; i < n; ++i) {
+            const int z = znext;
+            if (i + 1 < n) znext = slab(it.t0 + i + 1);
+            const int ks = i % kMKStages, vs = i % kMVStages;
+            ok = ptx::mbar_wait(&S->k_empty[ks], ((uint32_t)(i / kMKStages) & 1u) ^ 1u, kATimeoutNs) &&
+                 ptx::mbar_wait(&S->v_empty[vs], ((uint32_t)(i / kMVStages) & 1u) ^ 1u, kATimeoutNs);
+            ok = __all_sync(0xFFFFFFFFu, ok && !*abort_flag);
+            if (!ok) {
+                attend_fail(p, abort_flag);
+                break;
+            }
+            if (lane == 0) {
+                ptx::mbar_arrive_expect_tx(&S->k_full[ks], kATileBytes);
+                ptx::mbar_arrive_expect_tx(&S->v_full[vs], kATileBytes);
+            }
+            __syncwarp();
+            if (lane < pages_tile) {
+                ptx::tma_load_3d(kring + (size_t)ks * kATileBytes + (size_t)lane * box, &maps.k, &S->k_full[ks], 0, 0, z,
+                                 pol);
+                ptx::tma_load_3d(vring + (size_t)vs * kATileBytes + (size_t)lane * box, &maps.v, &S->v_full[vs], 0, 0, z,
+                                 pol);
+            }
+            done = i + 1;
+        }
+        for (int i = max(0, done - kMKStages); i < done; ++i) {   // the copies have landed
+            ptx::mbar_wait(&S->k_full[i % kMKStages], (uint32_t)(i / kMKStages) & 1u, kATimeoutNs);
+            if (i >= done - kMVStages)
+                ptx::mbar_wait(&S->v_full[i % kMVStages], (uint32_t)(i / kMVStages) & 1u, kATimeoutNs);
+        }
+    } else if (warp == 13) {
+        if (lane == 0) {
+            // ---------------- MMA issuer ----------------
+            const uint32_t id_s = ptx::idesc_e4m3(128, 128, false, false), id_o = ptx::idesc_f16(128, p.D, false, true);
+            const uint64_t q_desc = ptx::smem_desc(ptx::smem_u32(qs), 16, 1024, 2);
+            const uint64_t k_desc = ptx::smem_desc(ptx::smem_u32(kring), 16, 1024, 2);
+            const uint64_t w_desc = ptx::smem_desc(ptx::smem_u32(wring), kATileBytes, 1024, 2);   // 64 channels: 16 KB
+            const int ksteps = (p.D + 31) >> 5;
+            bool ok = true;
+            auto wait = [&](uint64_t *bar, uint32_t parity) {
+                if (ok && !ptx::mbar_wait(bar, parity, kATimeoutNs)) {
+                    attend_fail(p, abort_flag);
+                    ok = false;
+                }
+                return ok;
+            };
+            auto logits = [&](int q, int i) {   // S of row tile q for tile i
+                const uint64_t a = q_desc + (uint64_t)(q * 2) * (kATileBytes >> 4);
+                const uint64_t b = k_desc + (uint64_t)(i % kMKStages) * (kATileBytes >> 4);
+                for (int half = 0; half < 2; ++half)
+                    for (int j = 0; j < ksteps; ++j)
+                        ptx::mma_e4m3(tmem + (uint32_t)(q * 128), a + (uint64_t)half * (kATileBytes >> 4) + (uint64_t)(2 * j),
+                                      b + (uint64_t)(2 * j), id_s, half | j);
+                if (q == qtiles - 1) ptx::mma_commit(&S->k_empty[i % kMKStages]);
+                ptx::mma_commit(&S->s_full[q]);
+            };
+            if (n > 0 && wait(&S->q_ready, 0) && wait(&S->k_full[0], 0)) {
+                ptx::tc_fence_after();
+                for (int q = 0; q < qtiles; ++q) logits(q, 0);
+                for (int i = 0; i < n && ok; ++i) {
+                    const uint32_t par = (uint32_t)i & 1u;
+                    for (int q = 0; q < qtiles && ok; ++q) {
+                        if (!wait(&S->p_ready[q], par) || !wait(&S->w_full[i & 1], (uint32_t)(i >> 1) & 1u)) break;
+                        ptx::tc_fence_after();
+                        const uint64_t b = w_desc + (uint64_t)(i & 1) * (2 * kATileBytes >> 4);
+#pragma unroll
+                        for (int s = 0; s < kATile / 16; ++s)   // 16 tokens: 8 columns of W, two groups of 8 rows of V
+                            ptx::mma_f16_ta(tmem + (uint32_t)(256 + q * 128), tmem + (uint32_t)(q * 128 + 8 * s),
+                                            b + (uint64_t)(s * (2048 >> 4)), id_o, i | s);
+                        if (q == qtiles - 1) ptx::mma_commit(&S->w_empty[i & 1]);
+                        ptx::mma_commit(&S->o_full[q]);
+                        if (i + 1 < n) {
+                            // S takes the place of the weights: their products have to be complete
+                            if (!wait(&S->k_full[(i + 1) % kMKStages], (uint32_t)((i + 1) / kMKStages) & 1u) ||
+                                !wait(&S->o_full[q], par))
+                                break;
+                            ptx::tc_fence_after();
+                            logits(q, i + 1);
+                        }
+                    }
+                }
+            }
+            ptx::mma_commit(&S->drain);
+            ptx::mbar_wait(&S->drain, 0, kATimeoutNs);
+        }
+    } else if (warp >= 8) {
+        // ---------------- V to f16: a warp takes two rows x four pieces of 16 channels at a time ----------------
+        const int c4 = lane & 3, odd = (lane >> 2) & 1, far = (lane >> 3) & 1, pair = lane >> 4;
+        bool ok = true;
+        for (int i = 0; i < n; ++i) {
+            const int vs = i % kMVStages, base = (it.t0 + i) * kATile;
+            ok = ptx::mbar_wait(&S->v_full[vs], (uint32_t)(i / kMVStages) & 1u, kATimeoutNs) &&
+                 ptx::mbar_wait(&S->w_empty[i & 1], ((uint32_t)(i >> 1) & 1u) ^ 1u, kATimeoutNs);
+            ok = __all_sync(0xFFFFFFFFu, ok && !*abort_flag);
+            if (!ok) {
+                attend_fail(p, abort_flag);
+                break;
+            }
+            const uint8_t *src = vring + (size_t)vs * kATileBytes;
+            uint8_t *dst = wring + (size_t)(i & 1) * (2 * kATileBytes) + (size_t)far * kATileBytes;
+            const bool mixed = base + kATile > minlim;
+            for (int g = 0; g < 8; ++g) {
+                const int t = (warp - 8) * 32 + 4 * g + 2 * pair + odd, x = t & 7;
+                const uint4 v = *reinterpret_cast<const uint4 *>(src + t * 128 + (((far * 4 + c4) ^ x) << 4));
+                uint32_t in[4] = {v.x, v.y, v.z, v.w};
+                if (mixed) {
+                    // codes that a weight of 0 must not meet
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (base + t >= maxlim) in[j] = 0;
+                        const uint32_t bad = __vcmpeq4(in[j] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                        if (bad && base + t >= minlim) {
+                            for (int u = 0; u < 4; ++u)
+                                if ((bad >> (8 * u)) & 1u)
+                                    atomicMin(&S->nan_min[far * 64 + c4 * 16 + 4 * j + u], base + t);
+                            in[j] &= ~bad;
+                        }
+                    }
+                }
+                uint32_t o[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const __half2 a = half2_of_e4m3((uint16_t)(in[j] & 0xFFFFu));
+                    const __half2 b = half2_of_e4m3((uint16_t)(in[j] >> 16));
+                    o[2 * j] = *reinterpret_cast<const uint32_t *>(&a);
+                    o[2 * j + 1] = *reinterpret_cast<const uint32_t *>(&b);
+                }
+                *reinterpret_cast<uint4 *>(dst + t * 128 + (((2 * c4) ^ x) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+                *reinterpret_cast<uint4 *>(dst + t * 128 + (((2 * c4 + 1) ^ x) << 4)) =
+                    make_uint4(o[4], o[5], o[6], o[7]);
+            }
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                ptx::mbar_arrive(&S->v_empty[vs]);
+                ptx::mbar_arrive(&S->w_full[i & 1]);
+            }
+        }
+    } else {
+        // ---------------- weights ----------------
+        const int q = warp >> 2, row = tid;               // this thread's row of the CTA
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t s_at = lanes + (uint32_t)(q * 128), o_at = lanes + (uint32_t)(256 + q * 128);
+        const uint32_t flip = p.scale2 < 0.f ? 0x80808080u : 0u;   // logits' factors are positive
+        float rowf = 0.f;
+        for (int j0 = 0; j0 < 32; j0 += 8) {   // eight rows' loads in flight
+            uint2 raw[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int at = it.r0 + warp * 32 + j0 + j;
+                const int i = at / p.G, g = at - i * p.G;
+                raw[j] = query_load(p, at < it.r1 ? p.q + (size_t)(it.x0 + i) * p.q_stride +
+                                                        (size_t)(it.h * p.G + g) * p.D
+                                                  : nullptr);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int r = warp * 32 + j0 + j;
+                const QueryPiece v = query_piece<false>(raw[j]);
+                uint8_t *d = qs + (size_t)(q * 2) * kATileBytes + (r & 127) * 128 + ((4 * lane) ^ ((r & 7) << 4));
+                *reinterpret_cast<uint32_t *>(d) = v.hi ^ flip;
+                *reinterpret_cast<uint32_t *>(d + kATileBytes) = v.lo ^ flip;
+                if (lane == j0 + j) rowf = v.factor * fabsf(p.scale2);
+            }
+        }
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&S->q_ready);
+        const int tok = (it.r0 + row) / p.G;
+        const bool real = it.r0 + row < it.r1;
+        const int lim = real ? max(0, min(it.kv, attend_visible(p, tok, it.n, it.kv))) : 0;
+
+        float ref = -INFINITY, sum = 0.f;
+        bool ok = true;
+        const int steps = q < qtiles ? n : 0;
+        // lane l < 8: scales of the l-th 16 tokens of a tile, loaded one tile ahead
+        auto scales_of = [&](int tile) {
+            float2 v = make_float2(1.f, 0.f);
+            const int t = tile * kATile + 16 * lane;
+            if (lane < 8 && t < it.kv) {
+                const int pg = attend_page(p, it.b, t);
+                if (pg >= 0)
+                    v = make_float2(p.k_scale[(size_t)pg * p.heads + it.h], p.v_scale[(size_t)pg * p.heads + it.h]);
+            }
+            return v;
+        };
+        float2 next = steps > 0 ? scales_of(it.t0) : make_float2(1.f, 0.f);
+        for (int i = 0; i < steps; ++i) {
+            const float my_k = next.x, my_lv = next.y > 0.f ? log2f(next.y) : -INFINITY;
+            const float my_inv = next.y > 0.f ? 1.f / next.y : 0.f;
+            if (i + 1 < steps) next = scales_of(it.t0 + i + 1);
+            const int rel = lim - (it.t0 + i) * kATile;       // columns of the tile that this row sees
+            const bool mixed = (it.t0 + i + 1) * kATile > minlim;
+            ok = ptx::mbar_wait(&S->s_full[q], (uint32_t)i & 1u, kATimeoutNs);
+            ok = __all_sync(0xFFFFFFFFu, ok && !*abort_flag);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            float top = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t s[32];
+                ptx::tmem_ld_32x32b_x32(s_at + (uint32_t)(32 * c), s);
+                ptx::tmem_ld_wait();
+                ptx::reg_fence32(s);
+                if (mixed) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (32 * c + j >= rel) s[j] = __float_as_uint(-3e38f);
+                }
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    float m = __uint_as_float(s[16 * g]);
+#pragma unroll
+                    for (int j = 1; j < 16; ++j) m = fmaxf(m, __uint_as_float(s[16 * g + j]));
+                    const float a = __shfl_sync(0xFFFFFFFFu, my_k, 2 * c + g) * rowf;
+                    top = fmaxf(top, fmaf(m, a, __shfl_sync(0xFFFFFFFFu, my_lv, 2 * c + g)));
+                }
+            }
+            const bool rise = top > ref + kMSlack;
+            if (__any_sync(0xFFFFFFFFu, rise)) {
+                const float to = rise ? top : ref, f = rise ? ex2(ref - to) : 1.f;
+                ref = to;
+                sum *= f;
+                if (i > 0) {   // the products of the tile before are complete: S followed them
+                    for (int c = 0; c < p.D; c += 16) {
+                        uint32_t o[16];
+                        ptx::tmem_ld_32x32b_x16(o_at + (uint32_t)c, o);
+                        ptx::tmem_ld_wait();
+                        ptx::reg_fence16(o);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                        ptx::tmem_st_32x32b_x16(o_at + (uint32_t)c, o);
+                    }
+                }
+            }
+            const float base = kMTop - (ref == -INFINITY ? 0.f : ref);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t s[32];
+                ptx::tmem_ld_32x32b_x32(s_at + (uint32_t)(32 * c), s);
+                ptx::tmem_ld_wait();
+                ptx::reg_fence32(s);
+                uint32_t w[16];
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const float a = __shfl_sync(0xFFFFFFFFu, my_k, 2 * c + g) * rowf;
+                    const float off = __shfl_sync(0xFFFFFFFFu, my_lv, 2 * c + g) + base;
+                    float part = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 16; j += 2) {
+                        float u = ex2(fmaf(__uint_as_float(s[16 * g + j]), a, off));
+                        float v = ex2(fmaf(__uint_as_float(s[16 * g + j + 1]), a, off));
+                        if (mixed) {
+                            if (32 * c + 16 * g + j >= rel) u = 0.f;
+                            if (32 * c + 16 * g + j + 1 >= rel) v = 0.f;
+                        }
+                        part += u + v;
+                        w[8 * g + j / 2] = pack_half2(u, v);
+                    }
+                    sum = fmaf(part, __shfl_sync(0xFFFFFFFFu, my_inv, 2 * c + g), sum);
+                }
+                ptx::tmem_st_32x32b_x16(s_at + (uint32_t)(16 * c), w);   // columns that have been read
+            }
+            ptx::tmem_st_wait();
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&S->p_ready[q]);
+        }
+        if (ok && steps > 0) {
+            ok = ptx::mbar_wait(&S->o_full[q], (uint32_t)(steps - 1) & 1u, kATimeoutNs);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+        }
+        if (!ok) attend_fail(p, abort_flag);
+        ptx::tc_fence_after();
+        if (ok && q < qtiles) {
+            const int hq = it.h * p.G + (it.r0 + row) - tok * p.G;
+            const size_t x = (size_t)(it.x0 + tok);
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            for (int c = 0; c < p.D; c += 16) {
+                uint32_t o[16];
+                if (steps > 0) {
+                    ptx::tmem_ld_32x32b_x16(o_at + (uint32_t)c, o);
+                    ptx::tmem_ld_wait();
+                    ptx::reg_fence16(o);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[j] = 0;
+                }
+                float f[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    f[j] = lim > S->nan_min[c + j] ? NAN : sum == 0.f ? 0.f : __uint_as_float(o[j]);
+                if (!real) continue;
+                if (splits == 1) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * j] * inv, f[2 * j + 1] * inv);
+                        w[j] = *reinterpret_cast<const uint32_t *>(&v);
+                    }
+                    if (wz_in_range(p.status, x < (size_t)p.T)) {
+                        uint4 *d = reinterpret_cast<uint4 *>(p.out + x * p.out_stride + (size_t)hq * p.D + c);
+                        d[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                        d[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                    }
+                } else {
+                    float4 *d = reinterpret_cast<float4 *>(p.part + ((size_t)blockIdx.x * kManyRows + row) * 128 + c);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) d[j] = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+                }
+            }
+            if (real) {
+                if (splits > 1)
+                    p.ml[(size_t)blockIdx.x * kManyRows + row] = make_float2(ref - kMTop, sum);
+                else if (p.lse)
+                    p.lse[x * p.Hq + hq] = sum == 0.f ? -INFINITY : (ref - kMTop + log2f(sum)) * kLn2;
+            }
+        }
+    }
+    __syncthreads();
+    if (warp == 13) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, kMTmem);
+    }
+}
+
+// Adds the pieces of each row, in order; a warp per row.
+__global__ void __launch_bounds__(256)
+attend_merge_kernel(const __grid_constant__ AttendParams p, int row_tiles, int splits) {
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31;
+    const int idx = (int)blockIdx.x / (kManyRows / 8), row = (int)blockIdx.x % (kManyRows / 8) * 8 + (threadIdx.x >> 5);
+    ManyItem it;
+    if (!many_item(p, row_tiles, splits, idx * splits, &it) || it.r0 + row >= it.r1) return;
+    const size_t first = (size_t)idx * splits;
+    float m = -INFINITY;
+    for (int s = 0; s < splits; ++s) m = fmaxf(m, p.ml[(first + s) * kManyRows + row].x);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+        const size_t at = (first + s) * kManyRows + row;
+        const float2 ml = p.ml[at];
+        const float f = ex2(ml.x - ref);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (4 * lane < p.D) v = *reinterpret_cast<const float4 *>(p.part + at * 128 + 4 * lane);
+        L = fmaf(ml.y, f, L);
+        o[0] = fmaf(v.x, f, o[0]);
+        o[1] = fmaf(v.y, f, o[1]);
+        o[2] = fmaf(v.z, f, o[2]);
+        o[3] = fmaf(v.w, f, o[3]);
+    }
+    const int tok = (it.r0 + row) / p.G, hq = it.h * p.G + (it.r0 + row) - tok * p.G;
+    const size_t x = (size_t)(it.x0 + tok);
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    if (4 * lane < p.D && wz_in_range(p.status, x < (size_t)p.T)) {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(o[0] * inv, o[1] * inv);
+        const __nv_bfloat162 b = __floats2bfloat162_rn(o[2] * inv, o[3] * inv);
+        *reinterpret_cast<uint2 *>(p.out + x * p.out_stride + (size_t)hq * p.D + 4 * lane) =
+            make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+    }
+    if (lane == 0 && p.lse) p.lse[x * p.Hq + hq] = L == 0.f ? -INFINITY : (m + log2f(L)) * kLn2;
+}
+
+cudaError_t launch_attend_many(const AttendMaps &maps, const AttendParams &p, int max_new, int splits, cudaStream_t s) {
+    cudaError_t e = allow_smem((const void *)attend_many_kernel, kMSmem);
+    if (e != cudaSuccess) return e;
+    int row_tiles = (int)(((int64_t)max_new * p.G + kManyRows - 1) / kManyRows);
+    const int64_t items = (int64_t)row_tiles * p.B * p.heads;
+    if (items * splits > INT32_MAX) return cudaErrorInvalidValue;
+    void *args[] = {const_cast<AttendMaps *>(&maps), const_cast<AttendParams *>(&p), &row_tiles, &splits};
+    e = launch_kernel((const void *)attend_many_kernel, dim3((unsigned)(items * splits)), dim3(kMThreads), kMSmem, s,
+                      args, true);
+    if (e != cudaSuccess || splits == 1) return e;
+    void *margs[] = {const_cast<AttendParams *>(&p), &row_tiles, &splits};
+    return launch_kernel((const void *)attend_merge_kernel, dim3((unsigned)(items * (kManyRows / 8))), dim3(256), 0, s,
+                         margs, true);
+}
+
+}  // namespace wz

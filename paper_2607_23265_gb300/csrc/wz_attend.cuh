@@ -1,6 +1,9 @@
 // What the attention kernels over the paged 8-bit cache share (wz_attend).
 #pragma once
 
+#include <cfloat>
+#include <cmath>
+
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -13,6 +16,9 @@ namespace wz {
 constexpr int kATile = 128;                  // tokens of a tile
 constexpr int kATileBytes = kATile * 128;    // its codes of one KV head, rows of 128 bytes
 constexpr int kFewSlots = 960;               // pieces of items that several CTAs share: two a CTA
+constexpr int kManyRows = 256;               // query rows of a CTA of attend_many
+constexpr int kManySlots = 320;              // pieces of its row tiles
+constexpr double kSplitTiles = 3;            // what a CTA's start and end cost, in tiles
 constexpr uint64_t kATimeoutNs = 2000000000ull;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -71,5 +77,58 @@ __device__ __forceinline__ int attend_page(const AttendParams &p, int b, int t) 
     const int pg = p.table[(size_t)b * p.max_pages + t / p.P];
     return pg >= 0 && pg < p.pages ? pg : -1;
 }
+
+__device__ __forceinline__ void attend_fail(const AttendParams &p, volatile int *abort_flag) {
+    *abort_flag = 1;
+    if (p.status) atomicOr(p.status, WZ_STATUS_WAIT_TIMEOUT);
+}
+
+// The second e4m3 number of a pair stands for what the first leaves, at most 1/32 of
+// the largest (half a step at 256 is 8).  In an accumulator of its own it is kept
+// 32 times as large, which keeps 8 bits of weights down to 2^-15 of the largest.
+constexpr float kRest = 32.f;
+
+struct QueryPiece {
+    uint32_t hi, lo;   // e4m3 codes of four channels: number and rest
+    float factor;      // what a dot with the codes is multiplied by; NaN where the row has infinities or NaN
+};
+
+// Channels 4 lane .. 4 lane + 3 of a query row; zeros for a null row.
+__device__ __forceinline__ uint2 query_load(const AttendParams &p, const __nv_bfloat16 *row) {
+    const int lane = threadIdx.x & 31;
+    return row && 4 * lane < p.D ? *reinterpret_cast<const uint2 *>(row + 4 * lane) : make_uint2(0, 0);
+}
+
+// They as two e4m3 numbers each, times the power of two that takes the row's largest
+// channel to [128, 256); by all lanes of a warp.  SCALED: the rest times kRest.
+template <bool SCALED>
+__device__ __forceinline__ QueryPiece query_piece(uint2 raw) {
+    const float v[4] = {__uint_as_float(raw.x << 16), __uint_as_float(raw.x & 0xFFFF0000u),
+                        __uint_as_float(raw.y << 16), __uint_as_float(raw.y & 0xFFFF0000u)};
+    const float m = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+    const bool finite = __all_sync(0xFFFFFFFFu, fabsf(v[0]) <= FLT_MAX && fabsf(v[1]) <= FLT_MAX &&
+                                                    fabsf(v[2]) <= FLT_MAX && fabsf(v[3]) <= FLT_MAX);
+    const uint32_t mb = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m));
+    int e = 134 - (int)(mb >> 23);
+    e = mb == 0 || !finite ? 0 : min(max(e, -126), 126);
+    const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+    QueryPiece r;
+    r.hi = r.lo = 0;
+    r.factor = finite ? __uint_as_float((uint32_t)(127 - e) << 23) : NAN;
+    if (!finite) return r;
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+        const float a = v[j] * up, b = v[j + 1] * up;
+        const uint32_t q = e4m3x2(a, b);
+        const float2 f = __half22float2(half2_of_e4m3((uint16_t)q));
+        const float s = SCALED ? kRest : 1.f;
+        r.hi |= q << (8 * j);
+        r.lo |= e4m3x2((a - f.x) * s, (b - f.y) * s) << (8 * j);
+    }
+    return r;
+}
+
+cudaError_t launch_attend_few(const AttendMaps &maps, const AttendParams &p, int max_new, int sms, cudaStream_t s);
+cudaError_t launch_attend_many(const AttendMaps &maps, const AttendParams &p, int max_new, int splits, cudaStream_t s);
 
 }  // namespace wz

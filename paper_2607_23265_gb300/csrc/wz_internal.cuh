@@ -350,9 +350,10 @@ cudaError_t launch_spatial_ml(const Ctx &c, cudaStream_t s);
 size_t spatial_ml_smem_bytes(int H, int W, int F, int J);   // 0 if the layout does not fit
 cudaError_t launch_project_gemm(const void *A, int M, int K, const void *B, int N, const float *bias, void *out,
                                 bool gelu, int *status, bool clear_status, bool pdl, cudaStream_t s);
-// Decoder cache (kv_append.cu, attend_few.cu); arguments checked.
+// Decoder cache (kv_append.cu, attend.cu); arguments checked.
 cudaError_t launch_kv_append(const wz_kv_append_args &a, cudaStream_t s);
-size_t attend_workspace_bytes(int64_t T, int Hq);
+size_t attend_workspace_bytes(int64_t T, int Hq);        // the most that a call of these sizes needs
+size_t attend_workspace_need(const wz_attend_args &a);   // what this call needs; 0: none
 cudaError_t launch_attend(const wz_attend_args &a, void *workspace, cudaStream_t s);
 // Max-over-query relevance in one pass over the features (maxsim.cu): token
 // norms, channel-sum partials and a_{t,n}, in place of the relevance pass and

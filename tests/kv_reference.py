@@ -139,5 +139,5 @@ def attend(cache, q, table, cu, kv_len, causal, scale):
                 lse[x0 + i, hs] = (top + total.log())[:, 0]
                 sums = qi.abs() @ K[:see].abs().T * 2.0 ** -20
                 step = qi.abs().amax(-1)[:, None] * 2.0 ** -17 * K[:see].abs().sum(-1)[None]
-                off[x0 + i, hs] = (sums + step).amax(-1) * scale
+                off[x0 + i, hs] = (sums + step).amax(-1) * abs(scale)
     return out, lse, mass, off

@@ -84,6 +84,33 @@ def test_few_rows(wz, case, causal):
     run(wz, *case, causal=causal)
 
 
+MANY = [
+    # page, heads, Hq, D, new, kv_len
+    (64, 1, 1, 128, [17], [17]),
+    (16, 2, 14, 128, [3], [3]),
+    (32, 4, 28, 128, [40], [741]),
+    (64, 2, 2, 64, [128, 129, 1, 0], [128, 129, 300, 50]),
+    (128, 1, 3, 96, [257], [1000]),
+    (16, 3, 3, 80, [300, 20], [300, 700]),
+    (64, 2, 10, 48, [60, 77], [33, 0]),          # more tokens than slots: rows that see nothing
+    (32, 8, 8, 112, [140], [269]),
+    (128, 1, 40, 16, [1, 2], [500, 129]),        # many heads to a group
+    (64, 1, 5, 128, [500], [1500]),
+]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("case", MANY, ids=[str(i) for i in range(len(MANY))])
+def test_many_rows(wz, case, causal):
+    run(wz, *case, causal=causal)
+
+
+def test_rows_whose_maximum_rises(wz):
+    """Logits that grow along the sequence by far more than a rescale's slack, and a negative scale."""
+    for scale, seed in ((3.0, 1), (-3.0, 2)):
+        run(wz, 32, 1, 2, 64, [64], [900], scale=scale, seed=seed, gain=4.0)
+
+
 def test_one_long_sequence(wz):
     """Every CTA holds a piece of the same item."""
     run(wz, 128, 1, 2, 64, [1], [128 * 700 + 5])
@@ -150,14 +177,16 @@ def nan_case(wz, heads, G, n, kv, D=64, P=32):
     assert torch.equal(got.cpu()[keep], want.cpu()[keep])
 
 
+@pytest.mark.parametrize("n", [4, 9, 150])
 @pytest.mark.parametrize("kv", [40, 128, 129, 1400])
-def test_nan_that_only_some_rows_see(wz, kv):
-    nan_case(wz, 2, 2, 4, kv)
+def test_nan_that_only_some_rows_see(wz, kv, n):
+    nan_case(wz, 2, 2, min(n, kv), kv)
 
 
-def test_nan_inputs(wz):
+@pytest.mark.parametrize("n", [3, 30])
+def test_nan_inputs(wz, n):
     """A NaN or an infinity in a query makes its row NaN, one in a key the rows that see it."""
-    P, D, kv, n = 32, 64, 200, 3
+    P, D, kv = 32, 64, 200
     table, pages = tables([kv], P, 3)
     host = ref.Cache(pages, 1, P, D, seed=6)
     q = torch.randn((n, 2, D), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
@@ -167,14 +196,14 @@ def test_nan_inputs(wz):
     bad[0, 1, 7], bad[2, 0, 3] = float("nan"), float("inf")
     got = wz.wz_attend(bad.cuda(), host.on_gpu(wz), *args)
     nan = torch.isnan(got).all(-1).cpu()
-    assert nan.tolist() == [[False, True], [False, False], [True, False]]
+    assert nan[:3].tolist() == [[False, True], [False, False], [True, False]] and not bool(nan[3:].any())
     assert torch.equal(got.cpu()[~nan], want.cpu()[~nan])
     gpu = host.on_gpu(wz)
     t = kv - 2                                       # seen by the last two tokens
     gpu.k.view(torch.uint8)[table[0][t // P], 0, t % P, 1] = 0x7F
     got = wz.wz_attend(q.cuda(), gpu, *args)
-    assert torch.isnan(got).all(-1).cpu().tolist() == [[False] * 2, [True] * 2, [True] * 2]
-    assert torch.equal(got[:1], want[:1])
+    assert torch.isnan(got).all(-1).cpu().tolist() == [[False] * 2] * (n - 2) + [[True] * 2] * 2
+    assert torch.equal(got[:n - 2], want[:n - 2])
 
 
 def test_strides_workspace_and_stream(wz):
