@@ -25,8 +25,11 @@ struct AttendPlan {
     bool few;
     int max_new;
     int splits;              // attend_many: CTAs that share the slots of a row tile
+    size_t rows;             // rows of pieces in the workspace
     size_t workspace;
 };
+
+constexpr size_t kPieceRow = 128 * sizeof(float) + sizeof(float2);
 
 AttendPlan attend_plan(const wz_attend_args &a, int sms) {
     AttendPlan pl;
@@ -35,7 +38,8 @@ AttendPlan attend_plan(const wz_attend_args &a, int sms) {
     pl.few = rows <= 16;
     pl.splits = 1;
     if (pl.few) {
-        pl.workspace = (size_t)kFewSlots * 16 * (128 * sizeof(float) + sizeof(float2));
+        pl.rows = (size_t)kFewSlots * 16;
+        pl.workspace = pl.rows * kPieceRow + (size_t)a.T * a.cache.heads * sizeof(int2);
         return pl;
     }
     // Few row tiles leave SMs idle: their slots are cut into pieces.  A split costs a
@@ -51,16 +55,16 @@ AttendPlan attend_plan(const wz_attend_args &a, int sms) {
             pl.splits = s;
         }
     }
-    pl.workspace = pl.splits > 1
-                       ? (size_t)(items * pl.splits) * kManyRows * (128 * sizeof(float) + sizeof(float2)) : 0;
+    pl.rows = pl.splits > 1 ? (size_t)(items * pl.splits) * kManyRows : 0;
+    pl.workspace = pl.rows * kPieceRow;
     return pl;
 }
 
 }  // namespace
 
 size_t attend_workspace_bytes(int64_t T, int Hq) {
-    const size_t few = (size_t)kFewSlots * 16 * (128 * sizeof(float) + sizeof(float2));
-    const size_t many = (size_t)kManySlots * kManyRows * (128 * sizeof(float) + sizeof(float2));
+    const size_t few = (size_t)kFewSlots * 16 * kPieceRow + (size_t)T * Hq * sizeof(int2);
+    const size_t many = (size_t)kManySlots * kManyRows * kPieceRow;
     return T * Hq <= 16 ? few : std::max(few, many);
 }
 
@@ -84,11 +88,12 @@ cudaError_t launch_attend(const wz_attend_args &a, void *workspace, cudaStream_t
     p.cu = a.cu; p.kv_len = a.kv_len; p.table = a.page_table;
     p.k_scale = a.cache.k_scale; p.v_scale = a.cache.v_scale;
     p.part = static_cast<float *>(workspace);
-    const size_t rows = pl.workspace / (128 * sizeof(float) + sizeof(float2));
-    p.ml = workspace ? reinterpret_cast<float2 *>(p.part + rows * 128) : nullptr;
+    p.ml = reinterpret_cast<float2 *>(p.part + pl.rows * 128);
+    p.spans = reinterpret_cast<int2 *>(p.ml + pl.rows);
     p.pages = a.cache.pages;
     p.T = (int)a.T; p.B = a.B; p.Hq = a.Hq; p.heads = a.cache.heads; p.G = a.Hq / a.cache.heads;
     p.D = a.cache.D; p.P = a.cache.page_tokens; p.max_pages = a.max_pages; p.causal = a.causal != 0;
+    while (1 << p.shift < p.P) ++p.shift;
     p.scale2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)p.D)) * kLog2e;
     p.status = a.device_status;
     return pl.few ? launch_attend_few(maps, p, pl.max_new, sms, s)

@@ -35,9 +35,12 @@ struct AttendParams {
     const float *k_scale, *v_scale;
     float *part;             // unnormalised outputs of pieces [slot][rows of a slot][128]
     float2 *ml;              // their maxima (base 2) and sums
+    int2 *spans;             // by first token and KV head: first CTA and pieces of an item
     int64_t pages;
     int T, B, Hq, heads, G, D, P, max_pages, causal;
+    int shift;               // log2(P)
     int ctas;                // CTAs that share the work
+    int whole;               // attend_few: items are not cut
     float scale2;            // scale * log2(e)
     int *status;
 };
@@ -74,7 +77,7 @@ __device__ __forceinline__ int attend_visible(const AttendParams &p, int i, int 
 
 // Page of token t of sequence b, or -1.
 __device__ __forceinline__ int attend_page(const AttendParams &p, int b, int t) {
-    const int pg = p.table[(size_t)b * p.max_pages + t / p.P];
+    const int pg = p.table[(size_t)b * p.max_pages + (t >> p.shift)];
     return pg >= 0 && pg < p.pages ? pg : -1;
 }
 

@@ -23,6 +23,13 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
     return r;
 }
 
+// The same of two halves.
+__device__ __forceinline__ uint32_t e4m3x2(__half2 v) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<const uint32_t *>(&v)));
+    return r;
+}
+
 // Two e4m3 codes as two halves (exact).
 __device__ __forceinline__ __half2 half2_of_e4m3(uint16_t codes) {
     uint32_t r;

@@ -589,7 +589,7 @@ class KvCache:
     """A paged cache in 8 bits: k, v [pages, heads, page_tokens, D] float8_e4m3fn and their
     scales [pages, heads] float32, all contiguous on one CUDA device and kept by the caller."""
 
-    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "heads", "page_tokens", "D", "device", "_struct")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "heads", "page_tokens", "D", "index", "_struct")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
         if k.dim() != 4 or k.shape != v.shape or k.dtype != torch.float8_e4m3fn or v.dtype != k.dtype:
@@ -600,7 +600,7 @@ class KvCache:
         for x in (k, v, k_scale, v_scale):
             if not x.is_cuda or x.device != k.device or not x.is_contiguous():
                 raise ValueError("a cache's tensors must be contiguous on one CUDA device")
-        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, k.device
+        self.k, self.v, self.k_scale, self.v_scale, self.index = k, v, k_scale, v_scale, k.get_device()
         self.pages, self.heads, self.page_tokens, self.D = k.shape
         self._struct = KvCacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
                                      self.pages, self.heads, self.page_tokens, self.D)
@@ -621,28 +621,39 @@ def rotation_table(positions: int, rot: int, base: float = 10000.0, device="cuda
     return torch.cat([angle.cos(), angle.sin()], 1).float()
 
 
-def _rows(t: torch.Tensor, T: int, D: int, dtype, device, name: str) -> int:
-    """Checks a [T, heads, D] tensor whose heads are contiguous; elements from row to row."""
-    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name} must be {dtype} of shape [{T}, heads, {D}] on {device}")
-    s = t.stride()
-    if s[2] != 1 or (t.shape[1] > 1 and s[1] != D):
+# The two calls below serve single tokens, where the host's time is the call's: their checks read each
+# attribute of a tensor once.
+
+def _rows(t: torch.Tensor, T: int, D: int, dtype, device: int, name: str):
+    """Checks a [T, heads, D] tensor whose heads are contiguous; its heads and the elements from row to row."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != T or shape[2] != D or t.dtype is not dtype or t.get_device() != device:
+        raise ValueError(f"{name} must be {dtype} of shape [{T}, heads, {D}] on the cache's device")
+    heads = shape[1]
+    if stride[2] != 1 or (heads > 1 and stride[1] != D):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
-    return s[0] if T > 1 else -(-t.shape[1] * D // 8) * 8
+    return heads, stride[0] if T > 1 else -(-heads * D // 8) * 8
 
 
-def _ints(t: torch.Tensor, device, name: str, dim: int = 1) -> int:
-    if t.dtype != torch.int32 or t.device != device or t.dim() != dim or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor of {dim} dimension(s) on {device}")
+def _ints(t: torch.Tensor, device: int, name: str, dim: int = 1) -> int:
+    if t.dtype is not torch.int32 or t.get_device() != device or t.dim() != dim or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {dim} dimension(s) on the cache's device")
     return t.data_ptr()
 
 
-def _sequences(a, cu, lens, page_table, device, name: str):
-    B = lens.numel()
+def _current_stream(stream, device: int) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _sequences(a, cu, lens, page_table, device: int, name: str):
     a.cu, a.page_table = _ints(cu, device, "cu"), _ints(page_table, device, "page_table", 2)
-    if cu.numel() != B + 1 or page_table.shape[0] != B:
+    B = lens.shape[0]
+    rows, a.max_pages = page_table.shape
+    if cu.shape[0] != B + 1 or rows != B:
         raise ValueError(f"shapes: cu [B + 1], {name} [B], page_table [B, max_pages]")
-    a.B, a.max_pages = B, page_table.shape[1]
+    a.B = B
     return _ints(lens, device, name)
 
 
@@ -653,29 +664,29 @@ def wz_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KvCache, page_table: t
                  device_status: torch.Tensor | None = None, stream=None):
     """wz_kv_append: k, v [T, heads, D] into the cache, keys (and queries q [T, Hq, D]) rotated on the way.
     Rows may be slices of a wider projection.  Returns the rotated queries (q_out), or None without q."""
-    dev, T, D = cache.device, k.shape[0], cache.D
+    dev, T, D, dtype = cache.index, k.shape[0], cache.D, k.dtype
     a = KvAppendArgs()
     a.cache, a.T, a.max_new, a.dtype, a.axes = cache._struct, T, max_new, _dtype_code(k), 1
-    if k.shape[1] != cache.heads or v.shape != k.shape:
+    heads, a.k_stride = _rows(k, T, D, dtype, dev, "k")
+    v_heads, a.v_stride = _rows(v, T, D, dtype, dev, "v")
+    if heads != cache.heads or v_heads != heads:
         raise ValueError(f"k and v must have the cache's {cache.heads} heads")
-    a.k_stride = _rows(k, T, D, k.dtype, dev, "k")
-    a.v_stride = _rows(v, T, D, k.dtype, dev, "v")
     a.k, a.v = k.data_ptr(), v.data_ptr()
     if q is not None:
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-        if q_out.shape != q.shape:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        a.Hq, a.q_stride = _rows(q, T, D, dtype, dev, "q")
+        out_heads, a.q_out_stride = _rows(q_out, T, D, dtype, dev, "q_out")
+        if out_heads != a.Hq:
             raise ValueError("q_out must have the shape of q")
-        a.q_stride = _rows(q, T, D, k.dtype, dev, "q")
-        a.q_out_stride = _rows(q_out, T, D, k.dtype, dev, "q_out")
-        a.q, a.q_out, a.Hq = q.data_ptr(), q_out.data_ptr(), q.shape[1]
+        a.q, a.q_out = q.data_ptr(), q_out.data_ptr()
     a.start = _sequences(a, cu, start, page_table, dev, "start")
     if rotation is not None:
-        if rotation.dtype != torch.float32 or rotation.dim() != 2 or rotation.device != dev or \
+        if rotation.dtype is not torch.float32 or rotation.dim() != 2 or rotation.get_device() != dev or \
                 not rotation.is_contiguous():
             raise ValueError("rotation must be a contiguous float32 tensor [positions, rot] on the cache's device")
         a.rotation, (a.rotation_rows, a.rot) = rotation.data_ptr(), rotation.shape
-        a.interleaved = int(interleaved)
+        a.interleaved = interleaved
         if positions is not None:
             a.positions = _ints(positions, dev, "positions", positions.dim())
             if tuple(positions.shape) not in ((T,), (T, 3)):
@@ -685,8 +696,10 @@ def wz_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KvCache, page_table: t
                 a.section[:] = sections
     if device_status is not None:
         a.device_status = _ints(device_status, dev, "device_status")
-    a.stream = _stream(stream, dev)
-    _check(_lib.wz_kv_append(C.byref(a)), "wz_kv_append")
+    a.stream = _current_stream(stream, dev)
+    st = _lib.wz_kv_append(a)
+    if st != OK:
+        raise WaveZipError(st, "wz_kv_append")
     return q_out if q is not None else None
 
 
@@ -700,25 +713,27 @@ def wz_attend(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, cu: tor
               device_status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """wz_attend: q [T, Hq, D] bf16 attends to the first kv_len[b] slots of its sequence.  Returns the
     output [T, Hq, D] bf16; lse [T, Hq] float32 is written where given."""
-    dev, (T, Hq, _) = cache.device, q.shape
-    a = AttendArgs()
+    dev, T, D = cache.index, q.shape[0], cache.D
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
-    if out.shape != q.shape:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    a = AttendArgs()
+    a.cache, a.T, a.max_new, a.causal, a.scale = cache._struct, T, max_new, causal, scale or 0.0
+    Hq, a.q_stride = _rows(q, T, D, torch.bfloat16, dev, "q")
+    out_heads, a.out_stride = _rows(out, T, D, torch.bfloat16, dev, "out")
+    if out_heads != Hq:
         raise ValueError("out must have the shape of q")
-    a.cache, a.T, a.Hq, a.max_new, a.causal, a.scale = cache._struct, T, Hq, max_new, int(causal), scale or 0.0
-    a.q_stride = _rows(q, T, cache.D, torch.bfloat16, dev, "q")
-    a.out_stride = _rows(out, T, cache.D, torch.bfloat16, dev, "out")
-    a.q, a.out = q.data_ptr(), out.data_ptr()
+    a.Hq, a.q, a.out = Hq, q.data_ptr(), out.data_ptr()
     if lse is not None:
-        if lse.dtype != torch.float32 or lse.shape != (T, Hq) or lse.device != dev or not lse.is_contiguous():
-            raise ValueError(f"lse must be a contiguous float32 tensor [{T}, {Hq}] on {dev}")
+        if lse.dtype is not torch.float32 or lse.shape != (T, Hq) or lse.get_device() != dev or not lse.is_contiguous():
+            raise ValueError(f"lse must be a contiguous float32 tensor [{T}, {Hq}] on the cache's device")
         a.lse = lse.data_ptr()
     a.kv_len = _sequences(a, cu, kv_len, page_table, dev, "kv_len")
     if workspace is not None:
-        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.nbytes
     if device_status is not None:
         a.device_status = _ints(device_status, dev, "device_status")
-    a.stream = _stream(stream, dev)
-    _check(_lib.wz_attend(C.byref(a)), "wz_attend")
+    a.stream = _current_stream(stream, dev)
+    st = _lib.wz_attend(a)
+    if st != OK:
+        raise WaveZipError(st, "wz_attend")
     return out
