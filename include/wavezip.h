@@ -451,7 +451,8 @@ typedef struct {
     int dtype;               /* WZ_DTYPE_BF16 or WZ_DTYPE_F32                */
     int64_t T;
     int B;                   /* sequences                                    */
-    int max_new;             /* the most new tokens of a sequence; 0: T      */
+    int max_new;             /* the most new tokens of a sequence; 0: T;     */
+                             /* tokens past it are left out and reported     */
     int Hq;                  /* query heads (0 with q NULL)                  */
     const int32_t *cu;       /* [B+1]                                        */
     const int32_t *start;    /* [B] tokens that the cache holds already      */
@@ -499,6 +500,7 @@ typedef struct {
     int64_t T;
     int B;                   /* sequences                                    */
     int max_new;             /* the most tokens of q of a sequence; 0: T     */
+                             /* (tokens past it may be left out)             */
     int Hq;                  /* a multiple of the cache's heads              */
     const int32_t *cu;       /* [B+1] rows of q of each sequence             */
     const int32_t *kv_len;   /* [B] slots in use                             */

@@ -1,11 +1,13 @@
 // Appending keys and values to the paged 8-bit cache, rotated by position on
 // the way (wz_kv_append).
 //
-// A unit is one page of one sequence that the call writes to; a CTA takes a
-// unit and a KV head and either its keys, its values or the queries of the
-// head's group.  Keys and values of a page stay in registers between the two
-// things that are done with them: the largest magnitude, which decides the
-// page's scale, and the conversion to e4m3, so that they are read once.
+// A unit is one page of one sequence that the call writes to.  A CTA takes a unit
+// and either the keys and values of some KV heads, as many as its threads have
+// registers for, or the queries of some tokens.  Keys and values of a
+// page stay in registers between the two things that are done with them: the
+// largest magnitude, which decides the page's scale, and the conversion to e4m3, so
+// that they are read once.  Each head has warps of its own.  The cosines and sines of
+// the CTA's tokens come to shared memory once, by cp.async beside the rows' loads.
 // A thread's item is 16 channels of a token as two vectors of 8; the vectors of a
 // rotated item hold both halves of its pairs, channels 8j.. and rot/2 + 8j..
 //   half split    frequencies 8j .. 8j+7, pairs across the two vectors
@@ -13,15 +15,19 @@
 //                 the second, pairs inside each
 // Bound by HBM for prompts and by a chain of dependent loads (lengths, table,
 // rows, scale) for single tokens.
+#include <algorithm>
 #include <cfloat>
 #include <cstring>
 
 #include "wz_internal.cuh"
 #include "wz_kv.cuh"
+#include "wz_ptx.cuh"
 
 namespace wz {
 
 namespace {
+
+constexpr int kAppendThreads = 256;
 
 struct AppendParams {
     uint8_t *cache[2];        // keys, values
@@ -30,7 +36,10 @@ struct AppendParams {
     void *q_out;
     int64_t in_stride[3], q_out_stride;
     int64_t pages;
-    int heads, P, D, G, T, B;
+    int heads, P, D, Hq, T, B;
+    int shift, items;         // log2(P), 16-channel items of a head
+    uint32_t items_inv, quads_inv;   // for by(): items, groups of four frequencies
+    int most;                 // new tokens of a sequence
     int ppb;                  // units a sequence (0: found through cu)
     const int32_t *cu, *start, *table;
     int max_pages;
@@ -38,27 +47,49 @@ struct AppendParams {
     int rows, rot, interleaved;
     const int32_t *positions;
     int axes, sec0, sec01;
+    int wph;                  // warps of a KV head, a power of two
+    int groups, parts;        // CTAs of a unit: groups of KV heads, parts of the queries
+    int q_tokens;             // tokens of a part
+    int step_j, step_h, step_r;   // kAppendThreads items as items, heads and tokens
+    int rows_cta;             // most tokens of a CTA
     int *status;
 };
+
+// n / d for n * d < 2^20, inv = 2^20 / d + 1.
+__device__ __forceinline__ int by(int n, uint32_t inv) { return (int)((uint32_t)n * inv >> 20); }
 
 struct Vec16 {
     float x[16];
 };
 
-__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float *x) {
-    const uint4 w = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t r[4] = {w.x, w.y, w.z, w.w};
+// Eight numbers as they are in memory.
+template <typename Tin>
+struct Raw8;
+template <>
+struct Raw8<__nv_bfloat16> {
+    uint4 w;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { w = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void get(float *x) const {
+        const uint32_t r[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(r[i] << 16);
-        x[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u);
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(r[i] << 16);
+            x[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u);
+        }
     }
-}
-__device__ __forceinline__ void load8(const float *p, float *x) {
-    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
+};
+template <>
+struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p) {
+        a = *reinterpret_cast<const float4 *>(p);
+        b = *reinterpret_cast<const float4 *>(p + 4);
+    }
+    __device__ __forceinline__ void get(float *x) const {
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+};
 __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float *x) {
     uint32_t w[4];
 #pragma unroll
@@ -80,66 +111,82 @@ __device__ __forceinline__ int2 item_channels(const AppendParams &p, int rot, in
     return make_int2(a, j < pairs ? (rot >> 1) + 8 * j : a + 8);
 }
 
-struct Angles {
-    float c[8], s[8];
-};
-
-// Position of frequency f of token x (its slot where no positions are given).
-__device__ __forceinline__ int position(const AppendParams &p, int x, int slot, int f) {
-    int pos = slot;
-    if (p.axes == 3)
-        pos = p.positions[(size_t)x * 3 + (f >= p.sec0) + (f >= p.sec01)];
-    else if (p.positions)
-        pos = p.positions[x];
-    if (pos < 0 || pos >= p.rows) {
-        kv_report(p.status);
-        pos = 0;
+// Starts the copies of the rotation rows of tokens x0 .. x0 + count - 1 to `rows`
+// [count][rot], four frequencies at a time.  `places` [count][axes]: room for the
+// tokens' positions, read once, together.
+__device__ __forceinline__ void fetch_angles(const AppendParams &p, float *rows, int *places, int x0, int slot0,
+                                             int count) {
+    const int half = p.rot >> 1, quads = half >> 2;
+    if (p.positions) {
+        for (int at = threadIdx.x; at < count * p.axes; at += kAppendThreads)
+            places[at] = p.positions[(size_t)x0 * p.axes + at];
+        __syncthreads();
     }
-    return pos;
-}
-
-// Cosines and sines of rotated item j of token x: four frequencies at fa, four at fb.
-__device__ __forceinline__ Angles item_angles(const AppendParams &p, int x, int slot, int j) {
-    const int half = p.rot >> 1;
-    const int f[2] = {p.interleaved ? 4 * j : 8 * j, p.interleaved ? (half >> 1) + 4 * j : 8 * j + 4};
-    Angles g;
-#pragma unroll
-    for (int v = 0; v < 2; ++v) {
-        const bool split = p.axes == 3 && ((f[v] < p.sec0 && f[v] + 3 >= p.sec0) ||
-                                           (f[v] < p.sec01 && f[v] + 3 >= p.sec01));
-        if (split) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float *row = p.rotation + (size_t)position(p, x, slot, f[v] + i) * p.rot;
-                g.c[4 * v + i] = row[f[v] + i];
-                g.s[4 * v + i] = row[half + f[v] + i];
+    auto row_of = [&](int r, int f) {   // of frequency f of token x0 + r
+        int pos = slot0 + r;
+        if (p.positions) pos = p.axes == 3 ? places[3 * r + (f >= p.sec0) + (f >= p.sec01)] : places[r];
+        if (pos < 0 || pos >= p.rows) {
+            kv_report(p.status);
+            pos = 0;
+        }
+        return p.rotation + (size_t)pos * p.rot;
+    };
+    for (int at = threadIdx.x; at < count * quads; at += kAppendThreads) {
+        const int r = by(at, p.quads_inv), f = 4 * (at - r * quads);
+        float *dst = rows + r * p.rot + f;
+        if (p.axes == 3 && ((f < p.sec0 && f + 3 >= p.sec0) || (f < p.sec01 && f + 3 >= p.sec01))) {
+            for (int i = 0; i < 4; ++i) {   // sections that meet inside the four
+                const float *src = row_of(r, f + i) + f + i;
+                ptx::copy_async4(dst + i, src);
+                ptx::copy_async4(dst + half + i, src + half);
             }
         } else {
-            const float *row = p.rotation + (size_t)position(p, x, slot, f[v]) * p.rot;
-            const float4 c = *reinterpret_cast<const float4 *>(row + f[v]);
-            const float4 s = *reinterpret_cast<const float4 *>(row + half + f[v]);
-            g.c[4 * v] = c.x; g.c[4 * v + 1] = c.y; g.c[4 * v + 2] = c.z; g.c[4 * v + 3] = c.w;
-            g.s[4 * v] = s.x; g.s[4 * v + 1] = s.y; g.s[4 * v + 2] = s.z; g.s[4 * v + 3] = s.w;
+            const float *src = row_of(r, f) + f;
+            ptx::copy_async16_l1(dst, src);   // few rows serve most tokens of a grid
+            ptx::copy_async16_l1(dst + half, src + half);
         }
     }
-    return g;
 }
 
-// Turns the pair (a, b).  Products and sums are rounded one by one, so that the
-// result does not depend on how a compiler contracts them.
-__device__ __forceinline__ void turn(float &a, float &b, float c, float s) {
-    const float x = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s));
-    b = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
-    a = x;
+// Two products.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "mul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
 }
 
-__device__ __forceinline__ void turn_item(Vec16 &v, const Angles &g, bool interleaved) {
-    if (interleaved) {
+// Turns the pairs (a.x, b.x) and (a.y, b.y).  Products and sums are rounded one by one,
+// so that the result does not depend on how a compiler contracts them (packed sums of
+// packed products come out contracted).
+__device__ __forceinline__ void turn(float2 &a, float2 &b, float2 c, float2 s) {
+    const float2 ac = mul2(a, c), bs = mul2(b, s), bc = mul2(b, c), as = mul2(a, s);
+    a = {__fsub_rn(ac.x, bs.x), __fsub_rn(ac.y, bs.y)};
+    b = {__fadd_rn(bc.x, as.x), __fadd_rn(bc.y, as.y)};
+}
+
+// Turns rotated item j by a token's row of angles.
+template <bool INTER>
+__device__ __forceinline__ void turn_item(const AppendParams &p, Vec16 &v, const float *row, int j) {
+    const int half = p.rot >> 1;
+    const int f[2] = {INTER ? 4 * j : 8 * j, INTER ? (half >> 1) + 4 * j : 8 * j + 4};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) turn(v.x[2 * i], v.x[2 * i + 1], g.c[i], g.s[i]);
-    } else {
+    for (int q = 0; q < 2; ++q) {
+        const float4 c4 = *reinterpret_cast<const float4 *>(row + f[q]);
+        const float4 s4 = *reinterpret_cast<const float4 *>(row + half + f[q]);
+        const float2 c[2] = {{c4.x, c4.y}, {c4.z, c4.w}}, s[2] = {{s4.x, s4.y}, {s4.z, s4.w}};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) turn(v.x[i], v.x[8 + i], g.c[i], g.s[i]);
+        for (int i = 0; i < 2; ++i) {
+            // pairs of the first two and the last two frequencies of the four
+            float *w = v.x + (INTER ? 8 * q + 4 * i : 4 * q + 2 * i);
+            float *z = INTER ? w + 1 : w + 8;
+            const int step = INTER ? 2 : 1;
+            float2 a = {w[0], w[step]}, b = {z[0], z[step]};
+            turn(a, b, c[i], s[i]);
+            w[0] = a.x; w[step] = a.y;
+            z[0] = b.x; z[step] = b.y;
+        }
     }
 }
 
@@ -150,118 +197,204 @@ __device__ __forceinline__ uint2 pack8(const float *x, float inv) {
     return r;
 }
 
-// Keys or values of `count` tokens from row `row0` of a page on.
-template <typename Tin, int IT>
-__device__ __forceinline__ void append_page(const AppendParams &p, int role, int head, int x0, int slot0, int count,
-                                            int row0, int64_t page) {
-    __shared__ uint32_t warp_max[8];
-    const int items = p.D >> 4, rot = role == 0 ? p.rot : 0;
-    const size_t block = (size_t)page * p.heads + head;
-    uint8_t *dst = p.cache[role] + block * (size_t)(p.P * p.D);
-    const float old = p.scale[role][block];
-    Vec16 v[IT];
-    float most = 0.f;
+// Keys and values of `count` tokens from row `row0` of a page on, a head of each wph
+// warps.  `page_at` is read beside the rows.
+template <typename Tin, int IT, bool INTER>
+__device__ __forceinline__ void append_page(const AppendParams &p, float *angles, int *places, int group, int x0,
+                                            int slot0, int count, int row0, const int32_t *page_at) {
+    constexpr bool kBoth = IT * sizeof(Tin) <= 4;   // registers for the values' rows beside the keys'
+    __shared__ uint32_t warp_max[2][kAppendThreads / 32];
+    const int items = p.items;
+    const int warp = threadIdx.x >> 5, first_warp = warp & ~(p.wph - 1), width = p.wph * 32;
+    const int lane = threadIdx.x - first_warp * 32;   // among the head's threads
+    const int head = group * (kAppendThreads / 32 / p.wph) + first_warp / p.wph;
+    const bool mine = head < p.heads;
+    Raw8<Tin> a[kBoth ? 2 : 1][IT], b[kBoth ? 2 : 1][IT];
+    auto load = [&](int role, Raw8<Tin> (&lo)[IT], Raw8<Tin> (&hi)[IT]) {
 #pragma unroll
-    for (int t = 0; t < IT; ++t) {
-        const int at = (int)threadIdx.x + t * (int)blockDim.x;
-        const int r = at / items, j = at - r * items;
-        if (r < count) {
-            const int2 ch = item_channels(p, rot, j);
-            const Tin *src = static_cast<const Tin *>(p.in[role]) + (size_t)(x0 + r) * p.in_stride[role] +
-                             (size_t)head * p.D;
-            load8(src + ch.x, v[t].x);
-            load8(src + ch.y, v[t].x + 8);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[t].x[i] = 0.f;
+        for (int t = 0; t < IT; ++t) {
+            const int at = lane + t * width, r = by(at, p.items_inv), j = at - r * items;
+            if (mine && r < count) {
+                const int2 ch = item_channels(p, role ? 0 : p.rot, j);
+                const Tin *src = static_cast<const Tin *>(p.in[role]) + (size_t)(x0 + r) * p.in_stride[role] +
+                                 (size_t)head * p.D;
+                lo[t].load(src + ch.x);
+                hi[t].load(src + ch.y);
+            }
         }
+    };
+    const int page = page_at ? *page_at : -1;
+    load(0, a[0], b[0]);
+    if (kBoth) load(1, a[kBoth], b[kBoth]);
+    if (p.rot) fetch_angles(p, angles, places, x0, slot0, count);
+    if (page < 0 || page >= p.pages) {
+        ptx::copy_async_wait_all();
+        kv_report(p.status);
+        return;
     }
-#pragma unroll
-    for (int t = 0; t < IT; ++t) {
-        const int at = (int)threadIdx.x + t * (int)blockDim.x;
-        const int r = at / items, j = at - r * items;
-        if (r < count && j < rot >> 4) turn_item(v[t], item_angles(p, x0 + r, slot0 + r, j), p.interleaved);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float m = fabsf(v[t].x[i]);
-            most = fmaxf(most, m <= FLT_MAX ? m : 0.f);   // infinities and NaN have no say in the scale
-        }
-    }
-    const uint32_t wm = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));   // order of bits = order of floats >= 0
-    if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = wm;
+    const size_t block = (size_t)page * p.heads + (mine ? head : 0);
+    const float olds[2] = {p.scale[0][block], p.scale[1][block]};
+    ptx::copy_async_wait_all();
     __syncthreads();
-    uint32_t all = 0;
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) all = max(all, warp_max[w]);
-    const float fit = fitting_scale(all);
-    const float now = row0 == 0 ? fit : fmaxf(old, fit);
-    const float inv = 1.f / now;
 #pragma unroll
-    for (int t = 0; t < IT; ++t) {
-        const int at = (int)threadIdx.x + t * (int)blockDim.x;
-        const int r = at / items, j = at - r * items;
-        if (r < count && wz_in_range(p.status, row0 + r < p.P)) {
-            const int2 ch = item_channels(p, rot, j);
-            uint8_t *d = dst + (row0 + r) * p.D;
-            *reinterpret_cast<uint2 *>(d + ch.x) = pack8(v[t].x, inv);
-            *reinterpret_cast<uint2 *>(d + ch.y) = pack8(v[t].x + 8, inv);
+    for (int role = 0; role < 2; ++role) {
+        const int rot = role ? 0 : p.rot;
+        uint8_t *dst = p.cache[role] + block * (size_t)(p.P * p.D);
+        const float old = olds[role];
+        if (!kBoth && role) load(1, a[0], b[0]);
+        Vec16 v[IT];
+        float most = 0.f;
+#pragma unroll
+        for (int t = 0; t < IT; ++t) {
+            const int at = lane + t * width, r = by(at, p.items_inv), j = at - r * items;
+            if (mine && r < count) {
+                a[kBoth ? role : 0][t].get(v[t].x);
+                b[kBoth ? role : 0][t].get(v[t].x + 8);
+                if (j < rot >> 4) turn_item<INTER>(p, v[t], angles + r * p.rot, j);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(v[t].x[i]));   // leaves out NaN
+            }
         }
-    }
-    if (row0 > 0 && now > old) {
-        // the rows that the page holds already, in the larger scale
-        const float ratio = old * inv;
-        for (int at = threadIdx.x; at < row0 * items; at += blockDim.x) {
-            uint4 *d = reinterpret_cast<uint4 *>(dst + 16 * at);
-            const uint4 w = *d;
-            *d = make_uint4(e4m3x4_times(w.x, ratio), e4m3x4_times(w.y, ratio), e4m3x4_times(w.z, ratio),
-                            e4m3x4_times(w.w, ratio));
+        if (most > FLT_MAX) {   // and infinities have no say in the scale either
+            most = 0.f;
+#pragma unroll
+            for (int t = 0; t < IT; ++t) {
+                const int at = lane + t * width;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float m = fabsf(v[t].x[i]);
+                    if (mine && by(at, p.items_inv) < count && m <= FLT_MAX) most = fmaxf(most, m);
+                }
+            }
         }
+        const uint32_t wm = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));   // >= 0: bits order as floats
+        if ((threadIdx.x & 31) == 0) warp_max[role][warp] = wm;
+        __syncthreads();
+        uint32_t all = 0;
+        for (int w = 0; w < p.wph; ++w) all = max(all, warp_max[role][first_warp + w]);
+        const float fit = fitting_scale(all);
+        const float now = row0 == 0 ? fit : fmaxf(old, fit);
+        const float inv = 1.f / now;
+#pragma unroll
+        for (int t = 0; t < IT; ++t) {
+            const int at = lane + t * width, r = by(at, p.items_inv), j = at - r * items;
+            if (mine && r < count && wz_in_range(p.status, row0 + r < p.P)) {
+                const int2 ch = item_channels(p, rot, j);
+                uint8_t *d = dst + (row0 + r) * p.D;
+                *reinterpret_cast<uint2 *>(d + ch.x) = pack8(v[t].x, inv);
+                *reinterpret_cast<uint2 *>(d + ch.y) = pack8(v[t].x + 8, inv);
+            }
+        }
+        if (mine && row0 > 0 && now > old) {
+            // the rows that the page holds already, in the larger scale
+            const float ratio = old * inv;
+            for (int at = lane; at < row0 * items; at += width) {
+                uint4 *d = reinterpret_cast<uint4 *>(dst + 16 * at);
+                const uint4 w = *d;
+                *d = make_uint4(e4m3x4_times(w.x, ratio), e4m3x4_times(w.y, ratio), e4m3x4_times(w.z, ratio),
+                                e4m3x4_times(w.w, ratio));
+            }
+        }
+        if (mine && lane == 0) p.scale[role][block] = now;   // every thread has read `old` before the barriers
     }
-    if (threadIdx.x == 0) p.scale[role][block] = now;   // every thread has read `old` before the barrier
 }
 
-// The group's queries of `count` tokens.
-template <typename Tin>
-__device__ __forceinline__ void rotate_queries(const AppendParams &p, int head, int x0, int slot0, int count) {
-    const int items = p.D >> 4;
-    for (int at = threadIdx.x; at < count * items; at += blockDim.x) {
-        const int r = at / items, j = at - r * items;
-        const int2 ch = item_channels(p, p.rot, j);
-        const size_t x = (size_t)(x0 + r);
-        const Tin *src = static_cast<const Tin *>(p.in[2]) + x * p.in_stride[2] + (size_t)head * p.G * p.D;
-        Tin *dst = static_cast<Tin *>(p.q_out) + x * p.q_out_stride + (size_t)head * p.G * p.D;
-        const bool turned = j < p.rot >> 4;
-        Angles g{};
-        if (turned) g = item_angles(p, x0 + r, slot0 + r, j);
-#pragma unroll 4
-        for (int h = 0; h < p.G; ++h) {
-            Vec16 v;
-            load8(src + (size_t)h * p.D + ch.x, v.x);
-            load8(src + (size_t)h * p.D + ch.y, v.x + 8);
-            if (turned) turn_item(v, g, p.interleaved);
-            if (wz_in_range(p.status, x < (size_t)p.T)) {
-                store8(dst + (size_t)h * p.D + ch.x, v.x);
-                store8(dst + (size_t)h * p.D + ch.y, v.x + 8);
+// Queries of tokens part * q_tokens .. of `count`: their heads lie side by side, so
+// that the CTA reads and writes whole rows from one end to the other.
+template <typename Tin, bool INTER>
+__device__ __forceinline__ void rotate_queries(const AppendParams &p, float *angles, int *places, int part, int x0,
+                                               int slot0, int count) {
+    constexpr int kAhead = 2;   // items of a thread whose loads are in flight
+    const int items = p.items, heads = p.Hq;
+    const int r0 = part * p.q_tokens, tokens = min(count - r0, p.q_tokens);
+    if (tokens <= 0) return;
+    x0 += r0;
+    struct Place {
+        int r, h, j;
+    };
+    auto advance = [&](Place &w) {   // kAppendThreads items on
+        w.j += p.step_j;
+        w.h += p.step_h;
+        w.r += p.step_r;
+        if (w.j >= items) {
+            w.j -= items;
+            ++w.h;
+        }
+        if (w.h >= heads) {
+            w.h -= heads;
+            ++w.r;
+        }
+    };
+    Place at{0, by(threadIdx.x, p.items_inv), 0};
+    at.j = (int)threadIdx.x - at.h * items;
+    if (at.h >= heads) {
+        at.r = at.h / heads;
+        at.h -= at.r * heads;
+    }
+    Place ahead = at;
+    Raw8<Tin> a[kAhead], b[kAhead];
+    auto load = [&](int u) {
+        if (ahead.r < tokens) {
+            const int2 ch = item_channels(p, p.rot, ahead.j);
+            const Tin *src = static_cast<const Tin *>(p.in[2]) + (size_t)(x0 + ahead.r) * p.in_stride[2] +
+                             (size_t)ahead.h * p.D;
+            a[u].load(src + ch.x);
+            b[u].load(src + ch.y);
+        }
+        advance(ahead);
+    };
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) load(u);
+    if (p.rot) {
+        fetch_angles(p, angles, places, x0, slot0 + r0, tokens);
+        ptx::copy_async_wait_all();
+        __syncthreads();
+    }
+    while (at.r < tokens) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (at.r < tokens) {
+                Vec16 v;
+                a[u].get(v.x);
+                b[u].get(v.x + 8);
+                if (at.j < p.rot >> 4) turn_item<INTER>(p, v, angles + at.r * p.rot, at.j);
+                const int2 ch = item_channels(p, p.rot, at.j);
+                const size_t x = (size_t)(x0 + at.r);
+                Tin *dst = static_cast<Tin *>(p.q_out) + x * p.q_out_stride + (size_t)at.h * p.D;
+                if (wz_in_range(p.status, x < (size_t)p.T)) {
+                    store8(dst + ch.x, v.x);
+                    store8(dst + ch.y, v.x + 8);
+                }
             }
+            load(u);
+            advance(at);
         }
     }
 }
 
 }  // namespace
 
-// Grid: units x KV heads x (keys, values, queries).
-template <typename Tin, int IT>
-__global__ void __launch_bounds__(256) kv_append_kernel(AppendParams p) {
+// Grid: units x (groups of KV heads, parts of the queries), a
+// unit's CTAs one after the other: they share its tokens' rows, and so DRAM pages.  18,699
+// tokens of 28 + 4 + 4 heads x 128, at positions (t, i, j): 63 us (5.2 TB/s); 87 with
+// the units of one head after those of another.
+template <typename Tin, int IT, bool INTER>
+__global__ void __launch_bounds__(kAppendThreads, IT == 4 ? 2 : sizeof(Tin) == 2 ? 4 : 3)
+kv_append_kernel(const __grid_constant__ AppendParams p) {
+    extern __shared__ __align__(16) float angles[];      // [rows][rot], then the positions
+    int *places = reinterpret_cast<int *>(angles + p.rows_cta * p.rot);
     pdl_wait();
     pdl_trigger();
+    const int share = p.groups + p.parts, unit = (int)blockIdx.x / share, place = (int)blockIdx.x - unit * share;
     int b, j;
     if (p.ppb) {
-        b = (int)blockIdx.x / p.ppb;
-        j = (int)blockIdx.x - b * p.ppb;
+        b = unit / p.ppb;
+        j = unit - b * p.ppb;
     } else {
         // sequence b has units cu[b] / P + 2b up to the next one's: enough for its
         // pages wherever it starts, and known without the sequences before it
-        b = kv_find_sequence(p.cu, p.B, (int)blockIdx.x, p.P);
-        j = (int)blockIdx.x - (p.cu[b] / p.P + 2 * b);
+        b = kv_find_sequence(p.cu, p.B, unit, p.shift);
+        j = unit - ((p.cu[b] >> p.shift) + 2 * b);
     }
     const int x0 = p.cu[b], x1 = p.cu[b + 1], s0 = p.start[b];
     if (x0 < 0 || x1 < x0 || x1 > p.T || s0 < 0 || s0 > INT32_MAX - (x1 - x0) - p.P || j < 0) {
@@ -269,29 +402,25 @@ __global__ void __launch_bounds__(256) kv_append_kernel(AppendParams p) {
         return;
     }
     if (x0 == x1) return;
-    const int col = s0 / p.P + j, end = s0 + (x1 - x0);
-    if (j == 0 && p.ppb && (end + p.P - 1) / p.P - col > p.ppb) kv_report(p.status);   // more tokens than max_new
-    const int64_t first = (int64_t)col * p.P;
+    if (j == 0 && x1 - x0 > p.most) kv_report(p.status);   // more tokens than max_new: the rest is left out
+    const int col = (s0 >> p.shift) + j, end = s0 + min(x1 - x0, p.most);
+    const int64_t first = (int64_t)col << p.shift;
     const int lo = first > s0 ? (int)min(first, (int64_t)end) : s0;
     const int hi = (int)min(first + p.P, (int64_t)end);
     if (lo >= hi) return;
-    const int x = x0 + (lo - s0), role = blockIdx.z, head = blockIdx.y;
-    if (role == 2) {
-        rotate_queries<Tin>(p, head, x, lo, hi - lo);
-        return;
-    }
-    const int64_t page = col < p.max_pages ? p.table[(size_t)b * p.max_pages + col] : -1;
-    if (page < 0 || page >= p.pages) {
-        kv_report(p.status);
-        return;
-    }
-    append_page<Tin, IT>(p, role, head, x, lo, hi - lo, (int)(lo - first), page);
+    const int x = x0 + (lo - s0);
+    if (place >= p.groups)
+        rotate_queries<Tin, INTER>(p, angles, places, place - p.groups, x, lo, hi - lo);
+    else
+        append_page<Tin, IT, INTER>(p, angles, places, place, x, lo, hi - lo, (int)(lo - first),
+                                    col < p.max_pages ? p.table + (size_t)b * p.max_pages + col : nullptr);
 }
 
-template <typename Tin>
+template <typename Tin, bool INTER>
 static const void *append_kernel(int it) {
-    return it == 1 ? (const void *)kv_append_kernel<Tin, 1>
-                   : it == 2 ? (const void *)kv_append_kernel<Tin, 2> : (const void *)kv_append_kernel<Tin, 4>;
+    return it == 1 ? (const void *)kv_append_kernel<Tin, 1, INTER>
+                   : it == 2 ? (const void *)kv_append_kernel<Tin, 2, INTER>
+                             : (const void *)kv_append_kernel<Tin, 4, INTER>;
 }
 
 cudaError_t launch_kv_append(const wz_kv_append_args &a, cudaStream_t s) {
@@ -305,29 +434,54 @@ cudaError_t launch_kv_append(const wz_kv_append_args &a, cudaStream_t s) {
     p.in_stride[0] = a.k_stride; p.in_stride[1] = a.v_stride; p.in_stride[2] = a.q_stride;
     p.q_out = a.q_out; p.q_out_stride = a.q_out_stride;
     p.pages = a.cache.pages; p.heads = a.cache.heads; p.P = a.cache.page_tokens; p.D = a.cache.D;
-    p.G = a.q ? a.Hq / p.heads : 0;
+    while (1 << p.shift < p.P) ++p.shift;
+    p.items = p.D >> 4;
+    p.items_inv = (1u << 20) / p.items + 1;
+    p.Hq = a.Hq;
     p.T = (int)a.T; p.B = a.B;
     p.cu = a.cu; p.start = a.start; p.table = a.page_table; p.max_pages = a.max_pages;
     if (a.rotation) {
         p.rotation = a.rotation; p.rows = (int)a.rotation_rows; p.rot = a.rot; p.interleaved = a.interleaved != 0;
         p.positions = a.positions; p.axes = a.axes;
+        p.quads_inv = (1u << 20) / (p.rot >> 3) + 1;
         p.sec0 = a.section[0]; p.sec01 = a.section[0] + a.section[1];
     }
     p.status = a.device_status;
     // pages that a sequence of max_new tokens can reach, wherever it starts
-    const int most = a.max_new ? a.max_new : p.T;
+    const int most = p.most = a.max_new ? std::min(a.max_new, p.T) : p.T;
     const int64_t ppb = ((int64_t)most + p.P - 2) / p.P + 1;
     int64_t units = (int64_t)p.T / p.P + 2 * (int64_t)p.B;
     if (ppb * p.B <= units) {
         p.ppb = (int)ppb;
         units = ppb * p.B;
     }
-    const int threads = p.P > 64 ? 256 : 128;
-    const int items = p.P * (p.D >> 4);
-    const int it = items <= threads ? 1 : items <= 2 * threads ? 2 : 4;
-    const void *fn = a.dtype == WZ_DTYPE_BF16 ? append_kernel<__nv_bfloat16>(it) : append_kernel<float>(it);
+    // The items of a page's head: two to a thread, or one where 32 are all; four only
+    // for the largest pages.
+    const int rows = std::min(p.P, most), items = p.P * p.items;
+    const int it = items <= 32 ? 1 : items <= 2 * kAppendThreads ? 2 : 4;
+    p.wph = 1;
+    while (p.wph * 32 * it < items) p.wph *= 2;
+    const int kv_heads = (kAppendThreads / 32) / p.wph;
+    p.groups = (p.heads + kv_heads - 1) / kv_heads;
+    if (a.q) {   // eight items of a query to a thread
+        p.q_tokens = std::max(1, std::min(rows, 8 * kAppendThreads / (a.Hq * p.items)));
+        p.parts = (rows + p.q_tokens - 1) / p.q_tokens;
+        p.q_tokens = (rows + p.parts - 1) / p.parts;
+        p.step_j = kAppendThreads % p.items;
+        p.step_h = kAppendThreads / p.items % p.Hq;
+        p.step_r = kAppendThreads / p.items / p.Hq;
+    }
+    p.rows_cta = rows;
+    const size_t smem = (size_t)rows * (p.rot + (p.positions ? p.axes : 0)) * sizeof(float);
+    const void *fn = a.dtype == WZ_DTYPE_BF16
+                         ? (p.interleaved ? append_kernel<__nv_bfloat16, true>(it) : append_kernel<__nv_bfloat16, false>(it))
+                         : (p.interleaved ? append_kernel<float, true>(it) : append_kernel<float, false>(it));
+    cudaError_t e = smem > 48 * 1024 ? allow_smem(fn, smem) : cudaSuccess;
+    if (e != cudaSuccess) return e;
     void *args[] = {&p};
-    return launch_kernel(fn, dim3((unsigned)units, (unsigned)p.heads, a.q ? 3u : 2u), dim3(threads), 0, s, args, true);
+    const int64_t grid = units * (p.groups + p.parts);
+    if (grid > INT32_MAX) return cudaErrorInvalidValue;
+    return launch_kernel(fn, dim3((unsigned)grid), dim3(kAppendThreads), smem, s, args, true);
 }
 
 }  // namespace wz

@@ -52,15 +52,15 @@ __device__ __forceinline__ float fitting_scale(uint32_t bits) {
     return __uint_as_float((uint32_t)(n + 127) << 23);
 }
 
-// The sequence b with cu[b] / P + 2b <= u < cu[b+1] / P + 2(b+1), by all lanes of
+// The sequence b with (cu[b] >> shift) + 2b <= u < (cu[b+1] >> shift) + 2(b+1), by all lanes of
 // a warp: 32 places at a time.
-__device__ __forceinline__ int kv_find_sequence(const int32_t *cu, int B, int u, int P) {
+__device__ __forceinline__ int kv_find_sequence(const int32_t *cu, int B, int u, int shift) {
     const int lane = threadIdx.x & 31;
     int lo = 0, hi = B;   // the sequence lies in [lo, hi)
     while (hi - lo > 1) {
         const int step = (hi - lo + 31) >> 5;
         const int at = lo + lane * step;
-        const bool before = at < hi && cu[at] / P + 2 * at <= u;
+        const bool before = at < hi && (cu[at] >> shift) + 2 * at <= u;
         const int n = max(__popc(__ballot_sync(0xFFFFFFFFu, before)), 1);
         lo += (n - 1) * step;
         hi = min(hi, lo + step);
