@@ -309,7 +309,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
         for (int s = max(0, seq - Sh::kStages); s < seq; ++s)   // the copies have landed
             ptx::mbar_wait(&S->full[s % Sh::kStages], (uint32_t)(s / Sh::kStages) & 1u, kATimeoutNs);
     } else if (warp == 5) {
-        if (lane == 0) {
+        if (ptx::elect_one()) {
             // ---------------- MMA issuer ----------------
             const uint32_t id_s = ptx::idesc_e4m3(128, N, false, false), id_o = ptx::idesc_e4m3(128, N, true, true);
             const uint32_t ring32 = ptx::smem_u32(ring);
@@ -318,7 +318,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
             const uint64_t q_desc = ptx::smem_desc(ptx::smem_u32(qs), 16, 1024, 2);
             // weights: N bytes a token, 8 tokens after 8 tokens; 16 bytes without, 32 with a 32-byte swizzle
             const uint64_t p_desc = ptx::smem_desc(ptx::smem_u32(ps), 8 * N, 8 * N, N == 16 ? 0 : 6);
-            const int ksteps = (p.D + 31) >> 5;
+            const bool wide = p.D > 64;
             int k = 0, item = 0;                                             // tiles and items begun
             bool ok = true;
             auto wait = [&](uint64_t *bar, uint32_t parity) {
@@ -328,7 +328,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                 }
                 return ok;
             };
-            for (; w.any && ok && !*abort_flag; w.next(p), ++item) {
+            for (; w.any && ok; w.next(p), ++item) {
                 const int n = w.t1 - w.t0;
                 if (!wait(&S->q_ready[item & 1], (uint32_t)(item >> 1) & 1u)) break;
                 const uint64_t bq = q_desc + (uint64_t)(item & 1) * (Sh::kOpBytes >> 4);
@@ -338,9 +338,11 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                         if (!wait(&S->full[st], (uint32_t)(seq / Sh::kStages) & 1u)) break;
                         ptx::tc_fence_after();
                         const uint64_t a = k_desc + (uint64_t)st * (kATileBytes >> 4);
-                        for (int j = 0; j < ksteps; ++j)   // K = 32 bytes along the swizzled row
-                            ptx::mma_e4m3(tmem + (uint32_t)((k & 1) * N), a + (uint64_t)(2 * j),
-                                          bq + (uint64_t)(2 * j), id_s, j > 0);
+    #pragma unroll
+                        for (int j = 0; j < 4; ++j)   // K = 32 bytes along the swizzled row
+                            if (j < 2 || wide)
+                                ptx::mma_e4m3(tmem + (uint32_t)((k & 1) * N), a + (uint64_t)(2 * j), bq + (uint64_t)(2 * j),
+                                              id_s, j > 0);
                         ptx::mma_commit(&S->empty[st]);
                         ptx::mma_commit(&S->s_full[k & 1]);
                     }
@@ -352,7 +354,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                         ptx::tc_fence_after();
                         const uint64_t a = v_desc + (uint64_t)st * (kATileBytes >> 4);
                         const uint64_t bp = p_desc + (uint64_t)(j & 1) * (Sh::kOpBytes >> 4);
-#pragma unroll
+    #pragma unroll
                         for (int s = 0; s < kATile / 32; ++s)   // 32 tokens: four groups of 8 rows of V
                             ptx::mma_e4m3(tmem + (uint32_t)((2 + (j & 1)) * N), a + (uint64_t)(s * (4096 >> 4)),
                                           bp + (uint64_t)(s * (32 * N >> 4)), id_o, s > 0);

@@ -25,6 +25,7 @@
 // Every wait is bounded; where one gives up the kernel sets a status bit, ends its
 // copies, frees tensor memory and returns.
 #include <cstring>
+#include <type_traits>
 
 #include "wz_attend.cuh"
 
@@ -32,7 +33,7 @@ namespace wz {
 
 namespace {
 
-constexpr int kMThreads = 14 * 32;
+constexpr int kMThreads = 16 * 32;   // four warpgroups; two warps of the last have nothing to do
 constexpr int kMKStages = 3, kMVStages = 2;
 constexpr int kMTmem = 512;
 constexpr float kMTop = 7.f;     // a row's largest weight is about 2^7 ..
@@ -79,6 +80,13 @@ __device__ __forceinline__ bool many_item(const AttendParams &p, int row_tiles, 
     it->t0 = (int)(tiles * s / splits);
     it->t1 = (int)(tiles * (s + 1) / splits);
     return true;
+}
+
+// The largest of three, given as bits.
+__device__ __forceinline__ float max3(uint32_t a, uint32_t b, uint32_t c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+    return r;
 }
 
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
@@ -148,7 +156,10 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
     const int minlim = max(0, min(it.kv, attend_visible(p, it.r0 / p.G, it.n, it.kv)));
     const int maxlim = max(0, min(it.kv, attend_visible(p, (it.r1 - 1) / p.G, it.n, it.kv)));
 
-    if (warp == 12) {
+    // 512 threads start with 128 registers: 256 x 184 + 128 x 64 + 128 x 80 = 512 x 128
+    if (warp >= 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        if (warp == 12) {
         // ---------------- TMA producer: lane = page of the tile ----------------
         const uint64_t pol = ptx::policy_evict_last();   // other row tiles read the same slots
         const int pages_tile = kATile / p.P, box = p.P * 128;
@@ -168,8 +179,8 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             const int z = znext;
             if (i + 1 < n) znext = slab(it.t0 + i + 1);
             const int ks = i % kMKStages, vs = i % kMVStages;
-            ok = ptx::mbar_wait(&S->k_empty[ks], ((uint32_t)(i / kMKStages) & 1u) ^ 1u, kATimeoutNs) &&
-                 ptx::mbar_wait(&S->v_empty[vs], ((uint32_t)(i / kMVStages) & 1u) ^ 1u, kATimeoutNs);
+            ok = warp_wait(&S->k_empty[ks], ((uint32_t)(i / kMKStages) & 1u) ^ 1u) &&
+                 warp_wait(&S->v_empty[vs], ((uint32_t)(i / kMVStages) & 1u) ^ 1u);
             ok = __all_sync(0xFFFFFFFFu, ok && !*abort_flag);
             if (!ok) {
                 attend_fail(p, abort_flag);
@@ -193,14 +204,12 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             if (i >= done - kMVStages)
                 ptx::mbar_wait(&S->v_full[i % kMVStages], (uint32_t)(i / kMVStages) & 1u, kATimeoutNs);
         }
-    } else if (warp == 13) {
-        if (lane == 0) {
+        } else if (warp == 13 && ptx::elect_one()) {
             // ---------------- MMA issuer ----------------
             const uint32_t id_s = ptx::idesc_e4m3(128, 128, false, false), id_o = ptx::idesc_f16(128, p.D, false, true);
             const uint64_t q_desc = ptx::smem_desc(ptx::smem_u32(qs), 16, 1024, 2);
             const uint64_t k_desc = ptx::smem_desc(ptx::smem_u32(kring), 16, 1024, 2);
             const uint64_t w_desc = ptx::smem_desc(ptx::smem_u32(wring), kATileBytes, 1024, 2);   // 64 channels: 16 KB
-            const int ksteps = (p.D + 31) >> 5;
             bool ok = true;
             auto wait = [&](uint64_t *bar, uint32_t parity) {
                 if (ok && !ptx::mbar_wait(bar, parity, kATimeoutNs)) {
@@ -209,53 +218,71 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
                 }
                 return ok;
             };
-            auto logits = [&](int q, int i) {   // S of row tile q for tile i
+            // S of row tile q for tile i: 32 channels of the codes, of the rests, of the codes ..
+            auto logits = [&](auto q_, int i) {
+                constexpr int q = decltype(q_)::value;
                 const uint64_t a = q_desc + (uint64_t)(q * 2) * (kATileBytes >> 4);
                 const uint64_t b = k_desc + (uint64_t)(i % kMKStages) * (kATileBytes >> 4);
-                for (int half = 0; half < 2; ++half)
-                    for (int j = 0; j < ksteps; ++j)
-                        ptx::mma_e4m3(tmem + (uint32_t)(q * 128), a + (uint64_t)half * (kATileBytes >> 4) + (uint64_t)(2 * j),
-                                      b + (uint64_t)(2 * j), id_s, half | j);
+                const uint32_t d = tmem + (uint32_t)(q * 128);
+                constexpr uint64_t rest = kATileBytes >> 4;
+                if (p.D > 64) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        ptx::mma_e4m3(d, a + (uint64_t)(j & 1) * rest + (uint64_t)(2 * (j >> 1)),
+                                      b + (uint64_t)(2 * (j >> 1)), id_s, j > 0);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        ptx::mma_e4m3(d, a + (uint64_t)(j & 1) * rest + (uint64_t)(2 * (j >> 1)),
+                                      b + (uint64_t)(2 * (j >> 1)), id_s, j > 0);
+                }
                 if (q == qtiles - 1) ptx::mma_commit(&S->k_empty[i % kMKStages]);
                 ptx::mma_commit(&S->s_full[q]);
             };
+            // O of row tile q after its weights of tile i, then its logits of the next tile
+            auto step = [&](auto q_, int i) {
+                constexpr int q = decltype(q_)::value;
+                const uint32_t par = (uint32_t)i & 1u;
+                if (q == 0 && !wait(&S->w_full[i & 1], (uint32_t)(i >> 1) & 1u)) return;
+                if (!wait(&S->p_ready[q], par)) return;
+                ptx::tc_fence_after();
+                const uint64_t b = w_desc + (uint64_t)(i & 1) * (2 * kATileBytes >> 4);
+#pragma unroll
+                for (int s = 0; s < kATile / 16; ++s)   // 16 tokens: 8 columns of W, two groups of 8 rows of V
+                    ptx::mma_f16_ta(tmem + (uint32_t)(256 + q * 128), tmem + (uint32_t)(q * 128 + 8 * s),
+                                    b + (uint64_t)(s * (2048 >> 4)), id_o, s ? 1u : (uint32_t)i);
+                if (q == qtiles - 1) ptx::mma_commit(&S->w_empty[i & 1]);
+                ptx::mma_commit(&S->o_full[q]);
+                if (i + 1 == n) return;
+                if (q == 0 && !wait(&S->k_full[(i + 1) % kMKStages], (uint32_t)((i + 1) / kMKStages) & 1u)) return;
+                // S takes the place of the weights: their products have to be complete
+                if (!wait(&S->o_full[q], par)) return;
+                ptx::tc_fence_after();
+                logits(q_, i + 1);
+            };
+            constexpr std::integral_constant<int, 0> q0{};
+            constexpr std::integral_constant<int, 1> q1{};
             if (n > 0 && wait(&S->q_ready, 0) && wait(&S->k_full[0], 0)) {
                 ptx::tc_fence_after();
-                for (int q = 0; q < qtiles; ++q) logits(q, 0);
+                logits(q0, 0);
+                if (qtiles == 2) logits(q1, 0);
                 for (int i = 0; i < n && ok; ++i) {
-                    const uint32_t par = (uint32_t)i & 1u;
-                    for (int q = 0; q < qtiles && ok; ++q) {
-                        if (!wait(&S->p_ready[q], par) || !wait(&S->w_full[i & 1], (uint32_t)(i >> 1) & 1u)) break;
-                        ptx::tc_fence_after();
-                        const uint64_t b = w_desc + (uint64_t)(i & 1) * (2 * kATileBytes >> 4);
-#pragma unroll
-                        for (int s = 0; s < kATile / 16; ++s)   // 16 tokens: 8 columns of W, two groups of 8 rows of V
-                            ptx::mma_f16_ta(tmem + (uint32_t)(256 + q * 128), tmem + (uint32_t)(q * 128 + 8 * s),
-                                            b + (uint64_t)(s * (2048 >> 4)), id_o, i | s);
-                        if (q == qtiles - 1) ptx::mma_commit(&S->w_empty[i & 1]);
-                        ptx::mma_commit(&S->o_full[q]);
-                        if (i + 1 < n) {
-                            // S takes the place of the weights: their products have to be complete
-                            if (!wait(&S->k_full[(i + 1) % kMKStages], (uint32_t)((i + 1) / kMKStages) & 1u) ||
-                                !wait(&S->o_full[q], par))
-                                break;
-                            ptx::tc_fence_after();
-                            logits(q, i + 1);
-                        }
-                    }
+                    step(q0, i);
+                    if (qtiles == 2 && ok) step(q1, i);
                 }
             }
             ptx::mma_commit(&S->drain);
             ptx::mbar_wait(&S->drain, 0, kATimeoutNs);
         }
     } else if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         // ---------------- V to f16: a warp takes two rows x four pieces of 16 channels at a time ----------------
         const int c4 = lane & 3, odd = (lane >> 2) & 1, far = (lane >> 3) & 1, pair = lane >> 4;
         bool ok = true;
         for (int i = 0; i < n; ++i) {
             const int vs = i % kMVStages, base = (it.t0 + i) * kATile;
-            ok = ptx::mbar_wait(&S->v_full[vs], (uint32_t)(i / kMVStages) & 1u, kATimeoutNs) &&
-                 ptx::mbar_wait(&S->w_empty[i & 1], ((uint32_t)(i >> 1) & 1u) ^ 1u, kATimeoutNs);
+            ok = warp_wait(&S->v_full[vs], (uint32_t)(i / kMVStages) & 1u) &&
+                 warp_wait(&S->w_empty[i & 1], ((uint32_t)(i >> 1) & 1u) ^ 1u);
             ok = __all_sync(0xFFFFFFFFu, ok && !*abort_flag);
             if (!ok) {
                 attend_fail(p, abort_flag);
@@ -264,35 +291,52 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             const uint8_t *src = vring + (size_t)vs * kATileBytes;
             uint8_t *dst = wring + (size_t)(i & 1) * (2 * kATileBytes) + (size_t)far * kATileBytes;
             const bool mixed = base + kATile > minlim;
-            for (int g = 0; g < 8; ++g) {
-                const int t = (warp - 8) * 32 + 4 * g + 2 * pair + odd, x = t & 7;
-                const uint4 v = *reinterpret_cast<const uint4 *>(src + t * 128 + (((far * 4 + c4) ^ x) << 4));
-                uint32_t in[4] = {v.x, v.y, v.z, v.w};
+            const int t0 = (warp - 8) * 32 + 2 * pair + odd;   // and every fourth row from here
+            for (int g0 = 0; g0 < 8; g0 += 4) {
+                uint32_t in[4][4];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int t = t0 + 4 * (g0 + g);
+                    const uint4 v = *reinterpret_cast<const uint4 *>(src + t * 128 + (((far * 4 + c4) ^ (t & 7)) << 4));
+                    in[g][0] = v.x;
+                    in[g][1] = v.y;
+                    in[g][2] = v.z;
+                    in[g][3] = v.w;
+                }
                 if (mixed) {
                     // codes that a weight of 0 must not meet
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (base + t >= maxlim) in[j] = 0;
-                        const uint32_t bad = __vcmpeq4(in[j] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
-                        if (bad && base + t >= minlim) {
-                            for (int u = 0; u < 4; ++u)
-                                if ((bad >> (8 * u)) & 1u)
-                                    atomicMin(&S->nan_min[far * 64 + c4 * 16 + 4 * j + u], base + t);
-                            in[j] &= ~bad;
+                    for (int g = 0; g < 4; ++g) {
+                        const int t = base + t0 + 4 * (g0 + g);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (t >= maxlim) in[g][j] = 0;
+                            const uint32_t bad = __vcmpeq4(in[g][j] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                            if (bad && t >= minlim) {
+                                for (int u = 0; u < 4; ++u)
+                                    if ((bad >> (8 * u)) & 1u)
+                                        atomicMin(&S->nan_min[far * 64 + c4 * 16 + 4 * j + u], t);
+                                in[g][j] &= ~bad;
+                            }
                         }
                     }
                 }
-                uint32_t o[8];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const __half2 a = half2_of_e4m3((uint16_t)(in[j] & 0xFFFFu));
-                    const __half2 b = half2_of_e4m3((uint16_t)(in[j] >> 16));
-                    o[2 * j] = *reinterpret_cast<const uint32_t *>(&a);
-                    o[2 * j + 1] = *reinterpret_cast<const uint32_t *>(&b);
+                for (int g = 0; g < 4; ++g) {
+                    const int t = t0 + 4 * (g0 + g), x = t & 7;
+                    uint32_t o[8];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const __half2 a = half2_of_e4m3((uint16_t)(in[g][j] & 0xFFFFu));
+                        const __half2 b = half2_of_e4m3((uint16_t)(in[g][j] >> 16));
+                        o[2 * j] = *reinterpret_cast<const uint32_t *>(&a);
+                        o[2 * j + 1] = *reinterpret_cast<const uint32_t *>(&b);
+                    }
+                    *reinterpret_cast<uint4 *>(dst + t * 128 + (((2 * c4) ^ x) << 4)) =
+                        make_uint4(o[0], o[1], o[2], o[3]);
+                    *reinterpret_cast<uint4 *>(dst + t * 128 + (((2 * c4 + 1) ^ x) << 4)) =
+                        make_uint4(o[4], o[5], o[6], o[7]);
                 }
-                *reinterpret_cast<uint4 *>(dst + t * 128 + (((2 * c4) ^ x) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-                *reinterpret_cast<uint4 *>(dst + t * 128 + (((2 * c4 + 1) ^ x) << 4)) =
-                    make_uint4(o[4], o[5], o[6], o[7]);
             }
             ptx::fence_proxy_async_smem();
             __syncwarp();
@@ -302,6 +346,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             }
         }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         // ---------------- weights ----------------
         const int q = warp >> 2, row = tid;               // this thread's row of the CTA
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
@@ -338,48 +383,49 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         float ref = -INFINITY, sum = 0.f;
         bool ok = true;
         const int steps = q < qtiles ? n : 0;
-        // lane l < 8: scales of the l-th 16 tokens of a tile, loaded one tile ahead
-        auto scales_of = [&](int tile) {
-            float2 v = make_float2(1.f, 0.f);
+        // lane l < 8: scales of the l-th 16 tokens of a tile, loaded one tile ahead, their page two
+        auto page_of = [&](int tile) {
             const int t = tile * kATile + 16 * lane;
-            if (lane < 8 && t < it.kv) {
-                const int pg = attend_page(p, it.b, t);
-                if (pg >= 0)
-                    v = make_float2(p.k_scale[(size_t)pg * p.heads + it.h], p.v_scale[(size_t)pg * p.heads + it.h]);
-            }
-            return v;
+            return lane < 8 && tile < it.t1 && t < it.kv ? attend_page(p, it.b, t) : -1;
         };
-        float2 next = steps > 0 ? scales_of(it.t0) : make_float2(1.f, 0.f);
+        auto scales_of = [&](int pg) {
+            return pg < 0 ? make_float2(1.f, 0.f)
+                          : make_float2(p.k_scale[(size_t)pg * p.heads + it.h], p.v_scale[(size_t)pg * p.heads + it.h]);
+        };
+        int pg_next = steps > 0 ? page_of(it.t0 + 1) : -1;
+        float2 next = scales_of(steps > 0 ? page_of(it.t0) : -1);
         for (int i = 0; i < steps; ++i) {
-            const float my_k = next.x, my_lv = next.y > 0.f ? log2f(next.y) : -INFINITY;
-            const float my_inv = next.y > 0.f ? 1.f / next.y : 0.f;
-            if (i + 1 < steps) next = scales_of(it.t0 + i + 1);
+            const float my_k = next.x, my_lv = next.y > 0.f ? __log2f(next.y) : -INFINITY;
+            const float my_inv = next.y > 0.f ? __frcp_rn(next.y) : 0.f;
+            next = scales_of(pg_next);
+            pg_next = page_of(it.t0 + i + 2);
             const int rel = lim - (it.t0 + i) * kATile;       // columns of the tile that this row sees
             const bool mixed = (it.t0 + i + 1) * kATile > minlim;
-            ok = ptx::mbar_wait(&S->s_full[q], (uint32_t)i & 1u, kATimeoutNs);
+            ok = warp_wait(&S->s_full[q], (uint32_t)i & 1u);
             ok = __all_sync(0xFFFFFFFFu, ok && !*abort_flag);
             if (!ok) break;
             ptx::tc_fence_after();
+            // the row's logits, all in registers
+            uint32_t s[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32b_x32(s_at + (uint32_t)(32 * c), s[c]);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int c = 0; c < 4; ++c) ptx::reg_fence32(s[c]);
+            if (mixed) {
+#pragma unroll
+                for (int j = 0; j < 128; ++j)
+                    if (j >= rel) s[j / 32][j % 32] = __float_as_uint(-3e38f);
+            }
             float top = -INFINITY;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t s[32];
-                ptx::tmem_ld_32x32b_x32(s_at + (uint32_t)(32 * c), s);
-                ptx::tmem_ld_wait();
-                ptx::reg_fence32(s);
-                if (mixed) {
+            for (int g = 0; g < 8; ++g) {
+                float m = max3(s[g / 2][16 * (g % 2)], s[g / 2][16 * (g % 2) + 1], s[g / 2][16 * (g % 2) + 2]);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (32 * c + j >= rel) s[j] = __float_as_uint(-3e38f);
-                }
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    float m = __uint_as_float(s[16 * g]);
-#pragma unroll
-                    for (int j = 1; j < 16; ++j) m = fmaxf(m, __uint_as_float(s[16 * g + j]));
-                    const float a = __shfl_sync(0xFFFFFFFFu, my_k, 2 * c + g) * rowf;
-                    top = fmaxf(top, fmaf(m, a, __shfl_sync(0xFFFFFFFFu, my_lv, 2 * c + g)));
-                }
+                for (int j = 3; j < 15; j += 2)
+                    m = max3(__float_as_uint(m), s[g / 2][16 * (g % 2) + j], s[g / 2][16 * (g % 2) + j + 1]);
+                m = fmaxf(m, __uint_as_float(s[g / 2][16 * (g % 2) + 15]));
+                top = fmaxf(top, fmaf(m, __shfl_sync(0xFFFFFFFFu, my_k, g) * rowf, __shfl_sync(0xFFFFFFFFu, my_lv, g)));
             }
             const bool rise = top > ref + kMSlack;
             if (__any_sync(0xFFFFFFFFu, rise)) {
@@ -400,31 +446,29 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             }
             const float base = kMTop - (ref == -INFINITY ? 0.f : ref);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t s[32];
-                ptx::tmem_ld_32x32b_x32(s_at + (uint32_t)(32 * c), s);
-                ptx::tmem_ld_wait();
-                ptx::reg_fence32(s);
-                uint32_t w[16];
+            for (int g = 0; g < 8; ++g) {
+                const float a = __shfl_sync(0xFFFFFFFFu, my_k, g) * rowf;
+                const float off = __shfl_sync(0xFFFFFFFFu, my_lv, g) + base;
+                const f2_t a2 = pack2(a, a), off2 = pack2(off, off);
+                f2_t part = 0;   // two zeros
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const float a = __shfl_sync(0xFFFFFFFFu, my_k, 2 * c + g) * rowf;
-                    const float off = __shfl_sync(0xFFFFFFFFu, my_lv, 2 * c + g) + base;
-                    float part = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 16; j += 2) {
-                        float u = ex2(fmaf(__uint_as_float(s[16 * g + j]), a, off));
-                        float v = ex2(fmaf(__uint_as_float(s[16 * g + j + 1]), a, off));
-                        if (mixed) {
-                            if (32 * c + 16 * g + j >= rel) u = 0.f;
-                            if (32 * c + 16 * g + j + 1 >= rel) v = 0.f;
-                        }
-                        part += u + v;
-                        w[8 * g + j / 2] = pack_half2(u, v);
+                for (int j = 0; j < 16; j += 2) {
+                    const int at = 16 * (g % 2) + j;
+                    const float2 x =
+                        unpack2(fma2(pack2(__uint_as_float(s[g / 2][at]), __uint_as_float(s[g / 2][at + 1])), a2, off2));
+                    float u = ex2(x.x), v = ex2(x.y);
+                    if (mixed) {
+                        if (16 * g + j >= rel) u = 0.f;
+                        if (16 * g + j + 1 >= rel) v = 0.f;
                     }
-                    sum = fmaf(part, __shfl_sync(0xFFFFFFFFu, my_inv, 2 * c + g), sum);
+                    part = add2(part, pack2(u, v));
+                    s[g / 2][8 * (g % 2) + j / 2] = pack_half2(u, v);   // past the logits that are still to come
                 }
-                ptx::tmem_st_32x32b_x16(s_at + (uint32_t)(16 * c), w);   // columns that have been read
+                const float2 both = unpack2(part);
+                sum = fmaf(both.x + both.y, __shfl_sync(0xFFFFFFFFu, my_inv, g), sum);
+                if (g % 2)   // 32 tokens' weights, in the place of logits that have been read
+                    ptx::tmem_st_32x32b_x16(s_at + (uint32_t)(8 * (g - 1)),
+                                            *reinterpret_cast<const uint32_t(*)[16]>(&s[g / 2]));
             }
             ptx::tmem_st_wait();
             ptx::tc_fence_before();
