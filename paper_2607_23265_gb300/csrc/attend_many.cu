@@ -16,10 +16,11 @@
 // pages multiply the weights, those of K's the logits, one of each for 16 tokens.
 // A thread of warps 0-7 has one row: maximum, weights and sum need no other lane.
 // The maximum that weights are relative to follows the true one only when that is
-// 2^8 above it; O is rescaled in tensor memory then.
+// 2^8 above it: the tile's weights are formed without waiting for its maximum, and
+// where it turns out so O is rescaled in tensor memory and they are formed again.
 //   warps 0-3, 4-7  weights of row tile 0, 1
 //   warps 8-11      V to f16
-//   warp 12         TMA producer: rings of K and V tiles
+//   warps 12, 14    TMA producers: rings of K and of V tiles
 //   warp 13         TMEM allocation, MMA issuer (one thread)
 // Tensor memory: S (then W) of the tiles in columns 0 and 128, O in 256 and 384.
 // Every wait is bounded; where one gives up the kernel sets a status bit, ends its
@@ -46,6 +47,8 @@ struct ManyShared {
     uint64_t q_ready, drain;
     uint32_t tmem_base;
     int abort;
+    float rowf[kManyRows];
+    int any_nan;
     int nan_min[128];                            // per channel: first token that some rows see and whose V is NaN
 };
 
@@ -95,6 +98,44 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
     return r;
 }
 
+// A row's 128 logits to weights in f16, 16 to the first half of each s[c]; lanes 0-7
+// hold the scales of 16 tokens each.  top: the largest logit with its weight of V,
+// add: the weights' sum.  MIXED: columns from `rel` on are not seen.
+template <bool MIXED>
+__device__ __forceinline__ void weights(uint32_t (&s)[4][32], float my_k, float my_lv, float my_inv, float rowf,
+                                        float base, int rel, float &top, float &add) {
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+        uint32_t *x = s[g / 2] + 16 * (g % 2);
+        if (MIXED) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (16 * g + j >= rel) x[j] = __float_as_uint(-3e38f);
+        }
+        const float a = __shfl_sync(0xFFFFFFFFu, my_k, g) * rowf, lv = __shfl_sync(0xFFFFFFFFu, my_lv, g);
+        float m = max3(x[0], x[1], x[2]);
+#pragma unroll
+        for (int j = 3; j < 15; j += 2) m = max3(__float_as_uint(m), x[j], x[j + 1]);
+        m = fmaxf(m, __uint_as_float(x[15]));
+        top = fmaxf(top, fmaf(m, a, lv));
+        const f2_t a2 = pack2(a, a), off2 = pack2(lv + base, lv + base);
+        f2_t part[2] = {0, 0};   // zeros
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) {
+            const float2 v = unpack2(fma2(pack2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), a2, off2));
+            float w0 = ex2(v.x), w1 = ex2(v.y);
+            if (MIXED) {
+                if (16 * g + j >= rel) w0 = 0.f;
+                if (16 * g + j + 1 >= rel) w1 = 0.f;
+            }
+            part[(j / 2) % 2] = add2(part[(j / 2) % 2], pack2(w0, w1));
+            s[g / 2][8 * (g % 2) + j / 2] = pack_half2(w0, w1);   // past the logits that are still to come
+        }
+        const float2 both = unpack2(add2(part[0], part[1]));
+        add = fmaf(both.x + both.y, __shfl_sync(0xFFFFFFFFu, my_inv, g), add);
+    }
+}
+
 }  // namespace
 
 __global__ void __launch_bounds__(kMThreads, 1)
@@ -140,6 +181,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         ptx::fence_proxy_async_smem();
     }
     if (tid < 128) S->nan_min[tid] = INT32_MAX;
+    if (tid == 128) S->any_nan = 0;
     if (warp == 13) {
         ptx::tmem_alloc(&S->tmem_base, kMTmem);
         ptx::tmem_relinquish();
@@ -159,51 +201,47 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
     // 512 threads start with 128 registers: 256 x 184 + 128 x 64 + 128 x 80 = 512 x 128
     if (warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-        if (warp == 12) {
-        // ---------------- TMA producer: lane = page of the tile ----------------
-        const uint64_t pol = ptx::policy_evict_last();   // other row tiles read the same slots
-        const int pages_tile = kATile / p.P, box = p.P * 128;
-        const int absent = (int)(p.pages * p.heads);     // past the cache: zeros
-        auto slab = [&](int tile) {
-            const int t = tile * kATile + lane * p.P;
-            int pg = -1;
-            if (lane < pages_tile && t < it.kv) {
-                pg = attend_page(p, it.b, t);
-                if (pg < 0) kv_report(p.status);
+        if (warp == 12 || warp == 14) {
+            // ---------------- TMA producers of K and of V: lane = page of the tile ----------------
+            const bool v = warp == 14;
+            const int stages = v ? kMVStages : kMKStages;
+            uint64_t *full = v ? S->v_full : S->k_full, *empty = v ? S->v_empty : S->k_empty;
+            uint8_t *ring = v ? vring : kring;
+            const CUtensorMap *map = v ? &maps.v : &maps.k;
+            const uint64_t pol = ptx::policy_evict_last();   // other row tiles read the same slots
+            const int pages_tile = kATile / p.P, box = p.P * 128;
+            const int absent = (int)(p.pages * p.heads);     // past the cache: zeros
+            auto slab = [&](int tile) {
+                const int t = tile * kATile + (lane << p.shift);
+                int pg = -1;
+                if (lane < pages_tile && tile < it.t1 && t < it.kv) {
+                    pg = attend_page(p, it.b, t);
+                    if (pg < 0) kv_report(p.status);
+                }
+                return pg < 0 ? absent : pg * p.heads + it.h;
+            };
+            int znext = slab(it.t0), done = 0, st = 0;
+            uint32_t phase = 0;
+            for (int i = 0; i < n; ++i) {
+                const int z = znext;
+                znext = slab(it.t0 + i + 1);
+                const bool ok = __all_sync(0xFFFFFFFFu, warp_wait(&empty[st], phase ^ 1u) && !*abort_flag);
+                if (!ok) {
+                    attend_fail(p, abort_flag);
+                    break;
+                }
+                if (lane == 0) ptx::mbar_arrive_expect_tx(&full[st], kATileBytes);
+                __syncwarp();
+                if (lane < pages_tile)
+                    ptx::tma_load_3d(ring + (size_t)st * kATileBytes + (size_t)lane * box, map, &full[st], 0, 0, z, pol);
+                done = i + 1;
+                if (++st == stages) {
+                    st = 0;
+                    phase ^= 1u;
+                }
             }
-            return pg < 0 ? absent : pg * p.heads + it.h;
-        };
-        int znext = n > 0 ? slab(it.t0) : absent, done = 0;
-        bool ok = true;
-        for (int i = 0; i < n; ++i) {
-            const int z = znext;
-            if (i + 1 < n) znext = slab(it.t0 + i + 1);
-            const int ks = i % kMKStages, vs = i % kMVStages;
-            ok = warp_wait(&S->k_empty[ks], ((uint32_t)(i / kMKStages) & 1u) ^ 1u) &&
-                 warp_wait(&S->v_empty[vs], ((uint32_t)(i / kMVStages) & 1u) ^ 1u);
-            ok = __all_sync(0xFFFFFFFFu, ok && !*abort_flag);
-            if (!ok) {
-                attend_fail(p, abort_flag);
-                break;
-            }
-            if (lane == 0) {
-                ptx::mbar_arrive_expect_tx(&S->k_full[ks], kATileBytes);
-                ptx::mbar_arrive_expect_tx(&S->v_full[vs], kATileBytes);
-            }
-            __syncwarp();
-            if (lane < pages_tile) {
-                ptx::tma_load_3d(kring + (size_t)ks * kATileBytes + (size_t)lane * box, &maps.k, &S->k_full[ks], 0, 0, z,
-                                 pol);
-                ptx::tma_load_3d(vring + (size_t)vs * kATileBytes + (size_t)lane * box, &maps.v, &S->v_full[vs], 0, 0, z,
-                                 pol);
-            }
-            done = i + 1;
-        }
-        for (int i = max(0, done - kMKStages); i < done; ++i) {   // the copies have landed
-            ptx::mbar_wait(&S->k_full[i % kMKStages], (uint32_t)(i / kMKStages) & 1u, kATimeoutNs);
-            if (i >= done - kMVStages)
-                ptx::mbar_wait(&S->v_full[i % kMVStages], (uint32_t)(i / kMVStages) & 1u, kATimeoutNs);
-        }
+            for (int i = max(0, done - stages); i < done; ++i)   // the copies have landed
+                ptx::mbar_wait(&full[i % stages], (uint32_t)(i / stages) & 1u, kATimeoutNs);
         } else if (warp == 13 && ptx::elect_one()) {
             // ---------------- MMA issuer ----------------
             const uint32_t id_s = ptx::idesc_e4m3(128, 128, false, false), id_o = ptx::idesc_f16(128, p.D, false, true);
@@ -317,6 +355,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
                                     if ((bad >> (8 * u)) & 1u)
                                         atomicMin(&S->nan_min[far * 64 + c4 * 16 + 4 * j + u], t);
                                 in[g][j] &= ~bad;
+                                S->any_nan = 1;
                             }
                         }
                     }
@@ -352,30 +391,61 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t s_at = lanes + (uint32_t)(q * 128), o_at = lanes + (uint32_t)(256 + q * 128);
         const uint32_t flip = p.scale2 < 0.f ? 0x80808080u : 0u;   // logits' factors are positive
-        float rowf = 0.f;
-        for (int j0 = 0; j0 < 32; j0 += 8) {   // eight rows' loads in flight
-            uint2 raw[8];
+        {
+            // eight lanes to a row, 16 channels to a lane; all of a warp's rows in flight
+            const int sub = lane & 7, r0 = warp * 32 + (lane >> 3);
+            uint4 raw[8][2];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int at = it.r0 + warp * 32 + j0 + j;
-                const int i = at / p.G, g = at - i * p.G;
-                raw[j] = query_load(p, at < it.r1 ? p.q + (size_t)(it.x0 + i) * p.q_stride +
-                                                        (size_t)(it.h * p.G + g) * p.D
-                                                  : nullptr);
+                const int at = it.r0 + r0 + 4 * j, i = at / p.G, g = at - i * p.G;
+                raw[j][0] = raw[j][1] = make_uint4(0, 0, 0, 0);
+                if (at < it.r1 && 16 * sub < p.D) {
+                    const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (size_t)(it.x0 + i) * p.q_stride +
+                                                                       (size_t)(it.h * p.G + g) * p.D + 16 * sub);
+                    raw[j][0] = src[0];
+                    raw[j][1] = src[1];
+                }
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int r = warp * 32 + j0 + j;
-                const QueryPiece v = query_piece<false>(raw[j]);
-                uint8_t *d = qs + (size_t)(q * 2) * kATileBytes + (r & 127) * 128 + ((4 * lane) ^ ((r & 7) << 4));
-                *reinterpret_cast<uint32_t *>(d) = v.hi ^ flip;
-                *reinterpret_cast<uint32_t *>(d + kATileBytes) = v.lo ^ flip;
-                if (lane == j0 + j) rowf = v.factor * fabsf(p.scale2);
+                const int r = r0 + 4 * j;
+                const uint32_t w[8] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w,
+                                       raw[j][1].x, raw[j][1].y, raw[j][1].z, raw[j][1].w};
+                uint32_t m = 0;   // bits of the largest magnitude: as floats, and infinities and NaN above all
+#pragma unroll
+                for (int u = 0; u < 8; ++u) m = max(m, max((w[u] << 16) & 0x7FFFFFFFu, w[u] & 0x7FFF0000u));
+#pragma unroll
+                for (int d = 1; d < 8; d <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+                const bool finite = m < 0x7F800000u;
+                int e = 134 - (int)(m >> 23);   // takes the largest to [128, 256)
+                e = m == 0 || !finite ? 0 : min(e, 126);
+                const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const float a = __uint_as_float(w[u] << 16) * up, b = __uint_as_float(w[u] & 0xFFFF0000u) * up;
+                    const uint32_t c = e4m3x2(a, b);
+                    const float2 f = __half22float2(half2_of_e4m3((uint16_t)c));
+                    const uint32_t d = e4m3x2(a - f.x, b - f.y);
+                    hi[u / 2] = u % 2 ? hi[u / 2] | c << 16 : c;
+                    lo[u / 2] = u % 2 ? lo[u / 2] | d << 16 : d;
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    hi[u] = finite ? hi[u] ^ flip : 0;
+                    lo[u] = finite ? lo[u] ^ flip : 0;
+                }
+                uint8_t *dst = qs + (size_t)(q * 2) * kATileBytes + (r & 127) * 128 + ((sub ^ (r & 7)) << 4);
+                *reinterpret_cast<uint4 *>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                *reinterpret_cast<uint4 *>(dst + kATileBytes) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                if (sub == 0)
+                    S->rowf[r] = finite ? __uint_as_float((uint32_t)(127 - e) << 23) * fabsf(p.scale2) : NAN;
             }
         }
         ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&S->q_ready);
+        const float rowf = S->rowf[row];   // this warp's rows
         const int tok = (it.r0 + row) / p.G;
         const bool real = it.r0 + row < it.r1;
         const int lim = real ? max(0, min(it.kv, attend_visible(p, tok, it.n, it.kv))) : 0;
@@ -394,41 +464,43 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         };
         int pg_next = steps > 0 ? page_of(it.t0 + 1) : -1;
         float2 next = scales_of(steps > 0 ? page_of(it.t0) : -1);
-        for (int i = 0; i < steps; ++i) {
-            const float my_k = next.x, my_lv = next.y > 0.f ? __log2f(next.y) : -INFINITY;
-            const float my_inv = next.y > 0.f ? __frcp_rn(next.y) : 0.f;
+        // factor of the logits, log2 and reciprocal of V's scale
+        float my_k, my_lv, my_inv;
+        auto take_scales = [&](int tile_after) {
+            my_k = next.x;
+            my_lv = next.y > 0.f ? __log2f(next.y) : -INFINITY;
+            my_inv = next.y > 0.f ? __frcp_rn(next.y) : 0.f;
             next = scales_of(pg_next);
-            pg_next = page_of(it.t0 + i + 2);
+            pg_next = page_of(tile_after);
+        };
+        take_scales(it.t0 + 2);
+        for (int i = 0; i < steps; ++i) {
             const int rel = lim - (it.t0 + i) * kATile;       // columns of the tile that this row sees
             const bool mixed = (it.t0 + i + 1) * kATile > minlim;
             ok = warp_wait(&S->s_full[q], (uint32_t)i & 1u);
             ok = __all_sync(0xFFFFFFFFu, ok && !*abort_flag);
             if (!ok) break;
             ptx::tc_fence_after();
-            // the row's logits, all in registers
             uint32_t s[4][32];
+            // Weights relative to the maximum of the tiles before; where this tile's is too
+            // far above it, once more relative to that.
+            for (;;) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32b_x32(s_at + (uint32_t)(32 * c), s[c]);
-            ptx::tmem_ld_wait();
+                for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32b_x32(s_at + (uint32_t)(32 * c), s[c]);
+                const float base = kMTop - (ref == -INFINITY ? 0.f : ref);
+                float top = -INFINITY, add = 0.f;
+                ptx::tmem_ld_wait();
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ptx::reg_fence32(s[c]);
-            if (mixed) {
-#pragma unroll
-                for (int j = 0; j < 128; ++j)
-                    if (j >= rel) s[j / 32][j % 32] = __float_as_uint(-3e38f);
-            }
-            float top = -INFINITY;
-#pragma unroll
-            for (int g = 0; g < 8; ++g) {
-                float m = max3(s[g / 2][16 * (g % 2)], s[g / 2][16 * (g % 2) + 1], s[g / 2][16 * (g % 2) + 2]);
-#pragma unroll
-                for (int j = 3; j < 15; j += 2)
-                    m = max3(__float_as_uint(m), s[g / 2][16 * (g % 2) + j], s[g / 2][16 * (g % 2) + j + 1]);
-                m = fmaxf(m, __uint_as_float(s[g / 2][16 * (g % 2) + 15]));
-                top = fmaxf(top, fmaf(m, __shfl_sync(0xFFFFFFFFu, my_k, g) * rowf, __shfl_sync(0xFFFFFFFFu, my_lv, g)));
-            }
-            const bool rise = top > ref + kMSlack;
-            if (__any_sync(0xFFFFFFFFu, rise)) {
+                for (int c = 0; c < 4; ++c) ptx::reg_fence32(s[c]);
+                if (mixed)
+                    weights<true>(s, my_k, my_lv, my_inv, rowf, base, rel, top, add);
+                else
+                    weights<false>(s, my_k, my_lv, my_inv, rowf, base, rel, top, add);
+                const bool rise = top > ref + kMSlack;
+                if (!__any_sync(0xFFFFFFFFu, rise)) {
+                    sum += add;
+                    break;
+                }
                 const float to = rise ? top : ref, f = rise ? ex2(ref - to) : 1.f;
                 ref = to;
                 sum *= f;
@@ -444,36 +516,14 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
                     }
                 }
             }
-            const float base = kMTop - (ref == -INFINITY ? 0.f : ref);
 #pragma unroll
-            for (int g = 0; g < 8; ++g) {
-                const float a = __shfl_sync(0xFFFFFFFFu, my_k, g) * rowf;
-                const float off = __shfl_sync(0xFFFFFFFFu, my_lv, g) + base;
-                const f2_t a2 = pack2(a, a), off2 = pack2(off, off);
-                f2_t part = 0;   // two zeros
-#pragma unroll
-                for (int j = 0; j < 16; j += 2) {
-                    const int at = 16 * (g % 2) + j;
-                    const float2 x =
-                        unpack2(fma2(pack2(__uint_as_float(s[g / 2][at]), __uint_as_float(s[g / 2][at + 1])), a2, off2));
-                    float u = ex2(x.x), v = ex2(x.y);
-                    if (mixed) {
-                        if (16 * g + j >= rel) u = 0.f;
-                        if (16 * g + j + 1 >= rel) v = 0.f;
-                    }
-                    part = add2(part, pack2(u, v));
-                    s[g / 2][8 * (g % 2) + j / 2] = pack_half2(u, v);   // past the logits that are still to come
-                }
-                const float2 both = unpack2(part);
-                sum = fmaf(both.x + both.y, __shfl_sync(0xFFFFFFFFu, my_inv, g), sum);
-                if (g % 2)   // 32 tokens' weights, in the place of logits that have been read
-                    ptx::tmem_st_32x32b_x16(s_at + (uint32_t)(8 * (g - 1)),
-                                            *reinterpret_cast<const uint32_t(*)[16]>(&s[g / 2]));
-            }
+            for (int c = 0; c < 4; ++c)
+                ptx::tmem_st_32x32b_x16(s_at + (uint32_t)(16 * c), *reinterpret_cast<const uint32_t(*)[16]>(&s[c]));
             ptx::tmem_st_wait();
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&S->p_ready[q]);
+            take_scales(it.t0 + i + 3);
         }
         if (ok && steps > 0) {
             ok = ptx::mbar_wait(&S->o_full[q], (uint32_t)(steps - 1) & 1u, kATimeoutNs);
@@ -485,6 +535,8 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             const int hq = it.h * p.G + (it.r0 + row) - tok * p.G;
             const size_t x = (size_t)(it.x0 + tok);
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            const bool nans = *reinterpret_cast<volatile int *>(&S->any_nan);
+#pragma unroll 2
             for (int c = 0; c < p.D; c += 16) {
                 uint32_t o[16];
                 if (steps > 0) {
@@ -498,7 +550,12 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
                 float f[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
-                    f[j] = lim > S->nan_min[c + j] ? NAN : sum == 0.f ? 0.f : __uint_as_float(o[j]);
+                    f[j] = sum == 0.f ? 0.f : __uint_as_float(o[j]);
+                if (nans) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (lim > S->nan_min[c + j]) f[j] = NAN;
+                }
                 if (!real) continue;
                 if (splits == 1) {
                     uint32_t w[8];
