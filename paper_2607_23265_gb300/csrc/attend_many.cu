@@ -11,13 +11,14 @@
 //                                                take the place of S), V from shared memory
 // The codes of K go to the tensor cores as they are.  Those of V are converted to
 // f16 once for both row tiles, because weights in f16 need no second number: 11
-// bits, and relative to the running maximum a range of 2^-32, so that the many small
-// weights of a long context are not lost beside one large one.  The scales of V's
+// bits down to 2^-17 of the running maximum and steps of 2^-27 of it below, so that
+// the many small weights of a long context are not lost beside one large one.  The scales of V's
 // pages multiply the weights, those of K's the logits, one of each for 16 tokens.
 // A thread of warps 0-7 has one row: maximum, weights and sum need no other lane.
 // The maximum that weights are relative to follows the true one only when that is
-// 2^8 above it: the tile's weights are formed without waiting for its maximum, and
-// where it turns out so O is rescaled in tensor memory and they are formed again.
+// 2^12 above it (2^8: one tile in five of logits of a few units, a fifth of the time):
+// the tile's weights are formed without waiting for its maximum, and where it turns
+// out so O is rescaled in tensor memory and they are formed again.
 //   warps 0-3, 4-7  weights of row tile 0, 1
 //   warps 8-11      V to f16
 //   warps 12, 14    TMA producers: rings of K and of V tiles
@@ -37,8 +38,8 @@ namespace {
 constexpr int kMThreads = 16 * 32;   // four warpgroups; two warps of the last have nothing to do
 constexpr int kMKStages = 3, kMVStages = 2;
 constexpr int kMTmem = 512;
-constexpr float kMTop = 7.f;     // a row's largest weight is about 2^7 ..
-constexpr float kMSlack = 8.f;   // .. and at most 2^15, below f16's largest
+constexpr float kMTop = 3.f;     // a row's largest weight is about 2^3 ..
+constexpr float kMSlack = 12.f;  // .. and at most 2^15, below f16's largest
 
 struct ManyShared {
     uint64_t k_full[kMKStages], k_empty[kMKStages], v_full[kMVStages], v_empty[kMVStages];
