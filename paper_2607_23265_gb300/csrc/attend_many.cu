@@ -65,12 +65,15 @@ struct ManyItem {
 };
 
 __device__ __forceinline__ bool many_item(const AttendParams &p, int row_tiles, int splits, int idx, ManyItem *it) {
-    const int s = idx % splits;
-    idx /= splits;
-    it->h = idx % p.heads;
-    idx /= p.heads;
-    it->b = idx % p.B;
-    const int rt = row_tiles - 1 - idx / p.B;   // the longest rows of causal calls first
+    uint32_t at = (uint32_t)idx, s = 0;
+    if (splits > 1) {
+        s = at % (uint32_t)splits;
+        at /= (uint32_t)splits;
+    }
+    it->h = (int)(at % (uint32_t)p.heads);
+    at /= (uint32_t)p.heads;
+    it->b = p.B > 1 ? (int)(at % (uint32_t)p.B) : 0;
+    const int rt = row_tiles - 1 - (int)(p.B > 1 ? at / (uint32_t)p.B : at);   // the longest rows of causal calls first
     const int2 len = attend_lengths(p, it->b);
     const int64_t rows = (int64_t)len.x * p.G;
     if ((int64_t)rt * kManyRows >= rows) return false;
@@ -80,9 +83,9 @@ __device__ __forceinline__ bool many_item(const AttendParams &p, int row_tiles, 
     it->r0 = rt * kManyRows;
     it->r1 = (int)min(rows, (int64_t)it->r0 + kManyRows);
     const int most = min(it->kv, attend_visible(p, (it->r1 - 1) / p.G, it->n, it->kv));
-    const int64_t tiles = (most + kATile - 1) / kATile;
-    it->t0 = (int)(tiles * s / splits);
-    it->t1 = (int)(tiles * (s + 1) / splits);
+    const uint32_t tiles = (uint32_t)(most + kATile - 1) / kATile;   // below 2^24, splits at most 32
+    it->t0 = splits > 1 ? (int)(tiles * s / (uint32_t)splits) : 0;
+    it->t1 = splits > 1 ? (int)(tiles * (s + 1) / (uint32_t)splits) : (int)tiles;
     return true;
 }
 
@@ -424,10 +427,11 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
                 uint32_t hi[4], lo[4];
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
-                    const float a = __uint_as_float(w[u] << 16) * up, b = __uint_as_float(w[u] & 0xFFFF0000u) * up;
-                    const uint32_t c = e4m3x2(a, b);
-                    const float2 f = __half22float2(half2_of_e4m3((uint16_t)c));
-                    const uint32_t d = e4m3x2(a - f.x, b - f.y);
+                    // f16 holds the 8 bits of a bf16 number, and what the code leaves of it
+                    const __half2 x = __floats2half2_rn(__uint_as_float(w[u] << 16) * up,
+                                                        __uint_as_float(w[u] & 0xFFFF0000u) * up);
+                    const uint32_t c = e4m3x2(x);
+                    const uint32_t d = e4m3x2(__hsub2(x, half2_of_e4m3((uint16_t)c)));
                     hi[u / 2] = u % 2 ? hi[u / 2] | c << 16 : c;
                     lo[u / 2] = u % 2 ? lo[u / 2] | d << 16 : d;
                 }
@@ -537,43 +541,65 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             const size_t x = (size_t)(it.x0 + tok);
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
             const bool nans = *reinterpret_cast<volatile int *>(&S->any_nan);
-#pragma unroll 2
-            for (int c = 0; c < p.D; c += 16) {
-                uint32_t o[16];
-                if (steps > 0) {
-                    ptx::tmem_ld_32x32b_x16(o_at + (uint32_t)c, o);
-                    ptx::tmem_ld_wait();
-                    ptx::reg_fence16(o);
-                } else {
+            uint32_t o[4][32];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) o[j] = 0;
+            for (int c = 0; c < 4; ++c)
+                if (32 * c < p.D) ptx::tmem_ld_32x32b_x32(o_at + (uint32_t)(32 * c), o[c]);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int c = 0; c < 4; ++c) ptx::reg_fence32(o[c]);
+            // Rows go through shared memory (the queries' place: their products are complete),
+            // 256 bytes a row at a time, so that a warp's stores are whole rows: row by row of
+            // its own a thread takes ten times as long.
+            uint8_t *stage = qs + (size_t)(q * 2) * kATileBytes + (size_t)(warp & 3) * 32 * 256;
+            auto flush = [&](void *dst, int bytes) {   // dst: where this thread's row goes, or null
+                __syncwarp();
+                const unsigned long long mine = reinterpret_cast<unsigned long long>(dst);
+#pragma unroll 4
+                for (int k = 0; k < 16; ++k) {
+                    const int r = 2 * k + (lane >> 4), c = lane & 15;
+                    const unsigned long long to = __shfl_sync(0xFFFFFFFFu, mine, r);
+                    if (to && 16 * c < bytes)
+                        *reinterpret_cast<uint4 *>(to + 16 * c) =
+                            *reinterpret_cast<const uint4 *>(stage + r * 256 + ((c ^ (r & 15)) << 4));
                 }
-                float f[16];
+                __syncwarp();
+            };
+            auto put = [&](int c, uint4 v) {           // 16 bytes of this thread's row
+                *reinterpret_cast<uint4 *>(stage + lane * 256 + ((c ^ (lane & 15)) << 4)) = v;
+            };
+            if (sum == 0.f || nans) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    f[j] = sum == 0.f ? 0.f : __uint_as_float(o[j]);
-                if (nans) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (lim > S->nan_min[c + j]) f[j] = NAN;
+                for (int j = 0; j < 128; ++j) {
+                    if (sum == 0.f) o[j / 32][j % 32] = 0;
+                    if (lim > S->nan_min[j]) o[j / 32][j % 32] = __float_as_uint(NAN);
                 }
-                if (!real) continue;
-                if (splits == 1) {
-                    uint32_t w[8];
+            }
+            if (splits == 1) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * j] * inv, f[2 * j + 1] * inv);
+                for (int c = 0; c < 16; ++c) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const __nv_bfloat162 v =
+                            __floats2bfloat162_rn(__uint_as_float(o[c / 4][8 * (c % 4) + 2 * j]) * inv,
+                                                  __uint_as_float(o[c / 4][8 * (c % 4) + 2 * j + 1]) * inv);
                         w[j] = *reinterpret_cast<const uint32_t *>(&v);
                     }
-                    if (wz_in_range(p.status, x < (size_t)p.T)) {
-                        uint4 *d = reinterpret_cast<uint4 *>(p.out + x * p.out_stride + (size_t)hq * p.D + c);
-                        d[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                        d[1] = make_uint4(w[4], w[5], w[6], w[7]);
-                    }
-                } else {
-                    float4 *d = reinterpret_cast<float4 *>(p.part + ((size_t)blockIdx.x * kManyRows + row) * 128 + c);
+                    put(c, make_uint4(w[0], w[1], w[2], w[3]));
+                }
+                const bool in = wz_in_range(p.status, !real || x < (size_t)p.T) && real;
+                flush(in ? p.out + x * p.out_stride + (size_t)hq * p.D : nullptr, 2 * p.D);
+            } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) d[j] = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+                for (int part = 0; part < 2; ++part) {
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        const uint32_t *f = &o[2 * part + c / 8][4 * (c % 8)];
+                        put(c, make_uint4(f[0], f[1], f[2], f[3]));
+                    }
+                    float *to = p.part + ((size_t)blockIdx.x * kManyRows + row) * 128 + 64 * part;
+                    flush(real ? to : nullptr, 4 * (p.D - 64 * part));
                 }
             }
             if (real) {
