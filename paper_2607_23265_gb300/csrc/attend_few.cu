@@ -13,8 +13,8 @@
 // scale of V), so that their 8 bits never lose a tile whose weights are small
 // beside another's; each tile's O^T is read back and added in fp32 registers.
 //
-// Work is the list of all tiles of all (sequence, KV head) items, kItemCost more
-// for each item's start and end, cut into one contiguous range per CTA, so that any
+// Work is the list of all tiles of all (sequence, KV head) items, item_cost more for
+// each item's start and end, cut into one contiguous range per CTA, so that any
 // mixture of lengths keeps every SM busy; a range finds its first item by a scan
 // over the sequences' tile counts.  An item inside one range is finished there; the
 // pieces of others are written unnormalised, and attend_join_kernel adds them in
@@ -41,7 +41,6 @@ constexpr int kFMaxStages = 6;
 constexpr float kPTop = 8.f;   // log2 of a tile's largest weight
 
 constexpr int kWholeTiles = 8;   // tiles of a sequence up to which items are not cut
-constexpr int kItemCost = 1;     // tiles that an item's start and end take the time of
 
 // A piece of an item, as the weight warps see it.
 struct Piece {
@@ -76,6 +75,7 @@ struct FewShape {
     static constexpr int N = 2 * R;
     static constexpr int kStages = R == 8 ? 4 : 5;
     static constexpr int kCtas = R == 8 ? 3 : 2;      // per SM
+    static constexpr int kItemCost = R == 8 ? 2 : 5;  // tiles that an item's start and end take the time of
     static constexpr int kTmem = 4 * N;               // S and O, two buffers each
     static constexpr int kOpBytes = N * 128;          // q or p operand, two buffers each
     static constexpr size_t kSmem =
@@ -110,7 +110,7 @@ __device__ __forceinline__ int few_tiles(const AttendParams &p, int b) {
 
 // Units of an item of this many tiles: those that cost time or, whole, an answer.
 __device__ __forceinline__ int few_units(const AttendParams &p, int tiles) {
-    return tiles > 0 || (tiles == 0 && p.whole) ? tiles + kItemCost : 0;
+    return tiles > 0 || (tiles == 0 && p.whole) ? tiles + p.item_cost : 0;
 }
 
 // Sum of x over the threads before this one and over all, blockDim.x a multiple of 32.
@@ -190,8 +190,8 @@ private:
                 t1 = tiles;
                 if (unit == 0) return;
             } else {
-                t0 = max(unit - kItemCost, 0);
-                t1 = max((int)min((long long)unit + left, (long long)tiles + kItemCost) - kItemCost, 0);
+                t0 = max(unit - p.item_cost, 0);
+                t1 = max((int)min((long long)unit + left, (long long)tiles + p.item_cost) - p.item_cost, 0);
                 if (t1 > t0) return;
             }
         }
@@ -274,21 +274,26 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
         const int pages_tile = kATile / p.P, box = p.P * 128;
         const int absent = (int)(p.pages * p.heads);   // past the cache: zeros
         int seq = 0;                                   // copies issued: K, V, K, V, ..
-        for (; w.any && __all_sync(0xFFFFFFFFu, !*abort_flag); w.next(p)) {
-            const int kv = attend_lengths(p, w.b).y;
+        auto slab = [&](const Walk &u, int kv, int tile) {
+            const int t = tile * kATile + (lane << p.shift);
+            int pg = -1;
+            if (lane < pages_tile && tile < u.t1 && t < kv) pg = attend_page(p, u.b, t);
+            return pg < 0 ? absent : pg * p.heads + u.h;
+        };
+        int znext = absent;
+        if (w.any) znext = slab(w, attend_lengths(p, w.b).y, w.t0);
+        while (w.any && __all_sync(0xFFFFFFFFu, !*abort_flag)) {
+            const Walk now = w;
+            const int n = now.t1 - now.t0, kv = attend_lengths(p, now.b).y;
             bool ok = true;
-            const int n = w.t1 - w.t0;
-            int z = absent, znext = absent;
-            auto slab = [&](int tile) {
-                const int t = tile * kATile + (lane << p.shift);
-                int pg = -1;
-                if (lane < pages_tile && t < kv) pg = attend_page(p, w.b, t);
-                return pg < 0 ? absent : pg * p.heads + w.h;
-            };
-            znext = slab(w.t0);
+            int zafter = absent;                       // of the next piece's first tile
+            if (n == 0) {
+                w.next(p);
+                if (w.any) zafter = slab(w, attend_lengths(p, w.b).y, w.t0);
+            }
             for (int i = 0; i < n && ok; ++i) {
-                z = znext;
-                if (i + 1 < n) znext = slab(w.t0 + i + 1);
+                const int z = znext;
+                if (i + 1 < n) znext = slab(now, kv, now.t0 + i + 1);
                 for (int c = 0; c < 2; ++c, ++seq) {
                     const int st = seq % Sh::kStages;
                     ok = ptx::mbar_wait(&S->empty[st], ((uint32_t)(seq / Sh::kStages) & 1u) ^ 1u, kATimeoutNs);
@@ -303,8 +308,13 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                         ptx::tma_load_3d(ring + (size_t)st * kATileBytes + (size_t)lane * box, c ? &maps.v : &maps.k,
                                          &S->full[st], 0, 0, z, pol);
                 }
+                if (i == 0) {
+                    w.next(p);
+                    if (w.any) zafter = slab(w, attend_lengths(p, w.b).y, w.t0);
+                }
             }
             if (!ok) break;
+            znext = zafter;
         }
         for (int s = max(0, seq - Sh::kStages); s < seq; ++s)   // the copies have landed
             ptx::mbar_wait(&S->full[s % Sh::kStages], (uint32_t)(s / Sh::kStages) & 1u, kATimeoutNs);
@@ -328,7 +338,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                 }
                 return ok;
             };
-            for (; w.any && ok; w.next(p), ++item) {
+            for (; w.any && ok; ++item) {
                 const int n = w.t1 - w.t0;
                 if (!wait(&S->q_ready[item & 1], (uint32_t)(item >> 1) & 1u)) break;
                 const uint64_t bq = q_desc + (uint64_t)(item & 1) * (Sh::kOpBytes >> 4);
@@ -346,6 +356,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                         ptx::mma_commit(&S->empty[st]);
                         ptx::mma_commit(&S->s_full[k & 1]);
                     }
+                    if (i == 0) w.next(p);   // its loads run beside the first weights
                     if (i > 0) {
                         const int j = k - 1, seq = 2 * j + 1, st = seq % Sh::kStages;
                         if (!wait(&S->p_ready[j & 1], (uint32_t)(j >> 1) & 1u) ||
@@ -392,7 +403,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
             u.t0 = w.t0;
             u.t1 = w.t1;
             u.tiles = w.tiles;
-            u.first = w.item0 + kItemCost;
+            u.first = w.item0 + p.item_cost;
             u.kv = len.y;
             u.x0 = p.cu[u.b];
             u.rows = len.x * p.G;
@@ -786,6 +797,7 @@ cudaError_t launch_few(const AttendMaps &maps, AttendParams p, int max_new, int 
     const int64_t items = (int64_t)p.B * p.heads;
     const int64_t tiles = ((int64_t)p.max_pages * p.P + kATile - 1) / kATile;
     p.whole = tiles <= kWholeTiles;
+    p.item_cost = Sh::kItemCost;
     // no more CTAs than items or tiles there can be
     p.ctas = (int)std::min<int64_t>({(int64_t)sms * Sh::kCtas, kFewSlots / 2, p.whole ? items : items * tiles});
     void *args[] = {const_cast<AttendMaps *>(&maps), &p};

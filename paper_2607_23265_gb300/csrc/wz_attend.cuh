@@ -40,7 +40,7 @@ struct AttendParams {
     int T, B, Hq, heads, G, D, P, max_pages, causal;
     int shift;               // log2(P)
     int ctas;                // CTAs that share the work
-    int whole;               // attend_few: items are not cut
+    int whole, item_cost;    // attend_few: items are not cut; tiles that an item's start and end count as
     float scale2;            // scale * log2(e)
     int *status;
 };
