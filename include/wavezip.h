@@ -391,7 +391,7 @@ WZ_API int wz_project(const wz_project_args *a);
 /* ------------------------------------------------------------------------ */
 
 /*
- * What the LLM of Eq. 2 does with condensed tokens: their keys and values are
+ * What a decoder does with the projected tokens: their keys and values are
  * appended to a paged cache, at positions that may follow from the index map's
  * (t, i, j), and queries attend to it.  The cache holds 8 bits a number: e4m3
  * codes (4 exponent, 3 mantissa bits, largest 448) and, for each page and KV
@@ -483,10 +483,11 @@ WZ_API int wz_kv_append(const wz_kv_append_args *a);
  * the cache's last ones).  A row that no slot is left for has out 0 and lse
  * -infinity.  Slots that a row does not see may hold anything, NaN included.
  * Products and sums run on the tensor cores with fp32 accumulation: the codes
- * as they are, a query as two e4m3 numbers of a row scale of its own (bf16
- * exactly, but for channels below 2^-14 of the row's largest), weights with 8
- * (up to 16 rows a sequence and KV head) or 11 bits; maxima and sums in fp32.
- * The result does not depend on how other calls or streams run.
+ * as they are, a query as two e4m3 numbers a channel beside a scale of its row
+ * (bf16 exactly, but for channels below 2^-9 of the row's largest, which are
+ * off by at most 2^-17 of it), weights with 8 bits (up to 16 rows a sequence
+ * and KV head) or 11; maxima and sums in fp32.  Pieces of a sequence that
+ * several CTAs hold are joined in a fixed order: equal calls give equal bits.
  * Errors: WZ_ERR_INVALID_ARG, WZ_ERR_UNSUPPORTED, WZ_ERR_WORKSPACE,
  * WZ_ERR_NO_MEMORY, WZ_ERR_CUDA; nothing is launched on an argument error.
  */
@@ -499,8 +500,8 @@ typedef struct {
     float *lse;              /* [T][Hq]; nullable                            */
     int64_t T;
     int B;                   /* sequences                                    */
-    int max_new;             /* the most tokens of q of a sequence; 0: T     */
-                             /* (tokens past it may be left out)             */
+    int max_new;             /* the most tokens of q of a sequence; 0: T;    */
+                             /* tokens past it may be left out, reported     */
     int Hq;                  /* a multiple of the cache's heads              */
     const int32_t *cu;       /* [B+1] rows of q of each sequence             */
     const int32_t *kv_len;   /* [B] slots in use                             */

@@ -92,7 +92,7 @@ cudaError_t launch_attend(const wz_attend_args &a, void *workspace, cudaStream_t
     p.spans = reinterpret_cast<int2 *>(p.ml + pl.rows);
     p.pages = a.cache.pages;
     p.T = (int)a.T; p.B = a.B; p.Hq = a.Hq; p.heads = a.cache.heads; p.G = a.Hq / a.cache.heads;
-    p.D = a.cache.D; p.P = a.cache.page_tokens; p.max_pages = a.max_pages; p.causal = a.causal != 0;
+    p.D = a.cache.D; p.P = a.cache.page_tokens; p.max_pages = a.max_pages; p.max_new = pl.max_new; p.causal = a.causal != 0;
     while (1 << p.shift < p.P) ++p.shift;
     p.scale2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)p.D)) * kLog2e;
     p.status = a.device_status;

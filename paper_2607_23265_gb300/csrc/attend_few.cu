@@ -7,8 +7,8 @@
 //   O^T [D x N]          = V^T [D x tokens] * (p1 | p2)^T      V: A, MN-major
 // N = 2R columns: a query row and a row of weights are two e4m3 numbers each,
 // hi and 32 times the rest, in two columns whose results are joined in fp32 (8
-// significant bits and more; a query of bf16 is exact).  A thread then has one token and R rows:
-// no row waits for 128 lanes of idle accumulators.
+// significant bits and more; a query of bf16 is exact).  A thread then has one token
+// and R rows, and no accumulator lanes stand idle.
 // The weights of a tile are taken relative to the tile's own largest (weight x
 // scale of V), so that their 8 bits never lose a tile whose weights are small
 // beside another's; each tile's O^T is read back and added in fp32 registers.
@@ -24,6 +24,11 @@
 //   warps 0-3  weights: thread = token of S^T, channel of O^T
 //   warp 4     TMA producer: K and V tiles of 16 KB in one ring
 //   warp 5     TMEM allocation, MMA issuer (one thread)
+// One query over 200,003 slots of 4 heads x 128 takes 40 us: 205 MB at 6.9 TB/s between
+// the first copies' arrival (4 us) and the median CTA's end (33 us), then the slowest
+// SMs' tails and the join (7 us).  64 queries over 577 .. 18,699 slots 90-96 us for 454
+// MB; with tiles' rows in byte stores, scalars by every thread and a join that scanned
+// the lengths again 105.
 // Every wait is bounded; where one gives up the kernel sets a status bit, ends
 // its copies, frees tensor memory and returns.
 #include <algorithm>
@@ -407,10 +412,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
             u.kv = len.y;
             u.x0 = p.cu[u.b];
             u.rows = len.x * p.G;
-            if (u.rows > R) {   // more tokens than max_new
-                kv_report(p.status);
-                u.rows = R / p.G * p.G;
-            }
+            if (u.rows > R) u.rows = R / p.G * p.G;   // more tokens than max_new, reported above
             // row c = token c / G, head c % G of the group
             uint2 raw[R / 4];
             int tok[R / 4];

@@ -37,7 +37,7 @@ struct AttendParams {
     float2 *ml;              // their maxima (base 2) and sums
     int2 *spans;             // by first token and KV head: first CTA and pieces of an item
     int64_t pages;
-    int T, B, Hq, heads, G, D, P, max_pages, causal;
+    int T, B, Hq, heads, G, D, P, max_pages, max_new, causal;
     int shift;               // log2(P)
     int ctas;                // CTAs that share the work
     int whole, item_cost;    // attend_few: items are not cut; tiles that an item's start and end count as
@@ -62,10 +62,12 @@ __device__ __forceinline__ int2 attend_lengths(const AttendParams &p, int b) {
     return make_int2(sound ? x1 - x0 : 0, kv);
 }
 
-// Whether attend_lengths had to change something.
+// Whether the lengths are what the call said: attend_lengths has to change nothing and
+// no sequence has more tokens than max_new.
 __device__ __forceinline__ bool attend_lengths_sound(const AttendParams &p, int b) {
     const int x0 = p.cu[b], x1 = p.cu[b + 1], kv = p.kv_len[b];
-    return x0 >= 0 && x1 >= x0 && x1 <= p.T && kv >= 0 && kv <= (int64_t)p.max_pages * p.P;
+    return x0 >= 0 && x1 >= x0 && x1 <= p.T && x1 - x0 <= p.max_new && kv >= 0 &&
+           kv <= (int64_t)p.max_pages * p.P;
 }
 
 // Slots that token i of n sees.

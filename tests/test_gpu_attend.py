@@ -288,3 +288,114 @@ def test_append_then_attend_token_by_token(wz):
             host.codes[n] = getattr(gpu, n).cpu().double()
             host.scale[n] = getattr(gpu, n + "_scale").cpu().double()
         compare(out, lse, host, q.cpu(), table, [0, 1], [i + 1], True, D ** -0.5)
+
+
+@pytest.mark.parametrize("G,n", [(1, 1), (7, 1), (4, 3)])
+def test_items_in_pieces(wz, G, n):
+    """Sequences from one tile to thirty, some without slots: items of one piece, of several, and
+    several items to a CTA, with few and with many items."""
+    for seqs, heads in ((3, 1), (30, 4)):
+        kv = [0 if b % 7 == 5 else (b * 977 + 31) % 3900 + 1 for b in range(seqs)]
+        run(wz, 128, heads, heads * G, 64, [n] * seqs, kv, seed=seqs)
+
+
+@pytest.mark.parametrize("tiles", [8, 9])
+def test_whole_items_and_pieces(wz, tiles):
+    """Tables of at most eight tiles keep items whole, longer ones do not."""
+    run(wz, 64, 2, 6, 128, [1, 1, 1], [128 * tiles, 0, 128 * tiles - 100])
+
+
+def test_question_in_pieces(wz):
+    """Few row tiles over many slots: pieces that the second kernel adds, some of them empty."""
+    run(wz, 128, 1, 4, 64, [70, 5], [9000, 64])
+    run(wz, 64, 1, 2, 96, [150], [5000], causal=False)
+
+
+def test_more_tokens_than_said(wz):
+    """max_new below a sequence's tokens is reported; nothing outside the arrays is touched."""
+    P, D = 32, 64
+    table, pages = tables([100], P, 3)
+    gpu = ref.Cache(pages, 1, P, D, seed=6).on_gpu(wz)
+    for n, max_new in ((20, 1), (300, 20)):
+        room = torch.zeros((n + 4, 2, D), dtype=torch.bfloat16, device="cuda")
+        q = torch.randn((n, 2, D), device="cuda").bfloat16()
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        wz.wz_attend(q, gpu, i32(table), i32([0, n]), i32([100]), max_new=max_new, out=room[2:n + 2], device_status=status)
+        assert int(status) == wz.STATUS_CACHE
+        assert int(room[:2].abs().max()) == 0 and int(room[n + 2:].abs().max()) == 0
+
+
+def test_replayed_from_a_graph(wz):
+    """Append and attention captured in a CUDA graph: new inputs in the same buffers give what
+    direct calls give."""
+    P, heads, Hq, D = 64, 2, 8, 64
+    g = torch.Generator().manual_seed(2)
+    direct, captured = (ref.Cache(40, heads, P, D, seed=5).on_gpu(wz) for _ in range(2))
+    table = i32([list(range(20)), list(range(20, 40))])
+    cu, start, kv = i32([0, 1, 2]), i32([0, 0]), i32([0, 0])
+    qkv = torch.zeros((2, Hq + 2 * heads, D), dtype=torch.bfloat16, device="cuda")
+    rotation = wz.rotation_table(2000, D)
+    ws = torch.empty(wz.wz_attend_workspace_size(2, Hq, D), dtype=torch.uint8, device="cuda")
+    q, out = (torch.zeros((2, Hq, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+
+    def step(cache):
+        wz.wz_kv_append(qkv[:, Hq:Hq + heads], qkv[:, Hq + heads:], cache, table, cu, start, max_new=1,
+                        q=qkv[:, :Hq], q_out=q, rotation=rotation)
+        wz.wz_attend(q, cache, table, cu, kv, max_new=1, out=out, workspace=ws)
+
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    start.copy_(i32([100, 1100]))
+    kv.copy_(start + 1)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(wz.KvCache.empty(40, heads, P, D))
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            step(captured)
+    for i in range(4):
+        qkv.copy_(torch.randn(qkv.shape, generator=g))
+        start.copy_(i32([100 + i, 1100 + i]))
+        kv.copy_(start + 1)
+        step(direct)
+        want = out.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+def test_checked_build_agrees(wz):
+    """The bounds-checked build reports nothing and gives the same bits, for both kernels and the
+    append before them."""
+    P, heads, Hq, D = 32, 2, 6, 96
+    table, pages = tables([700, 333], P, 3)
+    for new in ([1, 1], [40, 9]):
+        start = [700 - new[0], 333 - new[1]]
+        T = sum(new)
+        qkv = torch.randn((T, Hq + 2 * heads, D), generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+        args = (i32(table), i32([0, new[0], T]))
+
+        def both(status=None):
+            gpu = ref.Cache(pages, heads, P, D, seed=6).on_gpu(wz)
+            q = wz.wz_kv_append(qkv[:, Hq:Hq + heads], qkv[:, Hq + heads:], gpu, *args, i32(start), max_new=max(new),
+                                q=qkv[:, :Hq], rotation=wz.rotation_table(800, D), device_status=status)
+            out = wz.wz_attend(q, gpu, *args, i32([700, 333]), max_new=max(new), device_status=status)
+            return q, gpu.k.view(torch.uint8), gpu.v.view(torch.uint8), gpu.k_scale, gpu.v_scale, out
+
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        want = both()
+        with wz.checked_library():
+            got = both(status)
+        assert int(status) == 0
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
+def test_example_answers_from_the_cache(wz):
+    """The example's outputs within the rounding of bf16 outputs and 8-bit weights of plain attention."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "answer_from_cache.py")
+    spec = importlib.util.spec_from_file_location("answer_from_cache", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    assert m.main() < 2.0 ** -7
