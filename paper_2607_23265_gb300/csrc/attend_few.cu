@@ -45,7 +45,10 @@ constexpr int kFThreads = 192;
 constexpr int kFMaxStages = 6;
 constexpr float kPTop = 8.f;   // log2 of a tile's largest weight
 
-constexpr int kWholeTiles = 8;   // tiles of a sequence up to which items are not cut
+// Tiles of a sequence up to which items are not cut.  741 slots (six tiles) of 4 KV heads
+// through the binding: 10.0 us in pieces, 11.8 whole; a tile more takes a CTA 1 us, the
+// second kernel 4 us of the device's time and 2 of the host's.
+constexpr int kWholeTiles = 4;
 
 // A piece of an item, as the weight warps see it.
 struct Piece {
@@ -799,7 +802,8 @@ cudaError_t launch_few(const AttendMaps &maps, AttendParams p, int max_new, int 
     const int64_t items = (int64_t)p.B * p.heads;
     const int64_t tiles = ((int64_t)p.max_pages * p.P + kATile - 1) / kATile;
     p.whole = tiles <= kWholeTiles;
-    p.item_cost = Sh::kItemCost;
+    // 0: a CTA for each tile; whole items have at least the unit that an empty one is found by
+    p.item_cost = p.whole || items * tiles > (int64_t)sms * Sh::kCtas ? Sh::kItemCost : 0;
     // no more CTAs than items or tiles there can be
     p.ctas = (int)std::min<int64_t>({(int64_t)sms * Sh::kCtas, kFewSlots / 2, p.whole ? items : items * tiles});
     void *args[] = {const_cast<AttendMaps *>(&maps), &p};

@@ -299,9 +299,9 @@ def test_items_in_pieces(wz, G, n):
         run(wz, 128, heads, heads * G, 64, [n] * seqs, kv, seed=seqs)
 
 
-@pytest.mark.parametrize("tiles", [8, 9])
+@pytest.mark.parametrize("tiles", [4, 5, 8, 9])
 def test_whole_items_and_pieces(wz, tiles):
-    """Tables of at most eight tiles keep items whole, longer ones do not."""
+    """Tables of few tiles keep items whole, longer ones do not."""
     run(wz, 64, 2, 6, 128, [1, 1, 1], [128 * tiles, 0, 128 * tiles - 100])
 
 
