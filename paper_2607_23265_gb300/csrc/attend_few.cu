@@ -209,7 +209,10 @@ private:
 
 }  // namespace
 
-template <int R>
+// R: rows that the operands have room for (N = 16 columns is the least for M = 128); U: rows
+// that a call can have.  A row alone (single tokens, no grouped heads) is its own variant: 16
+// sequences of up to 4,098 slots, 16 heads x 64, take 24 us so and 27 with eight rows' weights.
+template <int R, int U>
 __global__ void __launch_bounds__(kFThreads, FewShape<R>::kCtas)
 attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant__ AttendParams p) {
     using Sh = FewShape<R>;
@@ -415,7 +418,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
             u.kv = len.y;
             u.x0 = p.cu[u.b];
             u.rows = len.x * p.G;
-            if (u.rows > R) u.rows = R / p.G * p.G;   // more tokens than max_new, reported above
+            if (u.rows > U) u.rows = U / p.G * p.G;   // more tokens than max_new, reported above
             // row c = token c / G, head c % G of the group
             uint2 raw[R / 4];
             int tok[R / 4];
@@ -463,9 +466,9 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
             const int minlim = cur.minlim, maxlim = cur.maxlim, ib = item & 1;
             const bool whole = n == cur.tiles;
 
-            float acc[R], l[R], run = -INFINITY;   // run: lane c's maximum of row c so far
+            float acc[U], l[U], run = -INFINITY;   // run: lane c's maximum of row c so far
 #pragma unroll
-            for (int c = 0; c < R; ++c) acc[c] = l[c] = 0.f;
+            for (int c = 0; c < U; ++c) acc[c] = l[c] = 0.f;
 
             auto read_output = [&](int kk) {   // O^T of tile kk into the sums
                 ok = ptx::mbar_wait(&S->o_full[kk & 1], (uint32_t)(kk >> 1) & 1u, kATimeoutNs) && ok;
@@ -478,12 +481,12 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
 #pragma unroll
                 for (int j = 0; j < N / 16; ++j) ptx::reg_fence16(o[j]);
 #pragma unroll
-                for (int c = 0; c < R; c += 4) {
+                for (int c = 0; c < U; c += 4) {
                     const float4 al = *reinterpret_cast<const float4 *>(&S->alpha[warp][kk & 1][c]);
                     const float4 be = *reinterpret_cast<const float4 *>(&S->beta[warp][kk & 1][c]);
                     const float a4[4] = {al.x, al.y, al.z, al.w}, b4[4] = {be.x, be.y, be.z, be.w};
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
+                    for (int u = 0; u < 4 && c + u < U; ++u) {
                         const int c1 = c + u, c2 = R + c + u;
                         const float sum = fmaf(__uint_as_float(o[c2 / 16][c2 % 16]), 1.f / kRest,
                                                __uint_as_float(o[c1 / 16][c1 % 16]));
@@ -503,7 +506,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
 
                 ok = ptx::mbar_wait(&S->s_full[k & 1], (uint32_t)(k >> 1) & 1u, kATimeoutNs) && ok;
                 ptx::tc_fence_after();
-                float x[R];
+                float x[U];
                 {
                     uint32_t s[N / 16][16];
 #pragma unroll
@@ -512,14 +515,14 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                     ptx::tmem_ld_wait();
 #pragma unroll
                     for (int j = 0; j < N / 16; ++j) ptx::reg_fence16(s[j]);
-                    float rf[R];
+                    float rf[(U + 3) / 4 * 4];
 #pragma unroll
-                    for (int c = 0; c < R; c += 4)
+                    for (int c = 0; c < U; c += 4)
                         *reinterpret_cast<float4 *>(&rf[c]) = *reinterpret_cast<const float4 *>(&S->rowf[ib][c]);
                     // base-2 logit + log2 of V's scale: the weight of a code of V
                     const float lv = pg_now < 0 ? -INFINITY : __log2f(sc_now.y);
 #pragma unroll
-                    for (int c = 0; c < R; ++c) {
+                    for (int c = 0; c < U; ++c) {
                         const int c2 = R + c;
                         const float dot = fmaf(__uint_as_float(s[c2 / 16][c2 % 16]), 1.f / kRest,
                                                __uint_as_float(s[c / 16][c % 16]));
@@ -528,21 +531,22 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                 }
                 if ((tile + 1) * kATile > minlim) {
 #pragma unroll
-                    for (int c = 0; c < R; ++c)
+                    for (int c = 0; c < U; ++c)
                         if (t >= S->lim[ib][c]) x[c] = -INFINITY;
                 }
                 float(*wm)[R] = S->wmax[k & 1];
 #pragma unroll
-                for (int c = 0; c < R; c += 4) {
-                    const float4 m = make_float4(warp_max(x[c]), warp_max(x[c + 1]), warp_max(x[c + 2]),
-                                                 warp_max(x[c + 3]));
-                    if (lane == 0) *reinterpret_cast<float4 *>(&wm[warp][c]) = m;
+                for (int c = 0; c < U; c += 4) {
+                    float m[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) m[u] = c + u < U ? warp_max(x[(c + u) % U]) : -INFINITY;
+                    if (lane == 0) *reinterpret_cast<float4 *>(&wm[warp][c]) = make_float4(m[0], m[1], m[2], m[3]);
                 }
                 ok = all_agree(ok);
                 if (!ok) break;
-                uint32_t codes[N / 4];
+                uint32_t codes[N / 4] = {};
 #pragma unroll
-                for (int c = 0; c < R; c += 4) {
+                for (int c = 0; c < U; c += 4) {
                     float m4[4];
                     *reinterpret_cast<float4 *>(m4) = *reinterpret_cast<const float4 *>(&wm[0][c]);
 #pragma unroll
@@ -555,13 +559,13 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                     }
                     uint32_t hi = 0, lo = 0;
 #pragma unroll
-                    for (int u = 0; u < 4; u += 2) {
+                    for (int u = 0; u < 4 && c + u < U; u += 2) {
                         // relative to the tile's largest, which becomes 2^kPTop
 #pragma unroll
-                        for (int v = u; v < u + 2; ++v)
+                        for (int v = u; v < u + 2 && c + v < U; ++v)
                             x[c + v] = ex2(x[c + v] - ((m4[v] == -INFINITY ? 0.f : m4[v]) - kPTop));
                         // number and rest in f16, whose 11 bits hold both
-                        const __half2 wt = __floats2half2_rn(x[c + u], x[c + u + 1]);
+                        const __half2 wt = __floats2half2_rn(x[c + u], c + u + 1 < U ? x[(c + u + 1) % U] : 0.f);
                         const uint32_t q = e4m3x2(wt);
                         const __half2 rest = __hfma2(half2_of_e4m3((uint16_t)q), __float2half2_rn(-kRest),
                                                      __hmul2(wt, __float2half2_rn(kRest)));
@@ -604,7 +608,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&S->p_ready[k & 1]);
                 // sums, while the products run
-                if (lane < R) {
+                if (lane < U) {
                     const float m = fmaxf(fmaxf(wm[0][lane], wm[1][lane]), fmaxf(wm[2][lane], wm[3][lane]));
                     const float top = fmaxf(run, m), to = top == -INFINITY ? 0.f : top;
                     S->alpha[warp][k & 1][lane] = ex2(run - to);
@@ -614,13 +618,13 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                 __syncwarp();
                 const float inv_v = pg_now < 0 ? 0.f : __frcp_rn(sc_now.y);
 #pragma unroll
-                for (int c = 0; c < R; c += 4) {
+                for (int c = 0; c < U; c += 4) {
                     const float4 al = *reinterpret_cast<const float4 *>(&S->alpha[warp][k & 1][c]);
                     const float4 be = *reinterpret_cast<const float4 *>(&S->beta[warp][k & 1][c]);
-                    l[c] = fmaf(l[c], al.x, x[c] * inv_v * be.x);
-                    l[c + 1] = fmaf(l[c + 1], al.y, x[c + 1] * inv_v * be.y);
-                    l[c + 2] = fmaf(l[c + 2], al.z, x[c + 2] * inv_v * be.z);
-                    l[c + 3] = fmaf(l[c + 3], al.w, x[c + 3] * inv_v * be.w);
+                    const float a4[4] = {al.x, al.y, al.z, al.w}, b4[4] = {be.x, be.y, be.z, be.w};
+#pragma unroll
+                    for (int u = 0; u < 4 && c + u < U; ++u)
+                        l[c + u] = fmaf(l[c + u], a4[u], x[c + u] * inv_v * b4[u]);
                 }
                 if (i > 0) read_output(k - 1);
                 if (i == 0) {   // the next item's first products follow this one's last
@@ -641,7 +645,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
             }
             // sums over the tokens: halves of the rows change lanes until a lane has one row
 #pragma unroll
-            for (int half = R / 2, d = 16; half; half >>= 1, d >>= 1) {
+            for (int half = U / 2, d = 16; half; half >>= 1, d >>= 1) {
                 const bool up = lane & d;
 #pragma unroll
                 for (int c = 0; c < half; ++c) {
@@ -650,14 +654,14 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                 }
             }
 #pragma unroll
-            for (int d = 16 / R; d; d >>= 1) l[0] += __shfl_xor_sync(0xFFFFFFFFu, l[0], d);
-            if (lane % (32 / R) == 0) S->lsum[warp][lane / (32 / R)] = l[0];
+            for (int d = 16 / U; d; d >>= 1) l[0] += __shfl_xor_sync(0xFFFFFFFFu, l[0], d);
+            if (lane % (32 / U) == 0) S->lsum[warp][lane / (32 / U)] = l[0];
             ok = all_agree(ok);
             if (!ok) break;
             const uint32_t nan_at = S->nan_bits[tid >> 1] >> (16 * (tid & 1)) & 0xFFFFu;
             const size_t slot = 2 * (size_t)blockIdx.x + (cur.t0 == 0 ? 1 : 0);
             // lane c: the sum of row c, its reciprocal for all lanes
-            const int cl = lane % R;
+            const int cl = lane % U;
             const float L = (S->lsum[0][cl] + S->lsum[1][cl]) + (S->lsum[2][cl] + S->lsum[3][cl]);
             const float inv_mine = L == 0.f ? 0.f : 1.f / L;
             if (warp == 0 && lane < rows) {
@@ -668,7 +672,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                         L == 0.f ? -INFINITY : (run + log2f(L)) * kLn2;
             }
 #pragma unroll
-            for (int c = 0; c < R; ++c) {
+            for (int c = 0; c < U; ++c) {
                 const float inv = __shfl_sync(0xFFFFFFFFu, inv_mine, c);
                 if (c >= rows) continue;
                 float o = acc[c];
@@ -794,10 +798,10 @@ __global__ void __launch_bounds__(512) attend_join_kernel(const __grid_constant_
 
 namespace {
 
-template <int R>
+template <int R, int U>
 cudaError_t launch_few(const AttendMaps &maps, AttendParams p, int max_new, int sms, cudaStream_t s) {
     using Sh = FewShape<R>;
-    cudaError_t e = allow_smem((const void *)attend_few_kernel<R>, Sh::kSmem);
+    cudaError_t e = allow_smem((const void *)attend_few_kernel<R, U>, Sh::kSmem);
     if (e != cudaSuccess) return e;
     const int64_t items = (int64_t)p.B * p.heads;
     const int64_t tiles = ((int64_t)p.max_pages * p.P + kATile - 1) / kATile;
@@ -807,7 +811,7 @@ cudaError_t launch_few(const AttendMaps &maps, AttendParams p, int max_new, int 
     // no more CTAs than items or tiles there can be
     p.ctas = (int)std::min<int64_t>({(int64_t)sms * Sh::kCtas, kFewSlots / 2, p.whole ? items : items * tiles});
     void *args[] = {const_cast<AttendMaps *>(&maps), &p};
-    e = launch_kernel((const void *)attend_few_kernel<R>, dim3(p.ctas), dim3(kFThreads), Sh::kSmem, s, args, true);
+    e = launch_kernel((const void *)attend_few_kernel<R, U>, dim3(p.ctas), dim3(kFThreads), Sh::kSmem, s, args, true);
     if (e != cudaSuccess || p.whole) return e;
     void *jargs[] = {&p};
     const bool by_row = p.ctas <= 8 * items;   // a batch of pieces to an item, if all are alike
@@ -819,8 +823,10 @@ cudaError_t launch_few(const AttendMaps &maps, AttendParams p, int max_new, int 
 }  // namespace
 
 cudaError_t launch_attend_few(const AttendMaps &maps, const AttendParams &p, int max_new, int sms, cudaStream_t s) {
-    return (int64_t)max_new * p.G <= 8 ? launch_few<8>(maps, p, max_new, sms, s)
-                                       : launch_few<16>(maps, p, max_new, sms, s);
+    const int64_t rows = (int64_t)max_new * p.G;
+    return rows <= 1   ? launch_few<8, 1>(maps, p, max_new, sms, s)
+           : rows <= 8 ? launch_few<8, 8>(maps, p, max_new, sms, s)
+                       : launch_few<16, 16>(maps, p, max_new, sms, s);
 }
 
 }  // namespace wz

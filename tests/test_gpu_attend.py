@@ -299,6 +299,12 @@ def test_items_in_pieces(wz, G, n):
         run(wz, 128, heads, heads * G, 64, [n] * seqs, kv, seed=seqs)
 
 
+@pytest.mark.parametrize("D,P", [(64, 16), (128, 64)])
+def test_one_row(wz, D, P):
+    """Single tokens of heads that share nothing: one row a sequence and head."""
+    run(wz, D, 16, 16, P, [1] * 9, [1, 2, 127, 128, 129, 0, 640, 4098, 1025], seed=D)
+
+
 @pytest.mark.parametrize("tiles", [4, 5, 8, 9])
 def test_whole_items_and_pieces(wz, tiles):
     """Tables of few tiles keep items whole, longer ones do not."""
