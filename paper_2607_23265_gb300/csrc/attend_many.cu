@@ -25,14 +25,18 @@
 //   warps 12, 14    TMA producers: rings of K and of V tiles
 //   warp 13         TMEM allocation, MMA issuer (one thread)
 // Tensor memory: S (then W) of the tiles in columns 0 and 128, O in 256 and 384.
-// A prompt of 6,151 tokens of 28 heads x 128 takes 290 us (940 TFLOP/s): 4,100 cycles for
+// A prompt of 6,151 tokens of 28 heads x 128 takes 262 us (1,035 TFLOP/s): 4,100 cycles for
 // each 256 x 128 block, of which a row tile's chain is 300 to read S, 1,200 to 1,900 to
 // form the weights (floor of both tiles' exponentials on an SM sub-partition: 1,300), 400
-// to store them, and 600 + 600 in its products; starts and ends of CTAs are a sixth.
-// Measured slower: halves of 64 tokens with the logits one half ahead (342: N = 64
-// products cost what N = 128 cost), two threads to a row (301).
+// to store them, and 600 + 600 in its products; then starts and ends of CTAs.  What these
+// cost: queries loaded under a condition, each load behind the one before, 7,000 cycles; the
+// first tile's weights formed twice 2,500; columns hidden one by one, logit and weight,
+// 4,000 a tile (292 us with all three).
+// Measured slower, against 290: halves of 64 tokens with the logits one half ahead (342: N =
+// 64 products cost what N = 128 cost), two threads to a row (301).
 // Every wait is bounded; where one gives up the kernel sets a status bit, ends its
 // copies, frees tensor memory and returns.
+#include <cfloat>
 #include <cstring>
 #include <type_traits>
 
@@ -109,36 +113,57 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
     return r;
 }
 
-// A row's 128 logits to weights in f16, 16 to the first half of each s[c]; lanes 0-7
-// hold the scales of 16 tokens each.  top: the largest logit with its weight of V,
-// add: the weights' sum.  MIXED: columns from `rel` on are not seen.
-template <bool MIXED>
-__device__ __forceinline__ void weights(uint32_t (&s)[4][32], float my_k, float my_lv, float my_inv, float rowf,
-                                        float base, int rel, float &top, float &add) {
+// Columns from rel on are not seen: logits of -infinity.
+__device__ __forceinline__ void hide(uint32_t (&s)[4][32], int rel) {
 #pragma unroll
     for (int g = 0; g < 8; ++g) {
+        if (!__any_sync(0xFFFFFFFFu, 16 * g + 16 > rel)) continue;
         uint32_t *x = s[g / 2] + 16 * (g % 2);
-        if (MIXED) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (16 * g + j >= rel) x[j] = __float_as_uint(-3e38f);
-        }
-        const float a = __shfl_sync(0xFFFFFFFFu, my_k, g) * rowf, lv = __shfl_sync(0xFFFFFFFFu, my_lv, g);
-        float m = max3(x[0], x[1], x[2]);
+        for (int j = 0; j < 16; ++j)
+            if (16 * g + j >= rel) x[j] = 0xFF800000u;
+    }
+}
+
+// Factor of 16 columns' logits: not 0, for those of -infinity.
+__device__ __forceinline__ float factor(float k, float rowf) {
+    const float a = k * rowf;
+    return a == 0.f ? FLT_MIN : a;
+}
+
+// The largest of 16 logits.
+__device__ __forceinline__ float max16(const uint32_t *x) {
+    float m = max3(x[0], x[1], x[2]);
 #pragma unroll
-        for (int j = 3; j < 15; j += 2) m = max3(__float_as_uint(m), x[j], x[j + 1]);
-        m = fmaxf(m, __uint_as_float(x[15]));
-        top = fmaxf(top, fmaf(m, a, lv));
+    for (int j = 3; j < 15; j += 2) m = max3(__float_as_uint(m), x[j], x[j + 1]);
+    return fmaxf(m, __uint_as_float(x[15]));
+}
+
+// A row's largest logit with its weight of V; lanes 0-7 hold the scales of 16 tokens each.
+__device__ __forceinline__ float largest(const uint32_t (&s)[4][32], float my_k, float my_lv, float rowf) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int g = 0; g < 8; ++g)
+        top = fmaxf(top, fmaf(max16(s[g / 2] + 16 * (g % 2)), factor(__shfl_sync(0xFFFFFFFFu, my_k, g), rowf),
+                              __shfl_sync(0xFFFFFFFFu, my_lv, g)));
+    return top;
+}
+
+// A row's 128 logits to weights in f16, 16 to the first half of each s[c].  top: as
+// above, add: the weights' sum.
+__device__ __forceinline__ void weights(uint32_t (&s)[4][32], float my_k, float my_lv, float my_inv, float rowf,
+                                        float base, float &top, float &add) {
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+        const uint32_t *x = s[g / 2] + 16 * (g % 2);
+        const float a = factor(__shfl_sync(0xFFFFFFFFu, my_k, g), rowf), lv = __shfl_sync(0xFFFFFFFFu, my_lv, g);
+        top = fmaxf(top, fmaf(max16(x), a, lv));
         const f2_t a2 = pack2(a, a), off2 = pack2(lv + base, lv + base);
         f2_t part[2] = {0, 0};   // zeros
 #pragma unroll
         for (int j = 0; j < 16; j += 2) {
             const float2 v = unpack2(fma2(pack2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), a2, off2));
-            float w0 = ex2(v.x), w1 = ex2(v.y);
-            if (MIXED) {
-                if (16 * g + j >= rel) w0 = 0.f;
-                if (16 * g + j + 1 >= rel) w1 = 0.f;
-            }
+            const float w0 = ex2(v.x), w1 = ex2(v.y);
             part[(j / 2) % 2] = add2(part[(j / 2) % 2], pack2(w0, w1));
             s[g / 2][8 * (g % 2) + j / 2] = pack_half2(w0, w1);   // past the logits that are still to come
         }
@@ -408,20 +433,22 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             uint4 raw[8][2];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int at = it.r0 + r0 + 4 * j, i = at / p.G, g = at - i * p.G;
-                raw[j][0] = raw[j][1] = make_uint4(0, 0, 0, 0);
-                if (at < it.r1 && 16 * sub < p.D) {
-                    const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (size_t)(it.x0 + i) * p.q_stride +
-                                                                       (size_t)(it.h * p.G + g) * p.D + 16 * sub);
-                    raw[j][0] = src[0];
-                    raw[j][1] = src[1];
-                }
+                // every lane loads, so that no load waits for the one before: past the rows the last
+                const int at = min(it.r0 + r0 + 4 * j, it.r1 - 1), i = at / p.G, g = at - i * p.G;
+                const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (size_t)(it.x0 + i) * p.q_stride +
+                                                                   (size_t)(it.h * p.G + g) * p.D +
+                                                                   (16 * sub < p.D ? 16 * sub : 0));
+                raw[j][0] = src[0];
+                raw[j][1] = src[1];
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int r = r0 + 4 * j;
-                const uint32_t w[8] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w,
-                                       raw[j][1].x, raw[j][1].y, raw[j][1].z, raw[j][1].w};
+                uint32_t w[8] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w,
+                                 raw[j][1].x, raw[j][1].y, raw[j][1].z, raw[j][1].w};
+                const bool none = it.r0 + r >= it.r1 || 16 * sub >= p.D;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) w[u] = none ? 0 : w[u];
                 uint32_t m = 0;   // bits of the largest magnitude: as floats, and infinities and NaN above all
 #pragma unroll
                 for (int u = 0; u < 8; ++u) m = max(m, max((w[u] << 16) & 0x7FFFFFFFu, w[u] & 0x7FFF0000u));
@@ -499,15 +526,14 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             for (;;) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32b_x32(s_at + (uint32_t)(32 * c), s[c]);
-                const float base = kMTop - (ref == -INFINITY ? 0.f : ref);
                 float top = -INFINITY, add = 0.f;
                 ptx::tmem_ld_wait();
 #pragma unroll
                 for (int c = 0; c < 4; ++c) ptx::reg_fence32(s[c]);
-                if (mixed)
-                    weights<true>(s, my_k, my_lv, my_inv, rowf, base, rel, top, add);
-                else
-                    weights<false>(s, my_k, my_lv, my_inv, rowf, base, rel, top, add);
+                if (mixed) hide(s, rel);
+                if (i == 0) ref = largest(s, my_k, my_lv, rowf);   // else most rows would come here twice
+                const float base = kMTop - (ref == -INFINITY ? 0.f : ref);
+                weights(s, my_k, my_lv, my_inv, rowf, base, top, add);
                 const bool rise = top > ref + kMSlack;
                 if (!__any_sync(0xFFFFFFFFu, rise)) {
                     sum += add;
