@@ -25,7 +25,7 @@
 //   warps 12, 14    TMA producers: rings of K and of V tiles
 //   warp 13         TMEM allocation, MMA issuer (one thread)
 // Tensor memory: S (then W) of the tiles in columns 0 and 128, O in 256 and 384.
-// A prompt of 6,151 tokens of 28 heads x 128 takes 262 us (1,035 TFLOP/s): 4,100 cycles for
+// A prompt of 6,151 tokens of 28 heads x 128 takes 260 us (1,040 TFLOP/s): 4,100 cycles for
 // each 256 x 128 block, of which a row tile's chain is 300 to read S, 1,200 to 1,900 to
 // form the weights (floor of both tiles' exponentials on an SM sub-partition: 1,300), 400
 // to store them, and 600 + 600 in its products; then starts and ends of CTAs.  What these
@@ -441,19 +441,29 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
                 raw[j][0] = src[0];
                 raw[j][1] = src[1];
             }
+            uint32_t most[8];   // bits of the largest magnitude: as floats, and infinities and NaN above all
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool none = it.r0 + r0 + 4 * j >= it.r1 || 16 * sub >= p.D;
+                uint32_t m = 0;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    uint32_t &w = (&raw[j][u / 4].x)[u % 4];
+                    w = none ? 0 : w;
+                    m = max(m, max((w << 16) & 0x7FFFFFFFu, w & 0x7FFF0000u));
+                }
+                most[j] = m;
+            }
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) most[j] = max(most[j], __shfl_xor_sync(0xFFFFFFFFu, most[j], d));
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int r = r0 + 4 * j;
-                uint32_t w[8] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w,
-                                 raw[j][1].x, raw[j][1].y, raw[j][1].z, raw[j][1].w};
-                const bool none = it.r0 + r >= it.r1 || 16 * sub >= p.D;
-#pragma unroll
-                for (int u = 0; u < 8; ++u) w[u] = none ? 0 : w[u];
-                uint32_t m = 0;   // bits of the largest magnitude: as floats, and infinities and NaN above all
-#pragma unroll
-                for (int u = 0; u < 8; ++u) m = max(m, max((w[u] << 16) & 0x7FFFFFFFu, w[u] & 0x7FFF0000u));
-#pragma unroll
-                for (int d = 1; d < 8; d <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+                const uint32_t w[8] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w,
+                                       raw[j][1].x, raw[j][1].y, raw[j][1].z, raw[j][1].w};
+                const uint32_t m = most[j];
                 const bool finite = m < 0x7F800000u;
                 int e = 134 - (int)(m >> 23);   // takes the largest to [128, 256)
                 e = m == 0 || !finite ? 0 : min(e, 126);
