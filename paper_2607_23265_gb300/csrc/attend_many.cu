@@ -20,6 +20,8 @@
 // 2^12 above it (2^8: one tile in five of logits of a few units, a fifth of the time):
 // the tile's weights are formed without waiting for its maximum, and where it turns
 // out so O is rescaled in tensor memory and they are formed again.
+// Where a call has 128 rows at most a sequence and KV head, both tiles hold the same rows
+// (paired) and take the tiles of tokens in turn; their pieces are added as those of splits.
 //   warps 0-3, 4-7  weights of row tile 0, 1
 //   warps 8-11      V to f16
 //   warps 12, 14    TMA producers: rings of K and of V tiles
@@ -174,6 +176,8 @@ __device__ __forceinline__ void weights(uint32_t (&s)[4][32], float my_k, float 
 
 }  // namespace
 
+// PAIRED: a variant of its own, since the choice at run time costs every call 3 % (260 us to 267).
+template <bool PAIRED>
 __global__ void __launch_bounds__(kMThreads, 1)
 attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant__ AttendParams p, int row_tiles,
                    int splits) {
@@ -230,7 +234,9 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
     ptx::tc_fence_after();
     const uint32_t tmem = S->tmem_base;
     const int n = it.t1 - it.t0;
-    const int qtiles = it.r1 - it.r0 > 128 ? 2 : 1;
+    if (PAIRED) it.r1 = min(it.r1, it.r0 + 128);          // more tokens than max_new, reported above
+    const int qtiles = PAIRED || it.r1 - it.r0 > 128 ? 2 : 1;
+    const int stride = PAIRED ? 2 : 1;                    // tiles from one of a row tile's to its next
     const int minlim = max(0, min(it.kv, attend_visible(p, it.r0 / p.G, it.n, it.kv)));
     const int maxlim = max(0, min(it.kv, attend_visible(p, (it.r1 - 1) / p.G, it.n, it.kv)));
 
@@ -310,39 +316,44 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
                         ptx::mma_e4m3(d, a + (uint64_t)(j & 1) * rest + (uint64_t)(2 * (j >> 1)),
                                       b + (uint64_t)(2 * (j >> 1)), id_s, j > 0);
                 }
-                if (q == qtiles - 1) ptx::mma_commit(&S->k_empty[i % kMKStages]);
+                if (PAIRED || q == qtiles - 1) ptx::mma_commit(&S->k_empty[i % kMKStages]);
                 ptx::mma_commit(&S->s_full[q]);
             };
             // O of row tile q after its weights of tile i, then its logits of the next tile
             auto step = [&](auto q_, int i) {
                 constexpr int q = decltype(q_)::value;
-                const uint32_t par = (uint32_t)i & 1u;
-                if (q == 0 && !wait(&S->w_full[i & 1], (uint32_t)(i >> 1) & 1u)) return;
+                const uint32_t par = (uint32_t)(PAIRED ? i >> 1 : i) & 1u;
+                if ((PAIRED || q == 0) && !wait(&S->w_full[i & 1], (uint32_t)(i >> 1) & 1u)) return;
                 if (!wait(&S->p_ready[q], par)) return;
                 ptx::tc_fence_after();
                 const uint64_t b = w_desc + (uint64_t)(i & 1) * (2 * kATileBytes >> 4);
 #pragma unroll
                 for (int s = 0; s < kATile / 16; ++s)   // 16 tokens: 8 columns of W, two groups of 8 rows of V
                     ptx::mma_f16_ta(tmem + (uint32_t)(256 + q * 128), tmem + (uint32_t)(q * 128 + 8 * s),
-                                    b + (uint64_t)(s * (2048 >> 4)), id_o, s ? 1u : (uint32_t)i);
-                if (q == qtiles - 1) ptx::mma_commit(&S->w_empty[i & 1]);
+                                    b + (uint64_t)(s * (2048 >> 4)), id_o, s > 0 || i >= stride);
+                if (PAIRED || q == qtiles - 1) ptx::mma_commit(&S->w_empty[i & 1]);
                 ptx::mma_commit(&S->o_full[q]);
-                if (i + 1 == n) return;
-                if (q == 0 && !wait(&S->k_full[(i + 1) % kMKStages], (uint32_t)((i + 1) / kMKStages) & 1u)) return;
+                const int next = i + stride;
+                if (next >= n) return;
+                if ((PAIRED || q == 0) && !wait(&S->k_full[next % kMKStages], (uint32_t)(next / kMKStages) & 1u)) return;
                 // S takes the place of the weights: their products have to be complete
                 if (!wait(&S->o_full[q], par)) return;
                 ptx::tc_fence_after();
-                logits(q_, i + 1);
+                logits(q_, next);
             };
             constexpr std::integral_constant<int, 0> q0{};
             constexpr std::integral_constant<int, 1> q1{};
             if (n > 0 && wait(&S->q_ready, 0) && wait(&S->k_full[0], 0)) {
                 ptx::tc_fence_after();
                 logits(q0, 0);
-                if (qtiles == 2) logits(q1, 0);
+                if (PAIRED && n > 1 && wait(&S->k_full[1], 0)) {
+                    ptx::tc_fence_after();
+                    logits(q1, 1);
+                }
+                if (!PAIRED && qtiles == 2) logits(q1, 0);
                 for (int i = 0; i < n && ok; ++i) {
-                    step(q0, i);
-                    if (qtiles == 2 && ok) step(q1, i);
+                    if (!PAIRED || i % 2 == 0) step(q0, i);
+                    if ((PAIRED ? i % 2 == 1 : qtiles == 2) && ok) step(q1, i);
                 }
             }
             ptx::mma_commit(&S->drain);
@@ -423,7 +434,8 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         // ---------------- weights ----------------
-        const int q = warp >> 2, row = tid;               // this thread's row of the CTA
+        const int q = warp >> 2, row = tid;               // this thread's row of the CTA's two tiles
+        const int same = PAIRED ? q * 128 : 0;            // paired: both hold the same rows
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t s_at = lanes + (uint32_t)(q * 128), o_at = lanes + (uint32_t)(256 + q * 128);
         const uint32_t flip = p.scale2 < 0.f ? 0x80808080u : 0u;   // logits' factors are positive
@@ -434,7 +446,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 // every lane loads, so that no load waits for the one before: past the rows the last
-                const int at = min(it.r0 + r0 + 4 * j, it.r1 - 1), i = at / p.G, g = at - i * p.G;
+                const int at = min(it.r0 + r0 - same + 4 * j, it.r1 - 1), i = at / p.G, g = at - i * p.G;
                 const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (size_t)(it.x0 + i) * p.q_stride +
                                                                    (size_t)(it.h * p.G + g) * p.D +
                                                                    (16 * sub < p.D ? 16 * sub : 0));
@@ -444,7 +456,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             uint32_t most[8];   // bits of the largest magnitude: as floats, and infinities and NaN above all
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const bool none = it.r0 + r0 + 4 * j >= it.r1 || 16 * sub >= p.D;
+                const bool none = it.r0 + r0 - same + 4 * j >= it.r1 || 16 * sub >= p.D;
                 uint32_t m = 0;
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
@@ -495,13 +507,14 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&S->q_ready);
         const float rowf = S->rowf[row];   // this warp's rows
-        const int tok = (it.r0 + row) / p.G;
-        const bool real = it.r0 + row < it.r1;
+        const int at = it.r0 + row - same, tok = at / p.G;
+        const bool real = at < it.r1;
         const int lim = real ? max(0, min(it.kv, attend_visible(p, tok, it.n, it.kv))) : 0;
 
         float ref = -INFINITY, sum = 0.f;
         bool ok = true;
-        const int steps = q < qtiles ? n : 0;
+        const int steps = PAIRED ? (n + 1 - q) / 2 : q < qtiles ? n : 0;
+        const int first = it.t0 + (PAIRED ? q : 0);   // this row tile's first
         // lane l < 8: scales of the l-th 16 tokens of a tile, loaded one tile ahead, their page two
         auto page_of = [&](int tile) {
             const int t = tile * kATile + 16 * lane;
@@ -511,8 +524,8 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             return pg < 0 ? make_float2(1.f, 0.f)
                           : make_float2(p.k_scale[(size_t)pg * p.heads + it.h], p.v_scale[(size_t)pg * p.heads + it.h]);
         };
-        int pg_next = steps > 0 ? page_of(it.t0 + 1) : -1;
-        float2 next = scales_of(steps > 0 ? page_of(it.t0) : -1);
+        int pg_next = steps > 0 ? page_of(first + stride) : -1;
+        float2 next = scales_of(steps > 0 ? page_of(first) : -1);
         // factor of the logits, log2 and reciprocal of V's scale
         float my_k, my_lv, my_inv;
         auto take_scales = [&](int tile_after) {
@@ -522,10 +535,10 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             next = scales_of(pg_next);
             pg_next = page_of(tile_after);
         };
-        take_scales(it.t0 + 2);
+        take_scales(first + 2 * stride);
         for (int i = 0; i < steps; ++i) {
-            const int rel = lim - (it.t0 + i) * kATile;       // columns of the tile that this row sees
-            const bool mixed = (it.t0 + i + 1) * kATile > minlim;
+            const int tile = first + i * stride, rel = lim - tile * kATile;   // columns of the tile that this row sees
+            const bool mixed = (tile + 1) * kATile > minlim;
             ok = warp_wait(&S->s_full[q], (uint32_t)i & 1u);
             ok = __all_sync(0xFFFFFFFFu, ok && !*abort_flag);
             if (!ok) break;
@@ -571,7 +584,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&S->p_ready[q]);
-            take_scales(it.t0 + i + 3);
+            take_scales(tile + 3 * stride);
         }
         if (ok && steps > 0) {
             ok = ptx::mbar_wait(&S->o_full[q], (uint32_t)(steps - 1) & 1u, kATimeoutNs);
@@ -580,7 +593,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         if (!ok) attend_fail(p, abort_flag);
         ptx::tc_fence_after();
         if (ok && q < qtiles) {
-            const int hq = it.h * p.G + (it.r0 + row) - tok * p.G;
+            const int hq = it.h * p.G + at - tok * p.G;
             const size_t x = (size_t)(it.x0 + tok);
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
             const bool nans = *reinterpret_cast<volatile int *>(&S->any_nan);
@@ -618,7 +631,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
                     if (lim > S->nan_min[j]) o[j / 32][j % 32] = __float_as_uint(NAN);
                 }
             }
-            if (splits == 1) {
+            if (splits == 1 && !PAIRED) {
 #pragma unroll
                 for (int c = 0; c < 16; ++c) {
                     uint32_t w[4];
@@ -646,7 +659,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
                 }
             }
             if (real) {
-                if (splits > 1)
+                if (splits > 1 || PAIRED)
                     p.ml[(size_t)blockIdx.x * kManyRows + row] = make_float2(ref - kMTop, sum);
                 else if (p.lse)
                     p.lse[x * p.Hq + hq] = sum == 0.f ? -INFINITY : (ref - kMTop + log2f(sum)) * kLn2;
@@ -662,21 +675,24 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
 
 // Adds the pieces of each row, in order; a warp per row.
 __global__ void __launch_bounds__(256)
-attend_merge_kernel(const __grid_constant__ AttendParams p, int row_tiles, int splits) {
+attend_merge_kernel(const __grid_constant__ AttendParams p, int row_tiles, int splits, int paired) {
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
     const int idx = (int)blockIdx.x / (kManyRows / 8), row = (int)blockIdx.x % (kManyRows / 8) * 8 + (threadIdx.x >> 5);
     ManyItem it;
     if (!many_item(p, row_tiles, splits, idx * splits, &it) || it.r0 + row >= it.r1) return;
-    const size_t first = (size_t)idx * splits;
+    if (paired && row >= kManyRows / 2) return;
+    // pieces of `step` rows: a CTA's, or of either of its tiles
+    const int pieces = paired ? 2 * splits : splits, step = paired ? kManyRows / 2 : kManyRows;
+    const size_t first = (size_t)idx * splits * kManyRows + row;
     float m = -INFINITY;
-    for (int s = 0; s < splits; ++s) m = fmaxf(m, p.ml[(first + s) * kManyRows + row].x);
+    for (int s = 0; s < pieces; ++s) m = fmaxf(m, p.ml[first + (size_t)s * step].x);
     const float ref = m == -INFINITY ? 0.f : m;
     float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int s = 0; s < splits; ++s) {
-        const size_t at = (first + s) * kManyRows + row;
+    for (int s = 0; s < pieces; ++s) {
+        const size_t at = first + (size_t)s * step;
         const float2 ml = p.ml[at];
         const float f = ex2(ml.x - ref);
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -699,17 +715,19 @@ attend_merge_kernel(const __grid_constant__ AttendParams p, int row_tiles, int s
     if (lane == 0 && p.lse) p.lse[x * p.Hq + hq] = L == 0.f ? -INFINITY : (m + log2f(L)) * kLn2;
 }
 
-cudaError_t launch_attend_many(const AttendMaps &maps, const AttendParams &p, int max_new, int splits, cudaStream_t s) {
-    cudaError_t e = allow_smem((const void *)attend_many_kernel, kMSmem);
+cudaError_t launch_attend_many(const AttendMaps &maps, const AttendParams &p, int max_new, int splits, int paired,
+                               cudaStream_t s) {
+    const void *kernel = paired ? (const void *)attend_many_kernel<true> : (const void *)attend_many_kernel<false>;
+    cudaError_t e = allow_smem(kernel, kMSmem);
     if (e != cudaSuccess) return e;
     int row_tiles = (int)(((int64_t)max_new * p.G + kManyRows - 1) / kManyRows);
     const int64_t items = (int64_t)row_tiles * p.B * p.heads;
     if (items * splits > INT32_MAX) return cudaErrorInvalidValue;
     void *args[] = {const_cast<AttendMaps *>(&maps), const_cast<AttendParams *>(&p), &row_tiles, &splits};
-    e = launch_kernel((const void *)attend_many_kernel, dim3((unsigned)(items * splits)), dim3(kMThreads), kMSmem, s,
+    e = launch_kernel(kernel, dim3((unsigned)(items * splits)), dim3(kMThreads), kMSmem, s,
                       args, true);
-    if (e != cudaSuccess || splits == 1) return e;
-    void *margs[] = {const_cast<AttendParams *>(&p), &row_tiles, &splits};
+    if (e != cudaSuccess || (splits == 1 && !paired)) return e;
+    void *margs[] = {const_cast<AttendParams *>(&p), &row_tiles, &splits, &paired};
     return launch_kernel((const void *)attend_merge_kernel, dim3((unsigned)(items * (kManyRows / 8))), dim3(256), 0, s,
                          margs, true);
 }

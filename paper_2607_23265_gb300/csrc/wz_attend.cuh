@@ -141,6 +141,7 @@ __device__ __forceinline__ QueryPiece query_piece(uint2 raw) {
 }
 
 cudaError_t launch_attend_few(const AttendMaps &maps, const AttendParams &p, int max_new, int sms, cudaStream_t s);
-cudaError_t launch_attend_many(const AttendMaps &maps, const AttendParams &p, int max_new, int splits, cudaStream_t s);
+cudaError_t launch_attend_many(const AttendMaps &maps, const AttendParams &p, int max_new, int splits, int paired,
+                               cudaStream_t s);
 
 }  // namespace wz

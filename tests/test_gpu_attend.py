@@ -302,7 +302,7 @@ def test_items_in_pieces(wz, G, n):
 @pytest.mark.parametrize("D,P", [(64, 16), (128, 64)])
 def test_one_row(wz, D, P):
     """Single tokens of heads that share nothing: one row a sequence and head."""
-    run(wz, D, 16, 16, P, [1] * 9, [1, 2, 127, 128, 129, 0, 640, 4098, 1025], seed=D)
+    run(wz, P, 16, 16, D, [1] * 9, [1, 2, 127, 128, 129, 0, 640, 4098, 1025], seed=D)
 
 
 @pytest.mark.parametrize("tiles", [4, 5, 8, 9])
@@ -405,3 +405,13 @@ def test_example_answers_from_the_cache(wz):
     m = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(m)
     assert m.main() < 2.0 ** -7
+
+
+@pytest.mark.parametrize("G,n", [(7, 10), (4, 32), (1, 128), (1, 17), (17, 1), (32, 4)])
+def test_one_tile_of_rows(wz, G, n):
+    """17 to 128 rows: both row tiles of a CTA hold them, in calls of few items; no slots, one tile,
+    even and odd numbers of tiles, with and without splits."""
+    for causal in (True, False):
+        run(wz, 128, 1, G, 64, [n] * 5, [0, n, 129 + n, 257, 4000], causal=causal, seed=n)
+    run(wz, 64, 8, 8 * G, 32, [n] * 30, [128 * (b % 9) + 7 * b + 1 for b in range(30)], seed=G)
+    run(wz, 128, 8, 8 * G, 80, [n if b % 3 else max(1, n // 2) for b in range(45)], [b * 13 + 1 for b in range(45)], seed=G)
