@@ -26,7 +26,7 @@
 //   warp 5     TMEM allocation, MMA issuer (one thread)
 // One query over 200,003 slots of 4 heads x 128 takes 40 us: 205 MB at 6.9 TB/s between
 // the first copies' arrival (4 us) and the median CTA's end (33 us), then the slowest
-// SMs' tails and the join (7 us).  64 queries over 577 .. 18,699 slots 90-96 us for 454
+// SMs' tails and the join (7 us).  64 queries over up to 18,699 slots 92-98 us for 454
 // MB; with tiles' rows in byte stores, scalars by every thread and a join that scanned
 // the lengths again 105.
 // Every wait is bounded; where one gives up the kernel sets a status bit, ends
