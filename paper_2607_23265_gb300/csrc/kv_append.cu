@@ -477,7 +477,9 @@ cudaError_t launch_kv_append(const wz_kv_append_args &a, cudaStream_t s) {
     const void *fn = a.dtype == WZ_DTYPE_BF16
                          ? (p.interleaved ? append_kernel<__nv_bfloat16, true>(it) : append_kernel<__nv_bfloat16, false>(it))
                          : (p.interleaved ? append_kernel<float, true>(it) : append_kernel<float, false>(it));
-    cudaError_t e = smem > 48 * 1024 ? allow_smem(fn, smem) : cudaSuccess;
+    // 48 KB a CTA need no leave, the kernel's static arrays included; asking takes host time,
+    // and calls of a few tokens, which that matters to, have less than this
+    cudaError_t e = smem > 32 * 1024 ? allow_smem(fn, smem) : cudaSuccess;
     if (e != cudaSuccess) return e;
     void *args[] = {&p};
     const int64_t grid = units * (p.groups + p.parts);
