@@ -506,10 +506,11 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&S->q_ready);
-        const float rowf = S->rowf[row];   // this warp's rows
         const int at = it.r0 + row - same, tok = at / p.G;
         const bool real = at < it.r1;
         const int lim = real ? max(0, min(it.kv, attend_visible(p, tok, it.n, it.kv))) : 0;
+        // of this warp's rows; not NaN for a row that sees nothing, whose hidden logits it multiplies
+        const float rowf = lim > 0 ? S->rowf[row] : 1.f;
 
         float ref = -INFINITY, sum = 0.f;
         bool ok = true;
