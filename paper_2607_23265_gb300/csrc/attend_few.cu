@@ -417,8 +417,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
             u.first = w.item0 + p.item_cost;
             u.kv = len.y;
             u.x0 = p.cu[u.b];
-            u.rows = len.x * p.G;
-            if (u.rows > U) u.rows = U / p.G * p.G;   // more tokens than max_new, reported above
+            u.rows = min(len.x, p.most) * p.G;   // tokens past them, reported above, are left out
             // row c = token c / G, head c % G of the group
             uint2 raw[R / 4];
             int tok[R / 4];
@@ -726,7 +725,7 @@ __global__ void __launch_bounds__(512) attend_join_kernel(const __grid_constant_
     const int x0 = p.cu[b];
     pdl_wait();
     pdl_trigger();
-    const int rows = min(len.x * p.G, R);
+    const int rows = min(len.x, p.most) * p.G;   // those that the kernel before formed
     if (rows == 0) return;
     const int2 span = len.y > 0 ? p.spans[(size_t)x0 * p.heads + h] : make_int2(0, 0);
     if (span.y == 1) return;   // one CTA had the whole item
@@ -806,6 +805,7 @@ cudaError_t launch_few(const AttendMaps &maps, AttendParams p, int max_new, int 
     const int64_t items = (int64_t)p.B * p.heads;
     const int64_t tiles = ((int64_t)p.max_pages * p.P + kATile - 1) / kATile;
     p.whole = tiles <= kWholeTiles;
+    p.most = U / p.G;
     // 0: a CTA for each tile; whole items have at least the unit that an empty one is found by
     p.item_cost = p.whole || items * tiles > (int64_t)sms * Sh::kCtas ? Sh::kItemCost : 0;
     // no more CTAs than items or tiles there can be

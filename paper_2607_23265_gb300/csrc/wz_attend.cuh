@@ -41,6 +41,7 @@ struct AttendParams {
     int shift;               // log2(P)
     int ctas;                // CTAs that share the work
     int whole, item_cost;    // attend_few: items are not cut; tiles that an item's start and end count as
+    int most;                // attend_few: tokens of a sequence that its rows have room for, max_new or more
     float scale2;            // scale * log2(e)
     int *status;
 };
