@@ -412,9 +412,11 @@ typedef struct {
 
 /* device_status bits of the two calls below, OR-ed in by the device (the
  * caller clears the word): a page number outside the cache, a sequence past
- * its row of the page table, a position outside the rotation table, lengths
- * that contradict each other.  What such an entry concerns is skipped and
- * nothing outside the arrays is touched. */
+ * its row of the page table, a position outside the rotation table (of an axis
+ * that some frequency takes), lengths that contradict each other.  What such an
+ * entry concerns is skipped (of a position, the token's key and query: its
+ * slot's key and its row of q_out stay as they were) and nothing outside the
+ * arrays is touched. */
 #define WZ_STATUS_CACHE 0x400
 
 /*

@@ -28,6 +28,8 @@ namespace wz {
 namespace {
 
 constexpr int kAppendThreads = 256;
+constexpr int kMaxPage = 128;   // tokens
+static_assert(kMaxPage <= kAppendThreads, "a thread for each token of a page");
 
 struct AppendParams {
     uint8_t *cache[2];        // keys, values
@@ -113,23 +115,33 @@ __device__ __forceinline__ int2 item_channels(const AppendParams &p, int rot, in
 
 // Starts the copies of the rotation rows of tokens x0 .. x0 + count - 1 to `rows`
 // [count][rot], four frequencies at a time.  `places` [count][axes]: room for the
-// tokens' positions, read once, together.
-__device__ __forceinline__ void fetch_angles(const AppendParams &p, float *rows, int *places, int x0, int slot0,
-                                             int count) {
+// tokens' positions, read once, together.  outside[r]: token x0 + r has a position that the
+// table does not, and neither key nor query of it is written; true for a thread that found one.
+__device__ __forceinline__ bool fetch_angles(const AppendParams &p, float *rows, int *places, uint8_t *outside, int x0,
+                                             int slot0, int count) {
     const int half = p.rot >> 1, quads = half >> 2;
     if (p.positions) {
         for (int at = threadIdx.x; at < count * p.axes; at += kAppendThreads)
             places[at] = p.positions[(size_t)x0 * p.axes + at];
         __syncthreads();
     }
+    auto in_table = [&](int pos) { return pos >= 0 && pos < p.rows; };
+    bool found = false;
+    if (const int r = threadIdx.x; r < count) {   // a page has fewer tokens than the CTA threads
+        if (!p.positions)
+            found = !in_table(slot0 + r);
+        else if (p.axes == 3)   // axes that some frequency takes
+            found = (p.sec0 > 0 && !in_table(places[3 * r])) ||
+                    (p.sec01 > p.sec0 && !in_table(places[3 * r + 1])) || (half > p.sec01 && !in_table(places[3 * r + 2]));
+        else
+            found = !in_table(places[r]);
+        outside[r] = found;
+        if (found) kv_report(p.status);
+    }
     auto row_of = [&](int r, int f) {   // of frequency f of token x0 + r
         int pos = slot0 + r;
         if (p.positions) pos = p.axes == 3 ? places[3 * r + (f >= p.sec0) + (f >= p.sec01)] : places[r];
-        if (pos < 0 || pos >= p.rows) {
-            kv_report(p.status);
-            pos = 0;
-        }
-        return p.rotation + (size_t)pos * p.rot;
+        return p.rotation + (size_t)(in_table(pos) ? pos : 0) * p.rot;
     };
     for (int at = threadIdx.x; at < count * quads; at += kAppendThreads) {
         const int r = by(at, p.quads_inv), f = 4 * (at - r * quads);
@@ -146,6 +158,7 @@ __device__ __forceinline__ void fetch_angles(const AppendParams &p, float *rows,
             ptx::copy_async16_l1(dst + half, src + half);
         }
     }
+    return found;
 }
 
 // Two products.
@@ -200,8 +213,9 @@ __device__ __forceinline__ uint2 pack8(const float *x, float inv) {
 // Keys and values of `count` tokens from row `row0` of a page on, a head of each wph
 // warps.  `page_at` is read beside the rows.
 template <typename Tin, int IT, bool INTER>
-__device__ __forceinline__ void append_page(const AppendParams &p, float *angles, int *places, int group, int x0,
-                                            int slot0, int count, int row0, const int32_t *page_at) {
+__device__ __forceinline__ void append_page(const AppendParams &p, float *angles, int *places, uint8_t *outside,
+                                            int group, int x0, int slot0, int count, int row0,
+                                            const int32_t *page_at) {
     constexpr bool kBoth = IT * sizeof(Tin) <= 4;   // registers for the values' rows beside the keys'
     __shared__ uint32_t warp_max[2][kAppendThreads / 32];
     const int items = p.items;
@@ -228,7 +242,7 @@ __device__ __forceinline__ void append_page(const AppendParams &p, float *angles
     const int page = page_at ? *page_at : -1;
     load(0, a[0], b[0]);
     if (kBoth) load(1, a[kBoth], b[kBoth]);
-    if (p.rot) fetch_angles(p, angles, places, x0, slot0, count);
+    const bool found = p.rot && fetch_angles(p, angles, places, outside, x0, slot0, count);
     if (page < 0 || page >= p.pages) {
         ptx::copy_async_wait_all();
         kv_report(p.status);
@@ -237,10 +251,17 @@ __device__ __forceinline__ void append_page(const AppendParams &p, float *angles
     const size_t block = (size_t)page * p.heads + (mine ? head : 0);
     const float olds[2] = {p.scale[0][block], p.scale[1][block]};
     ptx::copy_async_wait_all();
-    __syncthreads();
+    const bool some_outside = __syncthreads_or(found);
+    uint32_t absent = 0;   // this thread's items whose key is left out
+    if (some_outside)
+        for (int t = 0; t < IT; ++t) {
+            const int r = by(lane + t * width, p.items_inv);
+            if (r < count && outside[r]) absent |= 1u << t;
+        }
 #pragma unroll
     for (int role = 0; role < 2; ++role) {
         const int rot = role ? 0 : p.rot;
+        auto takes = [&](int t, int r) { return mine && r < count && !(role == 0 && (absent >> t & 1u)); };
         uint8_t *dst = p.cache[role] + block * (size_t)(p.P * p.D);
         const float old = olds[role];
         if (!kBoth && role) load(1, a[0], b[0]);
@@ -249,7 +270,7 @@ __device__ __forceinline__ void append_page(const AppendParams &p, float *angles
 #pragma unroll
         for (int t = 0; t < IT; ++t) {
             const int at = lane + t * width, r = by(at, p.items_inv), j = at - r * items;
-            if (mine && r < count) {
+            if (takes(t, r)) {
                 a[kBoth ? role : 0][t].get(v[t].x);
                 b[kBoth ? role : 0][t].get(v[t].x + 8);
                 if (j < rot >> 4) turn_item<INTER>(p, v[t], angles + r * p.rot, j);
@@ -265,7 +286,7 @@ __device__ __forceinline__ void append_page(const AppendParams &p, float *angles
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const float m = fabsf(v[t].x[i]);
-                    if (mine && by(at, p.items_inv) < count && m <= FLT_MAX) most = fmaxf(most, m);
+                    if (takes(t, by(at, p.items_inv)) && m <= FLT_MAX) most = fmaxf(most, m);
                 }
             }
         }
@@ -280,7 +301,7 @@ __device__ __forceinline__ void append_page(const AppendParams &p, float *angles
 #pragma unroll
         for (int t = 0; t < IT; ++t) {
             const int at = lane + t * width, r = by(at, p.items_inv), j = at - r * items;
-            if (mine && r < count && wz_in_range(p.status, row0 + r < p.P)) {
+            if (takes(t, r) && wz_in_range(p.status, row0 + r < p.P)) {
                 const int2 ch = item_channels(p, rot, j);
                 uint8_t *d = dst + (row0 + r) * p.D;
                 *reinterpret_cast<uint2 *>(d + ch.x) = pack8(v[t].x, inv);
@@ -304,8 +325,8 @@ __device__ __forceinline__ void append_page(const AppendParams &p, float *angles
 // Queries of tokens part * q_tokens .. of `count`: their heads lie side by side, so
 // that the CTA reads and writes whole rows from one end to the other.
 template <typename Tin, bool INTER>
-__device__ __forceinline__ void rotate_queries(const AppendParams &p, float *angles, int *places, int part, int x0,
-                                               int slot0, int count) {
+__device__ __forceinline__ void rotate_queries(const AppendParams &p, float *angles, int *places, uint8_t *outside,
+                                               int part, int x0, int slot0, int count) {
     constexpr int kAhead = 2;   // items of a thread whose loads are in flight
     const int items = p.items, heads = p.Hq;
     const int r0 = part * p.q_tokens, tokens = min(count - r0, p.q_tokens);
@@ -346,10 +367,11 @@ __device__ __forceinline__ void rotate_queries(const AppendParams &p, float *ang
     };
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) load(u);
+    bool some_outside = false;
     if (p.rot) {
-        fetch_angles(p, angles, places, x0, slot0 + r0, tokens);
+        const bool found = fetch_angles(p, angles, places, outside, x0, slot0 + r0, tokens);
         ptx::copy_async_wait_all();
-        __syncthreads();
+        some_outside = __syncthreads_or(found);
     }
     while (at.r < tokens) {
 #pragma unroll
@@ -362,7 +384,7 @@ __device__ __forceinline__ void rotate_queries(const AppendParams &p, float *ang
                 const int2 ch = item_channels(p, p.rot, at.j);
                 const size_t x = (size_t)(x0 + at.r);
                 Tin *dst = static_cast<Tin *>(p.q_out) + x * p.q_out_stride + (size_t)at.h * p.D;
-                if (wz_in_range(p.status, x < (size_t)p.T)) {
+                if (!(some_outside && outside[at.r]) && wz_in_range(p.status, x < (size_t)p.T)) {
                     store8(dst + ch.x, v.x);
                     store8(dst + ch.y, v.x + 8);
                 }
@@ -383,6 +405,7 @@ template <typename Tin, int IT, bool INTER>
 __global__ void __launch_bounds__(kAppendThreads, IT == 4 ? 2 : sizeof(Tin) == 2 ? 4 : 3)
 kv_append_kernel(const __grid_constant__ AppendParams p) {
     extern __shared__ __align__(16) float angles[];      // [rows][rot], then the positions
+    __shared__ uint8_t outside[kMaxPage];
     int *places = reinterpret_cast<int *>(angles + p.rows_cta * p.rot);
     pdl_wait();
     pdl_trigger();
@@ -411,9 +434,9 @@ kv_append_kernel(const __grid_constant__ AppendParams p) {
     if (lo >= hi) return;
     const int x = x0 + (lo - s0);
     if (place >= p.groups)
-        rotate_queries<Tin, INTER>(p, angles, places, place - p.groups, x, lo, hi - lo);
+        rotate_queries<Tin, INTER>(p, angles, places, outside, place - p.groups, x, lo, hi - lo);
     else
-        append_page<Tin, IT, INTER>(p, angles, places, place, x, lo, hi - lo, (int)(lo - first),
+        append_page<Tin, IT, INTER>(p, angles, places, outside, place, x, lo, hi - lo, (int)(lo - first),
                                     col < p.max_pages ? p.table + (size_t)b * p.max_pages + col : nullptr);
 }
 
