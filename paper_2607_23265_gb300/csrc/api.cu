@@ -905,7 +905,8 @@ int wz_kv_append(const wz_kv_append_args *a) {
     const wz_kv_cache &c = a->cache;
     if (a->dtype != WZ_DTYPE_BF16 && a->dtype != WZ_DTYPE_F32) return WZ_ERR_INVALID_ARG;
     if (a->T < 0 || a->T > INT32_MAX || a->B < 0 || a->max_new < 0 || a->max_pages < 1) return WZ_ERR_INVALID_ARG;
-    if (a->q ? a->Hq < 1 || a->Hq % c.heads != 0 : a->Hq != 0) return WZ_ERR_INVALID_ARG;
+    // queries of no tokens may have no address
+    if (a->q || (a->T == 0 && a->Hq != 0) ? a->Hq < 1 || a->Hq % c.heads != 0 : a->Hq != 0) return WZ_ERR_INVALID_ARG;
     if (a->rotation) {
         if (!aligned(a->rotation, 16) || a->rotation_rows < 1 || a->rotation_rows > INT32_MAX || a->rot < 16 ||
             a->rot > c.D || a->rot % 16 != 0 || (a->axes != 1 && a->axes != 3) || !aligned(a->positions, 4))
