@@ -455,7 +455,7 @@ typedef struct {
     int B;                   /* sequences                                    */
     int max_new;             /* the most new tokens of a sequence; 0: T;     */
                              /* tokens past it are left out and reported     */
-    int Hq;                  /* query heads (0 with q NULL)                  */
+    int Hq;                  /* query heads (0 with q NULL), at most 65536   */
     const int32_t *cu;       /* [B+1]                                        */
     const int32_t *start;    /* [B] tokens that the cache holds already      */
     const int32_t *page_table; /* [B][max_pages]                             */
@@ -504,7 +504,7 @@ typedef struct {
     int B;                   /* sequences                                    */
     int max_new;             /* the most tokens of q of a sequence; 0: T;    */
                              /* tokens past it may be left out, reported     */
-    int Hq;                  /* a multiple of the cache's heads              */
+    int Hq;                  /* a multiple of the cache's heads, the same    */
     const int32_t *cu;       /* [B+1] rows of q of each sequence             */
     const int32_t *kv_len;   /* [B] slots in use                             */
     const int32_t *page_table; /* [B][max_pages]                             */

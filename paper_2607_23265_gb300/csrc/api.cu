@@ -874,6 +874,8 @@ int wz_project(const wz_project_args *a) {
     return WZ_OK;
 }
 
+constexpr int kMaxQueryHeads = 65536;
+
 // What both calls ask of a cache.
 static int check_cache(const wz_kv_cache &c) {
     if (!c.k || !c.v || !c.k_scale || !c.v_scale || !aligned(c.k, 16) || !aligned(c.v, 16) || !aligned(c.k_scale, 4) ||
@@ -920,7 +922,7 @@ int wz_kv_append(const wz_kv_append_args *a) {
             if (!a->positions || sum != a->rot / 2) return WZ_ERR_INVALID_ARG;
         }
     }
-    if (a->B > (1 << 24)) return WZ_ERR_UNSUPPORTED;
+    if (a->Hq > kMaxQueryHeads || a->B > (1 << 24)) return WZ_ERR_UNSUPPORTED;
     if (a->T == 0 || a->B == 0) return a->T == 0 ? WZ_OK : WZ_ERR_INVALID_ARG;
     const int64_t width = (int64_t)c.heads * c.D;
     if (!rows_ok(a->k, a->k_stride, width) || !rows_ok(a->v, a->v_stride, width)) return WZ_ERR_INVALID_ARG;
@@ -954,7 +956,7 @@ int wz_attend(const wz_attend_args *a) {
     if (a->T < 0 || a->T > INT32_MAX || a->B < 0 || a->max_new < 0 || a->max_pages < 1 || a->Hq < 1 ||
         a->Hq % c.heads != 0 || !std::isfinite(a->scale))
         return WZ_ERR_INVALID_ARG;
-    if (a->Hq > 65536 || (int64_t)a->B * c.heads > INT32_MAX || a->B > (1 << 24)) return WZ_ERR_UNSUPPORTED;
+    if (a->Hq > kMaxQueryHeads || (int64_t)a->B * c.heads > INT32_MAX || a->B > (1 << 24)) return WZ_ERR_UNSUPPORTED;
     if (a->T == 0 || a->B == 0) return a->T == 0 ? WZ_OK : WZ_ERR_INVALID_ARG;
     if (!rows_ok(a->q, a->q_stride, (int64_t)a->Hq * c.D) || !rows_ok(a->out, a->out_stride, (int64_t)a->Hq * c.D))
         return WZ_ERR_INVALID_ARG;
