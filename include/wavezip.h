@@ -490,8 +490,9 @@ WZ_API int wz_kv_append(const wz_kv_append_args *a);
  * off by at most 2^-17 of it), weights with 8 bits (up to 16 rows a sequence
  * and KV head) or 11; maxima and sums in fp32.  Pieces of a sequence that
  * several CTAs hold are joined in a fixed order: equal calls give equal bits.
- * Errors: WZ_ERR_INVALID_ARG, WZ_ERR_UNSUPPORTED, WZ_ERR_WORKSPACE,
- * WZ_ERR_NO_MEMORY, WZ_ERR_CUDA; nothing is launched on an argument error.
+ * Errors: WZ_ERR_INVALID_ARG, WZ_ERR_UNSUPPORTED (max_new * Hq / heads past
+ * 2^31 - 256 among them), WZ_ERR_WORKSPACE, WZ_ERR_NO_MEMORY, WZ_ERR_CUDA;
+ * nothing is launched on an argument error.
  */
 typedef struct {
     wz_kv_cache cache;

@@ -958,6 +958,9 @@ int wz_attend(const wz_attend_args *a) {
         return WZ_ERR_INVALID_ARG;
     if (a->Hq > kMaxQueryHeads || (int64_t)a->B * c.heads > INT32_MAX || a->B > (1 << 24)) return WZ_ERR_UNSUPPORTED;
     if (a->T == 0 || a->B == 0) return a->T == 0 ? WZ_OK : WZ_ERR_INVALID_ARG;
+    // a sequence's rows for a KV head, with a row tile's more, are counted in 31 bits
+    const int64_t most_new = a->max_new ? std::min<int64_t>(a->max_new, a->T) : a->T;
+    if (most_new * (a->Hq / c.heads) > INT32_MAX - 255) return WZ_ERR_UNSUPPORTED;
     if (!rows_ok(a->q, a->q_stride, (int64_t)a->Hq * c.D) || !rows_ok(a->out, a->out_stride, (int64_t)a->Hq * c.D))
         return WZ_ERR_INVALID_ARG;
     if (!a->cu || !a->kv_len || !a->page_table || !aligned(a->cu, 4) || !aligned(a->kv_len, 4) ||

@@ -7,7 +7,7 @@ import sys
 
 import pytest
 
-from test_kv_abi import append_args, wz  # noqa: F401
+from test_kv_abi import append_args, attend_args, wz  # noqa: F401
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -35,3 +35,13 @@ def test_append_refuses_more_heads_than_attention_takes(wz, Hq):  # noqa: F811
     program = HEADS.format(root=ROOT, tests=os.path.join(ROOT, "tests"), Hq=Hq)
     r = subprocess.run([sys.executable, "-c", program], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.split() == ["returned", "-2"], (r.returncode, r.stdout, r.stderr[-500:])
+
+
+@pytest.mark.parametrize("T,max_new,Hq,heads", [
+    (1 << 30, 0, 28, 4), (1 << 30, 1 << 29, 16, 4), ((1 << 31) - 1, 0, 1, 1), (1 << 27, 0, 16, 1),
+    (1 << 16, 0, 65536, 1),
+])
+def test_attend_refuses_rows_past_31_bits(wz, T, max_new, Hq, heads):  # noqa: F811
+    """Rows of a sequence and KV head: max_new tokens of Hq / heads heads."""
+    a = attend_args(wz, T=T, max_new=max_new, Hq=Hq, q_stride=Hq * 128, out_stride=Hq * 128, **{"cache.heads": heads})
+    assert wz._lib.wz_attend(C.byref(a)) == -2
