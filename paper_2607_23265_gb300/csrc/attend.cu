@@ -30,6 +30,10 @@ struct AttendPlan {
     size_t workspace;
 };
 
+#ifdef WZ_CHECKED
+uint64_t check_wait_ns = kATimeoutNs;
+#endif
+
 constexpr size_t kPieceRow = 128 * sizeof(float) + sizeof(float2);
 
 AttendPlan attend_plan(const wz_attend_args &a, int sms) {
@@ -104,8 +108,18 @@ cudaError_t launch_attend(const wz_attend_args &a, void *workspace, cudaStream_t
     while (1 << p.shift < p.P) ++p.shift;
     p.scale2 = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)p.D)) * kLog2e;
     p.status = a.device_status;
+#ifdef WZ_CHECKED
+    p.wait_ns = check_wait_ns;
+#endif
     return pl.few ? launch_attend_few(maps, p, pl.max_new, sms, s)
                   : launch_attend_many(maps, p, pl.max_new, pl.splits, pl.paired, s);
 }
 
 }  // namespace wz
+
+#ifdef WZ_CHECKED
+// Test hook: the limit of the waits that the attention kernels give up on; 0: the ordinary one.
+extern "C" __attribute__((visibility("default"))) void wz_check_attend_wait(uint64_t ns) {
+    wz::check_wait_ns = ns ? ns : wz::kATimeoutNs;
+}
+#endif

@@ -307,7 +307,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                 if (i + 1 < n) znext = slab(now, kv, now.t0 + i + 1);
                 for (int c = 0; c < 2; ++c, ++seq) {
                     const int st = seq % Sh::kStages;
-                    ok = ptx::mbar_wait(&S->empty[st], ((uint32_t)(seq / Sh::kStages) & 1u) ^ 1u, kATimeoutNs);
+                    ok = ptx::mbar_wait(&S->empty[st], ((uint32_t)(seq / Sh::kStages) & 1u) ^ 1u, wait_limit(p));
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     if (!ok) {
                         attend_fail(p, abort_flag);
@@ -343,7 +343,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
             int k = 0, item = 0;                                             // tiles and items begun
             bool ok = true;
             auto wait = [&](uint64_t *bar, uint32_t parity) {
-                if (ok && !ptx::mbar_wait(bar, parity, kATimeoutNs)) {
+                if (ok && !ptx::mbar_wait(bar, parity, wait_limit(p))) {
                     attend_fail(p, abort_flag);
                     ok = false;
                 }
@@ -470,7 +470,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
             for (int c = 0; c < U; ++c) acc[c] = l[c] = 0.f;
 
             auto read_output = [&](int kk) {   // O^T of tile kk into the sums
-                ok = ptx::mbar_wait(&S->o_full[kk & 1], (uint32_t)(kk >> 1) & 1u, kATimeoutNs) && ok;
+                ok = ptx::mbar_wait(&S->o_full[kk & 1], (uint32_t)(kk >> 1) & 1u, wait_limit(p)) && ok;
                 ptx::tc_fence_after();
                 uint32_t o[N / 16][16];
 #pragma unroll
@@ -494,7 +494,10 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                 }
             };
 
-            for (int i = 0; i < n; ++i, ++k) {
+            // A thread's `ok` is its own from a wait to the next verdict: the loops are left on verdicts
+            // alone, so that no warp is missing where the others wait for it.
+            int i = 0;
+            for (; i < n; ++i, ++k) {
                 const int tile = cur.t0 + i, t = tile * kATile + tid;
                 const float2 sc_now = sc;
                 const int pg_now = pg;
@@ -503,7 +506,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                 pg_next = page_of(cur, tile + 2);
                 if (pg_now < 0 && t < kv) kv_report(p.status);
 
-                ok = ptx::mbar_wait(&S->s_full[k & 1], (uint32_t)(k >> 1) & 1u, kATimeoutNs) && ok;
+                ok = ptx::mbar_wait(&S->s_full[k & 1], (uint32_t)(k >> 1) & 1u, wait_limit(p)) && ok;
                 ptx::tc_fence_after();
                 float x[U];
                 {
@@ -583,7 +586,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                     // rows of V that a weight of 0 must not meet: past the sequence, or
                     // NaN where only some rows see the token
                     const int seq = 2 * k + 1, st = seq % Sh::kStages;
-                    ok = ptx::mbar_wait(&S->full[st], (uint32_t)(seq / Sh::kStages) & 1u, kATimeoutNs) && ok;
+                    ok = ptx::mbar_wait(&S->full[st], (uint32_t)(seq / Sh::kStages) & 1u, wait_limit(p)) && ok;
                     uint4 *row = reinterpret_cast<uint4 *>(ring + (size_t)st * kATileBytes + (size_t)tid * 128);
                     if (t >= maxlim) {
 #pragma unroll
@@ -632,7 +635,7 @@ attend_few_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant
                     if (more) prepare(item + 1, after_pg, after_pg_next, after_sc);
                 }
             }
-            if (!ok) break;   // agreed on: every warp of the four leaves here
+            if (i < n) break;
             if (n > 0) {
                 read_output(k - 1);
             } else {

@@ -267,7 +267,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             for (int i = 0; i < n; ++i) {
                 const int z = znext;
                 znext = slab(it.t0 + i + 1);
-                const bool ok = __all_sync(0xFFFFFFFFu, warp_wait(&empty[st], phase ^ 1u) && !*abort_flag);
+                const bool ok = __all_sync(0xFFFFFFFFu, warp_wait(p, &empty[st], phase ^ 1u) && !*abort_flag);
                 if (!ok) {
                     attend_fail(p, abort_flag);
                     break;
@@ -292,7 +292,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             const uint64_t w_desc = ptx::smem_desc(ptx::smem_u32(wring), kATileBytes, 1024, 2);   // 64 channels: 16 KB
             bool ok = true;
             auto wait = [&](uint64_t *bar, uint32_t parity) {
-                if (ok && !ptx::mbar_wait(bar, parity, kATimeoutNs)) {
+                if (ok && !ptx::mbar_wait(bar, parity, wait_limit(p))) {
                     attend_fail(p, abort_flag);
                     ok = false;
                 }
@@ -366,8 +366,8 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         bool ok = true;
         for (int i = 0; i < n; ++i) {
             const int vs = i % kMVStages, base = (it.t0 + i) * kATile;
-            ok = warp_wait(&S->v_full[vs], (uint32_t)(i / kMVStages) & 1u) &&
-                 warp_wait(&S->w_empty[i & 1], ((uint32_t)(i >> 1) & 1u) ^ 1u);
+            ok = warp_wait(p, &S->v_full[vs], (uint32_t)(i / kMVStages) & 1u) &&
+                 warp_wait(p, &S->w_empty[i & 1], ((uint32_t)(i >> 1) & 1u) ^ 1u);
             ok = __all_sync(0xFFFFFFFFu, ok && !*abort_flag);
             if (!ok) {
                 attend_fail(p, abort_flag);
@@ -540,7 +540,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         for (int i = 0; i < steps; ++i) {
             const int tile = first + i * stride, rel = lim - tile * kATile;   // columns of the tile that this row sees
             const bool mixed = (tile + 1) * kATile > minlim;
-            ok = warp_wait(&S->s_full[q], (uint32_t)i & 1u);
+            ok = warp_wait(p, &S->s_full[q], (uint32_t)i & 1u);
             ok = __all_sync(0xFFFFFFFFu, ok && !*abort_flag);
             if (!ok) break;
             ptx::tc_fence_after();
@@ -588,7 +588,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
             take_scales(tile + 3 * stride);
         }
         if (ok && steps > 0) {
-            ok = ptx::mbar_wait(&S->o_full[q], (uint32_t)(steps - 1) & 1u, kATimeoutNs);
+            ok = ptx::mbar_wait(&S->o_full[q], (uint32_t)(steps - 1) & 1u, wait_limit(p));
             ok = __all_sync(0xFFFFFFFFu, ok);
         }
         if (!ok) attend_fail(p, abort_flag);

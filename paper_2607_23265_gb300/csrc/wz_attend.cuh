@@ -19,7 +19,7 @@ constexpr int kFewSlots = 960;               // pieces of items that several CTA
 constexpr int kManyRows = 256;               // query rows of a CTA of attend_many
 constexpr int kManySlots = 320;              // pieces of its row tiles
 constexpr double kSplitTiles = 3;            // what a CTA's start and end cost, in tiles
-constexpr uint64_t kATimeoutNs = 2000000000ull;
+constexpr uint64_t kATimeoutNs = 2000000000ull;   // limit of every wait
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttendMaps {
@@ -44,7 +44,20 @@ struct AttendParams {
     int most;                // attend_few: tokens of a sequence that its rows have room for, max_new or more
     float scale2;            // scale * log2(e)
     int *status;
+#ifdef WZ_CHECKED
+    uint64_t wait_ns;        // limit of the waits that a warp gives up on (a test's may be short)
+#endif
 };
+
+// Limit of a wait for another warp, a copy or a product that the kernel gives up on.  Waits for
+// what is in flight when it ends, after it gave up too, keep kATimeoutNs.
+__device__ __forceinline__ uint64_t wait_limit(const AttendParams &p) {
+#ifdef WZ_CHECKED
+    return p.wait_ns;
+#else
+    return kATimeoutNs;
+#endif
+}
 
 __device__ __forceinline__ float ex2(float x) {
     float r;
@@ -87,8 +100,8 @@ __device__ __forceinline__ int attend_page(const AttendParams &p, int b, int t) 
 // A barrier's phase, waited for by a whole warp; the same answer in every lane, false
 // where the wait gave up.  (Lane 0 alone, the others behind it, took longer: prompts of
 // 6,151 tokens 510 us instead of 451.)
-__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity) {
-    return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, kATimeoutNs));
+__device__ __forceinline__ bool warp_wait(const AttendParams &p, uint64_t *bar, uint32_t parity) {
+    return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, wait_limit(p)));
 }
 
 __device__ __forceinline__ void attend_fail(const AttendParams &p, volatile int *abort_flag) {
