@@ -732,7 +732,8 @@ __global__ void __launch_bounds__(512) attend_join_kernel(const __grid_constant_
     if (rows == 0) return;
     const int2 span = len.y > 0 ? p.spans[(size_t)x0 * p.heads + h] : make_int2(0, 0);
     if (span.y == 1) return;   // one CTA had the whole item
-    if (span.x < 0 || span.y < 0 || span.x + span.y > p.ctas) return;   // never written: the kernel before gave up
+    // never written: the kernel before gave up (any numbers, so no sum of them)
+    if (span.x < 0 || span.y < 0 || span.x > p.ctas - span.y) return;
     for (int c = BY_ROW ? warp : (int)blockIdx.y; c < rows; c += R) {
         float m = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
         constexpr int kStep = BY_ROW ? 1 : kWarps;

@@ -72,3 +72,22 @@ def test_calls_end_and_the_next_is_right(wz, case):
     out = wz.wz_attend(*args, max_new=n, workspace=workspace, lse=lse)
     assert bool(torch.isfinite(out).all())
     compare(out, lse, host, q, table, cu, kv, True, D ** -0.5)
+
+
+@pytest.mark.parametrize("first,pieces", [(2 ** 31 - 1, 2), (2 ** 31 - 1, 2 ** 31 - 1), (-1, 5), (5, -1), (0, 2 ** 31 - 1),
+                                          (400, 2 ** 30), (-2 ** 31, -2 ** 31)])
+def test_pieces_that_nobody_wrote(wz, first, pieces):
+    """Items whose CTAs gave up before they wrote where their pieces lie: the join finds what the workspace held."""
+    P, heads, D, kv = 32, 2, 64, [5000] * 40
+    table, pages = tables(kv, P, 3)
+    gpu = ref.Cache(pages, heads, P, D, seed=6).on_gpu(wz)
+    q = torch.randn((40, 4, D), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    args = (q, gpu, i32(table), i32(list(range(41))), i32(kv))
+    want = wz.wz_attend(*args, max_new=1).clone()
+    workspace = torch.empty(wz.wz_attend_workspace_size(40, 4, D) // 8 * 8, dtype=torch.uint8, device="cuda")
+    workspace.view(torch.int32).view(-1, 2)[:] = i32([first, pieces])
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    with impatient(wz):
+        wz.wz_attend(*args, max_new=1, workspace=workspace, device_status=status)
+    assert int(status) == wz.STATUS_WAIT_TIMEOUT
+    assert torch.equal(wz.wz_attend(*args, max_new=1, workspace=workspace), want)
