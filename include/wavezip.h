@@ -507,7 +507,7 @@ typedef struct {
                              /* tokens past it may be left out, reported     */
     int Hq;                  /* a multiple of the cache's heads, the same    */
     const int32_t *cu;       /* [B+1] rows of q of each sequence             */
-    const int32_t *kv_len;   /* [B] slots in use                             */
+    const int32_t *kv_len;   /* [B] slots in use, at most 2^31 - 257         */
     const int32_t *page_table; /* [B][max_pages]                             */
     int max_pages;
     int causal;

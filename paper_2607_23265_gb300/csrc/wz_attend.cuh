@@ -65,10 +65,15 @@ __device__ __forceinline__ float ex2(float x) {
     return r;
 }
 
+// The most slots of a sequence: what the table has room for; tiles past them are counted in int too.
+__device__ __forceinline__ int64_t attend_most(const AttendParams &p) {
+    return min((int64_t)p.max_pages * p.P, (int64_t)INT32_MAX - 2 * kATile);
+}
+
 // Tokens of q and slots of sequence b; no tokens where its lengths make no sense.
 __device__ __forceinline__ int2 attend_lengths(const AttendParams &p, int b) {
     const int x0 = p.cu[b], x1 = p.cu[b + 1];
-    const int64_t most = min((int64_t)p.max_pages * p.P, (int64_t)INT32_MAX - 2 * kATile);
+    const int64_t most = attend_most(p);
     int kv = p.kv_len[b];
     if (kv < 0) kv = 0;
     if (kv > most) kv = (int)most;
@@ -81,7 +86,7 @@ __device__ __forceinline__ int2 attend_lengths(const AttendParams &p, int b) {
 __device__ __forceinline__ bool attend_lengths_sound(const AttendParams &p, int b) {
     const int x0 = p.cu[b], x1 = p.cu[b + 1], kv = p.kv_len[b];
     return x0 >= 0 && x1 >= x0 && x1 <= p.T && x1 - x0 <= p.max_new && kv >= 0 &&
-           kv <= (int64_t)p.max_pages * p.P;
+           kv <= attend_most(p);
 }
 
 // Slots that token i of n sees.
