@@ -647,6 +647,17 @@ def _current_stream(stream, device: int) -> int:
     return torch._C._cuda_getCurrentRawStream(device)
 
 
+def _call(fn, a, device: int, where: str):
+    """Calls the library with the cache's device current: launches, and a stream's number 0, are the current device's."""
+    if torch._C._cuda_getDevice() == device:
+        st = fn(a)
+    else:
+        with torch.cuda.device(device):
+            st = fn(a)
+    if st != OK:
+        raise WaveZipError(st, where)
+
+
 def _sequences(a, cu, lens, page_table, device: int, name: str):
     a.cu, a.page_table = _ints(cu, device, "cu"), _ints(page_table, device, "page_table", 2)
     B = lens.shape[0]
@@ -697,9 +708,7 @@ def wz_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KvCache, page_table: t
     if device_status is not None:
         a.device_status = _ints(device_status, dev, "device_status")
     a.stream = _current_stream(stream, dev)
-    st = _lib.wz_kv_append(a)
-    if st != OK:
-        raise WaveZipError(st, "wz_kv_append")
+    _call(_lib.wz_kv_append, a, dev, "wz_kv_append")
     return q_out if q is not None else None
 
 
@@ -733,7 +742,5 @@ def wz_attend(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, cu: tor
     if device_status is not None:
         a.device_status = _ints(device_status, dev, "device_status")
     a.stream = _current_stream(stream, dev)
-    st = _lib.wz_attend(a)
-    if st != OK:
-        raise WaveZipError(st, "wz_attend")
+    _call(_lib.wz_attend, a, dev, "wz_attend")
     return out
