@@ -738,6 +738,8 @@ def wz_attend(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, cu: tor
         a.lse = lse.data_ptr()
     a.kv_len = _sequences(a, cu, kv_len, page_table, dev, "kv_len")
     if workspace is not None:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the cache's device")
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.nbytes
     if device_status is not None:
         a.device_status = _ints(device_status, dev, "device_status")

@@ -91,3 +91,12 @@ def call(wz, monkeypatch):
 @pytest.mark.parametrize("current", [0, 1])
 def test_the_cache_s_device_is_current_in_the_call(call, name, current):
     assert call(name, current) == [1]
+
+
+@pytest.mark.parametrize("workspace", [Fake(1 << 26, dtype=torch.uint8, device=-1),
+                                       Fake(1 << 26, dtype=torch.uint8, device=0),
+                                       Fake(1 << 26, dtype=torch.uint8, contiguous=False)])
+def test_workspaces_that_the_device_cannot_use(call, workspace):
+    with pytest.raises(ValueError, match="workspace"):
+        call("attend", workspace=workspace)
+    assert call("attend", workspace=Fake(1 << 26, dtype=torch.uint8)) == [1]
