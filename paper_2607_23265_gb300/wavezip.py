@@ -721,16 +721,12 @@ def wz_attend(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, cu: tor
               lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
               device_status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """wz_attend: q [T, Hq, D] bf16 attends to the first kv_len[b] slots of its sequence.  Returns the
-    output [T, Hq, D] bf16; lse [T, Hq] float32 is written where given.  scale: None for 1 / sqrt(D)."""
+    output [T, Hq, D] bf16; lse [T, Hq] float32 is written where given."""
     dev, T, D = cache.index, q.shape[0], cache.D
     if out is None:
         out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-    if scale is None:
-        scale = 0.0
-    elif scale == 0:
-        raise ValueError("scale must not be 0, which stands for 1 / sqrt(D) in the library; None does here")
     a = AttendArgs()
-    a.cache, a.T, a.max_new, a.causal, a.scale = cache._struct, T, max_new, causal, scale
+    a.cache, a.T, a.max_new, a.causal, a.scale = cache._struct, T, max_new, causal, scale or 0.0
     Hq, a.q_stride = _rows(q, T, D, torch.bfloat16, dev, "q")
     out_heads, a.out_stride = _rows(out, T, D, torch.bfloat16, dev, "out")
     if out_heads != Hq:

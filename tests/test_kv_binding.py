@@ -100,9 +100,3 @@ def test_workspaces_that_the_device_cannot_use(call, workspace):
     with pytest.raises(ValueError, match="workspace"):
         call("attend", workspace=workspace)
     assert call("attend", workspace=Fake(1 << 26, dtype=torch.uint8)) == [1]
-
-
-def test_a_scale_of_zero_is_not_the_default(call):
-    with pytest.raises(ValueError, match="scale"):
-        call("attend", scale=0.0)
-    assert len(call("attend", scale=None)) == 1 and len(call("attend", scale=-0.5)) == 1
