@@ -641,6 +641,15 @@ def _ints(t: torch.Tensor, device: int, name: str, dim: int = 1) -> int:
     return t.data_ptr()
 
 
+def _output(shape, dtype, device, stream) -> torch.Tensor:
+    """A new tensor that belongs to the stream it is written on: memory of the current stream's may still be in use
+    there, and is given out there again as soon as the tensor goes."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _current_stream(stream, device: int) -> int:
     if stream is not None:
         return stream.cuda_stream
@@ -674,7 +683,8 @@ def wz_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KvCache, page_table: t
                  positions: torch.Tensor | None = None, sections=None, interleaved: bool = False,
                  device_status: torch.Tensor | None = None, stream=None):
     """wz_kv_append: k, v [T, heads, D] into the cache, keys (and queries q [T, Hq, D]) rotated on the way.
-    Rows may be slices of a wider projection.  Returns the rotated queries (q_out), or None without q."""
+    Rows may be slices of a wider projection.  Returns the rotated queries (q_out), or None without q.  What is
+    allocated here for a call on a given stream belongs to that stream."""
     dev, T, D, dtype = cache.index, k.shape[0], cache.D, k.dtype
     a = KvAppendArgs()
     a.cache, a.T, a.max_new, a.dtype, a.axes = cache._struct, T, max_new, _dtype_code(k), 1
@@ -685,7 +695,7 @@ def wz_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KvCache, page_table: t
     a.k, a.v = k.data_ptr(), v.data_ptr()
     if q is not None:
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = _output(q.shape, q.dtype, q.device, stream)
         a.Hq, a.q_stride = _rows(q, T, D, dtype, dev, "q")
         out_heads, a.q_out_stride = _rows(q_out, T, D, dtype, dev, "q_out")
         if out_heads != a.Hq:
@@ -724,7 +734,7 @@ def wz_attend(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, cu: tor
     output [T, Hq, D] bf16; lse [T, Hq] float32 is written where given."""
     dev, T, D = cache.index, q.shape[0], cache.D
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        out = _output(q.shape, torch.bfloat16, q.device, stream)
     a = AttendArgs()
     a.cache, a.T, a.max_new, a.causal, a.scale = cache._struct, T, max_new, causal, scale or 0.0
     Hq, a.q_stride = _rows(q, T, D, torch.bfloat16, dev, "q")
