@@ -53,8 +53,9 @@ AttendPlan attend_plan(const wz_attend_args &a, int sms) {
     const int64_t items = (rows + kManyRows - 1) / kManyRows * a.cache.heads * a.B;
     const int64_t tiles = ((int64_t)a.max_pages * a.cache.page_tokens + kATile - 1) / kATile;
     // Up to 128 rows fill one of a CTA's two tiles.  Paired, both work on them, which takes
-    // 0.62 to 0.75 of the time a tile, but twice the pieces: 70 rows on 328,032 slots 192 us
-    // for 238, 128 on 8 x 4,097 42 for 47; 112 on 18,699, where a CTA has five tiles, 35 for 28.
+    // 0.62 to 0.75 of the time a tile, but twice the pieces: 10 tokens of 28/4 heads x 96 on 2 x
+    // 328,032 slots 193 us for 237, 32 of 32/8 x 128 on 8 x 4,097 44 for 48; 16 of 28/4 x 128
+    // on 18,699, where a CTA has five tiles, 37 for 29.
     double best = 0;
     for (int paired = 0; paired <= (rows <= 128 && items <= kManySlots ? 1 : 0); ++paired)
         for (int s = 1; s <= 32 && (s == 1 || (items * s <= kManySlots && s <= tiles)); ++s) {

@@ -26,9 +26,9 @@
 //   warp 5     TMEM allocation, MMA issuer (one thread)
 // One query over 200,003 slots of 4 heads x 128 takes 40 us: 205 MB at 6.9 TB/s between
 // the first copies' arrival (4 us) and the median CTA's end (33 us), then the slowest
-// SMs' tails and the join (7 us).  64 queries over up to 18,699 slots 92-98 us for 454
-// MB; with tiles' rows in byte stores, scalars by every thread and a join that scanned
-// the lengths again 105.
+// SMs' tails and the join (7 us).  64 queries over up to 18,699 slots 78 us for 454 MB
+// (95 with a join whose loads wait for one another; 105 beside that with tiles' rows in byte
+// stores, scalars by every thread and a join that scanned the lengths again).
 // Every wait is bounded; where one gives up the kernel sets a status bit, ends
 // its copies, frees tensor memory and returns.
 #include <algorithm>
@@ -728,7 +728,10 @@ __global__ void __launch_bounds__(512) attend_join_kernel(const __grid_constant_
     const int x0 = p.cu[b];
     pdl_wait();
     pdl_trigger();
-    const int rows = min(len.x, p.most) * p.G;   // those that the kernel before formed
+    // Those that the kernel before formed.  (Where the compiler sees that they are R at most it
+    // gives the loads of a batch of pieces 42 registers instead of 63 and one waits for the
+    // other: 64 ragged queries 97 us instead of 78, 741 slots 9.3 instead of 8.7.)
+    const int rows = min(len.x, p.most) * p.G;
     if (rows == 0) return;
     const int2 span = len.y > 0 ? p.spans[(size_t)x0 * p.heads + h] : make_int2(0, 0);
     if (span.y == 1) return;   // one CTA had the whole item

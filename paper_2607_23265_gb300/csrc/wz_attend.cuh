@@ -103,8 +103,8 @@ __device__ __forceinline__ int attend_page(const AttendParams &p, int b, int t) 
 }
 
 // A barrier's phase, waited for by a whole warp; the same answer in every lane, false
-// where the wait gave up.  (Lane 0 alone, the others behind it, took longer: prompts of
-// 6,151 tokens 510 us instead of 451.)
+// where the wait gave up.  (Lane 0 alone, the others behind it, took longer: a prompt of 6,151
+// tokens 510 us instead of 451, when that was its time; 260 now.)
 __device__ __forceinline__ bool warp_wait(const AttendParams &p, uint64_t *bar, uint32_t parity) {
     return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, wait_limit(p)));
 }

@@ -731,7 +731,9 @@ def wz_attend(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, cu: tor
               lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
               device_status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """wz_attend: q [T, Hq, D] bf16 attends to the first kv_len[b] slots of its sequence.  Returns the
-    output [T, Hq, D] bf16; lse [T, Hq] float32 is written where given."""
+    output [T, Hq, D] bf16; lse [T, Hq] float32 is written where given.  scale: None or 0 for 1 / sqrt(D).
+    max_new: the most tokens of a sequence (0: T), from which, and from the table's width, the call is planned:
+    give it for decoding.  What is allocated here for a call on a given stream belongs to that stream."""
     dev, T, D = cache.index, q.shape[0], cache.D
     if out is None:
         out = _output(q.shape, torch.bfloat16, q.device, stream)
