@@ -506,11 +506,10 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&S->q_ready);
+        const float rowf = S->rowf[row];   // this warp's rows
         const int at = it.r0 + row - same, tok = at / p.G;
         const bool real = at < it.r1;
         const int lim = real ? max(0, min(it.kv, attend_visible(p, tok, it.n, it.kv))) : 0;
-        // of this warp's rows; not NaN for a row that sees nothing, whose hidden logits it multiplies
-        const float rowf = lim > 0 ? S->rowf[row] : 1.f;
 
         float ref = -INFINITY, sum = 0.f;
         bool ok = true;
@@ -596,6 +595,7 @@ attend_many_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         if (ok && q < qtiles) {
             const int hq = it.h * p.G + at - tok * p.G;
             const size_t x = (size_t)(it.x0 + tok);
+            if (lim == 0) sum = 0.f;   // a row that sees nothing: NaN where its query, and so its factor, is
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
             const bool nans = *reinterpret_cast<volatile int *>(&S->any_nan);
             uint32_t o[4][32];
