@@ -534,6 +534,138 @@ WZ_API size_t wz_attend_workspace_size(int64_t T, int Hq, int D);
 WZ_API int wz_attend(const wz_attend_args *a);
 
 /* ------------------------------------------------------------------------ */
+/* A layer's matrix products, forward and backward                            */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * What stands around wz_attend in a decoder layer (queries, keys and values
+ * from a token, its attention's output back into the residual stream, the gated
+ * feed-forward block), and what trains those products and the projector P.
+ * Rows x [M][K], weights [N][K] (torch.nn.Linear, out x in), results and weight
+ * gradients are bf16; biases and their gradients f32.  Products run on the
+ * tensor cores (tcgen05) with fp32 accumulation; bias, activation and residual are
+ * applied to the fp32 sums, which are rounded once, when they are stored.
+ *   M >= 0, N and K from 1 to 65536, odd ones among them; a stride is the
+ * elements from one row to the next, a multiple of 8 that is no less than the row;
+ * what lies between a row's end and the next row is neither read nor written.
+ * Every bf16 array 16-byte aligned, f32 arrays 4-byte.  Results do not depend
+ * on the order in which blocks run: equal calls give equal bits.
+ *   Outputs must not overlap inputs, but for `out` of wz_linear, which may be
+ * `residual` itself (same address and stride).
+ * Errors of all four: WZ_ERR_INVALID_ARG (null, misaligned, bad size or enum),
+ * WZ_ERR_UNSUPPORTED (M past 2^31 - 513, N or K past 65536, M N or M K past 2^40),
+ * WZ_ERR_WORKSPACE, WZ_ERR_NO_MEMORY, WZ_ERR_CUDA; nothing is launched on an
+ * argument error.  device_status: a bounded wait that gives up ORs WZ_STATUS_WAIT_TIMEOUT into it.
+ */
+#define WZ_ACT_NONE      0 /* p                                               */
+#define WZ_ACT_GELU      1 /* p (1 + erf(p / sqrt 2)) / 2                     */
+#define WZ_ACT_GELU_TANH 2 /* p (1 + tanh(sqrt(2 / pi) (p + 0.044715 p^3))) / 2 */
+#define WZ_ACT_SILU      3 /* p / (1 + exp(-p))                               */
+
+/* out = act(p) + residual, p = x W^T + bias. */
+typedef struct {
+    const void *x;           /* [M] rows of K                                */
+    const void *w;           /* [N] rows of K                                */
+    const float *bias;       /* [N]; nullable                                */
+    const void *residual;    /* [M] rows of N; nullable                      */
+    void *out;               /* [M] rows of N                                */
+    void *pre;               /* [M] rows of N: p, for the backward pass; nullable */
+    int64_t x_stride, w_stride, residual_stride, out_stride, pre_stride;
+    int64_t M;
+    int N, K;
+    int act;                 /* WZ_ACT_*                                     */
+    int32_t *device_status;  /* [1]; nullable                                */
+    wz_stream_t stream;
+} wz_linear_args;
+
+WZ_API void wz_linear_args_init(wz_linear_args *a);   /* zeros */
+WZ_API int wz_linear(const wz_linear_args *a);
+
+/*
+ * Gradients of wz_linear: d = dy act'(p), dx = d W, dw = d^T x, db = sum_m d
+ * (the residual's gradient is dy itself).  p is `pre` as wz_linear left it or,
+ * with pre NULL and an activation, formed again from x, w and bias.  d enters the
+ * products in bf16, db's sum unrounded.  dx, dw and db may each be NULL: not wanted.
+ * With M = 0, dw and db are zeros.
+ */
+typedef struct {
+    const void *dy;          /* [M] rows of N                                */
+    const void *x;           /* [M] rows of K                                */
+    const void *w;           /* [N] rows of K                                */
+    const float *bias;       /* [N], read only where p is formed again; nullable */
+    const void *pre;         /* [M] rows of N; nullable                      */
+    void *dx;                /* [M] rows of K; nullable                      */
+    void *dw;                /* [N] rows of K; nullable                      */
+    float *db;               /* [N]; nullable                                */
+    int64_t dy_stride, x_stride, w_stride, pre_stride, dx_stride, dw_stride;
+    int64_t M;
+    int N, K;
+    int act;                 /* WZ_ACT_*                                     */
+    void *workspace;         /* >= wz_linear_backward_workspace_size(), 256-B */
+    size_t workspace_bytes;  /* aligned; NULL = cudaMallocAsync on stream    */
+    int32_t *device_status;  /* [1]; nullable                                */
+    wz_stream_t stream;
+} wz_linear_backward_args;
+
+WZ_API void wz_linear_backward_args_init(wz_linear_backward_args *a);   /* zeros */
+/* Bytes that a call of these sizes needs at most; 0 for sizes that it refuses. */
+WZ_API size_t wz_linear_backward_workspace_size(int64_t M, int K, int N);
+WZ_API int wz_linear_backward(const wz_linear_backward_args *a);
+
+/* The first half of a gated feed-forward block: out = act(g) u with
+ * g = x Wg^T + b_gate and u = x Wu^T + b_up; the second half is wz_linear with the
+ * block's input as its residual. */
+typedef struct {
+    const void *x;           /* [M] rows of K                                */
+    const void *w_gate, *w_up; /* [N] rows of K                              */
+    const float *b_gate, *b_up; /* [N]; nullable                             */
+    void *out;               /* [M] rows of N                                */
+    void *gate, *up;         /* [M] rows of N: g and u, for the backward pass; */
+                             /* both or neither                              */
+    int64_t x_stride, w_gate_stride, w_up_stride, out_stride, gate_stride, up_stride;
+    int64_t M;
+    int N, K;
+    int act;                 /* WZ_ACT_*                                     */
+    int32_t *device_status;  /* [1]; nullable                                */
+    wz_stream_t stream;
+} wz_gated_args;
+
+WZ_API void wz_gated_args_init(wz_gated_args *a);   /* zeros, act = WZ_ACT_SILU */
+WZ_API int wz_gated(const wz_gated_args *a);
+
+/*
+ * Gradients of wz_gated: dg = dout u act'(g), du = dout act(g), dx = dg Wg + du Wu,
+ * dw_gate = dg^T x, dw_up = du^T x, db_gate = sum_m dg, db_up = sum_m du.  g and u are
+ * as wz_gated left them or, with both NULL, formed again from x and the weights;
+ * the rest as for wz_linear_backward.  dw_gate and dw_up go together, db_gate and
+ * db_up may each be NULL.
+ */
+typedef struct {
+    const void *dout;        /* [M] rows of N                                */
+    const void *x;           /* [M] rows of K                                */
+    const void *w_gate, *w_up; /* [N] rows of K                              */
+    const float *b_gate, *b_up; /* [N], read only where g and u are formed again; */
+                             /* nullable                                     */
+    const void *gate, *up;   /* [M] rows of N; both or neither               */
+    void *dx;                /* [M] rows of K; nullable                      */
+    void *dw_gate, *dw_up;   /* [N] rows of K; both or neither               */
+    float *db_gate, *db_up;  /* [N]; nullable                                */
+    int64_t dout_stride, x_stride, w_gate_stride, w_up_stride, gate_stride, up_stride;
+    int64_t dx_stride, dw_gate_stride, dw_up_stride;
+    int64_t M;
+    int N, K;
+    int act;                 /* WZ_ACT_*                                     */
+    void *workspace;         /* >= wz_gated_backward_workspace_size(), 256-B */
+    size_t workspace_bytes;  /* aligned; NULL = cudaMallocAsync on stream    */
+    int32_t *device_status;  /* [1]; nullable                                */
+    wz_stream_t stream;
+} wz_gated_backward_args;
+
+WZ_API void wz_gated_backward_args_init(wz_gated_backward_args *a);   /* zeros, act = WZ_ACT_SILU */
+WZ_API size_t wz_gated_backward_workspace_size(int64_t M, int K, int N);
+WZ_API int wz_gated_backward(const wz_gated_backward_args *a);
+
+/* ------------------------------------------------------------------------ */
 /* Single-level DWT (Eq. 8, 10, 11, 14)                                      */
 /* ------------------------------------------------------------------------ */
 

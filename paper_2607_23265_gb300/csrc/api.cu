@@ -975,6 +975,120 @@ int wz_attend(const wz_attend_args *a) {
     return WZ_OK;
 }
 
+// Sizes that all four layer calls share.
+static int check_layer(int64_t M, int N, int K, int act) {
+    if (M < 0 || N < 1 || K < 1 || act < WZ_ACT_NONE || act > WZ_ACT_SILU) return WZ_ERR_INVALID_ARG;
+    const int64_t most = (int64_t)1 << 40;
+    if (M > INT32_MAX - 512 || N > 65536 || K > 65536 || M * N > most || M * K > most) return WZ_ERR_UNSUPPORTED;
+    return WZ_OK;
+}
+
+// As rows_ok, for an array that may be null.
+static bool rows_or_null(const void *p, int64_t stride, int64_t width) { return !p || rows_ok(p, stride, width); }
+
+void wz_linear_args_init(wz_linear_args *a) {
+    if (a) memset(a, 0, sizeof(*a));
+}
+
+int wz_linear(const wz_linear_args *a) {
+    if (!a) return WZ_ERR_INVALID_ARG;
+    const int st = check_layer(a->M, a->N, a->K, a->act);
+    if (st != WZ_OK || a->M == 0) return st;
+    if (!rows_ok(a->x, a->x_stride, a->K) || !rows_ok(a->w, a->w_stride, a->K) || !rows_ok(a->out, a->out_stride, a->N) ||
+        !rows_or_null(a->residual, a->residual_stride, a->N) || !rows_or_null(a->pre, a->pre_stride, a->N) ||
+        !aligned(a->bias, 4) || !aligned(a->device_status, 4))
+        return WZ_ERR_INVALID_ARG;
+    Nvtx range("wz::linear");
+    WZ_CUDA(launch_linear(*a, (cudaStream_t)a->stream));
+    return WZ_OK;
+}
+
+void wz_linear_backward_args_init(wz_linear_backward_args *a) {
+    if (a) memset(a, 0, sizeof(*a));
+}
+
+size_t wz_linear_backward_workspace_size(int64_t M, int K, int N) {
+    return check_layer(M, N, K, WZ_ACT_NONE) == WZ_OK ? align_up(linear_backward_bytes(M, N)) : 0;
+}
+
+int wz_linear_backward(const wz_linear_backward_args *a) {
+    if (!a) return WZ_ERR_INVALID_ARG;
+    int st = check_layer(a->M, a->N, a->K, a->act);
+    if (st != WZ_OK) return st;
+    if (!rows_or_null(a->dw, a->dw_stride, a->K) || !aligned(a->db, 4) || !aligned(a->bias, 4) ||
+        !aligned(a->device_status, 4) || !aligned(a->workspace, kAlign))
+        return WZ_ERR_INVALID_ARG;
+    if (a->M > 0 && (!rows_ok(a->dy, a->dy_stride, a->N) || !rows_ok(a->x, a->x_stride, a->K) ||
+                     !rows_ok(a->w, a->w_stride, a->K) || !rows_or_null(a->pre, a->pre_stride, a->N) ||
+                     !rows_or_null(a->dx, a->dx_stride, a->K)))
+        return WZ_ERR_INVALID_ARG;
+    const cudaStream_t s = (cudaStream_t)a->stream;
+    Scratch ws;
+    const size_t need = linear_backward_bytes(a->M, a->N);
+    // without an activation and db nothing is kept between kernels
+    const bool keeps = a->M > 0 && (a->act != WZ_ACT_NONE || a->db);
+    if ((a->workspace || keeps) && (st = ws.acquire(a->workspace, a->workspace_bytes, need, s)) != WZ_OK) return st;
+    Nvtx range("wz::linear_backward");
+    WZ_CUDA(launch_linear_backward(*a, ws.ptr, s));
+    return WZ_OK;
+}
+
+void wz_gated_args_init(wz_gated_args *a) {
+    if (!a) return;
+    memset(a, 0, sizeof(*a));
+    a->act = WZ_ACT_SILU;
+}
+
+int wz_gated(const wz_gated_args *a) {
+    if (!a) return WZ_ERR_INVALID_ARG;
+    const int st = check_layer(a->M, a->N, a->K, a->act);
+    if (st != WZ_OK) return st;
+    if (!a->gate != !a->up) return WZ_ERR_INVALID_ARG;
+    if (a->M == 0) return WZ_OK;
+    if (!rows_ok(a->x, a->x_stride, a->K) || !rows_ok(a->w_gate, a->w_gate_stride, a->K) ||
+        !rows_ok(a->w_up, a->w_up_stride, a->K) || !rows_ok(a->out, a->out_stride, a->N) ||
+        !rows_or_null(a->gate, a->gate_stride, a->N) || !rows_or_null(a->up, a->up_stride, a->N) ||
+        !aligned(a->b_gate, 4) || !aligned(a->b_up, 4) || !aligned(a->device_status, 4))
+        return WZ_ERR_INVALID_ARG;
+    Nvtx range("wz::gated");
+    WZ_CUDA(launch_gated(*a, (cudaStream_t)a->stream));
+    return WZ_OK;
+}
+
+void wz_gated_backward_args_init(wz_gated_backward_args *a) {
+    if (!a) return;
+    memset(a, 0, sizeof(*a));
+    a->act = WZ_ACT_SILU;
+}
+
+size_t wz_gated_backward_workspace_size(int64_t M, int K, int N) {
+    return check_layer(M, N, K, WZ_ACT_NONE) == WZ_OK ? align_up(gated_backward_bytes(M, N)) : 0;
+}
+
+int wz_gated_backward(const wz_gated_backward_args *a) {
+    if (!a) return WZ_ERR_INVALID_ARG;
+    int st = check_layer(a->M, a->N, a->K, a->act);
+    if (st != WZ_OK) return st;
+    if (!a->gate != !a->up || !a->dw_gate != !a->dw_up) return WZ_ERR_INVALID_ARG;
+    if (!rows_or_null(a->dw_gate, a->dw_gate_stride, a->K) || !rows_or_null(a->dw_up, a->dw_up_stride, a->K) ||
+        !aligned(a->db_gate, 4) || !aligned(a->db_up, 4) || !aligned(a->b_gate, 4) || !aligned(a->b_up, 4) ||
+        !aligned(a->device_status, 4) || !aligned(a->workspace, kAlign))
+        return WZ_ERR_INVALID_ARG;
+    if (a->M > 0 && (!rows_ok(a->dout, a->dout_stride, a->N) || !rows_ok(a->x, a->x_stride, a->K) ||
+                     !rows_ok(a->w_gate, a->w_gate_stride, a->K) || !rows_ok(a->w_up, a->w_up_stride, a->K) ||
+                     !rows_or_null(a->gate, a->gate_stride, a->N) || !rows_or_null(a->up, a->up_stride, a->N) ||
+                     !rows_or_null(a->dx, a->dx_stride, a->K)))
+        return WZ_ERR_INVALID_ARG;
+    const cudaStream_t s = (cudaStream_t)a->stream;
+    Scratch ws;
+    if ((a->workspace || a->M > 0) &&
+        (st = ws.acquire(a->workspace, a->workspace_bytes, gated_backward_bytes(a->M, a->N), s)) != WZ_OK)
+        return st;
+    Nvtx range("wz::gated_backward");
+    WZ_CUDA(launch_gated_backward(*a, ws.ptr, s));
+    return WZ_OK;
+}
+
 int wz_dwt_len(int n, int wavelet) {
     const int F = wavelet_taps(wavelet);
     if (n < 1 || F == 0) return -1;

@@ -1,0 +1,393 @@
+// A layer's matrix products and their gradients (wz_linear, wz_gated and their
+// backward passes): the launches of a call, and the kernels beside the products.
+//
+//   mm_delta_kernel   d = dy act'(p), or dg = dout u act'(g) and du = dout act(g), from
+//                     kept products, with column sums over 64 rows; or the sums alone
+//   mm_sum_kernel     bias gradients from those sums
+#include <cstring>
+#include <type_traits>
+
+#include "wz_mm.cuh"
+
+namespace wz {
+
+namespace {
+
+size_t pad256(size_t x) { return (x + 255) / 256 * 256; }
+
+constexpr int kDeltaRows = 64, kDeltaCols = 256, kDeltaWarps = 8;
+
+enum DeltaMode : int { kDeltaSums = 0, kDeltaSlope = 1, kDeltaGated = 2 };
+
+struct DeltaArgs {
+    const __nv_bfloat16 *dy, *pre[2];   // kDeltaSlope: p; kDeltaGated: g and u
+    __nv_bfloat16 *d[2];
+    float *part[2];                     // [ceil(M / 64)][N]; null: not wanted
+    int64_t dy_stride, pre_stride[2], d_stride;
+    int64_t M;
+    int N, act;
+};
+
+}  // namespace
+
+// A block takes 64 rows of 256 columns, a warp every eighth row, a lane eight columns: 16-byte
+// loads and stores, the column sums in registers and then over the warps in a fixed order.
+template <int MODE>
+__global__ void __launch_bounds__(32 * kDeltaWarps) mm_delta_kernel(const __grid_constant__ DeltaArgs p) {
+    __shared__ float sums[kDeltaWarps][kDeltaCols];
+    pdl_wait();
+    pdl_trigger();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n = (int)blockIdx.y * kDeltaCols + 8 * lane, left = p.N - n;
+    const int64_t m0 = (int64_t)blockIdx.x * kDeltaRows;
+    float a0[8] = {}, a1[8] = {};
+    if (left > 0) {
+        mm_with_act(p.act, [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+#pragma unroll 4
+            for (int r = warp; r < kDeltaRows; r += kDeltaWarps) {
+                const int64_t m = m0 + r;
+                if (m >= p.M) break;
+                float dy[8];
+                mm_load(p.dy + m * p.dy_stride + n, dy, left);
+                if constexpr (MODE == kDeltaSums) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) a0[j] += dy[j];
+                } else {
+                    float g[8], u[8];
+                    mm_load(p.pre[0] + m * p.pre_stride[0] + n, g, left);
+                    if constexpr (MODE == kDeltaGated) mm_load(p.pre[1] + m * p.pre_stride[1] + n, u, left);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        float value, slope;
+                        mm_slope1<ACT>(g[j], value, slope);
+                        if constexpr (MODE == kDeltaGated) {
+                            g[j] = dy[j] * u[j] * slope;
+                            u[j] = dy[j] * value;
+                            a1[j] += u[j];
+                        } else {
+                            g[j] = dy[j] * slope;
+                        }
+                        a0[j] += g[j];
+                    }
+                    mm_store(p.d[0] + m * p.d_stride + n, g, left);
+                    if constexpr (MODE == kDeltaGated) mm_store(p.d[1] + m * p.d_stride + n, u, left);
+                }
+            }
+        });
+    }
+#pragma unroll
+    for (int i = 0; i < (MODE == kDeltaGated ? 2 : 1); ++i) {
+        if (!p.part[i]) continue;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[warp][8 * lane + j] = i ? a1[j] : a0[j];
+        __syncthreads();
+        const int c = (int)blockIdx.y * kDeltaCols + (int)threadIdx.x;
+        if (c < p.N) {
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < kDeltaWarps; ++w) s += sums[w][threadIdx.x];
+            p.part[i][(size_t)blockIdx.x * p.N + c] = s;
+        }
+    }
+}
+
+constexpr int kSumRows = 16;
+
+// out[n] = the sum of part[.][n]; blockIdx.y chooses one of two.
+__global__ void __launch_bounds__(32 * kSumRows) mm_sum_kernel(const float *part0, const float *part1, float *out0,
+                                                               float *out1, int64_t rows, int N) {
+    __shared__ float sums[kSumRows][33];
+    pdl_wait();
+    pdl_trigger();
+    const float *part = blockIdx.y ? part1 : part0;
+    float *out = blockIdx.y ? out1 : out0;
+    const int c = (int)threadIdx.x & 31, r0 = (int)threadIdx.x >> 5, n = (int)blockIdx.x * 32 + c;
+    float s = 0.f;
+    if (n < N && out)
+        for (int64_t r = r0; r < rows; r += kSumRows) s += part[(size_t)r * N + n];
+    sums[r0][c] = s;
+    __syncthreads();
+    if (r0 == 0 && n < N && out) {
+#pragma unroll
+        for (int i = 1; i < kSumRows; ++i) s += sums[i][c];
+        out[n] = s;
+    }
+}
+
+namespace {
+
+cudaError_t launch_delta(DeltaMode mode, DeltaArgs &p, bool pdl, cudaStream_t s) {
+    const dim3 grid((unsigned)((p.M + kDeltaRows - 1) / kDeltaRows), (unsigned)((p.N + kDeltaCols - 1) / kDeltaCols));
+    const void *fn = mode == kDeltaSums    ? (const void *)mm_delta_kernel<kDeltaSums>
+                     : mode == kDeltaSlope ? (const void *)mm_delta_kernel<kDeltaSlope>
+                                           : (const void *)mm_delta_kernel<kDeltaGated>;
+    void *args[] = {&p};
+    return launch_kernel(fn, grid, dim3(32 * kDeltaWarps), 0, s, args, pdl);
+}
+
+cudaError_t launch_sum(const float *part0, const float *part1, float *out0, float *out1, int64_t rows, int N, bool pdl,
+                       cudaStream_t s) {
+    void *args[] = {&part0, &part1, &out0, &out1, &rows, &N};
+    return launch_kernel((const void *)mm_sum_kernel, dim3((unsigned)((N + 31) / 32), out1 ? 2 : 1), dim3(32 * kSumRows),
+                         0, s, args, pdl);
+}
+
+__nv_bfloat16 *half(void *p) { return static_cast<__nv_bfloat16 *>(p); }
+const __nv_bfloat16 *half(const void *p) { return static_cast<const __nv_bfloat16 *>(p); }
+
+MmArgs mm_args(int act, int *status) {
+    MmArgs p;
+    memset(&p, 0, sizeof(p));
+    p.problems = 1;
+    p.act = act;
+    p.status = status;
+    p.wait_ns = mm_wait_ns();
+    return p;
+}
+
+int64_t steps_of(int64_t k) { return (k + 63) / 64; }
+
+// A launch's products: maps are added as they are named.
+struct Builder {
+    MmMaps maps;
+    int count = 0;
+    bool ok = true;
+    Builder() { memset(&maps, 0, sizeof(maps)); }
+    int add(const void *base, int64_t rows, int cols, int64_t stride) {
+        ok = ok && count < kMmMaps && mm_map(&maps.m[count], base, rows, cols, stride);
+        return count++;
+    }
+};
+
+// One layer's gradients from d: dx = d W (+ d2 W2) and dW = d^T x (dW2 = d2^T x).
+struct Gradients {
+    int both;                       // 1 or 2 products
+    const void *d[2], *w[2], *x;
+    void *dx, *dw[2];
+    int64_t d_stride, w_stride[2], x_stride, dx_stride, dw_stride[2];
+    int64_t M;
+    int N, K;
+};
+
+cudaError_t launch_gradients(const Gradients &g, int *status, int sms, bool pdl, cudaStream_t s) {
+    Builder maps;
+    MmArgs p = mm_args(WZ_ACT_NONE, status);
+    int d[2], x = 0;
+    for (int i = 0; i < g.both; ++i) d[i] = maps.add(g.d[i], g.M, g.N, g.d_stride);
+    if (g.dw[0]) x = maps.add(g.x, g.M, g.K, g.x_stride);
+    MmProblem in{}, weight[2] = {};
+    if (g.dx) {
+        in.M = (int)g.M, in.N = g.K, in.segments = g.both, in.steps = (int)steps_of(g.N);
+        in.b_mn = 1;
+        in.out = half(g.dx), in.out_stride = g.dx_stride;
+        for (int i = 0; i < g.both; ++i) {
+            in.a[i] = d[i];
+            in.b[i] = maps.add(g.w[i], g.N, g.K, g.w_stride[i]);
+        }
+    }
+    if (g.dw[0])
+        for (int i = 0; i < g.both; ++i) {
+            MmProblem &q = weight[i];
+            q.M = g.N, q.N = g.K, q.segments = 1, q.steps = (int)steps_of(g.M);
+            q.a_mn = q.b_mn = 1;
+            q.out = half(g.dw[i]), q.out_stride = g.dw_stride[i];
+            q.a[0] = d[i], q.b[0] = x;
+        }
+    if (!maps.ok) return cudaErrorInvalidValue;
+    // the longer tiles first, so that the shorter ones even out the ends
+    const bool weights_first = g.dw[0] && (!g.dx || weight[0].steps > in.steps * in.segments);
+    p.problems = 0;
+    if (g.dx && !weights_first) p.prob[p.problems++] = in;
+    if (g.dw[0])
+        for (int i = 0; i < g.both; ++i) p.prob[p.problems++] = weight[i];
+    if (g.dx && weights_first) p.prob[p.problems++] = in;
+    return p.problems ? launch_mm_pair(kMmStore, maps.maps, p, sms, pdl, s) : cudaSuccess;
+}
+
+cudaError_t zero_rows(void *p, int64_t stride, int rows, int cols, cudaStream_t s) {
+    return p ? cudaMemset2DAsync(p, (size_t)stride * 2, 0, (size_t)cols * 2, (size_t)rows, s) : cudaSuccess;
+}
+
+int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
+
+size_t delta_bytes(int64_t M, int N) { return pad256((size_t)M * (size_t)pad8(N) * 2); }
+
+size_t part_bytes(int64_t M, int N) { return pad256((size_t)((M + 31) / 32) * (size_t)N * 4); }
+
+#ifdef WZ_CHECKED
+uint64_t check_mm_wait_ns = kMmTimeoutNs;
+#endif
+
+}  // namespace
+
+uint64_t mm_wait_ns() {
+#ifdef WZ_CHECKED
+    return check_mm_wait_ns;
+#else
+    return kMmTimeoutNs;
+#endif
+}
+
+cudaError_t launch_linear(const wz_linear_args &a, cudaStream_t s) {
+    const int sms = sm_count();
+    if (sms < 2) return cudaErrorInvalidDevice;
+    Builder maps;
+    MmArgs p = mm_args(a.act, a.device_status);
+    MmProblem &q = p.prob[0];
+    q.M = (int)a.M, q.N = a.N, q.segments = 1, q.steps = (int)steps_of(a.K);
+    q.a[0] = maps.add(a.x, a.M, a.K, a.x_stride);
+    q.b[0] = maps.add(a.w, a.N, a.K, a.w_stride);
+    if (!maps.ok) return cudaErrorInvalidValue;
+    q.out = half(a.out), q.out_stride = a.out_stride;
+    p.bias[0] = a.bias;
+    p.residual = half(a.residual), p.residual_stride = a.residual_stride;
+    p.pre[0] = half(a.pre), p.pre_stride[0] = a.pre_stride;
+    return launch_mm_pair(kMmStore, maps.maps, p, sms, false, s);
+}
+
+cudaError_t launch_gated(const wz_gated_args &a, cudaStream_t s) {
+    const int sms = sm_count();
+    if (sms < 2) return cudaErrorInvalidDevice;
+    Builder maps;
+    MmArgs p = mm_args(a.act, a.device_status);
+    MmProblem &q = p.prob[0];
+    q.M = (int)a.M, q.N = a.N, q.segments = 1, q.steps = (int)steps_of(a.K);
+    q.a[0] = maps.add(a.x, a.M, a.K, a.x_stride);
+    q.b[0] = maps.add(a.w_gate, a.N, a.K, a.w_gate_stride);
+    q.b[1] = maps.add(a.w_up, a.N, a.K, a.w_up_stride);
+    if (!maps.ok) return cudaErrorInvalidValue;
+    q.out = half(a.out), q.out_stride = a.out_stride;
+    p.bias[0] = a.b_gate, p.bias[1] = a.b_up;
+    p.pre[0] = half(a.gate), p.pre_stride[0] = a.gate_stride;
+    p.pre[1] = half(a.up), p.pre_stride[1] = a.up_stride;
+    return launch_mm_pair(kMmGated, maps.maps, p, sms, false, s);
+}
+
+size_t linear_backward_bytes(int64_t M, int N) { return delta_bytes(M, N) + part_bytes(M, N); }
+size_t gated_backward_bytes(int64_t M, int N) { return 2 * (delta_bytes(M, N) + part_bytes(M, N)); }
+
+#define MM_TRY(call)                              \
+    do {                                          \
+        const cudaError_t mm_e = (call);          \
+        if (mm_e != cudaSuccess) return mm_e;     \
+    } while (0)
+
+cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, cudaStream_t s) {
+    const int sms = sm_count();
+    if (sms < 2) return cudaErrorInvalidDevice;
+    if (a.M == 0) {
+        MM_TRY(zero_rows(a.dw, a.dw_stride, a.N, a.K, s));
+        return a.db ? launch_sum(nullptr, nullptr, a.db, nullptr, 0, a.N, false, s) : cudaSuccess;
+    }
+    const int64_t d_stride = pad8(a.N);
+    __nv_bfloat16 *d = half((void *)ws);
+    float *part = a.db ? reinterpret_cast<float *>(ws + delta_bytes(a.M, a.N)) : nullptr;
+    int64_t part_rows = (a.M + kDeltaRows - 1) / kDeltaRows;
+    bool pdl = false;   // a kernel of this call is before the next one
+    if (a.act != WZ_ACT_NONE && !a.pre) {
+        Builder maps;
+        MmArgs p = mm_args(a.act, a.device_status);
+        MmProblem &q = p.prob[0];
+        q.M = (int)a.M, q.N = a.N, q.segments = 1, q.steps = (int)steps_of(a.K);
+        q.a[0] = maps.add(a.x, a.M, a.K, a.x_stride);
+        q.b[0] = maps.add(a.w, a.N, a.K, a.w_stride);
+        if (!maps.ok) return cudaErrorInvalidValue;
+        q.out = d, q.out_stride = d_stride;
+        p.bias[0] = a.bias;
+        p.dy = half(a.dy), p.dy_stride = a.dy_stride;
+        p.part[0] = part;
+        part_rows = (a.M + 31) / 32;
+        MM_TRY(launch_mm_pair(kMmSlope, maps.maps, p, sms, false, s));
+        pdl = true;
+    } else if (a.act != WZ_ACT_NONE || part) {
+        DeltaArgs p;
+        memset(&p, 0, sizeof(p));
+        p.dy = half(a.dy), p.dy_stride = a.dy_stride;
+        p.pre[0] = half(a.pre), p.pre_stride[0] = a.pre_stride;
+        p.d[0] = d, p.d_stride = d_stride;
+        p.part[0] = part;
+        p.M = a.M, p.N = a.N, p.act = a.act;
+        MM_TRY(launch_delta(a.act == WZ_ACT_NONE ? kDeltaSums : kDeltaSlope, p, false, s));
+        pdl = true;
+    }
+    Gradients g;
+    memset(&g, 0, sizeof(g));
+    g.both = 1;
+    g.d[0] = a.act == WZ_ACT_NONE ? a.dy : (const void *)d;
+    g.d_stride = a.act == WZ_ACT_NONE ? a.dy_stride : d_stride;
+    g.w[0] = a.w, g.w_stride[0] = a.w_stride;
+    g.x = a.x, g.x_stride = a.x_stride;
+    g.dx = a.dx, g.dx_stride = a.dx_stride;
+    g.dw[0] = a.dw, g.dw_stride[0] = a.dw_stride;
+    g.M = a.M, g.N = a.N, g.K = a.K;
+    MM_TRY(launch_gradients(g, a.device_status, sms, pdl, s));
+    return part ? launch_sum(part, nullptr, a.db, nullptr, part_rows, a.N, true, s) : cudaSuccess;
+}
+
+cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cudaStream_t s) {
+    const int sms = sm_count();
+    if (sms < 2) return cudaErrorInvalidDevice;
+    float *db[2] = {a.db_gate, a.db_up};
+    if (a.M == 0) {
+        MM_TRY(zero_rows(a.dw_gate, a.dw_gate_stride, a.N, a.K, s));
+        MM_TRY(zero_rows(a.dw_up, a.dw_up_stride, a.N, a.K, s));
+        return db[0] || db[1] ? launch_sum(nullptr, nullptr, db[0], db[1], 0, a.N, false, s) : cudaSuccess;
+    }
+    const int64_t d_stride = pad8(a.N);
+    const size_t db_at = 2 * delta_bytes(a.M, a.N);
+    __nv_bfloat16 *d[2] = {half((void *)ws), half((void *)(ws + delta_bytes(a.M, a.N)))};
+    float *part[2];
+    for (int i = 0; i < 2; ++i)
+        part[i] = db[i] ? reinterpret_cast<float *>(ws + db_at + i * part_bytes(a.M, a.N)) : nullptr;
+    int64_t part_rows = (a.M + kDeltaRows - 1) / kDeltaRows;
+    if (a.gate) {
+        DeltaArgs p;
+        memset(&p, 0, sizeof(p));
+        p.dy = half(a.dout), p.dy_stride = a.dout_stride;
+        p.pre[0] = half(a.gate), p.pre_stride[0] = a.gate_stride;
+        p.pre[1] = half(a.up), p.pre_stride[1] = a.up_stride;
+        p.d[0] = d[0], p.d[1] = d[1], p.d_stride = d_stride;
+        p.part[0] = part[0], p.part[1] = part[1];
+        p.M = a.M, p.N = a.N, p.act = a.act;
+        MM_TRY(launch_delta(kDeltaGated, p, false, s));
+    } else {
+        Builder maps;
+        MmArgs p = mm_args(a.act, a.device_status);
+        MmProblem &q = p.prob[0];
+        q.M = (int)a.M, q.N = a.N, q.segments = 1, q.steps = (int)steps_of(a.K);
+        q.a[0] = maps.add(a.x, a.M, a.K, a.x_stride);
+        q.b[0] = maps.add(a.w_gate, a.N, a.K, a.w_gate_stride);
+        q.b[1] = maps.add(a.w_up, a.N, a.K, a.w_up_stride);
+        if (!maps.ok) return cudaErrorInvalidValue;
+        q.out = d[0], q.out_stride = d_stride;
+        p.out2 = d[1], p.out2_stride = d_stride;
+        p.bias[0] = a.b_gate, p.bias[1] = a.b_up;
+        p.dy = half(a.dout), p.dy_stride = a.dout_stride;
+        p.part[0] = part[0], p.part[1] = part[1];
+        part_rows = (a.M + 31) / 32;
+        MM_TRY(launch_mm_pair(kMmGatedSlope, maps.maps, p, sms, false, s));
+    }
+    Gradients g;
+    memset(&g, 0, sizeof(g));
+    g.both = 2;
+    g.d[0] = d[0], g.d[1] = d[1], g.d_stride = d_stride;
+    g.w[0] = a.w_gate, g.w[1] = a.w_up, g.w_stride[0] = a.w_gate_stride, g.w_stride[1] = a.w_up_stride;
+    g.x = a.x, g.x_stride = a.x_stride;
+    g.dx = a.dx, g.dx_stride = a.dx_stride;
+    g.dw[0] = a.dw_gate, g.dw[1] = a.dw_up;
+    g.dw_stride[0] = a.dw_gate_stride, g.dw_stride[1] = a.dw_up_stride;
+    g.M = a.M, g.N = a.N, g.K = a.K;
+    MM_TRY(launch_gradients(g, a.device_status, sms, true, s));
+    return part[0] || part[1] ? launch_sum(part[0], part[1], db[0], db[1], part_rows, a.N, true, s) : cudaSuccess;
+}
+
+}  // namespace wz
+
+#ifdef WZ_CHECKED
+// Test hook: the limit of the waits that the matrix products give up on; 0: the ordinary one.
+extern "C" __attribute__((visibility("default"))) void wz_check_mm_wait(uint64_t ns) {
+    wz::check_mm_wait_ns = ns ? ns : wz::kMmTimeoutNs;
+}
+#endif

@@ -1,0 +1,199 @@
+// Matrix products of a decoder layer (wz_linear, wz_gated and their backward
+// passes): what their kernels share.
+//
+//   D[i][j] = sum_k A[i][k] B[j][k],  A and B bf16, fp32 accumulation
+//
+// An operand is either K-major (k is contiguous in memory) or MN-major (its row
+// index is), so that one layout in memory serves the forward product and both
+// gradients: x W^T reads both K-major, d W reads W MN-major, d^T x both.
+#pragma once
+
+#include <cuda.h>
+
+#include "wz_internal.cuh"
+#include "wz_ptx.cuh"
+
+namespace wz {
+
+constexpr int kMmMaps = 6;
+constexpr int kMmProblems = 3;
+constexpr uint64_t kMmTimeoutNs = 2000000000ull;
+
+struct MmMaps {
+    CUtensorMap m[kMmMaps];   // 2D, boxes of 64 x 64 with 128-byte swizzle
+};
+
+// What is done with the sums.
+enum MmEpilogue : int {
+    kMmStore = 0,     // out = act(p) + residual, p = sum + bias; p kept in pre[0]
+    kMmGated = 1,     // out = act(g) u; g and u kept in pre[0], pre[1]
+    kMmSlope = 2,     // out = dy act'(p), and its sums over 32 rows in part[0]
+    kMmGatedSlope = 3 // out = dout u act'(g), out2 = dout act(g), and their sums
+};
+
+// One product of a launch.  With two segments the second continues the sums.
+struct MmProblem {
+    int M, N;              // rows and columns of D
+    int mt, nt;            // tiles
+    int segments, steps;   // K segments of `steps` steps of 64
+    int a_mn, b_mn;        // operands MN-major
+    int a[2], b[2];        // tensor maps of the segments
+    __nv_bfloat16 *out;    // [M] rows of N
+    int64_t out_stride;
+};
+
+struct MmArgs {
+    MmProblem prob[kMmProblems];
+    int problems;
+    int act;                                // WZ_ACT_*
+    const float *bias[2];                   // [N]; null: none
+    const __nv_bfloat16 *residual;          // kMmStore; null: none
+    const __nv_bfloat16 *dy;                // the slopes' factor
+    __nv_bfloat16 *pre[2];                  // kept products; null: none
+    __nv_bfloat16 *out2;                    // kMmGatedSlope
+    float *part[2];                         // [ceil(M / 32)][N] sums over 32 rows; null: none
+    int64_t residual_stride, dy_stride, pre_stride[2], out2_stride;
+    int *status;
+    uint64_t wait_ns;
+};
+
+// ---- activations -------------------------------------------------------------
+// The logistic function and what follows from it are within a few 2^-22 of the
+// value: far below the bf16 rounding of what they go into, and of the order of the
+// f32 rounding of a bias gradient's terms.
+
+__device__ __forceinline__ float mm_sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+
+// tanh z = 2 sigmoid(2z) - 1, so that gelu_tanh is x sigmoid(2z).
+__device__ __forceinline__ float mm_gelu_arg(float x) { return 1.5957691216057308f * x * (1.f + 0.044715f * x * x); }
+
+template <int ACT>
+__device__ __forceinline__ float mm_act1(float x) {
+    if constexpr (ACT == WZ_ACT_GELU) return 0.5f * x * erfcf(-0.70710678118654752f * x);
+    if constexpr (ACT == WZ_ACT_GELU_TANH) return x * mm_sigmoid(mm_gelu_arg(x));
+    if constexpr (ACT == WZ_ACT_SILU) return x * mm_sigmoid(x);
+    return x;
+}
+
+// Value and slope.  A factor that has become 0 wins over an x, or a power of it, that
+// is infinite.
+template <int ACT>
+__device__ __forceinline__ void mm_slope1(float x, float &value, float &slope) {
+    if constexpr (ACT == WZ_ACT_NONE) {
+        value = x;
+        slope = 1.f;
+    } else if constexpr (ACT == WZ_ACT_GELU) {
+        const float phi = 0.5f * erfcf(-0.70710678118654752f * x);
+        const float e = 0.3989422804014327f * __expf(-0.5f * x * x);
+        value = x * phi;
+        slope = phi + (e > 0.f ? x * e : 0.f);
+    } else {
+        const bool tanh_form = ACT == WZ_ACT_GELU_TANH;
+        const float s = mm_sigmoid(tanh_form ? mm_gelu_arg(x) : x);
+        const float t = s * (1.f - s);
+        const float dz = tanh_form ? 1.5957691216057308f * (1.f + 0.134145f * x * x) : 1.f;
+        value = x * s;
+        slope = s + (t > 0.f ? x * t * dz : 0.f);
+    }
+}
+
+// f(constant of type) for the call's activation.
+template <typename F>
+__device__ __forceinline__ void mm_with_act(int act, F f) {
+    switch (act) {
+        case WZ_ACT_GELU: f(std::integral_constant<int, WZ_ACT_GELU>()); break;
+        case WZ_ACT_GELU_TANH: f(std::integral_constant<int, WZ_ACT_GELU_TANH>()); break;
+        case WZ_ACT_SILU: f(std::integral_constant<int, WZ_ACT_SILU>()); break;
+        default: f(std::integral_constant<int, WZ_ACT_NONE>()); break;
+    }
+}
+
+// ---- rows of bf16 --------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t mm_pack(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// x[0 .. C) to p, of which the first n are inside the row; p is 16-byte aligned.
+template <int C>
+__device__ __forceinline__ void mm_store(__nv_bfloat16 *p, const float (&x)[C], int n) {
+    if (n >= C) {
+#pragma unroll
+        for (int j = 0; j < C; j += 8)
+            reinterpret_cast<uint4 *>(p)[j / 8] = make_uint4(mm_pack(x[j], x[j + 1]), mm_pack(x[j + 2], x[j + 3]),
+                                                             mm_pack(x[j + 4], x[j + 5]), mm_pack(x[j + 6], x[j + 7]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+            if (j < n) p[j] = __float2bfloat16_rn(x[j]);
+    }
+}
+
+// C values from p, zeros from the n-th on.
+template <int C>
+__device__ __forceinline__ void mm_load(const __nv_bfloat16 *p, float (&x)[C], int n) {
+    if (n >= C) {
+        uint4 v[C / 8];
+#pragma unroll
+        for (int j = 0; j < C / 8; ++j) v[j] = reinterpret_cast<const uint4 *>(p)[j];
+#pragma unroll
+        for (int j = 0; j < C / 8; ++j) {
+            float f[8];
+            unpack(v[j], f, (__nv_bfloat16 *)nullptr);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[8 * j + i] = f[i];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < C; ++j) x[j] = j < n ? __bfloat162float(p[j]) : 0.f;
+    }
+}
+
+// Adds bias[0 .. n) (n <= C counts the row's columns that are left).
+template <int C>
+__device__ __forceinline__ void mm_add_bias(const float *bias, float (&x)[C], int n) {
+    if (!bias) return;
+    if (n >= C && ((uintptr_t)bias & 15) == 0) {
+#pragma unroll
+        for (int j = 0; j < C / 4; ++j) {
+            const float4 v = __ldg(reinterpret_cast<const float4 *>(bias) + j);
+            x[4 * j] += v.x;
+            x[4 * j + 1] += v.y;
+            x[4 * j + 2] += v.z;
+            x[4 * j + 3] += v.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+            if (j < n) x[j] += __ldg(bias + j);
+    }
+}
+
+// Sum over the warp's lanes of x[lane] (a halving exchange: 31 shuffles, a fixed
+// order); x is used up.
+__device__ __forceinline__ float mm_column_sum(float (&x)[32]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int j = 0; j < o; ++j) {
+            const float send = up ? x[j] : x[j + o], keep = up ? x[j + o] : x[j];
+            x[j] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+        }
+    }
+    return x[0];
+}
+
+// ---- launchers (arguments checked) -----------------------------------------------
+
+// Products with tiles of 256 x 256 on pairs of SMs (mm_pair.cu).
+cudaError_t launch_mm_pair(MmEpilogue epi, const MmMaps &maps, MmArgs &p, int sms, bool pdl, cudaStream_t s);
+
+uint64_t mm_wait_ns();   // the limit of the products' waits
+
+// The map of a matrix [rows][cols] bf16 with rows `stride` elements apart.
+bool mm_map(CUtensorMap *m, const void *base, int64_t rows, int cols, int64_t stride);
+
+}  // namespace wz

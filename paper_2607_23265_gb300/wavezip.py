@@ -32,6 +32,8 @@ TEMPORAL_MODES = {"wta": TEMPORAL_WTA, "raw": TEMPORAL_RAW, "uniform": TEMPORAL_
 SPATIAL_MODES = {"wsm": SPATIAL_WSM, "saliency": SPATIAL_SALIENCY, "none": SPATIAL_NONE}
 RELEVANCE_MEAN, RELEVANCE_MAXSIM = 0, 1
 RELEVANCE_MODES = {"mean": RELEVANCE_MEAN, "maxsim": RELEVANCE_MAXSIM}
+ACT_NONE, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3
+ACTS = {"none": ACT_NONE, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
 MAX_LQ_MAXSIM = 128
 MAX_LEVELS = 4
 
@@ -120,6 +122,33 @@ class AttendArgs(C.Structure):
     ]
 
 
+def _fields(pointers: str, strided: str):
+    """The members of a layer call down to its activation: pointers, strides of those that have one, sizes."""
+    return ([(n, C.c_void_p) for n in pointers.split()] + [(n + "_stride", C.c_int64) for n in strided.split()]
+            + [("M", C.c_int64), ("N", C.c_int), ("K", C.c_int), ("act", C.c_int)])
+
+
+_END = [("device_status", C.c_void_p), ("stream", C.c_void_p)]
+_WORKSPACE = [("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class LinearArgs(C.Structure):
+    _fields_ = _fields("x w bias residual out pre", "x w residual out pre") + _END
+
+
+class LinearBackwardArgs(C.Structure):
+    _fields_ = _fields("dy x w bias pre dx dw db", "dy x w pre dx dw") + _WORKSPACE + _END
+
+
+class GatedArgs(C.Structure):
+    _fields_ = _fields("x w_gate w_up b_gate b_up out gate up", "x w_gate w_up out gate up") + _END
+
+
+class GatedBackwardArgs(C.Structure):
+    _fields_ = _fields("dout x w_gate w_up b_gate b_up gate up dx dw_gate dw_up db_gate db_up",
+                       "dout x w_gate w_up gate up dx dw_gate dw_up") + _WORKSPACE + _END
+
+
 NUM_KERNELS = 6
 KERNEL_NAMES = ("query_pool", "relevance", "frame_stats", "temporal", "spatial", "condense")
 
@@ -151,6 +180,16 @@ def _load(path: str = LIB_PATH):
         "wz_attend_args_init": (None, [C.POINTER(AttendArgs)]),
         "wz_attend_workspace_size": (sz, [i64, i, i]),
         "wz_attend": (i, [C.POINTER(AttendArgs)]),
+        "wz_linear_args_init": (None, [C.POINTER(LinearArgs)]),
+        "wz_linear": (i, [C.POINTER(LinearArgs)]),
+        "wz_linear_backward_args_init": (None, [C.POINTER(LinearBackwardArgs)]),
+        "wz_linear_backward_workspace_size": (sz, [i64, i, i]),
+        "wz_linear_backward": (i, [C.POINTER(LinearBackwardArgs)]),
+        "wz_gated_args_init": (None, [C.POINTER(GatedArgs)]),
+        "wz_gated": (i, [C.POINTER(GatedArgs)]),
+        "wz_gated_backward_args_init": (None, [C.POINTER(GatedBackwardArgs)]),
+        "wz_gated_backward_workspace_size": (sz, [i64, i, i]),
+        "wz_gated_backward": (i, [C.POINTER(GatedBackwardArgs)]),
         "wz_dwt_len": (i, [i, i]),
         "wz_wavelet_filters": (i, [i] + [C.POINTER(C.c_double)] * 4),
         "wz_dwt1d": (i, [vp, i, i, i, i, vp, vp, vp]),
@@ -758,3 +797,185 @@ def wz_attend(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, cu: tor
     a.stream = _current_stream(stream, dev)
     _call(_lib.wz_attend, a, dev, "wz_attend")
     return out
+
+
+# --------------------------------------------------------------------------
+# A layer's matrix products
+# --------------------------------------------------------------------------
+
+# Rows are bf16 tensors [rows, width] whose rows are contiguous and begin a multiple of eight elements apart: slices
+# of a wider projection, and odd widths in padded rows, among them.  Weights are [out, in], as torch.nn.Linear's.
+
+def _matrix(t: torch.Tensor, rows: int, width: int, device: int, name: str):
+    """Checks a matrix; its address and the elements from row to row."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] != rows or shape[1] != width or t.dtype is not torch.bfloat16 or \
+            t.get_device() != device:
+        raise ValueError(f"{name} must be bfloat16 of shape [{rows}, {width}] on the weights' device")
+    apart = stride[0] if rows > 1 else -(-width // 8) * 8
+    if (width > 1 and stride[1] != 1) or apart % 8 or apart < width:
+        raise ValueError(f"{name}: rows must be contiguous and begin a multiple of 8 elements apart")
+    return t.data_ptr(), apart
+
+
+def _vector(t, n: int, device: int, name: str):
+    """The address of a contiguous float32 vector, or None."""
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.shape != (n,) or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor of shape [{n}] on the weights' device")
+    return t.data_ptr()
+
+
+def _row_output(rows: int, width: int, device, stream) -> torch.Tensor:
+    """A new matrix; an odd width's rows are padded to a multiple of eight."""
+    t = _output((rows, -(-width // 8) * 8), torch.bfloat16, device, stream)
+    return t if t.shape[1] == width else t[:, :width]
+
+
+def _sizes(a, x: torch.Tensor, w: torch.Tensor, act) -> int:
+    """M, K, N and the activation of a call; the weights' device."""
+    if x.dim() != 2 or w.dim() != 2 or not w.is_cuda:
+        raise ValueError("x must be [rows, in] and weights [out, in], on one CUDA device")
+    a.M, a.K = x.shape
+    a.N = w.shape[0]
+    a.act = _enum(ACTS, act)
+    return w.get_device()
+
+
+def _finish(a, fn, device: int, device_status, stream, where: str, workspace=None):
+    if workspace is not None:
+        if workspace.get_device() != device or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the weights' device")
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.nbytes
+    if device_status is not None:
+        a.device_status = _ints(device_status, device, "device_status")
+    a.stream = _current_stream(stream, device)
+    _call(fn, a, device, where)
+
+
+def wz_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, *, act="none",
+              residual: torch.Tensor | None = None, out: torch.Tensor | None = None, pre: torch.Tensor | None = None,
+              device_status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """wz_linear: act(x w^T + bias) + residual of x [M, K] and w [N, K], bf16, with the bias [N] in float32.  pre [M, N]
+    receives x w^T + bias for the backward pass.  act: "none", "gelu" (erf), "gelu_tanh" or "silu".  out may be residual
+    itself.  What is allocated here for a call on a given stream belongs to that stream."""
+    a = LinearArgs()
+    dev = _sizes(a, x, w, act)
+    M, N, K = a.M, a.N, a.K
+    if out is None:
+        out = _row_output(M, N, w.device, stream)
+    a.x, a.x_stride = _matrix(x, M, K, dev, "x")
+    a.w, a.w_stride = _matrix(w, N, K, dev, "w")
+    a.out, a.out_stride = _matrix(out, M, N, dev, "out")
+    a.bias = _vector(bias, N, dev, "bias")
+    if residual is not None:
+        a.residual, a.residual_stride = _matrix(residual, M, N, dev, "residual")
+    if pre is not None:
+        a.pre, a.pre_stride = _matrix(pre, M, N, dev, "pre")
+    _finish(a, _lib.wz_linear, dev, device_status, stream, "wz_linear")
+    return out
+
+
+def wz_linear_backward_workspace_size(M: int, K: int, N: int) -> int:
+    return int(_lib.wz_linear_backward_workspace_size(int(M), int(K), int(N)))
+
+
+def wz_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, *, act="none",
+                       pre: torch.Tensor | None = None, bias: torch.Tensor | None = None, need_x: bool = True,
+                       need_w: bool = True, need_b: bool = False, dx: torch.Tensor | None = None,
+                       dw: torch.Tensor | None = None, db: torch.Tensor | None = None,
+                       workspace: torch.Tensor | None = None, device_status: torch.Tensor | None = None, stream=None):
+    """wz_linear_backward: (dx [M, K], dw [N, K], db [N] float32) of act(x w^T + bias) from dy [M, N]; None in the place of
+    one that is not needed.  pre is what wz_linear kept; without it, and with an activation, it is formed again from x,
+    w and bias.  A residual's gradient is dy itself."""
+    a = LinearBackwardArgs()
+    dev = _sizes(a, x, w, act)
+    M, N, K = a.M, a.N, a.K
+    a.dy, a.dy_stride = _matrix(dy, M, N, dev, "dy")
+    a.x, a.x_stride = _matrix(x, M, K, dev, "x")
+    a.w, a.w_stride = _matrix(w, N, K, dev, "w")
+    a.bias = _vector(bias, N, dev, "bias")
+    if pre is not None:
+        a.pre, a.pre_stride = _matrix(pre, M, N, dev, "pre")
+    if need_x:
+        dx = _row_output(M, K, w.device, stream) if dx is None else dx
+        a.dx, a.dx_stride = _matrix(dx, M, K, dev, "dx")
+    if need_w:
+        dw = _row_output(N, K, w.device, stream) if dw is None else dw
+        a.dw, a.dw_stride = _matrix(dw, N, K, dev, "dw")
+    if need_b:
+        db = _output((N,), torch.float32, w.device, stream) if db is None else db
+        a.db = _vector(db, N, dev, "db")
+    _finish(a, _lib.wz_linear_backward, dev, device_status, stream, "wz_linear_backward", workspace)
+    return dx if need_x else None, dw if need_w else None, db if need_b else None
+
+
+def wz_gated(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_gate: torch.Tensor | None = None,
+             b_up: torch.Tensor | None = None, *, act="silu", out: torch.Tensor | None = None,
+             gate: torch.Tensor | None = None, up: torch.Tensor | None = None,
+             device_status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """wz_gated: act(x w_gate^T + b_gate) * (x w_up^T + b_up), the first half of a gated feed-forward block (wz_linear with
+    the block's input as its residual is the second).  gate and up [M, N] receive the two products for the backward
+    pass, both or neither."""
+    a = GatedArgs()
+    dev = _sizes(a, x, w_gate, act)
+    M, N, K = a.M, a.N, a.K
+    if out is None:
+        out = _row_output(M, N, w_gate.device, stream)
+    a.x, a.x_stride = _matrix(x, M, K, dev, "x")
+    a.w_gate, a.w_gate_stride = _matrix(w_gate, N, K, dev, "w_gate")
+    a.w_up, a.w_up_stride = _matrix(w_up, N, K, dev, "w_up")
+    a.out, a.out_stride = _matrix(out, M, N, dev, "out")
+    a.b_gate, a.b_up = _vector(b_gate, N, dev, "b_gate"), _vector(b_up, N, dev, "b_up")
+    if (gate is None) != (up is None):
+        raise ValueError("gate and up go together")
+    if gate is not None:
+        a.gate, a.gate_stride = _matrix(gate, M, N, dev, "gate")
+        a.up, a.up_stride = _matrix(up, M, N, dev, "up")
+    _finish(a, _lib.wz_gated, dev, device_status, stream, "wz_gated")
+    return out
+
+
+def wz_gated_backward_workspace_size(M: int, K: int, N: int) -> int:
+    return int(_lib.wz_gated_backward_workspace_size(int(M), int(K), int(N)))
+
+
+def wz_gated_backward(dout: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, *, act="silu",
+                      gate: torch.Tensor | None = None, up: torch.Tensor | None = None,
+                      b_gate: torch.Tensor | None = None, b_up: torch.Tensor | None = None, need_x: bool = True,
+                      need_w: bool = True, need_b: bool = False, dx: torch.Tensor | None = None,
+                      dw_gate: torch.Tensor | None = None, dw_up: torch.Tensor | None = None,
+                      db_gate: torch.Tensor | None = None, db_up: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None, device_status: torch.Tensor | None = None, stream=None):
+    """wz_gated_backward: (dx, dw_gate, dw_up, db_gate, db_up) of wz_gated from dout [M, N]; None in the place of what is
+    not needed.  gate and up are what wz_gated kept; without them they are formed again from x, the weights and
+    the biases."""
+    a = GatedBackwardArgs()
+    dev = _sizes(a, x, w_gate, act)
+    M, N, K = a.M, a.N, a.K
+    a.dout, a.dout_stride = _matrix(dout, M, N, dev, "dout")
+    a.x, a.x_stride = _matrix(x, M, K, dev, "x")
+    a.w_gate, a.w_gate_stride = _matrix(w_gate, N, K, dev, "w_gate")
+    a.w_up, a.w_up_stride = _matrix(w_up, N, K, dev, "w_up")
+    a.b_gate, a.b_up = _vector(b_gate, N, dev, "b_gate"), _vector(b_up, N, dev, "b_up")
+    if (gate is None) != (up is None):
+        raise ValueError("gate and up go together")
+    if gate is not None:
+        a.gate, a.gate_stride = _matrix(gate, M, N, dev, "gate")
+        a.up, a.up_stride = _matrix(up, M, N, dev, "up")
+    if need_x:
+        dx = _row_output(M, K, w_gate.device, stream) if dx is None else dx
+        a.dx, a.dx_stride = _matrix(dx, M, K, dev, "dx")
+    if need_w:
+        dw_gate = _row_output(N, K, w_gate.device, stream) if dw_gate is None else dw_gate
+        dw_up = _row_output(N, K, w_gate.device, stream) if dw_up is None else dw_up
+        a.dw_gate, a.dw_gate_stride = _matrix(dw_gate, N, K, dev, "dw_gate")
+        a.dw_up, a.dw_up_stride = _matrix(dw_up, N, K, dev, "dw_up")
+    if need_b:
+        db_gate = _output((N,), torch.float32, w_gate.device, stream) if db_gate is None else db_gate
+        db_up = _output((N,), torch.float32, w_gate.device, stream) if db_up is None else db_up
+        a.db_gate, a.db_up = _vector(db_gate, N, dev, "db_gate"), _vector(db_up, N, dev, "db_up")
+    _finish(a, _lib.wz_gated_backward, dev, device_status, stream, "wz_gated_backward", workspace)
+    return (dx if need_x else None, dw_gate if need_w else None, dw_up if need_w else None,
+            db_gate if need_b else None, db_up if need_b else None)

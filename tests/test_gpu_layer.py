@@ -1,0 +1,126 @@
+"""A layer's matrix products and their gradients on the GPU against 64 bits, element by element.
+
+The bounds are derived in layer_reference.py.  Rows are slices of wider buffers whose other elements are NaN: what is
+read from there spoils a result, and what is written there is seen.
+"""
+
+import pytest
+import torch
+
+import layer_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def wz():
+    import __graft_entry__
+    __graft_entry__.build()
+    import paper_2607_23265_gb300.wavezip as m
+    assert torch.cuda.is_available()
+    return m
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+class Layer:
+    """Inputs of one or two weights."""
+
+    def __init__(self, M, N, K, both, bias, pad, seed):
+        g = gen(seed)
+        self.M, self.N, self.K, self.pad, self.g = M, N, K, pad, g
+        self.x = ref.random_rows(M, K, 1.0, g, pad)
+        self.w = [ref.random_rows(N, K, 1.5 / K ** 0.5, g, pad) for _ in range(both)]
+        self.b = [0.3 * torch.randn(N, generator=g, device="cuda") if bias else None for _ in range(both)]
+        self.dy = ref.random_rows(M, N, 0.1, g, pad)
+        self.pre = [ref.random_rows(M, N, 1.5, g, pad) for _ in range(both)]
+        self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        self.made = []
+
+    def out(self, n, width):
+        m, buffer = ref.rows(n, width, self.pad, "cuda")
+        self.made.append((m, buffer))
+        return m
+
+    def done(self):
+        torch.cuda.synchronize()
+        assert int(self.status.item()) == 0
+        for m, buffer in self.made:
+            assert ref.untouched(m, buffer), "written outside of the rows"
+
+
+# sizes where tiles, boxes, vectors and rows end: M, N, K
+SIZES = [
+    (1, 1, 1), (1, 64, 64), (1, 300, 520), (2, 7, 9), (3, 8, 1000), (5, 1000, 8), (16, 128, 64), (17, 129, 65),
+    (31, 96, 33), (32, 257, 127), (33, 31, 449), (64, 512, 1152), (65, 255, 256), (100, 640, 4100), (127, 127, 127),
+    (129, 385, 191), (200, 256, 2048), (255, 72, 577), (257, 1, 300), (300, 520, 31), (333, 896, 640), (513, 130, 1),
+    (577, 1152, 1160), (1000, 77, 3), (1025, 513, 511),
+]
+
+
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("M,N,K", SIZES)
+def test_linear(wz, M, N, K, act):
+    s = Layer(M, N, K, 1, bias=(M + N) % 2 == 0, pad=(N % 3) * 8, seed=M + N + K)
+    residual = ref.random_rows(M, N, 2.0, s.g, 8) if (M + K) % 2 else None
+    out, pre = s.out(M, N), s.out(M, N)
+    got = wz.wz_linear(s.x, s.w[0], s.b[0], act=act, residual=residual, out=out, pre=pre, device_status=s.status)
+    s.done()
+    want, kept = ref.linear(s.x, s.w[0], s.b[0], act, residual)
+    ref.check(got, want, "y")
+    ref.check(pre, kept, "pre")
+    # without the kept product, and with an output of the call's own: the same bits
+    again = wz.wz_linear(s.x, s.w[0], s.b[0], act=act, residual=residual)
+    assert torch.equal(again, got)
+
+
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("M,N,K", SIZES)
+def test_gated(wz, M, N, K, act):
+    s = Layer(M, N, K, 2, bias=(M + N) % 2 == 0, pad=(N % 3) * 8, seed=M + N + K)
+    out, gate, up = s.out(M, N), s.out(M, N), s.out(M, N)
+    got = wz.wz_gated(s.x, *s.w, *s.b, act=act, out=out, gate=gate, up=up, device_status=s.status)
+    s.done()
+    want, g, u = ref.gated(s.x, *s.w, *s.b, act)
+    ref.check(got, want, "h")
+    ref.check(gate, g, "gate")
+    ref.check(up, u, "up")
+    assert torch.equal(wz.wz_gated(s.x, *s.w, *s.b, act=act), got)
+
+
+@pytest.mark.parametrize("kept", [True, False])
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("M,N,K", SIZES)
+def test_linear_backward(wz, M, N, K, act, kept):
+    s = Layer(M, N, K, 1, bias=(M + N) % 2 == 0, pad=(N % 3) * 8, seed=M + N + K)
+    pre = s.pre[0] if kept else None
+    dx, dw, db = s.out(M, K), s.out(N, K), torch.full((N,), float("nan"), device="cuda")
+    wz.wz_linear_backward(s.dy, s.x, s.w[0], act=act, pre=pre, bias=s.b[0], need_b=True, dx=dx, dw=dw, db=db,
+                          device_status=s.status)
+    s.done()
+    delta = ref.linear_delta(s.dy, s.x, s.w[0], s.b[0], pre, act)
+    want_x, [want_w], [want_b] = ref.gradients(s.x, [delta], s.w, exact_delta=act == "none")
+    ref.check(db, want_b, "db")
+    ref.check(dx, want_x, "dx")
+    ref.check(dw, want_w, "dw")
+
+
+@pytest.mark.parametrize("kept", [True, False])
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("M,N,K", SIZES)
+def test_gated_backward(wz, M, N, K, act, kept):
+    s = Layer(M, N, K, 2, bias=(M + N) % 2 == 0, pad=(N % 3) * 8, seed=M + N + K)
+    gate, up = s.pre if kept else (None, None)
+    dx, dws = s.out(M, K), [s.out(N, K), s.out(N, K)]
+    dbs = [torch.full((N,), float("nan"), device="cuda") for _ in range(2)]
+    wz.wz_gated_backward(s.dy, s.x, *s.w, act=act, gate=gate, up=up, b_gate=s.b[0], b_up=s.b[1], need_b=True, dx=dx,
+                         dw_gate=dws[0], dw_up=dws[1], db_gate=dbs[0], db_up=dbs[1], device_status=s.status)
+    s.done()
+    deltas = ref.gated_delta(s.dy, s.x, *s.w, *s.b, gate, up, act)
+    want_x, want_w, want_b = ref.gradients(s.x, deltas, s.w)
+    for i, name in enumerate(("gate", "up")):
+        ref.check(dbs[i], want_b[i], "db_" + name)
+        ref.check(dws[i], want_w[i], "dw_" + name)
+    ref.check(dx, want_x, "dx")
