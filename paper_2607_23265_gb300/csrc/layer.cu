@@ -149,18 +149,6 @@ MmArgs mm_args(int act, int *status) {
 
 int64_t steps_of(int64_t k) { return (k + 63) / 64; }
 
-// A launch's products: maps are added as they are named.
-struct Builder {
-    MmMaps maps;
-    int count = 0;
-    bool ok = true;
-    Builder() { memset(&maps, 0, sizeof(maps)); }
-    int add(const void *base, int64_t rows, int cols, int64_t stride) {
-        ok = ok && count < kMmMaps && mm_map(&maps.m[count], base, rows, cols, stride);
-        return count++;
-    }
-};
-
 // One layer's gradients from d: dx = d W (+ d2 W2) and dW = d^T x (dW2 = d2^T x).
 struct Gradients {
     int both;                       // 1 or 2 products
@@ -172,30 +160,24 @@ struct Gradients {
 };
 
 cudaError_t launch_gradients(const Gradients &g, int *status, int sms, bool pdl, cudaStream_t s) {
-    Builder maps;
     MmArgs p = mm_args(WZ_ACT_NONE, status);
-    int d[2], x = 0;
-    for (int i = 0; i < g.both; ++i) d[i] = maps.add(g.d[i], g.M, g.N, g.d_stride);
-    if (g.dw[0]) x = maps.add(g.x, g.M, g.K, g.x_stride);
-    MmProblem in{}, weight[2] = {};
-    if (g.dx) {
-        in.M = (int)g.M, in.N = g.K, in.segments = g.both, in.steps = (int)steps_of(g.N);
-        in.b_mn = 1;
-        in.out = half(g.dx), in.out_stride = g.dx_stride;
-        for (int i = 0; i < g.both; ++i) {
-            in.a[i] = d[i];
-            in.b[i] = maps.add(g.w[i], g.N, g.K, g.w_stride[i]);
-        }
+    MmProblem in, weight[2];
+    memset(&in, 0, sizeof(in));
+    memset(weight, 0, sizeof(weight));
+    in.M = (int)g.M, in.N = g.K, in.segments = g.both, in.steps = (int)steps_of(g.N);
+    in.b_mn = 1;
+    in.out = half(g.dx), in.out_stride = g.dx_stride;
+    for (int i = 0; i < g.both; ++i) {
+        const MmOperand d{g.d[i], g.M, g.N, g.d_stride};
+        in.from_a[i] = d;
+        in.from_b[i] = MmOperand{g.w[i], g.N, g.K, g.w_stride[i]};
+        MmProblem &q = weight[i];
+        q.M = g.N, q.N = g.K, q.segments = 1, q.steps = (int)steps_of(g.M);
+        q.a_mn = q.b_mn = 1;
+        q.out = half(g.dw[i]), q.out_stride = g.dw_stride[i];
+        q.from_a[0] = d;
+        q.from_b[0] = MmOperand{g.x, g.M, g.K, g.x_stride};
     }
-    if (g.dw[0])
-        for (int i = 0; i < g.both; ++i) {
-            MmProblem &q = weight[i];
-            q.M = g.N, q.N = g.K, q.segments = 1, q.steps = (int)steps_of(g.M);
-            q.a_mn = q.b_mn = 1;
-            q.out = half(g.dw[i]), q.out_stride = g.dw_stride[i];
-            q.a[0] = d[i], q.b[0] = x;
-        }
-    if (!maps.ok) return cudaErrorInvalidValue;
     // the longer tiles first, so that the shorter ones even out the ends
     const bool weights_first = g.dw[0] && (!g.dx || weight[0].steps > in.steps * in.segments);
     p.problems = 0;
@@ -203,7 +185,7 @@ cudaError_t launch_gradients(const Gradients &g, int *status, int sms, bool pdl,
     if (g.dw[0])
         for (int i = 0; i < g.both; ++i) p.prob[p.problems++] = weight[i];
     if (g.dx && weights_first) p.prob[p.problems++] = in;
-    return p.problems ? launch_mm_pair(kMmStore, maps.maps, p, sms, pdl, s) : cudaSuccess;
+    return p.problems ? launch_mm(kMmStore, p, sms, pdl, s, nullptr) : cudaSuccess;
 }
 
 cudaError_t zero_rows(void *p, int64_t stride, int rows, int cols, cudaStream_t s) {
@@ -214,7 +196,17 @@ int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
 
 size_t delta_bytes(int64_t M, int N) { return pad256((size_t)M * (size_t)pad8(N) * 2); }
 
-size_t part_bytes(int64_t M, int N) { return pad256((size_t)((M + 31) / 32) * (size_t)N * 4); }
+size_t part_bytes(int64_t M, int N) { return pad256((size_t)mm_part_rows(M) * (size_t)N * 4); }
+
+// The forward products of a layer: x [M][K] with one or two weights [N][K].
+void forward_product(MmArgs &p, int64_t M, int N, int K, const void *x, int64_t x_stride, const void *w0,
+                     int64_t stride0, const void *w1, int64_t stride1) {
+    MmProblem &q = p.prob[0];
+    q.M = (int)M, q.N = N, q.segments = 1, q.steps = (int)steps_of(K);
+    q.from_a[0] = MmOperand{x, M, K, x_stride};
+    q.from_b[0] = MmOperand{w0, N, K, stride0};
+    q.from_b[1] = MmOperand{w1, N, K, stride1};
+}
 
 #ifdef WZ_CHECKED
 uint64_t check_mm_wait_ns = kMmTimeoutNs;
@@ -230,39 +222,34 @@ uint64_t mm_wait_ns() {
 #endif
 }
 
+cudaError_t launch_mm(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStream_t s, int64_t *part_rows) {
+    MmFewPlan plan;
+    if (plan_mm_few(epi, p, sms, &plan)) return launch_mm_few(epi, p, plan, pdl, s, part_rows);
+    return launch_mm_pair(epi, p, sms, pdl, s, part_rows);
+}
+
 cudaError_t launch_linear(const wz_linear_args &a, cudaStream_t s) {
     const int sms = sm_count();
     if (sms < 2) return cudaErrorInvalidDevice;
-    Builder maps;
     MmArgs p = mm_args(a.act, a.device_status);
-    MmProblem &q = p.prob[0];
-    q.M = (int)a.M, q.N = a.N, q.segments = 1, q.steps = (int)steps_of(a.K);
-    q.a[0] = maps.add(a.x, a.M, a.K, a.x_stride);
-    q.b[0] = maps.add(a.w, a.N, a.K, a.w_stride);
-    if (!maps.ok) return cudaErrorInvalidValue;
-    q.out = half(a.out), q.out_stride = a.out_stride;
+    forward_product(p, a.M, a.N, a.K, a.x, a.x_stride, a.w, a.w_stride, nullptr, 0);
+    p.prob[0].out = half(a.out), p.prob[0].out_stride = a.out_stride;
     p.bias[0] = a.bias;
     p.residual = half(a.residual), p.residual_stride = a.residual_stride;
     p.pre[0] = half(a.pre), p.pre_stride[0] = a.pre_stride;
-    return launch_mm_pair(kMmStore, maps.maps, p, sms, false, s);
+    return launch_mm(kMmStore, p, sms, false, s, nullptr);
 }
 
 cudaError_t launch_gated(const wz_gated_args &a, cudaStream_t s) {
     const int sms = sm_count();
     if (sms < 2) return cudaErrorInvalidDevice;
-    Builder maps;
     MmArgs p = mm_args(a.act, a.device_status);
-    MmProblem &q = p.prob[0];
-    q.M = (int)a.M, q.N = a.N, q.segments = 1, q.steps = (int)steps_of(a.K);
-    q.a[0] = maps.add(a.x, a.M, a.K, a.x_stride);
-    q.b[0] = maps.add(a.w_gate, a.N, a.K, a.w_gate_stride);
-    q.b[1] = maps.add(a.w_up, a.N, a.K, a.w_up_stride);
-    if (!maps.ok) return cudaErrorInvalidValue;
-    q.out = half(a.out), q.out_stride = a.out_stride;
+    forward_product(p, a.M, a.N, a.K, a.x, a.x_stride, a.w_gate, a.w_gate_stride, a.w_up, a.w_up_stride);
+    p.prob[0].out = half(a.out), p.prob[0].out_stride = a.out_stride;
     p.bias[0] = a.b_gate, p.bias[1] = a.b_up;
     p.pre[0] = half(a.gate), p.pre_stride[0] = a.gate_stride;
     p.pre[1] = half(a.up), p.pre_stride[1] = a.up_stride;
-    return launch_mm_pair(kMmGated, maps.maps, p, sms, false, s);
+    return launch_mm(kMmGated, p, sms, false, s, nullptr);
 }
 
 size_t linear_backward_bytes(int64_t M, int N) { return delta_bytes(M, N) + part_bytes(M, N); }
@@ -287,19 +274,13 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
     int64_t part_rows = (a.M + kDeltaRows - 1) / kDeltaRows;
     bool pdl = false;   // a kernel of this call is before the next one
     if (a.act != WZ_ACT_NONE && !a.pre) {
-        Builder maps;
         MmArgs p = mm_args(a.act, a.device_status);
-        MmProblem &q = p.prob[0];
-        q.M = (int)a.M, q.N = a.N, q.segments = 1, q.steps = (int)steps_of(a.K);
-        q.a[0] = maps.add(a.x, a.M, a.K, a.x_stride);
-        q.b[0] = maps.add(a.w, a.N, a.K, a.w_stride);
-        if (!maps.ok) return cudaErrorInvalidValue;
-        q.out = d, q.out_stride = d_stride;
+        forward_product(p, a.M, a.N, a.K, a.x, a.x_stride, a.w, a.w_stride, nullptr, 0);
+        p.prob[0].out = d, p.prob[0].out_stride = d_stride;
         p.bias[0] = a.bias;
         p.dy = half(a.dy), p.dy_stride = a.dy_stride;
         p.part[0] = part;
-        part_rows = (a.M + 31) / 32;
-        MM_TRY(launch_mm_pair(kMmSlope, maps.maps, p, sms, false, s));
+        MM_TRY(launch_mm(kMmSlope, p, sms, false, s, &part_rows));
         pdl = true;
     } else if (a.act != WZ_ACT_NONE || part) {
         DeltaArgs p;
@@ -353,21 +334,14 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
         p.M = a.M, p.N = a.N, p.act = a.act;
         MM_TRY(launch_delta(kDeltaGated, p, false, s));
     } else {
-        Builder maps;
         MmArgs p = mm_args(a.act, a.device_status);
-        MmProblem &q = p.prob[0];
-        q.M = (int)a.M, q.N = a.N, q.segments = 1, q.steps = (int)steps_of(a.K);
-        q.a[0] = maps.add(a.x, a.M, a.K, a.x_stride);
-        q.b[0] = maps.add(a.w_gate, a.N, a.K, a.w_gate_stride);
-        q.b[1] = maps.add(a.w_up, a.N, a.K, a.w_up_stride);
-        if (!maps.ok) return cudaErrorInvalidValue;
-        q.out = d[0], q.out_stride = d_stride;
+        forward_product(p, a.M, a.N, a.K, a.x, a.x_stride, a.w_gate, a.w_gate_stride, a.w_up, a.w_up_stride);
+        p.prob[0].out = d[0], p.prob[0].out_stride = d_stride;
         p.out2 = d[1], p.out2_stride = d_stride;
         p.bias[0] = a.b_gate, p.bias[1] = a.b_up;
         p.dy = half(a.dout), p.dy_stride = a.dout_stride;
         p.part[0] = part[0], p.part[1] = part[1];
-        part_rows = (a.M + 31) / 32;
-        MM_TRY(launch_mm_pair(kMmGatedSlope, maps.maps, p, sms, false, s));
+        MM_TRY(launch_mm(kMmGatedSlope, p, sms, false, s, &part_rows));
     }
     Gradients g;
     memset(&g, 0, sizeof(g));

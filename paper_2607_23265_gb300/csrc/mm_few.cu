@@ -1,0 +1,455 @@
+// Matrix products with few rows, or few tiles: tiles of 128 outputs x 16 .. 256 rows on one SM,
+//
+//   D^T[i][j] = sum_k B[i][k] A[j][k]     i: outputs (128 lanes of tensor memory), j: rows
+//
+// so that the number of rows is padded to 16 only, and a thread stands for an output of
+// which it writes one row after the other (a warp 64 contiguous bytes).  Weights of few
+// rows are a stream that has to come from HBM as fast as it can: K is shared by the CTAs
+// of a cluster, each with a ring of up to twelve stages in flight, and their sums are
+// joined through distributed shared memory, in the order of their ranks, each CTA
+// finishing its share of the rows.  No workspace, no second kernel, equal bits each time.
+//
+// A stage is 64 along K: 128 outputs' weights (16 KB; a gated product both projections',
+// whose sums lie beside one another in tensor memory) and the tile's rows, in boxes of
+// 64 x 64 (or fewer rows) with 128-byte swizzle, K-major or MN-major.  What lies outside
+// an operand arrives as zeros.
+// Warps: 0 copies, 1 products, then all eight the epilogue (two a TMEM lane quadrant).
+//
+// Tensor memory is taken by every CTA and held while it waits for its cluster.  So no two
+// such CTAs may share an SM unless both find room, or clusters could wait for one
+// another: a CTA of up to 256 columns asks for more than a third of an SM's shared
+// memory, one of 512 for more than two thirds, and the pairs of mm_pair.cu leave too little for either.
+#include <algorithm>
+#include <cstring>
+#include <type_traits>
+
+#include "wz_mm.cuh"
+
+namespace wz {
+
+namespace {
+
+constexpr int kOutputs = 128, kStepK = 64;
+constexpr int kWeightBytes = kOutputs * kStepK * 2;   // 16 KB
+constexpr int kBoxBytes = kWeightBytes / 2;           // 64 x 64
+constexpr int kMaxStages = 12;
+constexpr int kWarps = 8;
+constexpr int kThreads = kWarps * 32;
+constexpr int kMaxCluster = 8;
+
+struct Shared {
+    uint64_t full[kMaxStages];
+    uint64_t empty[kMaxStages];
+    uint64_t done;
+    uint32_t tmem_base;
+    int abort;
+};
+
+constexpr size_t kExtra = 1024 + sizeof(Shared);
+// an SM has 228 KB, of which a CTA's first kilobyte is the system's
+constexpr size_t kSmHas = 228 * 1024;
+constexpr size_t kSmemTwo = kSmHas / 2 - 1024;         // two CTAs an SM
+constexpr size_t kSmemOne = 227 * 1024;
+constexpr size_t kSmemLeastTwo = kSmHas / 3;           // not three
+constexpr size_t kSmemLeastOne = kSmHas * 2 / 3;       // not beside one of the others
+
+__device__ __forceinline__ void give_up(const MmArgs &p, volatile int *abort_flag) {
+    *abort_flag = 1;
+    if (p.status) atomicOr(p.status, WZ_STATUS_WAIT_TIMEOUT);
+}
+
+// What a thread needs to finish its output.
+struct Output {
+    int i;              // the output, N or more: none
+    float b[2];
+    float sum[2];       // over its rows, of the slopes
+};
+
+// R rows row .. of output o.i, of which `count` are there.
+template <int EPI, int ACT, int R>
+__device__ __forceinline__ void finish(const MmArgs &p, const MmProblem &q, Output &o, const float (&v)[R],
+                                       const float (&u)[R], int row, int count) {
+    if (o.i >= q.N) return;
+    float other[R];   // the residual, or dy
+    const __nv_bfloat16 *from = EPI == kMmStore ? p.residual : p.dy;
+    const int64_t from_stride = EPI == kMmStore ? p.residual_stride : p.dy_stride;
+    if (EPI != kMmGated && from) {
+#pragma unroll
+        for (int j = 0; j < R; ++j)
+            other[j] = j < count ? __bfloat162float(from[(row + j) * from_stride + o.i]) : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        if (j >= count) break;
+        const int64_t r = row + j;
+        const float x = v[j] + o.b[0];
+        if constexpr (EPI == kMmStore) {
+            if (p.pre[0]) p.pre[0][r * p.pre_stride[0] + o.i] = __float2bfloat16_rn(x);
+            float y = mm_act1<ACT>(x);
+            if (p.residual) y += other[j];
+            q.out[r * q.out_stride + o.i] = __float2bfloat16_rn(y);
+        } else if constexpr (EPI == kMmGated) {
+            const float y = u[j] + o.b[1];
+            if (p.pre[0]) {
+                p.pre[0][r * p.pre_stride[0] + o.i] = __float2bfloat16_rn(x);
+                p.pre[1][r * p.pre_stride[1] + o.i] = __float2bfloat16_rn(y);
+            }
+            q.out[r * q.out_stride + o.i] = __float2bfloat16_rn(mm_act1<ACT>(x) * y);
+        } else {
+            float value, slope;
+            mm_slope1<ACT>(x, value, slope);
+            if constexpr (EPI == kMmSlope) {
+                const float d = other[j] * slope;
+                o.sum[0] += d;
+                q.out[r * q.out_stride + o.i] = __float2bfloat16_rn(d);
+            } else {
+                const float dg = other[j] * (u[j] + o.b[1]) * slope, du = other[j] * value;
+                o.sum[0] += dg;
+                o.sum[1] += du;
+                q.out[r * q.out_stride + o.i] = __float2bfloat16_rn(dg);
+                p.out2[r * p.out2_stride + o.i] = __float2bfloat16_rn(du);
+            }
+        }
+    }
+}
+
+template <int C>
+__device__ __forceinline__ void read_columns(uint32_t tcol, float (&x)[C]) {
+    static_assert(C == 16, "columns of a read");
+    uint32_t v[16];
+    ptx::tmem_ld_32x32b_x16(tcol, v);
+    ptx::tmem_ld_wait();
+    ptx::reg_fence16(v);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(v[j]);
+}
+
+__device__ __forceinline__ uint32_t tmem_columns(int n) { return n <= 32 ? 32u : 1u << (32 - __clz(n - 1)); }
+
+}  // namespace
+
+template <int EPI>
+__global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_constant__ MmMaps maps,
+                                                             const __grid_constant__ MmArgs p) {
+    constexpr bool kBoth = mm_both(EPI);
+    constexpr int kSums = kBoth ? 2 : 1;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    Shared *S = reinterpret_cast<Shared *>(ring + p.ring_bytes);
+    volatile int *abort_flag = &S->abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    // this CTA's tile, and its share of K
+    const int cluster = p.cluster, id = (int)blockIdx.x / cluster, rank = (int)blockIdx.x - id * cluster;
+    int which = 0;
+    while (which + 1 < p.problems && id >= p.prob[which + 1].first) ++which;
+    const MmProblem &q = p.prob[which];
+    const bool shared_k = q.split > 1;
+    const int tile = shared_k ? id - q.first : (id - q.first) * cluster + rank;
+    const int part = shared_k ? rank : 0;
+    const bool active = tile < q.mt * q.nt;
+    const int tn = tile / q.mt, tm = tile - tn * q.mt;
+    const int row0 = tm * q.tile_m, out0 = tn * kOutputs;
+    const int total = q.segments * q.steps;
+    const int step0 = (int)((int64_t)total * part / q.split), step1 = (int)((int64_t)total * (part + 1) / q.split);
+    const uint32_t columns = tmem_columns(kSums * q.tile_m);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            ptx::mbar_init(&S->full[s], 1);
+            ptx::mbar_init(&S->empty[s], 1);
+        }
+        ptx::mbar_init(&S->done, 1);
+        S->abort = 0;
+        ptx::fence_barrier_init();
+        ptx::fence_proxy_async_smem();
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(&S->tmem_base, columns);
+        ptx::tmem_relinquish();
+    }
+    pdl_wait();   // an operand may be the previous grid's output
+    __syncthreads();
+    pdl_trigger();
+    ptx::tc_fence_after();
+    const uint32_t tmem = S->tmem_base;
+
+    if (active && warp == 0 && ptx::elect_one()) {
+        // ---------------- copies ----------------
+        const uint64_t once = ptx::policy_evict_first(), again = ptx::policy_evict_last();
+        const uint64_t weights = q.mt > 1 ? again : once;   // row tiles share them in L2
+        const int box_bytes = q.a_mn ? kBoxBytes : q.box_rows * kStepK * 2;
+        const uint32_t bytes = (uint32_t)(kSums * kWeightBytes + q.boxes * box_bytes);
+        int stage = 0;
+        uint32_t phase = 0;
+        for (int step = step0; step < step1; ++step) {
+            if (!ptx::mbar_wait(&S->empty[stage], phase ^ 1u, p.wait_ns)) {
+                give_up(p, abort_flag);
+                break;
+            }
+            if (*abort_flag) break;
+            const int seg = step / q.steps, k = (step - seg * q.steps) * kStepK;
+            uint8_t *st = ring + (size_t)stage * p.stage_bytes;
+            uint64_t *full = &S->full[stage];
+            ptx::mbar_arrive_expect_tx(full, bytes);
+#pragma unroll
+            for (int w = 0; w < kSums; ++w) {
+                const CUtensorMap *m = &maps.m[q.b[kBoth ? w : seg]];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    ptx::tma_load_2d(st + (2 * w + h) * kBoxBytes, m, full, q.b_mn ? out0 + 64 * h : k,
+                                     q.b_mn ? k : out0 + 64 * h, weights);
+            }
+            st += kSums * kWeightBytes;
+            const CUtensorMap *m = &maps.m[q.a[seg]];
+            for (int h = 0; h < q.boxes; ++h) {
+                const int r = row0 + h * (q.a_mn ? 64 : q.box_rows);
+                ptx::tma_load_2d(st + h * box_bytes, m, full, q.a_mn ? r : k, q.a_mn ? k : r, again);
+            }
+            if (++stage == p.stages) {
+                stage = 0;
+                phase ^= 1u;
+            }
+        }
+    } else if (active && warp == 1 && ptx::elect_one()) {
+        // ---------------- products ----------------
+        // K-major: rows of 128 bytes, 8 to a kilobyte; 16 k are 32 bytes.
+        // MN-major: a kilobyte is 8 k of 64 rows, 64 rows on is the next box; 16 k are 2 KB.
+        const uint32_t ring32 = ptx::smem_u32(ring);
+        const uint32_t idesc = ptx::idesc_bf16(kOutputs, q.tile_m, q.b_mn, q.a_mn);
+        const uint64_t w_base = ptx::smem_desc(ring32, q.b_mn ? kBoxBytes : 16, 1024, 2);
+        const uint64_t x_base = ptx::smem_desc(ring32 + kSums * kWeightBytes, q.a_mn ? kBoxBytes : 16, 1024, 2);
+        const uint64_t w_step = q.b_mn ? 128 : 2, x_step = q.a_mn ? 128 : 2;
+        int stage = 0;
+        uint32_t phase = 0;
+        for (int step = step0; step < step1; ++step) {
+            if (!ptx::mbar_wait(&S->full[stage], phase, p.wait_ns)) {
+                give_up(p, abort_flag);
+                break;
+            }
+            if (*abort_flag) break;
+            ptx::tc_fence_after();
+            const uint64_t so = (uint64_t)stage * (uint64_t)(p.stage_bytes >> 4);
+#pragma unroll
+            for (int w = 0; w < kSums; ++w)
+#pragma unroll
+                for (int k = 0; k < kStepK / 16; ++k)
+                    ptx::mma_bf16(tmem + (uint32_t)(w * q.tile_m), w_base + so + (uint64_t)(w * (kWeightBytes >> 4)) + k * w_step,
+                                  x_base + so + k * x_step, idesc, (step > step0 || k) ? 1u : 0u);
+            ptx::mma_commit(&S->empty[stage]);
+            if (++stage == p.stages) {
+                stage = 0;
+                phase ^= 1u;
+            }
+        }
+        ptx::mma_commit(&S->done);
+    }
+    __syncwarp();
+    // ---------------- epilogue ----------------
+    const int quadrant = warp & 3, half = warp >> 2;
+    const int rows = q.M - row0 < q.tile_m ? q.M - row0 : q.tile_m;
+    Output o;
+    o.i = out0 + quadrant * 32 + lane;
+    o.b[0] = p.bias[0] && o.i < q.N ? __ldg(p.bias[0] + o.i) : 0.f;
+    o.b[1] = kBoth && p.bias[1] && o.i < q.N ? __ldg(p.bias[1] + o.i) : 0.f;
+    o.sum[0] = o.sum[1] = 0.f;
+    // (a wait that gives up says so; the products under way are waited for all the same)
+    if (active && !ptx::mbar_wait(&S->done, 0, p.wait_ns)) {
+        give_up(p, abort_flag);
+        ptx::mbar_wait(&S->done, 0, kMmTimeoutNs);
+    }
+    __syncthreads();
+    const bool ok = active && !*abort_flag;
+    ptx::tc_fence_after();
+    const uint32_t tbase = tmem + ((uint32_t)(quadrant * 32) << 16);
+    if (!shared_k) {
+        if (ok)
+            mm_with_act(p.act, [&](auto act) {
+                constexpr int ACT = decltype(act)::value;
+                for (int c = 16 * half; c < rows; c += 32) {
+                    float v[16], u[16];
+                    read_columns(tbase + (uint32_t)c, v);
+                    if constexpr (kBoth) read_columns(tbase + (uint32_t)(q.tile_m + c), u);
+                    finish<EPI, ACT>(p, q, o, v, u, row0 + c, rows - c);
+                }
+            });
+    } else {
+        // the ring is free: every copy has been used, and every product is complete
+        float *mine = reinterpret_cast<float *>(ring);
+        if (ok)
+            for (int c = 16 * half; c < rows; c += 32)
+#pragma unroll
+                for (int w = 0; w < kSums; ++w) {
+                    float v[16];
+                    read_columns(tbase + (uint32_t)(w * q.tile_m + c), v);
+                    float *to = mine + (size_t)(w * q.tile_m + c) * kOutputs + quadrant * 32 + lane;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) to[j * kOutputs] = v[j];
+                }
+        ptx::cluster_sync();
+        if (ok) {
+            const int share = (rows + q.split - 1) / q.split, c0 = part * share;
+            const int c1 = c0 + share < rows ? c0 + share : rows;
+            mm_with_act(p.act, [&](auto act) {
+                constexpr int ACT = decltype(act)::value;
+                for (int c = c0 + 8 * half; c < c1; c += 16) {
+                    const int count = c1 - c;
+                    float v[8] = {}, u[8] = {};
+                    for (int r = 0; r < q.split; ++r) {
+                        const uint32_t at =
+                            ptx::map_cluster(mine + (size_t)c * kOutputs + quadrant * 32 + lane, (uint32_t)r);
+                        float t[kSums][8];
+#pragma unroll
+                        for (int w = 0; w < kSums; ++w)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                t[w][j] = j < count ? ptx::ld_cluster(at + (uint32_t)((w * q.tile_m + j) * kOutputs * 4))
+                                                    : 0.f;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            v[j] += t[0][j];
+                            if constexpr (kBoth) u[j] += t[kSums - 1][j];
+                        }
+                    }
+                    finish<EPI, ACT>(p, q, o, v, u, row0 + c, count);
+                }
+            });
+        }
+    }
+    if constexpr (EPI == kMmSlope || EPI == kMmGatedSlope) {
+        if (ok && o.i < q.N)
+#pragma unroll
+            for (int w = 0; w < kSums; ++w)
+                if (p.part[w]) p.part[w][(size_t)((tm * q.split + part) * 2 + half) * q.N + o.i] = o.sum[w];
+    }
+    ptx::tc_fence_before();
+    if (*abort_flag && threadIdx.x == 0) {
+        // copies that were issued before the wait ran out land within microseconds
+        const uint64_t t0 = ptx::globaltimer();
+        while (ptx::globaltimer() - t0 < 2000000) {
+        }
+    }
+    __syncthreads();
+    if (shared_k) ptx::cluster_sync();   // nobody reads this CTA's sums any more
+    if (warp == 1) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, columns);
+    }
+}
+
+namespace {
+
+int round_up(int x, int to) { return (x + to - 1) / to * to; }
+
+// A row tile's bytes of a stage.
+int row_bytes(const MmProblem &q, int tile_m) {
+    return q.a_mn || tile_m > 64 ? round_up(tile_m, 64) * kStepK * 2 : tile_m * kStepK * 2;
+}
+
+// Whether a product can take tiles of tile_m rows and `split` CTAs a tile: the sums fit
+// into tensor memory and, where they are joined, into shared memory, no CTA is without
+// a step, and the sums over rows have a place.
+bool fits(MmEpilogue epi, const MmProblem &q, int tile_m, int split) {
+    const int sums = mm_both(epi) ? 2 : 1;
+    if (tile_m % 16 != 0 || tile_m < 16 || tile_m > 256 || sums * tile_m > 512) return false;
+    if (split > 1 && sums * tile_m * kOutputs * 4 + kExtra > kSmemOne) return false;
+    if (split > q.segments * q.steps) return false;
+    const int64_t tiles = ((int64_t)q.M + tile_m - 1) / tile_m;
+    return (epi != kMmSlope && epi != kMmGatedSlope) || tiles * split * 2 <= mm_part_rows(q.M);
+}
+
+#ifdef WZ_CHECKED
+int check_kind = 0, check_cluster = 1, check_tile = 64;
+#endif
+
+}  // namespace
+
+bool plan_mm_few(MmEpilogue epi, const MmArgs &p, int sms, MmFewPlan *plan) {
+#ifdef WZ_CHECKED
+    if (check_kind) {
+        if (check_kind == 1) return false;
+        plan->cluster = check_cluster;
+        for (int i = 0; i < p.problems; ++i) {
+            const MmProblem &q = p.prob[i];
+            plan->tile_m[i] = std::min(check_tile, round_up(q.M, 16));
+            plan->split[i] = fits(epi, q, plan->tile_m[i], check_cluster) ? check_cluster : 1;
+            if (!fits(epi, q, plan->tile_m[i], plan->split[i])) return false;
+        }
+        return true;
+    }
+#endif
+    int cluster = 1;
+    for (int i = 0; i < p.problems; ++i) {
+        const MmProblem &q = p.prob[i];
+        plan->tile_m[i] = round_up(std::min(q.M, 64), 16);
+        plan->split[i] = 1;
+        if (q.M > 64 || !fits(epi, q, plan->tile_m[i], 1)) return false;
+        const int tiles = (q.N + kOutputs - 1) / kOutputs;
+        cluster = std::max(1, std::min({kMaxCluster, sms / tiles, q.segments * q.steps}));
+    }
+    if (p.problems > 1) return false;
+    while (!fits(epi, p.prob[0], plan->tile_m[0], cluster)) --cluster;
+    plan->cluster = cluster;
+    plan->split[0] = cluster;
+    return true;
+}
+
+cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool pdl, cudaStream_t s,
+                          int64_t *part_rows) {
+    const int sums = mm_both(epi) ? 2 : 1;
+    MmMapList list;
+    int64_t clusters = 0;
+    int columns = 0, dump = 0, most_steps = 1;
+    p.cluster = plan.cluster;
+    p.stage_bytes = 0;
+    for (int i = 0; i < p.problems; ++i) {
+        MmProblem &q = p.prob[i];
+        q.tile_m = plan.tile_m[i];
+        q.split = plan.split[i];
+        q.box_rows = std::min(q.tile_m, 64);
+        q.boxes = (q.tile_m + 63) / 64;
+        q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
+        q.nt = (q.N + kOutputs - 1) / kOutputs;
+        if ((int64_t)q.mt * q.nt > INT32_MAX / kMaxCluster) return cudaErrorInvalidValue;
+        q.first = (int)clusters;
+        clusters += q.split > 1 ? q.mt * q.nt : (q.mt * q.nt + plan.cluster - 1) / plan.cluster;
+        p.stage_bytes = std::max(p.stage_bytes, sums * kWeightBytes + row_bytes(q, q.tile_m));
+        columns = std::max(columns, sums * q.tile_m);
+        if (q.split > 1) dump = std::max(dump, sums * q.tile_m * kOutputs * 4);
+        most_steps = std::max(most_steps, (q.segments * q.steps + q.split - 1) / q.split);
+        for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.a_mn ? 64 : q.box_rows);
+        for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j) q.b[j] = list.add(q.from_b[j], 64);
+    }
+    if (!list.ok || clusters * plan.cluster > INT32_MAX) return cudaErrorInvalidValue;
+    p.stage_bytes = round_up(p.stage_bytes, 1024);
+    // two CTAs an SM where their tensor memory, and joining sums, allow it
+    const bool two = columns <= 256 && dump + kExtra <= kSmemTwo && clusters * plan.cluster > sm_count();
+    const size_t most = (two ? kSmemTwo : kSmemOne) - kExtra;
+    p.stages = (int)std::min<size_t>({(size_t)kMaxStages, most / p.stage_bytes, (size_t)std::max(most_steps, 1)});
+    p.ring_bytes = std::max(p.stages * p.stage_bytes, dump);
+    if (p.stages < 1 || (size_t)p.ring_bytes > most) return cudaErrorInvalidValue;
+    const size_t smem = std::max(kExtra + (size_t)p.ring_bytes,
+                                 (columns <= 256 ? kSmemLeastTwo : kSmemLeastOne) + 1);
+    if (part_rows) *part_rows = (int64_t)p.prob[0].mt * p.prob[0].split * 2;
+    const void *fn = epi == kMmStore   ? (const void *)mm_few_kernel<kMmStore>
+                     : epi == kMmGated ? (const void *)mm_few_kernel<kMmGated>
+                     : epi == kMmSlope ? (const void *)mm_few_kernel<kMmSlope>
+                                       : (const void *)mm_few_kernel<kMmGatedSlope>;
+    const cudaError_t e = allow_smem(fn, smem);
+    if (e != cudaSuccess) return e;
+    void *args[] = {&list.maps, &p};
+    return launch_kernel(fn, dim3((unsigned)(clusters * plan.cluster)), dim3(kThreads), smem, s, args, pdl,
+                         (unsigned)plan.cluster);
+}
+
+}  // namespace wz
+
+#ifdef WZ_CHECKED
+// Test hook: the kernel that products take. kind 0: by their sizes, 1: mm_pair.cu's, 2: this file's where it
+// can, with clusters and row tiles of these sizes.
+extern "C" __attribute__((visibility("default"))) void wz_check_mm_plan(int kind, int cluster, int tile_m) {
+    wz::check_kind = kind;
+    wz::check_cluster = cluster;
+    wz::check_tile = tile_m;
+}
+#endif

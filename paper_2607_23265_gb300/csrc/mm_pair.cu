@@ -205,7 +205,7 @@ __device__ __forceinline__ void gated_slope_columns(const MmArgs &p, const MmPro
 template <int EPI>
 __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_constant__ MmMaps maps,
                                                               const __grid_constant__ MmArgs p) {
-    constexpr bool kBoth = EPI == kMmGated || EPI == kMmGatedSlope;
+    constexpr bool kBoth = mm_both(EPI);
     constexpr int kTileN = kBoth ? kAccCols / 2 : kAccCols;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -363,28 +363,36 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
     }
 }
 
-bool mm_map(CUtensorMap *m, const void *base, int64_t rows, int cols, int64_t stride) {
+MmMapList::MmMapList() { memset(&maps, 0, sizeof(maps)); }
+
+int MmMapList::add(const MmOperand &o, int box_rows) {
     auto enc = tmap_encode_fn();
-    if (!enc) return false;
-    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)stride * 2};
-    cuuint32_t box[2] = {64, 64};
+    cuuint64_t dims[2] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows};
+    cuuint64_t strides[1] = {(cuuint64_t)o.stride * 2};
+    cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
     cuuint32_t es[2] = {1, 1};
-    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, es,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    ok = ok && enc && count < kMmMaps &&
+         enc(&maps.m[count], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(o.base), dims, strides, box, es,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return count++;
 }
 
-cudaError_t launch_mm_pair(MmEpilogue epi, const MmMaps &maps, MmArgs &p, int sms, bool pdl, cudaStream_t s) {
-    const int tile_n = epi == kMmGated || epi == kMmGatedSlope ? kAccCols / 2 : kAccCols;
+cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStream_t s, int64_t *part_rows) {
+    const int tile_n = mm_both(epi) ? kAccCols / 2 : kAccCols;
     int64_t tiles = 0;
+    MmMapList list;
     for (int i = 0; i < p.problems; ++i) {
         MmProblem &q = p.prob[i];
         q.mt = (int)(((int64_t)q.M + 2 * kRows - 1) / (2 * kRows));
         q.nt = (q.N + tile_n - 1) / tile_n;
         tiles += (int64_t)q.mt * q.nt;
+        for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], 64);
+        for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j) q.b[j] = list.add(q.from_b[j], 64);
     }
+    if (!list.ok) return cudaErrorInvalidValue;
     if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
+    if (part_rows) *part_rows = ((int64_t)p.prob[0].M + 31) / 32;
     const void *fn = epi == kMmStore   ? (const void *)mm_pair_kernel<kMmStore>
                      : epi == kMmGated ? (const void *)mm_pair_kernel<kMmGated>
                      : epi == kMmSlope ? (const void *)mm_pair_kernel<kMmSlope>
@@ -392,7 +400,7 @@ cudaError_t launch_mm_pair(MmEpilogue epi, const MmMaps &maps, MmArgs &p, int sm
     cudaError_t e = allow_smem(fn, kSmemBytes);
     if (e != cudaSuccess) return e;
     const int pairs = (int)(tiles < sms / 2 ? tiles : sms / 2);
-    void *args[] = {const_cast<MmMaps *>(&maps), &p};
+    void *args[] = {&list.maps, &p};
     return launch_kernel(fn, dim3(2 * pairs), dim3(kThreads), kSmemBytes, s, args, pdl, 2);
 }
 

@@ -15,31 +15,48 @@
 
 namespace wz {
 
-constexpr int kMmMaps = 6;
+constexpr int kMmMaps = 8;
 constexpr int kMmProblems = 3;
 constexpr uint64_t kMmTimeoutNs = 2000000000ull;
 
 struct MmMaps {
-    CUtensorMap m[kMmMaps];   // 2D, boxes of 64 x 64 with 128-byte swizzle
+    CUtensorMap m[kMmMaps];   // 2D, boxes of 64 x 64 (or fewer rows) with 128-byte swizzle
 };
 
 // What is done with the sums.
 enum MmEpilogue : int {
     kMmStore = 0,     // out = act(p) + residual, p = sum + bias; p kept in pre[0]
     kMmGated = 1,     // out = act(g) u; g and u kept in pre[0], pre[1]
-    kMmSlope = 2,     // out = dy act'(p), and its sums over 32 rows in part[0]
+    kMmSlope = 2,     // out = dy act'(p), and its sums over some rows in part[0]
     kMmGatedSlope = 3 // out = dout u act'(g), out2 = dout act(g), and their sums
 };
 
-// One product of a launch.  With two segments the second continues the sums.
+__host__ __device__ constexpr bool mm_both(int epi) { return epi == kMmGated || epi == kMmGatedSlope; }
+
+// A matrix in memory: [rows][cols], rows `stride` elements apart.
+struct MmOperand {
+    const void *base;
+    int64_t rows;
+    int cols;
+    int64_t stride;
+};
+
+// One product of a launch.  With two segments the second continues the sums; in a gated
+// launch b[0] and b[1] are the gate's and the up projection's weights.
 struct MmProblem {
     int M, N;              // rows and columns of D
-    int mt, nt;            // tiles
     int segments, steps;   // K segments of `steps` steps of 64
     int a_mn, b_mn;        // operands MN-major
-    int a[2], b[2];        // tensor maps of the segments
     __nv_bfloat16 *out;    // [M] rows of N
     int64_t out_stride;
+    MmOperand from_a[2], from_b[2];   // host: the operands
+    // set by the launch
+    int a[2], b[2];        // their tensor maps
+    int mt, nt;            // tiles
+    int tile_m;            // few-rows kernel: rows of a tile, boxes of a row tile and rows of a box,
+    int boxes, box_rows;
+    int split;             //   CTAs that share a tile's K
+    int first;             //   first cluster
 };
 
 struct MmArgs {
@@ -51,8 +68,9 @@ struct MmArgs {
     const __nv_bfloat16 *dy;                // the slopes' factor
     __nv_bfloat16 *pre[2];                  // kept products; null: none
     __nv_bfloat16 *out2;                    // kMmGatedSlope
-    float *part[2];                         // [ceil(M / 32)][N] sums over 32 rows; null: none
+    float *part[2];                         // [some rows][N] sums over rows; null: none
     int64_t residual_stride, dy_stride, pre_stride[2], out2_stride;
+    int cluster, stages, stage_bytes, ring_bytes; // few-rows kernel: CTAs of a cluster, the ring
     int *status;
     uint64_t wait_ns;
 };
@@ -186,14 +204,36 @@ __device__ __forceinline__ float mm_column_sum(float (&x)[32]) {
     return x[0];
 }
 
-// ---- launchers (arguments checked) -----------------------------------------------
+// ---- launches (arguments checked) ------------------------------------------------
 
-// Products with tiles of 256 x 256 on pairs of SMs (mm_pair.cu).
-cudaError_t launch_mm_pair(MmEpilogue epi, const MmMaps &maps, MmArgs &p, int sms, bool pdl, cudaStream_t s);
+// The most rows of sums over rows that a launch writes for M rows.
+__host__ __device__ inline int64_t mm_part_rows(int64_t M) { return (M + 31) / 32 + 16; }
+
+// The products with the kernel that suits their sizes; part_rows (nullable): the rows of
+// sums that it writes.
+cudaError_t launch_mm(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStream_t s, int64_t *part_rows);
+
+// Tiles of 256 x 256 on pairs of SMs (mm_pair.cu).
+cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStream_t s, int64_t *part_rows);
+
+// Tiles of 16 to 256 rows on one SM, K shared by a cluster (mm_few.cu).  False: they do not
+// suit it.
+struct MmFewPlan {
+    int cluster, tile_m[kMmProblems], split[kMmProblems];
+};
+bool plan_mm_few(MmEpilogue epi, const MmArgs &p, int sms, MmFewPlan *plan);
+cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool pdl, cudaStream_t s,
+                          int64_t *part_rows);
 
 uint64_t mm_wait_ns();   // the limit of the products' waits
 
-// The map of a matrix [rows][cols] bf16 with rows `stride` elements apart.
-bool mm_map(CUtensorMap *m, const void *base, int64_t rows, int cols, int64_t stride);
+// A launch's tensor maps.
+struct MmMapList {
+    MmMaps maps;
+    int count = 0;
+    bool ok = true;
+    MmMapList();
+    int add(const MmOperand &o, int box_rows);
+};
 
 }  // namespace wz

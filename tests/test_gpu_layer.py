@@ -21,6 +21,14 @@ def wz():
     return m
 
 
+@pytest.fixture
+def forced(wz):
+    """Calls of the bounds-checked build with a kernel of the test's choice."""
+    with wz.checked_library():
+        yield wz._lib.wz_check_mm_plan
+        wz._lib.wz_check_mm_plan(0, 1, 64)
+
+
 def gen(seed):
     return torch.Generator(device="cuda").manual_seed(seed)
 
@@ -60,9 +68,7 @@ SIZES = [
 ]
 
 
-@pytest.mark.parametrize("act", ref.ACTS)
-@pytest.mark.parametrize("M,N,K", SIZES)
-def test_linear(wz, M, N, K, act):
+def linear(wz, M, N, K, act):
     s = Layer(M, N, K, 1, bias=(M + N) % 2 == 0, pad=(N % 3) * 8, seed=M + N + K)
     residual = ref.random_rows(M, N, 2.0, s.g, 8) if (M + K) % 2 else None
     out, pre = s.out(M, N), s.out(M, N)
@@ -76,9 +82,7 @@ def test_linear(wz, M, N, K, act):
     assert torch.equal(again, got)
 
 
-@pytest.mark.parametrize("act", ref.ACTS)
-@pytest.mark.parametrize("M,N,K", SIZES)
-def test_gated(wz, M, N, K, act):
+def gated(wz, M, N, K, act):
     s = Layer(M, N, K, 2, bias=(M + N) % 2 == 0, pad=(N % 3) * 8, seed=M + N + K)
     out, gate, up = s.out(M, N), s.out(M, N), s.out(M, N)
     got = wz.wz_gated(s.x, *s.w, *s.b, act=act, out=out, gate=gate, up=up, device_status=s.status)
@@ -90,10 +94,7 @@ def test_gated(wz, M, N, K, act):
     assert torch.equal(wz.wz_gated(s.x, *s.w, *s.b, act=act), got)
 
 
-@pytest.mark.parametrize("kept", [True, False])
-@pytest.mark.parametrize("act", ref.ACTS)
-@pytest.mark.parametrize("M,N,K", SIZES)
-def test_linear_backward(wz, M, N, K, act, kept):
+def linear_backward(wz, M, N, K, act, kept):
     s = Layer(M, N, K, 1, bias=(M + N) % 2 == 0, pad=(N % 3) * 8, seed=M + N + K)
     pre = s.pre[0] if kept else None
     dx, dw, db = s.out(M, K), s.out(N, K), torch.full((N,), float("nan"), device="cuda")
@@ -107,10 +108,7 @@ def test_linear_backward(wz, M, N, K, act, kept):
     ref.check(dw, want_w, "dw")
 
 
-@pytest.mark.parametrize("kept", [True, False])
-@pytest.mark.parametrize("act", ref.ACTS)
-@pytest.mark.parametrize("M,N,K", SIZES)
-def test_gated_backward(wz, M, N, K, act, kept):
+def gated_backward(wz, M, N, K, act, kept):
     s = Layer(M, N, K, 2, bias=(M + N) % 2 == 0, pad=(N % 3) * 8, seed=M + N + K)
     gate, up = s.pre if kept else (None, None)
     dx, dws = s.out(M, K), [s.out(N, K), s.out(N, K)]
@@ -124,3 +122,34 @@ def test_gated_backward(wz, M, N, K, act, kept):
         ref.check(dbs[i], want_b[i], "db_" + name)
         ref.check(dws[i], want_w[i], "dw_" + name)
     ref.check(dx, want_x, "dx")
+
+
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("M,N,K", SIZES)
+def test_forward(wz, M, N, K, act):
+    linear(wz, M, N, K, act)
+    gated(wz, M, N, K, act)
+
+
+@pytest.mark.parametrize("kept", [True, False])
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("M,N,K", SIZES)
+def test_backward(wz, M, N, K, act, kept):
+    linear_backward(wz, M, N, K, act, kept)
+    gated_backward(wz, M, N, K, act, kept)
+
+
+# pairs of SMs; then clusters and row tiles of the few-rows kernel: one CTA, shared K, the widest tiles
+PLANS = [(1, 1, 64), (2, 1, 64), (2, 2, 16), (2, 3, 208), (2, 8, 48), (2, 5, 176), (2, 1, 256)]
+
+
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("M,N,K", SIZES[::2])
+def test_every_kernel(wz, forced, M, N, K, plan):
+    forced(*plan)
+    act = ref.ACTS[(M + N + K) % 4]
+    linear(wz, M, N, K, act)
+    gated(wz, M, N, K, act)
+    for kept in (True, False):
+        linear_backward(wz, M, N, K, act, kept)
+        gated_backward(wz, M, N, K, act, kept)
