@@ -2,8 +2,7 @@
 //
 //   D^T[i][j] = sum_k B[i][k] A[j][k]     i: outputs (128 lanes of tensor memory), j: rows
 //
-// so that the number of rows is padded to 16 only, and a thread stands for an output of
-// which it writes one row after the other (a warp 64 contiguous bytes).  Weights of few
+// so that the number of rows is padded to 16 only.  Weights of few
 // rows are a stream that has to come from HBM as fast as it can: K is shared by the CTAs
 // of a cluster, each with a ring of up to twelve stages in flight, and their sums are
 // joined through distributed shared memory, in the order of their ranks, each CTA
@@ -13,7 +12,7 @@
 // whose sums lie beside one another in tensor memory) and the tile's rows, in boxes of
 // 64 x 64 (or fewer rows) with 128-byte swizzle, K-major or MN-major.  What lies outside
 // an operand arrives as zeros.
-// Warps: 0 copies, 1 products, then all eight the epilogue (two a TMEM lane quadrant).
+// Warps: 0 copies, 1 products, then all eight the epilogue.
 //
 // Tensor memory is taken by every CTA and held while it waits for its cluster.  So no two
 // such CTAs may share an SM unless both find room, or clusters could wait for one
@@ -58,70 +57,14 @@ __device__ __forceinline__ void give_up(const MmArgs &p, volatile int *abort_fla
     if (p.status) atomicOr(p.status, WZ_STATUS_WAIT_TIMEOUT);
 }
 
-// What a thread needs to finish its output.
-struct Output {
-    int i;              // the output, N or more: none
-    float b[2];
-    float sum[2];       // over its rows, of the slopes
-};
-
-// R rows row .. of output o.i, of which `count` are there.
-template <int EPI, int ACT, int R>
-__device__ __forceinline__ void finish(const MmArgs &p, const MmProblem &q, Output &o, const float (&v)[R],
-                                       const float (&u)[R], int row, int count) {
-    if (o.i >= q.N) return;
-    float other[R];   // the residual, or dy
-    const __nv_bfloat16 *from = EPI == kMmStore ? p.residual : p.dy;
-    const int64_t from_stride = EPI == kMmStore ? p.residual_stride : p.dy_stride;
-    if (EPI != kMmGated && from) {
-#pragma unroll
-        for (int j = 0; j < R; ++j)
-            other[j] = j < count ? __bfloat162float(from[(row + j) * from_stride + o.i]) : 0.f;
-    }
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-        if (j >= count) break;
-        const int64_t r = row + j;
-        const float x = v[j] + o.b[0];
-        if constexpr (EPI == kMmStore) {
-            if (p.pre[0]) p.pre[0][r * p.pre_stride[0] + o.i] = __float2bfloat16_rn(x);
-            float y = mm_act1<ACT>(x);
-            if (p.residual) y += other[j];
-            q.out[r * q.out_stride + o.i] = __float2bfloat16_rn(y);
-        } else if constexpr (EPI == kMmGated) {
-            const float y = u[j] + o.b[1];
-            if (p.pre[0]) {
-                p.pre[0][r * p.pre_stride[0] + o.i] = __float2bfloat16_rn(x);
-                p.pre[1][r * p.pre_stride[1] + o.i] = __float2bfloat16_rn(y);
-            }
-            q.out[r * q.out_stride + o.i] = __float2bfloat16_rn(mm_act1<ACT>(x) * y);
-        } else {
-            float value, slope;
-            mm_slope1<ACT>(x, value, slope);
-            if constexpr (EPI == kMmSlope) {
-                const float d = other[j] * slope;
-                o.sum[0] += d;
-                q.out[r * q.out_stride + o.i] = __float2bfloat16_rn(d);
-            } else {
-                const float dg = other[j] * (u[j] + o.b[1]) * slope, du = other[j] * value;
-                o.sum[0] += dg;
-                o.sum[1] += du;
-                q.out[r * q.out_stride + o.i] = __float2bfloat16_rn(dg);
-                p.out2[r * p.out2_stride + o.i] = __float2bfloat16_rn(du);
-            }
-        }
-    }
-}
-
-template <int C>
-__device__ __forceinline__ void read_columns(uint32_t tcol, float (&x)[C]) {
-    static_assert(C == 16, "columns of a read");
-    uint32_t v[16];
-    ptx::tmem_ld_32x32b_x16(tcol, v);
-    ptx::tmem_ld_wait();
-    ptx::reg_fence16(v);
-#pragma unroll
-    for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(v[j]);
+// Four floats of another CTA's shared memory (or of this one's).
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(addr)
+                 : "memory");
+    return v;
 }
 
 __device__ __forceinline__ uint32_t tmem_columns(int n) { return n <= 32 ? 32u : 1u << (32 - __clz(n - 1)); }
@@ -154,6 +97,7 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     const int step0 = (int)((int64_t)total * part / q.split), step1 = (int)((int64_t)total * (part + 1) / q.split);
     const uint32_t columns = tmem_columns(kSums * q.tile_m);
 
+    if (warp == 2 && lane < p.maps) ptx::prefetch_tmap(&maps.m[lane]);
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
             ptx::mbar_init(&S->full[s], 1);
@@ -246,13 +190,12 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     }
     __syncwarp();
     // ---------------- epilogue ----------------
-    const int quadrant = warp & 3, half = warp >> 2;
+    // The sums go through shared memory, a warp writing 32 outputs of 16 rows, and then
+    // takes one row's 128 outputs after the other, four to a lane: 256 contiguous bytes.
+    const int quadrant = warp & 3, side = warp >> 2;
     const int rows = q.M - row0 < q.tile_m ? q.M - row0 : q.tile_m;
-    Output o;
-    o.i = out0 + quadrant * 32 + lane;
-    o.b[0] = p.bias[0] && o.i < q.N ? __ldg(p.bias[0] + o.i) : 0.f;
-    o.b[1] = kBoth && p.bias[1] && o.i < q.N ? __ldg(p.bias[1] + o.i) : 0.f;
-    o.sum[0] = o.sum[1] = 0.f;
+    MmOutputs o;
+    mm_outputs<kBoth>(p, q, o, out0 + 4 * lane);
     // (a wait that gives up says so; the products under way are waited for all the same)
     if (active && !ptx::mbar_wait(&S->done, 0, p.wait_ns)) {
         give_up(p, abort_flag);
@@ -261,66 +204,72 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     __syncthreads();
     const bool ok = active && !*abort_flag;
     ptx::tc_fence_after();
+    // the ring is free: every copy has been used, and every product is complete
+    float *sums = reinterpret_cast<float *>(ring);
     const uint32_t tbase = tmem + ((uint32_t)(quadrant * 32) << 16);
-    if (!shared_k) {
+    const int chunk = shared_k ? q.tile_m : p.chunk;   // rows that are in shared memory at a time
+    for (int c0 = 0; c0 < rows; c0 += chunk) {
+        const int c1 = c0 + chunk < rows ? c0 + chunk : rows;
         if (ok)
-            mm_with_act(p.act, [&](auto act) {
-                constexpr int ACT = decltype(act)::value;
-                for (int c = 16 * half; c < rows; c += 32) {
-                    float v[16], u[16];
-                    read_columns(tbase + (uint32_t)c, v);
-                    if constexpr (kBoth) read_columns(tbase + (uint32_t)(q.tile_m + c), u);
-                    finish<EPI, ACT>(p, q, o, v, u, row0 + c, rows - c);
-                }
-            });
-    } else {
-        // the ring is free: every copy has been used, and every product is complete
-        float *mine = reinterpret_cast<float *>(ring);
-        if (ok)
-            for (int c = 16 * half; c < rows; c += 32)
+            for (int c = c0 + 16 * side; c < c1; c += 32)
 #pragma unroll
                 for (int w = 0; w < kSums; ++w) {
                     float v[16];
-                    read_columns(tbase + (uint32_t)(w * q.tile_m + c), v);
-                    float *to = mine + (size_t)(w * q.tile_m + c) * kOutputs + quadrant * 32 + lane;
+                    mm_read16(tbase + (uint32_t)(w * q.tile_m + c), v);
+                    float *to = sums + (size_t)(w * chunk + c - c0) * kOutputs + quadrant * 32 + lane;
 #pragma unroll
                     for (int j = 0; j < 16; ++j) to[j * kOutputs] = v[j];
                 }
-        ptx::cluster_sync();
-        if (ok) {
-            const int share = (rows + q.split - 1) / q.split, c0 = part * share;
-            const int c1 = c0 + share < rows ? c0 + share : rows;
+        if (shared_k) ptx::cluster_sync();
+        else __syncthreads();
+        if (ok && o.left > 0)
             mm_with_act(p.act, [&](auto act) {
                 constexpr int ACT = decltype(act)::value;
-                for (int c = c0 + 8 * half; c < c1; c += 16) {
-                    const int count = c1 - c;
-                    float v[8] = {}, u[8] = {};
-                    for (int r = 0; r < q.split; ++r) {
-                        const uint32_t at =
-                            ptx::map_cluster(mine + (size_t)c * kOutputs + quadrant * 32 + lane, (uint32_t)r);
-                        float t[kSums][8];
+                constexpr int U = kBoth ? 1 : 2;   // rows in flight
+                // this CTA's share of the rows
+                const int share = shared_k ? (rows + q.split - 1) / q.split : c1 - c0;
+                const int lo = shared_k ? part * share : c0, hi = lo + share < c1 ? lo + share : c1;
+                for (int c = lo + warp; c < hi; c += U * kWarps) {
+                    float v[U][4] = {}, u[U][4] = {}, other[U][4];
+                    mm_fetch<EPI, U>(p, o, other, (int64_t)row0 + c, kWarps, (int64_t)row0 + hi);
+                    const float *at = sums + (size_t)(c - c0) * kOutputs + 4 * lane;
+                    if (!shared_k) {
 #pragma unroll
-                        for (int w = 0; w < kSums; ++w)
+                        for (int k = 0; k < U; ++k)
+                            if (c + k * kWarps < hi)
 #pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                t[w][j] = j < count ? ptx::ld_cluster(at + (uint32_t)((w * q.tile_m + j) * kOutputs * 4))
-                                                    : 0.f;
+                                for (int w = 0; w < kSums; ++w) {
+                                    const float4 t = *reinterpret_cast<const float4 *>(
+                                        at + (size_t)(w * chunk + k * kWarps) * kOutputs);
+                                    float(&d)[4] = w ? u[k] : v[k];
+                                    d[0] = t.x, d[1] = t.y, d[2] = t.z, d[3] = t.w;
+                                }
+                    } else {
+                        for (int r0 = 0; r0 < q.split; r0 += 4) {
+                            float4 t[4][U * kSums];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            v[j] += t[0][j];
-                            if constexpr (kBoth) u[j] += t[kSums - 1][j];
+                            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                                for (int x = 0; x < U * kSums; ++x) {
+                                    const int k = x / kSums, w = x % kSums;
+                                    t[r][x] = make_float4(0.f, 0.f, 0.f, 0.f);
+                                    if (r0 + r < q.split && c + k * kWarps < hi)
+                                        t[r][x] = ld_cluster4(ptx::map_cluster(
+                                            at + (size_t)(w * chunk + k * kWarps) * kOutputs, (uint32_t)(r0 + r)));
+                                }
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                                for (int x = 0; x < U * kSums; ++x) {
+                                    float(&d)[4] = x % kSums ? u[x / kSums] : v[x / kSums];
+                                    d[0] += t[r][x].x, d[1] += t[r][x].y, d[2] += t[r][x].z, d[3] += t[r][x].w;
+                                }
                         }
                     }
-                    finish<EPI, ACT>(p, q, o, v, u, row0 + c, count);
+                    mm_finish<EPI, ACT, U>(p, q, o, v, u, other, (int64_t)row0 + c, kWarps, (int64_t)row0 + hi);
                 }
             });
-        }
-    }
-    if constexpr (EPI == kMmSlope || EPI == kMmGatedSlope) {
-        if (ok && o.i < q.N)
-#pragma unroll
-            for (int w = 0; w < kSums; ++w)
-                if (p.part[w]) p.part[w][(size_t)((tm * q.split + part) * 2 + half) * q.N + o.i] = o.sum[w];
+        if (c1 < rows) __syncthreads();
     }
     ptx::tc_fence_before();
     if (*abort_flag && threadIdx.x == 0) {
@@ -331,6 +280,21 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     }
     __syncthreads();
     if (shared_k) ptx::cluster_sync();   // nobody reads this CTA's sums any more
+    if constexpr (EPI == kMmSlope || EPI == kMmGatedSlope) {
+        // the warps' sums over their rows, in order
+#pragma unroll
+        for (int w = 0; w < kSums; ++w)
+            *reinterpret_cast<float4 *>(sums + (w * kWarps + warp) * kOutputs + 4 * lane) =
+                make_float4(o.sum[w][0], o.sum[w][1], o.sum[w][2], o.sum[w][3]);
+        __syncthreads();
+        const int w = (int)threadIdx.x / kOutputs, i = (int)threadIdx.x % kOutputs;
+        if (ok && w < kSums && out0 + i < q.N && p.part[w]) {
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) s += sums[(w * kWarps + k) * kOutputs + i];
+            p.part[w][(size_t)(tm * q.split + part) * q.N + out0 + i] = s;
+        }
+    }
     if (warp == 1) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc(tmem, columns);
@@ -355,7 +319,7 @@ bool fits(MmEpilogue epi, const MmProblem &q, int tile_m, int split) {
     if (split > 1 && sums * tile_m * kOutputs * 4 + kExtra > kSmemOne) return false;
     if (split > q.segments * q.steps) return false;
     const int64_t tiles = ((int64_t)q.M + tile_m - 1) / tile_m;
-    return (epi != kMmSlope && epi != kMmGatedSlope) || tiles * split * 2 <= mm_part_rows(q.M);
+    return (epi != kMmSlope && epi != kMmGatedSlope) || tiles * split <= mm_part_rows(q.M);
 }
 
 #ifdef WZ_CHECKED
@@ -422,15 +386,17 @@ cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool
     }
     if (!list.ok || clusters * plan.cluster > INT32_MAX) return cudaErrorInvalidValue;
     p.stage_bytes = round_up(p.stage_bytes, 1024);
+    p.maps = list.count;
     // two CTAs an SM where their tensor memory, and joining sums, allow it
     const bool two = columns <= 256 && dump + kExtra <= kSmemTwo && clusters * plan.cluster > sm_count();
     const size_t most = (two ? kSmemTwo : kSmemOne) - kExtra;
     p.stages = (int)std::min<size_t>({(size_t)kMaxStages, most / p.stage_bytes, (size_t)std::max(most_steps, 1)});
     p.ring_bytes = std::max(p.stages * p.stage_bytes, dump);
     if (p.stages < 1 || (size_t)p.ring_bytes > most) return cudaErrorInvalidValue;
+    p.chunk = std::min(256, p.ring_bytes / (sums * kOutputs * 4) / 16 * 16);
     const size_t smem = std::max(kExtra + (size_t)p.ring_bytes,
                                  (columns <= 256 ? kSmemLeastTwo : kSmemLeastOne) + 1);
-    if (part_rows) *part_rows = (int64_t)p.prob[0].mt * p.prob[0].split * 2;
+    if (part_rows) *part_rows = (int64_t)p.prob[0].mt * p.prob[0].split;
     const void *fn = epi == kMmStore   ? (const void *)mm_few_kernel<kMmStore>
                      : epi == kMmGated ? (const void *)mm_few_kernel<kMmGated>
                      : epi == kMmSlope ? (const void *)mm_few_kernel<kMmSlope>

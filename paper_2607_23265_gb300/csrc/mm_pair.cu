@@ -1,21 +1,18 @@
-// Matrix products on pairs of SMs: tiles of 256 rows x 256 columns of
+// Matrix products on pairs of SMs: tiles of 256 outputs x up to 256 rows of
 //
-//   D[i][j] = sum_k A[i][k] B[j][k]
+//   D^T[i][j] = sum_k B[i][k] A[j][k]     i: outputs (lanes of tensor memory), j: rows
 //
-// with what follows a layer's product (bias, activation, residual, the gated product,
-// the slopes of the backward pass) applied to the fp32 sums.
-//
-// cta_group::2: a cluster of two CTAs holds 128 rows of A and 128 of B each, in six
-// stages of 64 along K (32 KB a CTA), and 128 rows of D (256 columns of tensor memory,
-// twice, so that a tile's epilogue overlaps the next one's main loop).  An operand
-// tile is two boxes of 64 x 64 with 128-byte swizzle, K-major (64 rows of 64 k) or
-// MN-major (64 k of 64 rows); what lies outside an operand arrives as zeros, so any
-// size works.  In a gated product the even CTA's B is the gate's weights and the odd
-// one's the up projection's: columns 0 .. 127 of D are g and 128 .. 255 are u of the
-// same 128 outputs, and a thread has both.
+// cta_group::2: a cluster of two CTAs holds 128 outputs' weights and half of the rows
+// each, in six stages of 64 along K (32 KB a CTA), and the sums of its 128 outputs (256
+// columns of tensor memory, twice, so that a tile's epilogue overlaps the next one's main
+// loop).  With the rows in the columns a tile's row count is a multiple of 32 and not of
+// 256: 333 rows are tiles of 192 and 160.  An operand tile is boxes of 64 x 64 (or
+// fewer rows) with 128-byte swizzle, K-major or MN-major; what lies outside an operand
+// arrives as zeros, so any size works.  In a gated product a CTA's 128 lanes are the
+// gate's weights of 64 outputs and the up projection's of the same 64.
 //   Persistent pairs walk the tiles of up to three products.
-// Warps: 0 copies, 1 products (the even CTA's), 2-9 epilogue (two a TMEM lane
-// quadrant, half of the columns each).
+// Warps: 0 copies, 1 products (the even CTA's), 2-9 epilogue: 32 rows' sums at a time go
+// through one of two buffers in shared memory and are finished row by row.
 #include <cstring>
 #include <type_traits>
 
@@ -25,15 +22,17 @@ namespace wz {
 
 namespace {
 
-constexpr int kRows = 128, kStepK = 64;              // rows of an operand tile of a CTA, K of a stage
-constexpr int kOperandBytes = kRows * kStepK * 2;    // 16 KB
-constexpr int kBoxBytes = kOperandBytes / 2;
+constexpr int kOutputs = 128, kStepK = 64;               // outputs of a CTA, K of a stage
+constexpr int kOperandBytes = kOutputs * kStepK * 2;     // 16 KB
+constexpr int kBoxBytes = kOperandBytes / 2;             // 64 x 64
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kStages = 6;
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = (2 + kEpiWarps) * 32;
-constexpr int kAccCols = 256;
-constexpr int kGroupRows = 8;                        // row tiles that are walked together
+constexpr int kAccCols = 256;                            // the most rows of a tile
+constexpr int kChunk = 32;                               // rows of sums in shared memory at a time
+constexpr int kChunkFloats = kChunk * kOutputs;
+constexpr int kGroupRows = 8;                            // row tiles that are walked together
 
 struct Shared {
     uint64_t full[kStages];
@@ -45,19 +44,19 @@ struct Shared {
     int abort;
 };
 
-constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + sizeof(Shared);
+constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + 2 * kChunkFloats * 4 + sizeof(Shared);
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of the pair CTA");
 
 struct Tile {
-    int prob, m, n;
+    int prob, row0, rows, n;   // rows: a multiple of 32, those behind the last one among them
 };
 
 // The tiles of pair `pair` of `pairs`, in order: the first product's dealt in turn,
 // then the others'.
 struct Walk {
     const MmArgs &p;
-    int pair, pairs, t;
-    __device__ Walk(const MmArgs &args, int pair_, int pairs_) : p(args), pair(pair_), pairs(pairs_), t(pair_) {}
+    int pairs, t;
+    __device__ Walk(const MmArgs &args, int pair, int pairs_) : p(args), pairs(pairs_), t(pair) {}
     __device__ bool next(Tile &tile) {
         int x = t, i = 0;
         for (; i < p.problems; ++i) {
@@ -67,15 +66,17 @@ struct Walk {
         }
         if (i == p.problems) return false;
         t += pairs;
-        // kGroupRows row tiles at a time, column by column: pairs that run side by
-        // side share both operands' tiles in L2
+        // kGroupRows row tiles at a time, output tile by output tile: pairs that run
+        // side by side share both operands' tiles in L2
         const MmProblem &q = p.prob[i];
         const int group = x / (kGroupRows * q.nt), left = q.mt - group * kGroupRows;
         const int rows = left < kGroupRows ? left : kGroupRows;
         x -= group * kGroupRows * q.nt;
         tile.prob = i;
         tile.n = x / rows;
-        tile.m = group * kGroupRows + x - tile.n * rows;
+        tile.row0 = (group * kGroupRows + x - tile.n * rows) * q.tile_m;
+        const int r = q.M - tile.row0;
+        tile.rows = r < q.tile_m ? (r + 31) / 32 * 32 : q.tile_m;
         return true;
     }
 };
@@ -85,119 +86,19 @@ __device__ __forceinline__ void give_up(const MmArgs &p, volatile int *abort_fla
     if (p.status) atomicOr(p.status, WZ_STATUS_WAIT_TIMEOUT);
 }
 
-// 128 rows r0 .. and 64 k of an operand.
-__device__ __forceinline__ void load_operand(uint8_t *dst, const CUtensorMap *m, uint32_t bar, int mn, int r0, int k0,
-                                             uint64_t policy) {
-    if (mn) {
-        ptx::tma_load_2d_pair(dst, m, bar, r0, k0, policy);
-        ptx::tma_load_2d_pair(dst + kBoxBytes, m, bar, r0 + 64, k0, policy);
-    } else {
-        ptx::tma_load_2d_pair(dst, m, bar, k0, r0, policy);
-        ptx::tma_load_2d_pair(dst + kBoxBytes, m, bar, k0, r0 + 64, policy);
-    }
-}
-
-// 32 columns of the warp's rows.
-__device__ __forceinline__ void read_columns(uint32_t tcol, float (&x)[32]) {
-    uint32_t v[32];
-    ptx::tmem_ld_32x32b_x32(tcol, v);
-    ptx::tmem_ld_wait();
-    ptx::reg_fence32(v);
-#pragma unroll
-    for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(v[j]);
-}
-
-// Columns n .. n + 31 of a row of a product, at tcol in tensor memory.
-template <int ACT>
-__device__ __forceinline__ void store_columns(const MmArgs &p, const MmProblem &q, uint32_t tcol, int row, int n) {
-    float x[32];
-    read_columns(tcol, x);
-    const int left = q.N - n;
-    mm_add_bias(p.bias[0] ? p.bias[0] + n : nullptr, x, left);
-    if (row >= q.M) return;
-    if (p.pre[0]) mm_store(p.pre[0] + row * p.pre_stride[0] + n, x, left);
-#pragma unroll
-    for (int j = 0; j < 32; ++j) x[j] = mm_act1<ACT>(x[j]);
-    if (p.residual) {
-        float r[32];
-        mm_load(p.residual + row * p.residual_stride + n, r, left);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) x[j] += r[j];
-    }
-    mm_store(q.out + row * q.out_stride + n, x, left);
-}
-
-template <int ACT>
-__device__ __forceinline__ void gated_columns(const MmArgs &p, const MmProblem &q, uint32_t tcol, int row, int n) {
-    float g[32], u[32];
-    read_columns(tcol, g);
-    read_columns(tcol + kAccCols / 2, u);
-    const int left = q.N - n;
-    mm_add_bias(p.bias[0] ? p.bias[0] + n : nullptr, g, left);
-    mm_add_bias(p.bias[1] ? p.bias[1] + n : nullptr, u, left);
-    if (row >= q.M) return;
-    if (p.pre[0]) {
-        mm_store(p.pre[0] + row * p.pre_stride[0] + n, g, left);
-        mm_store(p.pre[1] + row * p.pre_stride[1] + n, u, left);
-    }
-#pragma unroll
-    for (int j = 0; j < 32; ++j) g[j] = mm_act1<ACT>(g[j]) * u[j];
-    mm_store(q.out + row * q.out_stride + n, g, left);
-}
-
-// The sums over the warp's 32 rows, of which those behind M count nothing.
-__device__ __forceinline__ void store_sums(float *part, const MmProblem &q, float (&d)[32], int row, int n) {
-    if (row >= q.M) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) d[j] = 0.f;
-    }
-    const float sum = mm_column_sum(d);
-    const int lane = threadIdx.x & 31, first = row - lane;
-    if (first < q.M && lane < q.N - n) part[(size_t)(first >> 5) * q.N + n + lane] = sum;
-}
-
-template <int ACT>
-__device__ __forceinline__ void slope_columns(const MmArgs &p, const MmProblem &q, uint32_t tcol, int row, int n) {
-    float x[32], dy[32];
-    read_columns(tcol, x);
-    const int left = q.N - n;
-    mm_add_bias(p.bias[0] ? p.bias[0] + n : nullptr, x, left);
-    if (row < q.M) {
-        mm_load(p.dy + row * p.dy_stride + n, dy, left);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            float value, slope;
-            mm_slope1<ACT>(x[j], value, slope);
-            x[j] = dy[j] * slope;
-        }
-        mm_store(q.out + row * q.out_stride + n, x, left);
-    }
-    if (p.part[0]) store_sums(p.part[0], q, x, row, n);
-}
-
-template <int ACT>
-__device__ __forceinline__ void gated_slope_columns(const MmArgs &p, const MmProblem &q, uint32_t tcol, int row, int n) {
-    float g[32], u[32];
-    read_columns(tcol, g);
-    read_columns(tcol + kAccCols / 2, u);
-    const int left = q.N - n;
-    mm_add_bias(p.bias[0] ? p.bias[0] + n : nullptr, g, left);
-    mm_add_bias(p.bias[1] ? p.bias[1] + n : nullptr, u, left);
-    if (row < q.M) {
-        float dy[32];
-        mm_load(p.dy + row * p.dy_stride + n, dy, left);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            float value, slope;
-            mm_slope1<ACT>(g[j], value, slope);
-            g[j] = dy[j] * u[j] * slope;
-            u[j] = dy[j] * value;
-        }
-        mm_store(q.out + row * q.out_stride + n, g, left);
-        mm_store(p.out2 + row * p.out2_stride + n, u, left);
-    }
-    if (p.part[0]) store_sums(p.part[0], q, g, row, n);
-    if (p.part[1]) store_sums(p.part[1], q, u, row, n);
+// Barriers of the epilogue warps; the second says, to all alike, whether all came with `ok`.
+__device__ __forceinline__ void epilogue_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ bool epilogue_all(bool ok) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "bar.red.and.pred q, 1, 256, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"(ok ? 1u : 0u)
+        : "memory");
+    return r != 0;
 }
 
 }  // namespace
@@ -206,14 +107,16 @@ template <int EPI>
 __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_constant__ MmMaps maps,
                                                               const __grid_constant__ MmArgs p) {
     constexpr bool kBoth = mm_both(EPI);
-    constexpr int kTileN = kBoth ? kAccCols / 2 : kAccCols;
+    constexpr int kOwn = kBoth ? kOutputs / 2 : kOutputs;   // outputs of a CTA
     extern __shared__ uint8_t smem_raw[];
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    Shared *S = reinterpret_cast<Shared *>(ring + (size_t)kStages * kStageBytes);
+    float *sums = reinterpret_cast<float *>(ring + (size_t)kStages * kStageBytes);
+    Shared *S = reinterpret_cast<Shared *>(sums + 2 * kChunkFloats);
     volatile int *abort_flag = &S->abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = ptx::cluster_rank();
 
+    if (warp == 2 && lane < p.maps) ptx::prefetch_tmap(&maps.m[lane]);
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
             ptx::mbar_init(&S->full[s], 1);
@@ -233,8 +136,8 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
         ptx::tmem_relinquish_pair();
     }
     pdl_wait();   // an operand may be the previous grid's output
-    pdl_trigger();
     __syncthreads();
+    pdl_trigger();
     ptx::cluster_sync();   // both CTAs' barriers are ready
     ptx::tc_fence_after();
     const uint32_t tmem = S->tmem_base;
@@ -249,11 +152,14 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
         bool ok = true;
         while (ok && !*abort_flag && walk.next(t)) {
             const MmProblem &q = p.prob[t.prob];
-            const int m0 = t.m * 2 * kRows + (int)rank * kRows;
-            const int n0 = kBoth ? t.n * kTileN : t.n * kTileN + (int)rank * kRows;
+            const int i0 = (t.n * 2 + (int)rank) * kOwn, r0 = t.row0 + (int)rank * (t.rows / 2);
+            const int box_rows = q.a_mn ? 64 : q.box_rows, boxes = (t.rows / 2 + box_rows - 1) / box_rows;
+            const int box_bytes = box_rows * kStepK * 2;
+            const uint32_t bytes = 2u * (uint32_t)(kOperandBytes + boxes * box_bytes);
             for (int seg = 0; ok && seg < q.segments; ++seg) {
-                const CUtensorMap *a = &maps.m[q.a[seg]], *b = &maps.m[q.b[kBoth ? (int)rank : seg]];
+                const CUtensorMap *a = &maps.m[q.a[seg]];
                 for (int ks = 0; ks < q.steps; ++ks) {
+                    const int k = ks * kStepK;
                     if (!ptx::mbar_wait(&S->empty[stage], phase ^ 1u, p.wait_ns)) {
                         give_up(p, abort_flag);
                         ok = false;
@@ -261,9 +167,19 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                     }
                     uint8_t *st = ring + (size_t)stage * kStageBytes;
                     const uint32_t full = ptx::map_cluster(&S->full[stage], 0);
-                    if (rank == 0) ptx::mbar_arrive_expect_tx(&S->full[stage], 2u * kStageBytes);
-                    load_operand(st, a, full, q.a_mn, m0, ks * kStepK, policy);
-                    load_operand(st + kOperandBytes, b, full, q.b_mn, n0, ks * kStepK, policy);
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(&S->full[stage], bytes);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        // 64 outputs' weights; in a gated product the gate's, then the up projection's
+                        const CUtensorMap *b = &maps.m[q.b[kBoth ? h : seg]];
+                        const int i = kBoth ? i0 : i0 + 64 * h;
+                        ptx::tma_load_2d_pair(st + h * kBoxBytes, b, full, q.b_mn ? i : k, q.b_mn ? k : i, policy);
+                    }
+                    for (int h = 0; h < boxes; ++h) {
+                        const int r = r0 + h * box_rows;
+                        ptx::tma_load_2d_pair(st + kOperandBytes + h * box_bytes, a, full, q.a_mn ? r : k,
+                                              q.a_mn ? k : r, policy);
+                    }
                     if (++stage == kStages) {
                         stage = 0;
                         phase ^= 1u;
@@ -281,10 +197,10 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
             const MmProblem &q = p.prob[t.prob];
             // K-major: rows of 128 bytes, 8 to a kilobyte; 16 k are 32 bytes.
             // MN-major: a kilobyte is 8 k of 64 rows, 64 rows on is the next box; 16 k are 2 KB.
-            const uint32_t idesc = ptx::idesc_bf16(2 * kRows, kAccCols, q.a_mn, q.b_mn);
-            const uint64_t a_base = ptx::smem_desc(ring32, q.a_mn ? kBoxBytes : 16, 1024, 2);
-            const uint64_t b_base = ptx::smem_desc(ring32 + kOperandBytes, q.b_mn ? kBoxBytes : 16, 1024, 2);
-            const uint64_t a_step = q.a_mn ? 128 : 2, b_step = q.b_mn ? 128 : 2;
+            const uint32_t idesc = ptx::idesc_bf16(2 * kOutputs, t.rows, q.b_mn, q.a_mn);
+            const uint64_t w_base = ptx::smem_desc(ring32, q.b_mn ? kBoxBytes : 16, 1024, 2);
+            const uint64_t x_base = ptx::smem_desc(ring32 + kOperandBytes, q.a_mn ? kBoxBytes : 16, 1024, 2);
+            const uint64_t w_step = q.b_mn ? 128 : 2, x_step = q.a_mn ? 128 : 2;
             const int b = it & 1;
             if (!ptx::mbar_wait(&S->tempty[b], ((uint32_t)(it >> 1) & 1u) ^ 1u, p.wait_ns)) {
                 give_up(p, abort_flag);
@@ -303,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                 const uint64_t so = (uint64_t)stage * (uint64_t)(kStageBytes >> 4);
 #pragma unroll
                 for (int k = 0; k < kStepK / 16; ++k)
-                    ptx::mma_bf16_pair(d, a_base + so + k * a_step, b_base + so + k * b_step, idesc, (ks | k) ? 1u : 0u);
+                    ptx::mma_bf16_pair(d, w_base + so + k * w_step, x_base + so + k * x_step, idesc, (ks | k) ? 1u : 0u);
                 ptx::mma_commit_pair(&S->empty[stage]);
                 if (++stage == kStages) {
                     stage = 0;
@@ -318,33 +234,83 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
     } else if (warp == 1 && rank == 1 && ptx::elect_one()) {
         ptx::mbar_wait(&S->drain, 0, 2 * kMmTimeoutNs);   // the even CTA's last arrivals here
     } else if (warp >= 2) {
-        // ---------------- epilogue of this CTA's 128 rows ----------------
-        const int quadrant = warp & 3;   // TMEM lanes 32 quadrant ..
+        // ---------------- epilogue of this CTA's outputs ----------------
+        constexpr int U = kBoth ? 2 : 4;          // rows of a lane in a chunk
+        const int quadrant = warp & 3, side = (warp - 2) >> 2, w8 = warp - 2;
+        const int own = kBoth ? lane & 15 : lane;
+        // the lane's rows of a chunk: first, first + every, ..
+        const int first = kBoth ? 4 * w8 + (lane >> 4) : 4 * w8, every = kBoth ? 2 : 1;
         const uint32_t tempty[2] = {ptx::map_cluster(&S->tempty[0], 0), ptx::map_cluster(&S->tempty[1], 0)};
-        int it = 0;
-        while (!*abort_flag && walk.next(t)) {
+        int it = 0, buffer = 0;
+        while (walk.next(t)) {
             const MmProblem &q = p.prob[t.prob];
             const int b = it & 1;
-            if (!ptx::mbar_wait(&S->tfull[b], (uint32_t)(it >> 1) & 1u, p.wait_ns)) {
-                give_up(p, abort_flag);
-                break;
-            }
-            __syncwarp();
+            const int64_t end = t.row0 + t.rows < q.M ? t.row0 + t.rows : q.M;
+            MmOutputs o;
+            mm_outputs<kBoth>(p, q, o, (t.n * 2 + (int)rank) * kOwn + 4 * own);
+            const bool mine = o.left > 0;
+            float other[U][4];
+            if (mine) mm_fetch<EPI, U>(p, o, other, (int64_t)t.row0 + first, every, end);
+            // the warps leave together, on one verdict: their barriers count all of them
+            const bool full = ptx::mbar_wait(&S->tfull[b], (uint32_t)(it >> 1) & 1u, p.wait_ns);
+            if (!full) give_up(p, abort_flag);
+            if (!epilogue_all(full)) break;
             ptx::tc_fence_after();
-            const int row = t.m * 2 * kRows + (int)rank * kRows + quadrant * 32 + lane, n0 = t.n * kTileN;
             const uint32_t tbase = tmem + ((uint32_t)(quadrant * 32) << 16) + (uint32_t)(b * kAccCols);
             mm_with_act(p.act, [&](auto act) {
                 constexpr int ACT = decltype(act)::value;
-                for (int c = 32 * ((warp - 2) >> 2); c < kTileN && n0 + c < q.N; c += 64) {
-                    if constexpr (EPI == kMmStore) store_columns<ACT>(p, q, tbase + c, row, n0 + c);
-                    if constexpr (EPI == kMmGated) gated_columns<ACT>(p, q, tbase + c, row, n0 + c);
-                    if constexpr (EPI == kMmSlope) slope_columns<ACT>(p, q, tbase + c, row, n0 + c);
-                    if constexpr (EPI == kMmGatedSlope) gated_slope_columns<ACT>(p, q, tbase + c, row, n0 + c);
+                for (int c0 = 0; t.row0 + c0 < end; c0 += kChunk, buffer ^= 1) {
+                    float *at = sums + buffer * kChunkFloats;
+                    {
+                        float v[16];
+                        mm_read16(tbase + (uint32_t)(c0 + 16 * side), v);
+                        float *to = at + 16 * side * kOutputs + quadrant * 32 + lane;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) to[j * kOutputs] = v[j];
+                    }
+                    if (t.row0 + c0 + kChunk >= end) {   // the last of the tile's sums are read
+                        ptx::tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive_cluster(b ? tempty[1] : tempty[0]);
+                    }
+                    epilogue_barrier();
+                    if (mine) {
+                        float v[U][4], u[U][4];
+#pragma unroll
+                        for (int k = 0; k < U; ++k) {
+                            const float *row = at + (first + k * every) * kOutputs + 4 * own;
+                            const float4 x = *reinterpret_cast<const float4 *>(row);
+                            v[k][0] = x.x, v[k][1] = x.y, v[k][2] = x.z, v[k][3] = x.w;
+                            if constexpr (kBoth) {
+                                const float4 y = *reinterpret_cast<const float4 *>(row + kOutputs / 2);
+                                u[k][0] = y.x, u[k][1] = y.y, u[k][2] = y.z, u[k][3] = y.w;
+                            }
+                        }
+                        const int64_t r = (int64_t)t.row0 + c0 + first;
+                        mm_finish<EPI, ACT, U>(p, q, o, v, u, other, r, every, end);
+                        mm_fetch<EPI, U>(p, o, other, r + kChunk, every, end);
+                    }
                 }
             });
-            ptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive_cluster(b ? tempty[1] : tempty[0]);
+            if constexpr (EPI == kMmSlope || EPI == kMmGatedSlope) {
+                // the warps' sums over their rows, in order; a buffer holds eight warps' of one kind,
+                // and in a gated product those of a warp's even and odd rows
+                constexpr int kHalves = kBoth ? 2 : 1;
+#pragma unroll
+                for (int w = 0; w < (kBoth ? 2 : 1); ++w) {
+                    float *at = sums + buffer * kChunkFloats;
+                    *reinterpret_cast<float4 *>(at + (w8 * kHalves + (kBoth ? lane >> 4 : 0)) * kOwn + 4 * own) =
+                        make_float4(o.sum[w][0], o.sum[w][1], o.sum[w][2], o.sum[w][3]);
+                    epilogue_barrier();
+                    const int i = (int)threadIdx.x - 64, out = (t.n * 2 + (int)rank) * kOwn + i;
+                    if (i < kOwn && out < q.N && p.part[w]) {
+                        float s = 0.f;
+                        for (int k = 0; k < kEpiWarps * kHalves; ++k) s += at[k * kOwn + i];
+                        p.part[w][(size_t)(t.row0 / q.tile_m) * q.N + out] = s;
+                    }
+                    buffer ^= 1;
+                }
+            }
             ++it;
         }
     }
@@ -378,21 +344,35 @@ int MmMapList::add(const MmOperand &o, int box_rows) {
     return count++;
 }
 
+namespace {
+
+// Rows of a tile: 256, or the rows dealt evenly to as few tiles.
+int even_tile(int M) {
+    const int64_t tiles = ((int64_t)M + kAccCols - 1) / kAccCols;
+    return (int)(((int64_t)M + tiles * 32 - 1) / (tiles * 32) * 32);
+}
+
+}  // namespace
+
 cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStream_t s, int64_t *part_rows) {
-    const int tile_n = mm_both(epi) ? kAccCols / 2 : kAccCols;
+    const int tile_n = mm_both(epi) ? kOutputs : 2 * kOutputs;
     int64_t tiles = 0;
     MmMapList list;
     for (int i = 0; i < p.problems; ++i) {
         MmProblem &q = p.prob[i];
-        q.mt = (int)(((int64_t)q.M + 2 * kRows - 1) / (2 * kRows));
+        q.tile_m = even_tile(q.M);
+        // a CTA's half of a tile in as few boxes as it is made of
+        q.box_rows = q.tile_m % 128 == 0 ? 64 : q.tile_m % 64 == 0 ? 32 : 16;
+        q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
         q.nt = (q.N + tile_n - 1) / tile_n;
         tiles += (int64_t)q.mt * q.nt;
-        for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], 64);
+        for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.a_mn ? 64 : q.box_rows);
         for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j) q.b[j] = list.add(q.from_b[j], 64);
     }
     if (!list.ok) return cudaErrorInvalidValue;
+    p.maps = list.count;
     if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
-    if (part_rows) *part_rows = ((int64_t)p.prob[0].M + 31) / 32;
+    if (part_rows) *part_rows = p.prob[0].mt;
     const void *fn = epi == kMmStore   ? (const void *)mm_pair_kernel<kMmStore>
                      : epi == kMmGated ? (const void *)mm_pair_kernel<kMmGated>
                      : epi == kMmSlope ? (const void *)mm_pair_kernel<kMmSlope>

@@ -70,7 +70,10 @@ struct MmArgs {
     __nv_bfloat16 *out2;                    // kMmGatedSlope
     float *part[2];                         // [some rows][N] sums over rows; null: none
     int64_t residual_stride, dy_stride, pre_stride[2], out2_stride;
-    int cluster, stages, stage_bytes, ring_bytes; // few-rows kernel: CTAs of a cluster, the ring
+    int maps;                               // tensor maps in use
+    int cluster;                            // few-rows kernel: CTAs of a cluster, the ring,
+    int stages, stage_bytes, ring_bytes;
+    int chunk;                              //   rows of its sums in shared memory at a time
     int *status;
     uint64_t wait_ns;
 };
@@ -168,40 +171,112 @@ __device__ __forceinline__ void mm_load(const __nv_bfloat16 *p, float (&x)[C], i
     }
 }
 
-// Adds bias[0 .. n) (n <= C counts the row's columns that are left).
-template <int C>
-__device__ __forceinline__ void mm_add_bias(const float *bias, float (&x)[C], int n) {
-    if (!bias) return;
-    if (n >= C && ((uintptr_t)bias & 15) == 0) {
+// ---- finishing -------------------------------------------------------------------
+// The sums D^T of a tile go through shared memory, [row][output], and are finished row by
+// row, four outputs to a lane: a warp reads and writes 256 (or 128) contiguous bytes.
+
+struct MmOutputs {
+    int i, left;        // the lane's first output; how many there are from it on
+    float b[2][4];      // biases
+    float sum[2][4];    // of the slopes, over the rows that the lane has finished
+};
+
+template <bool BOTH>
+__device__ __forceinline__ void mm_outputs(const MmArgs &p, const MmProblem &q, MmOutputs &o, int i) {
+    o.i = i;
+    o.left = q.N - i;
 #pragma unroll
-        for (int j = 0; j < C / 4; ++j) {
-            const float4 v = __ldg(reinterpret_cast<const float4 *>(bias) + j);
-            x[4 * j] += v.x;
-            x[4 * j + 1] += v.y;
-            x[4 * j + 2] += v.z;
-            x[4 * j + 3] += v.w;
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            o.b[w][j] = (w == 0 || BOTH) && p.bias[w] && j < o.left ? __ldg(p.bias[w] + i + j) : 0.f;
+            o.sum[w][j] = 0.f;
         }
+}
+
+__device__ __forceinline__ void mm_load4(const __nv_bfloat16 *p, float (&x)[4], int left) {
+    if (left >= 4) {
+        const uint2 v = *reinterpret_cast<const uint2 *>(p);
+        x[0] = bf16_lo(v.x), x[1] = bf16_hi(v.x), x[2] = bf16_lo(v.y), x[3] = bf16_hi(v.y);
     } else {
 #pragma unroll
-        for (int j = 0; j < C; ++j)
-            if (j < n) x[j] += __ldg(bias + j);
+        for (int j = 0; j < 4; ++j) x[j] = j < left ? __bfloat162float(p[j]) : 0.f;
     }
 }
 
-// Sum over the warp's lanes of x[lane] (a halving exchange: 31 shuffles, a fixed
-// order); x is used up.
-__device__ __forceinline__ float mm_column_sum(float (&x)[32]) {
-    const int lane = threadIdx.x & 31;
+__device__ __forceinline__ void mm_store4(__nv_bfloat16 *p, const float (&x)[4], int left) {
+    if (left >= 4) {
+        *reinterpret_cast<uint2 *>(p) = make_uint2(mm_pack(x[0], x[1]), mm_pack(x[2], x[3]));
+    } else {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const bool up = lane & o;
-#pragma unroll
-        for (int j = 0; j < o; ++j) {
-            const float send = up ? x[j] : x[j + o], keep = up ? x[j + o] : x[j];
-            x[j] = keep + __shfl_xor_sync(0xffffffffu, send, o);
-        }
+        for (int j = 0; j < 4; ++j)
+            if (j < left) p[j] = __float2bfloat16_rn(x[j]);
     }
-    return x[0];
+}
+
+// The residual, or dy, of U rows `step` apart from `row` on, of which those below `end` are there.
+template <int EPI, int U>
+__device__ __forceinline__ void mm_fetch(const MmArgs &p, const MmOutputs &o, float (&other)[U][4], int64_t row, int step,
+                                         int64_t end) {
+    const __nv_bfloat16 *from = EPI == kMmStore ? p.residual : p.dy;
+    const int64_t stride = EPI == kMmStore ? p.residual_stride : p.dy_stride;
+    if (EPI == kMmGated || !from) return;
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+        if (row + k * step < end) mm_load4(from + (row + k * step) * stride + o.i, other[k], o.left);
+}
+
+// Finishes and stores them: v holds the sums (g in a gated product, u its other ones).
+template <int EPI, int ACT, int U>
+__device__ __forceinline__ void mm_finish(const MmArgs &p, const MmProblem &q, MmOutputs &o, float (&v)[U][4],
+                                          float (&u)[U][4], const float (&other)[U][4], int64_t row, int step,
+                                          int64_t end) {
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const int64_t r = row + k * step;
+        if (r >= end) break;
+        float y[4], z[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float x = v[k][j] + o.b[0][j];
+            if constexpr (EPI == kMmStore) {
+                v[k][j] = x;
+                y[j] = mm_act1<ACT>(x);
+                if (p.residual) y[j] += other[k][j];
+            } else if constexpr (EPI == kMmGated) {
+                v[k][j] = x;
+                u[k][j] += o.b[1][j];
+                y[j] = mm_act1<ACT>(x) * u[k][j];
+            } else {
+                float value, slope;
+                mm_slope1<ACT>(x, value, slope);
+                if constexpr (EPI == kMmSlope) {
+                    y[j] = other[k][j] * slope;
+                } else {
+                    y[j] = other[k][j] * (u[k][j] + o.b[1][j]) * slope;
+                    z[j] = other[k][j] * value;
+                    o.sum[1][j] += z[j];
+                }
+                o.sum[0][j] += y[j];
+            }
+        }
+        if constexpr (EPI == kMmStore || EPI == kMmGated)
+            if (p.pre[0]) mm_store4(p.pre[0] + r * p.pre_stride[0] + o.i, v[k], o.left);
+        if constexpr (EPI == kMmGated)
+            if (p.pre[0]) mm_store4(p.pre[1] + r * p.pre_stride[1] + o.i, u[k], o.left);
+        mm_store4(q.out + r * q.out_stride + o.i, y, o.left);
+        if constexpr (EPI == kMmGatedSlope) mm_store4(p.out2 + r * p.out2_stride + o.i, z, o.left);
+    }
+}
+
+// 16 columns of tensor memory (of the warp's 32 lanes).
+__device__ __forceinline__ void mm_read16(uint32_t tcol, float (&x)[16]) {
+    uint32_t v[16];
+    ptx::tmem_ld_32x32b_x16(tcol, v);
+    ptx::tmem_ld_wait();
+    ptx::reg_fence16(v);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(v[j]);
 }
 
 // ---- launches (arguments checked) ------------------------------------------------
