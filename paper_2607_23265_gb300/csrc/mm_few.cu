@@ -9,9 +9,9 @@
 // finishing its share of the rows.  No workspace, no second kernel, equal bits each time.
 //
 // A stage is 64 along K: 128 outputs' weights (16 KB; a gated product both projections',
-// whose sums lie beside one another in tensor memory) and the tile's rows, in boxes of
-// 64 x 64 (or fewer rows) with 128-byte swizzle, K-major or MN-major.  What lies outside
-// an operand arrives as zeros.
+// whose sums lie beside one another in tensor memory) and the tile's rows, each K-major,
+// one box of 64 k of its rows, or MN-major, a box of 64 rows of its 64 k each, with
+// 128-byte swizzle.  What lies outside an operand arrives as zeros.
 // Warps: 0 copies, 1 products, then all eight the epilogue.
 //
 // Tensor memory is taken by every CTA and held while it waits for its cluster.  So no two
@@ -118,75 +118,90 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     ptx::tc_fence_after();
     const uint32_t tmem = S->tmem_base;
 
-    if (active && warp == 0 && ptx::elect_one()) {
-        // ---------------- copies ----------------
-        const uint64_t once = ptx::policy_evict_first(), again = ptx::policy_evict_last();
-        const uint64_t weights = q.mt > 1 ? again : once;   // row tiles share them in L2
-        const int box_bytes = q.a_mn ? kBoxBytes : q.box_rows * kStepK * 2;
-        const uint32_t bytes = (uint32_t)(kSums * kWeightBytes + q.boxes * box_bytes);
-        int stage = 0;
-        uint32_t phase = 0;
-        for (int step = step0; step < step1; ++step) {
-            if (!ptx::mbar_wait(&S->empty[stage], phase ^ 1u, p.wait_ns)) {
-                give_up(p, abort_flag);
-                break;
-            }
-            if (*abort_flag) break;
-            const int seg = step / q.steps, k = (step - seg * q.steps) * kStepK;
-            uint8_t *st = ring + (size_t)stage * p.stage_bytes;
-            uint64_t *full = &S->full[stage];
-            ptx::mbar_arrive_expect_tx(full, bytes);
-#pragma unroll
-            for (int w = 0; w < kSums; ++w) {
-                const CUtensorMap *m = &maps.m[q.b[kBoth ? w : seg]];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    ptx::tma_load_2d(st + (2 * w + h) * kBoxBytes, m, full, q.b_mn ? out0 + 64 * h : k,
-                                     q.b_mn ? k : out0 + 64 * h, weights);
-            }
-            st += kSums * kWeightBytes;
-            const CUtensorMap *m = &maps.m[q.a[seg]];
-            for (int h = 0; h < q.boxes; ++h) {
-                const int r = row0 + h * (q.a_mn ? 64 : q.box_rows);
-                ptx::tma_load_2d(st + h * box_bytes, m, full, q.a_mn ? r : k, q.a_mn ? k : r, again);
-            }
-            if (++stage == p.stages) {
-                stage = 0;
-                phase ^= 1u;
-            }
-        }
-    } else if (active && warp == 1 && ptx::elect_one()) {
-        // ---------------- products ----------------
-        // K-major: rows of 128 bytes, 8 to a kilobyte; 16 k are 32 bytes.
-        // MN-major: a kilobyte is 8 k of 64 rows, 64 rows on is the next box; 16 k are 2 KB.
-        const uint32_t ring32 = ptx::smem_u32(ring);
-        const uint32_t idesc = ptx::idesc_bf16(kOutputs, q.tile_m, q.b_mn, q.a_mn);
-        const uint64_t w_base = ptx::smem_desc(ring32, q.b_mn ? kBoxBytes : 16, 1024, 2);
-        const uint64_t x_base = ptx::smem_desc(ring32 + kSums * kWeightBytes, q.a_mn ? kBoxBytes : 16, 1024, 2);
-        const uint64_t w_step = q.b_mn ? 128 : 2, x_step = q.a_mn ? 128 : 2;
-        int stage = 0;
-        uint32_t phase = 0;
-        for (int step = step0; step < step1; ++step) {
-            if (!ptx::mbar_wait(&S->full[stage], phase, p.wait_ns)) {
-                give_up(p, abort_flag);
-                break;
-            }
-            if (*abort_flag) break;
-            ptx::tc_fence_after();
-            const uint64_t so = (uint64_t)stage * (uint64_t)(p.stage_bytes >> 4);
-#pragma unroll
-            for (int w = 0; w < kSums; ++w)
-#pragma unroll
-                for (int k = 0; k < kStepK / 16; ++k)
-                    ptx::mma_bf16(tmem + (uint32_t)(w * q.tile_m), w_base + so + (uint64_t)(w * (kWeightBytes >> 4)) + k * w_step,
-                                  x_base + so + k * x_step, idesc, (step > step0 || k) ? 1u : 0u);
-            ptx::mma_commit(&S->empty[stage]);
-            if (++stage == p.stages) {
-                stage = 0;
-                phase ^= 1u;
+    if (active && warp == 0) {
+        if (ptx::elect_one()) {
+            // ---------------- copies ----------------
+            // (a step's issue has to be short: a division for its segment and a look at the abort
+            // word made it 390 cycles, more than its products take)
+            const uint64_t once = ptx::policy_evict_first(), again = ptx::policy_evict_last();
+            const uint64_t weights = q.mt > 1 ? again : once;   // row tiles share them in L2
+            // an operand K-major is one box, MN-major one for each 64 rows
+            const bool a_mn = q.a_mn, b_mn = q.b_mn;
+            const int boxes = a_mn ? (q.tile_m + 63) / 64 : 1, steps = q.steps, stages = p.stages;
+            const uint32_t bytes = (uint32_t)(kSums * kWeightBytes + (a_mn ? boxes * kBoxBytes : q.tile_m * kStepK * 2));
+            int seg = step0 / steps, k = (step0 - seg * steps) * kStepK, stage = 0;
+            const CUtensorMap *a = &maps.m[q.a[seg]], *b = &maps.m[q.b[seg]], *b2 = &maps.m[q.b[1]];
+            uint32_t phase = 1;
+            for (int left = step1 - step0; left > 0; --left) {
+                if (!ptx::mbar_wait(&S->empty[stage], phase, p.wait_ns)) {
+                    give_up(p, abort_flag);
+                    break;
+                }
+                uint8_t *st = ring + stage * p.stage_bytes;
+                uint64_t *full = &S->full[stage];
+                ptx::mbar_arrive_expect_tx(full, bytes);
+                if (b_mn) {
+                    ptx::tma_load_2d(st, b, full, out0, k, weights);
+                    ptx::tma_load_2d(st + kBoxBytes, b, full, out0 + 64, k, weights);
+                } else {
+                    ptx::tma_load_2d(st, b, full, k, out0, weights);
+                }
+                if constexpr (kBoth) ptx::tma_load_2d(st + kWeightBytes, b2, full, k, out0, weights);
+                st += kSums * kWeightBytes;
+                if (a_mn)
+                    for (int h = 0; h < boxes; ++h)
+                        ptx::tma_load_2d(st + h * kBoxBytes, a, full, row0 + 64 * h, k, again);
+                else
+                    ptx::tma_load_2d(st, a, full, k, row0, again);
+                k += kStepK;
+                if (k == steps * kStepK && seg + 1 < q.segments) {
+                    k = 0;
+                    ++seg;
+                    a = &maps.m[q.a[seg]];
+                    b = &maps.m[q.b[seg]];
+                }
+                if (++stage == stages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
             }
         }
-        ptx::mma_commit(&S->done);
+    } else if (active && warp == 1) {
+        if (ptx::elect_one()) {
+            // ---------------- products ----------------
+            // K-major: rows of 128 bytes, 8 to a kilobyte; 16 k are 32 bytes.
+            // MN-major: a kilobyte is 8 k of 64 rows, 64 rows on is the next box; 16 k are 2 KB.
+            const uint32_t ring32 = ptx::smem_u32(ring);
+            const uint32_t idesc = ptx::idesc_bf16(kOutputs, q.tile_m, q.b_mn, q.a_mn);
+            const uint64_t w_base = ptx::smem_desc(ring32, q.b_mn ? kBoxBytes : 16, 1024, 2);
+            const uint64_t x_base = ptx::smem_desc(ring32 + kSums * kWeightBytes, q.a_mn ? kBoxBytes : 16, 1024, 2);
+            const uint64_t w_step = q.b_mn ? 128 : 2, x_step = q.a_mn ? 128 : 2;
+            const int stages = p.stages, second = q.tile_m;
+            int stage = 0;
+            uint32_t phase = 0, more = 0;
+            for (int left = step1 - step0; left > 0; --left) {
+                if (!ptx::mbar_wait(&S->full[stage], phase, p.wait_ns)) {
+                    give_up(p, abort_flag);
+                    break;
+                }
+                ptx::tc_fence_after();
+                const uint64_t so = (uint64_t)(stage * (p.stage_bytes >> 4));
+#pragma unroll
+                for (int w = 0; w < kSums; ++w)
+#pragma unroll
+                    for (int k = 0; k < kStepK / 16; ++k)
+                        ptx::mma_bf16(tmem + (uint32_t)(w * second),
+                                      w_base + so + (uint64_t)(w * (kWeightBytes >> 4)) + k * w_step,
+                                      x_base + so + k * x_step, idesc, k ? 1u : more);
+                more = 1;
+                ptx::mma_commit(&S->empty[stage]);
+                if (++stage == stages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+            }
+            ptx::mma_commit(&S->done);
+        }
     }
     __syncwarp();
     // ---------------- epilogue ----------------
@@ -307,7 +322,7 @@ int round_up(int x, int to) { return (x + to - 1) / to * to; }
 
 // A row tile's bytes of a stage.
 int row_bytes(const MmProblem &q, int tile_m) {
-    return q.a_mn || tile_m > 64 ? round_up(tile_m, 64) * kStepK * 2 : tile_m * kStepK * 2;
+    return (q.a_mn ? round_up(tile_m, 64) : tile_m) * kStepK * 2;
 }
 
 // Whether a product can take tiles of tile_m rows and `split` CTAs a tile: the sums fit
@@ -370,8 +385,6 @@ cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool
         MmProblem &q = p.prob[i];
         q.tile_m = plan.tile_m[i];
         q.split = plan.split[i];
-        q.box_rows = std::min(q.tile_m, 64);
-        q.boxes = (q.tile_m + 63) / 64;
         q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
         q.nt = (q.N + kOutputs - 1) / kOutputs;
         if ((int64_t)q.mt * q.nt > INT32_MAX / kMaxCluster) return cudaErrorInvalidValue;
@@ -381,8 +394,8 @@ cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool
         columns = std::max(columns, sums * q.tile_m);
         if (q.split > 1) dump = std::max(dump, sums * q.tile_m * kOutputs * 4);
         most_steps = std::max(most_steps, (q.segments * q.steps + q.split - 1) / q.split);
-        for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.a_mn ? 64 : q.box_rows);
-        for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j) q.b[j] = list.add(q.from_b[j], 64);
+        for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.a_mn ? 64 : q.tile_m);
+        for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j) q.b[j] = list.add(q.from_b[j], q.b_mn ? 64 : kOutputs);
     }
     if (!list.ok || clusters * plan.cluster > INT32_MAX) return cudaErrorInvalidValue;
     p.stage_bytes = round_up(p.stage_bytes, 1024);

@@ -6,9 +6,10 @@
 // each, in six stages of 64 along K (32 KB a CTA), and the sums of its 128 outputs (256
 // columns of tensor memory, twice, so that a tile's epilogue overlaps the next one's main
 // loop).  With the rows in the columns a tile's row count is a multiple of 32 and not of
-// 256: 333 rows are tiles of 192 and 160.  An operand tile is boxes of 64 x 64 (or
-// fewer rows) with 128-byte swizzle, K-major or MN-major; what lies outside an operand
-// arrives as zeros, so any size works.  In a gated product a CTA's 128 lanes are the
+// 256: 333 rows are tiles of 192 and 160.  An operand tile is K-major, one box of
+// 64 k of its rows, or MN-major, a box of 64 rows of its 64 k each, both with 128-byte
+// swizzle; what lies outside an operand arrives as zeros, so any size works.  (A thread
+// issues a copy every 55 cycles: with boxes of 64 x 64 and 32 x 64 a step of 192 rows took 0.32 us.)  In a gated product a CTA's 128 lanes are the
 // gate's weights of 64 outputs and the up projection's of the same 64.
 //   Persistent pairs walk the tiles of up to three products.
 // Warps: 0 copies, 1 products (the even CTA's), 2-9 epilogue: 32 rows' sums at a time go
@@ -144,93 +145,103 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
     Walk walk(p, (int)blockIdx.x >> 1, (int)gridDim.x >> 1);
     Tile t;
 
-    if (warp == 0 && ptx::elect_one()) {
-        // ---------------- copies: this CTA's halves ----------------
-        const uint64_t policy = ptx::policy_evict_last();
-        int stage = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        while (ok && !*abort_flag && walk.next(t)) {
-            const MmProblem &q = p.prob[t.prob];
-            const int i0 = (t.n * 2 + (int)rank) * kOwn, r0 = t.row0 + (int)rank * (t.rows / 2);
-            const int box_rows = q.a_mn ? 64 : q.box_rows, boxes = (t.rows / 2 + box_rows - 1) / box_rows;
-            const int box_bytes = box_rows * kStepK * 2;
-            const uint32_t bytes = 2u * (uint32_t)(kOperandBytes + boxes * box_bytes);
-            for (int seg = 0; ok && seg < q.segments; ++seg) {
-                const CUtensorMap *a = &maps.m[q.a[seg]];
-                for (int ks = 0; ks < q.steps; ++ks) {
-                    const int k = ks * kStepK;
-                    if (!ptx::mbar_wait(&S->empty[stage], phase ^ 1u, p.wait_ns)) {
+    if (warp == 0) {
+        if (ptx::elect_one()) {
+            // ---------------- copies: this CTA's halves ----------------
+            const uint64_t policy = ptx::policy_evict_last();
+            const uint32_t full0 = ptx::map_cluster(&S->full[0], 0);   // the even CTA's barriers count both's
+            int stage = 0;
+            uint32_t phase = 1;
+            bool ok = true;
+            while (ok && walk.next(t)) {
+                const MmProblem &q = p.prob[t.prob];
+                const bool a_mn = q.a_mn, b_mn = q.b_mn;
+                const int i0 = (t.n * 2 + (int)rank) * kOwn, r0 = t.row0 + (int)rank * (t.rows / 2);
+                // an operand K-major is one box (a gated product's weights two), MN-major one for each 64 rows
+                const int boxes = a_mn ? (t.rows / 2 + 63) / 64 : 1, ends = q.steps * kStepK;
+                const uint32_t bytes = 2u * (uint32_t)(kOperandBytes + (a_mn ? boxes * kBoxBytes : q.box_rows * kStepK * 2));
+                for (int seg = 0; ok && seg < q.segments; ++seg) {
+                    const CUtensorMap *a = &maps.m[q.a[seg]], *b = &maps.m[q.b[kBoth ? 0 : seg]];
+                    const CUtensorMap *b2 = &maps.m[q.b[1]];
+                    for (int k = 0; k < ends; k += kStepK) {
+                        if (!ptx::mbar_wait(&S->empty[stage], phase, p.wait_ns)) {
+                            give_up(p, abort_flag);
+                            ok = false;
+                            break;
+                        }
+                        uint8_t *st = ring + stage * kStageBytes;
+                        const uint32_t full = full0 + (uint32_t)stage * 8;
+                        if (rank == 0) ptx::mbar_arrive_expect_tx(&S->full[stage], bytes);
+                        if constexpr (kBoth) {
+                            ptx::tma_load_2d_pair(st, b, full, k, i0, policy);
+                            ptx::tma_load_2d_pair(st + kBoxBytes, b2, full, k, i0, policy);
+                        } else if (b_mn) {
+                            ptx::tma_load_2d_pair(st, b, full, i0, k, policy);
+                            ptx::tma_load_2d_pair(st + kBoxBytes, b, full, i0 + 64, k, policy);
+                        } else {
+                            ptx::tma_load_2d_pair(st, b, full, k, i0, policy);
+                        }
+                        st += kOperandBytes;
+                        if (a_mn)
+                            for (int h = 0; h < boxes; ++h)
+                                ptx::tma_load_2d_pair(st + h * kBoxBytes, a, full, r0 + 64 * h, k, policy);
+                        else
+                            ptx::tma_load_2d_pair(st, a, full, k, r0, policy);
+                        if (++stage == kStages) {
+                            stage = 0;
+                            phase ^= 1u;
+                        }
+                    }
+                }
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
+        if (ptx::elect_one()) {
+            // ---------------- products of the pair ----------------
+            const uint32_t ring32 = ptx::smem_u32(ring);
+            int stage = 0, it = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            while (ok && walk.next(t)) {
+                const MmProblem &q = p.prob[t.prob];
+                // K-major: rows of 128 bytes, 8 to a kilobyte; 16 k are 32 bytes.
+                // MN-major: a kilobyte is 8 k of 64 rows, 64 rows on is the next box; 16 k are 2 KB.
+                const uint32_t idesc = ptx::idesc_bf16(2 * kOutputs, t.rows, q.b_mn, q.a_mn);
+                const uint64_t w_base = ptx::smem_desc(ring32, q.b_mn ? kBoxBytes : 16, 1024, 2);
+                const uint64_t x_base = ptx::smem_desc(ring32 + kOperandBytes, q.a_mn ? kBoxBytes : 16, 1024, 2);
+                const uint64_t w_step = q.b_mn ? 128 : 2, x_step = q.a_mn ? 128 : 2;
+                const int b = it & 1;
+                if (!ptx::mbar_wait(&S->tempty[b], ((uint32_t)(it >> 1) & 1u) ^ 1u, p.wait_ns)) {
+                    give_up(p, abort_flag);
+                    break;
+                }
+                ptx::tc_fence_after();
+                const uint32_t d = tmem + (uint32_t)(b * kAccCols);
+                uint32_t more = 0;
+                for (int left = q.segments * q.steps; left > 0; --left) {
+                    if (!ptx::mbar_wait(&S->full[stage], phase, p.wait_ns)) {
                         give_up(p, abort_flag);
                         ok = false;
                         break;
                     }
-                    uint8_t *st = ring + (size_t)stage * kStageBytes;
-                    const uint32_t full = ptx::map_cluster(&S->full[stage], 0);
-                    if (rank == 0) ptx::mbar_arrive_expect_tx(&S->full[stage], bytes);
+                    ptx::tc_fence_after();
+                    const uint64_t so = (uint64_t)(stage * (kStageBytes >> 4));
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        // 64 outputs' weights; in a gated product the gate's, then the up projection's
-                        const CUtensorMap *b = &maps.m[q.b[kBoth ? h : seg]];
-                        const int i = kBoth ? i0 : i0 + 64 * h;
-                        ptx::tma_load_2d_pair(st + h * kBoxBytes, b, full, q.b_mn ? i : k, q.b_mn ? k : i, policy);
-                    }
-                    for (int h = 0; h < boxes; ++h) {
-                        const int r = r0 + h * box_rows;
-                        ptx::tma_load_2d_pair(st + kOperandBytes + h * box_bytes, a, full, q.a_mn ? r : k,
-                                              q.a_mn ? k : r, policy);
-                    }
+                    for (int k = 0; k < kStepK / 16; ++k)
+                        ptx::mma_bf16_pair(d, w_base + so + k * w_step, x_base + so + k * x_step, idesc, k ? 1u : more);
+                    more = 1;
+                    ptx::mma_commit_pair(&S->empty[stage]);
                     if (++stage == kStages) {
                         stage = 0;
                         phase ^= 1u;
                     }
                 }
+                if (ok) ptx::mma_commit_pair(&S->tfull[b]);
+                ++it;
             }
+            ptx::mma_commit_pair(&S->drain);
+            ptx::mbar_wait(&S->drain, 0, kMmTimeoutNs);
         }
-    } else if (warp == 1 && rank == 0 && ptx::elect_one()) {
-        // ---------------- products of the pair ----------------
-        const uint32_t ring32 = ptx::smem_u32(ring);
-        int stage = 0, it = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        while (ok && !*abort_flag && walk.next(t)) {
-            const MmProblem &q = p.prob[t.prob];
-            // K-major: rows of 128 bytes, 8 to a kilobyte; 16 k are 32 bytes.
-            // MN-major: a kilobyte is 8 k of 64 rows, 64 rows on is the next box; 16 k are 2 KB.
-            const uint32_t idesc = ptx::idesc_bf16(2 * kOutputs, t.rows, q.b_mn, q.a_mn);
-            const uint64_t w_base = ptx::smem_desc(ring32, q.b_mn ? kBoxBytes : 16, 1024, 2);
-            const uint64_t x_base = ptx::smem_desc(ring32 + kOperandBytes, q.a_mn ? kBoxBytes : 16, 1024, 2);
-            const uint64_t w_step = q.b_mn ? 128 : 2, x_step = q.a_mn ? 128 : 2;
-            const int b = it & 1;
-            if (!ptx::mbar_wait(&S->tempty[b], ((uint32_t)(it >> 1) & 1u) ^ 1u, p.wait_ns)) {
-                give_up(p, abort_flag);
-                break;
-            }
-            ptx::tc_fence_after();
-            const uint32_t d = tmem + (uint32_t)(b * kAccCols);
-            const int steps = q.segments * q.steps;
-            for (int ks = 0; ks < steps; ++ks) {
-                if (!ptx::mbar_wait(&S->full[stage], phase, p.wait_ns)) {
-                    give_up(p, abort_flag);
-                    ok = false;
-                    break;
-                }
-                ptx::tc_fence_after();
-                const uint64_t so = (uint64_t)stage * (uint64_t)(kStageBytes >> 4);
-#pragma unroll
-                for (int k = 0; k < kStepK / 16; ++k)
-                    ptx::mma_bf16_pair(d, w_base + so + k * w_step, x_base + so + k * x_step, idesc, (ks | k) ? 1u : 0u);
-                ptx::mma_commit_pair(&S->empty[stage]);
-                if (++stage == kStages) {
-                    stage = 0;
-                    phase ^= 1u;
-                }
-            }
-            if (ok) ptx::mma_commit_pair(&S->tfull[b]);
-            ++it;
-        }
-        ptx::mma_commit_pair(&S->drain);
-        ptx::mbar_wait(&S->drain, 0, kMmTimeoutNs);
     } else if (warp == 1 && rank == 1 && ptx::elect_one()) {
         ptx::mbar_wait(&S->drain, 0, 2 * kMmTimeoutNs);   // the even CTA's last arrivals here
     } else if (warp >= 2) {
@@ -361,13 +372,12 @@ cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStr
     for (int i = 0; i < p.problems; ++i) {
         MmProblem &q = p.prob[i];
         q.tile_m = even_tile(q.M);
-        // a CTA's half of a tile in as few boxes as it is made of
-        q.box_rows = q.tile_m % 128 == 0 ? 64 : q.tile_m % 64 == 0 ? 32 : 16;
+        q.box_rows = q.tile_m / 2;   // a CTA's
         q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
         q.nt = (q.N + tile_n - 1) / tile_n;
         tiles += (int64_t)q.mt * q.nt;
         for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.a_mn ? 64 : q.box_rows);
-        for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j) q.b[j] = list.add(q.from_b[j], 64);
+        for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j) q.b[j] = list.add(q.from_b[j], q.b_mn || mm_both(epi) ? 64 : kOutputs);
     }
     if (!list.ok) return cudaErrorInvalidValue;
     p.maps = list.count;

@@ -20,7 +20,7 @@ constexpr int kMmProblems = 3;
 constexpr uint64_t kMmTimeoutNs = 2000000000ull;
 
 struct MmMaps {
-    CUtensorMap m[kMmMaps];   // 2D, boxes of 64 x 64 (or fewer rows) with 128-byte swizzle
+    CUtensorMap m[kMmMaps];   // 2D, boxes 64 wide with 128-byte swizzle
 };
 
 // What is done with the sums.
@@ -52,10 +52,10 @@ struct MmProblem {
     MmOperand from_a[2], from_b[2];   // host: the operands
     // set by the launch
     int a[2], b[2];        // their tensor maps
-    int mt, nt;            // tiles
-    int tile_m;            // few-rows kernel: rows of a tile, boxes of a row tile and rows of a box,
-    int boxes, box_rows;
-    int split;             //   CTAs that share a tile's K
+    int mt, nt;            // tiles along M and N
+    int tile_m;            // rows of a tile
+    int box_rows;          // pairs: a CTA's
+    int split;             // few-rows kernel: CTAs that share a tile's K,
     int first;             //   first cluster
 };
 
