@@ -244,9 +244,11 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
                 // this CTA's share of the rows
                 const int share = shared_k ? (rows + q.split - 1) / q.split : c1 - c0;
                 const int lo = shared_k ? part * share : c0, hi = lo + share < c1 ? lo + share : c1;
+                MmAt<EPI> rows_at(p, q, (int64_t)row0 + lo + warp, o.i);
                 for (int c = lo + warp; c < hi; c += U * kWarps) {
+                    const int count = (hi - c + kWarps - 1) / kWarps;
                     float v[U][4] = {}, u[U][4] = {}, other[U][4];
-                    mm_fetch<EPI, U>(p, o, other, (int64_t)row0 + c, kWarps, (int64_t)row0 + hi);
+                    mm_fetch<EPI, U, false>(rows_at, o.left, other, kWarps, count);
                     const float *at = sums + (size_t)(c - c0) * kOutputs + 4 * lane;
                     if (!shared_k) {
 #pragma unroll
@@ -281,7 +283,8 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
                                 }
                         }
                     }
-                    mm_finish<EPI, ACT, U>(p, q, o, v, u, other, (int64_t)row0 + c, kWarps, (int64_t)row0 + hi);
+                    mm_finish<EPI, ACT, U, false>(rows_at, o, v, u, other, kWarps, count);
+                    rows_at.advance(U * kWarps);
                 }
             });
         if (c1 < rows) __syncthreads();

@@ -12,8 +12,11 @@
 // issues a copy every 55 cycles: with boxes of 64 x 64 and 32 x 64 a step of 192 rows took 0.32 us.)  In a gated product a CTA's 128 lanes are the
 // gate's weights of 64 outputs and the up projection's of the same 64.
 //   Persistent pairs walk the tiles of up to three products.
-// Warps: 0 copies, 1 products (the even CTA's), 2-9 epilogue: 32 rows' sums at a time go
-// through one of two buffers in shared memory and are finished row by row.
+// Warps: 0 copies, 1 products (the even CTA's), 2-17 epilogue, four a TMEM lane quadrant.  A
+// lane of the epilogue has an output and takes 16 of its rows at a time: a warp reads and
+// writes 64 contiguous bytes of a row, and waits for no other one (in a gated product the
+// two that have the gate's and the up projection's sums of the same outputs exchange
+// halves of 32 rows, and each finishes one).
 #include <cstring>
 #include <type_traits>
 
@@ -28,11 +31,11 @@ constexpr int kOperandBytes = kOutputs * kStepK * 2;     // 16 KB
 constexpr int kBoxBytes = kOperandBytes / 2;             // 64 x 64
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kStages = 6;
-constexpr int kEpiWarps = 8;
+constexpr int kEpiWarps = 16;
 constexpr int kThreads = (2 + kEpiWarps) * 32;
 constexpr int kAccCols = 256;                            // the most rows of a tile
-constexpr int kChunk = 32;                               // rows of sums in shared memory at a time
-constexpr int kChunkFloats = kChunk * kOutputs;
+constexpr int kUnitRows = 16;                            // rows that an epilogue warp takes at a time
+constexpr int kGiveFloats = kUnitRows * 32;              // sums that a warp of a gated product gives away
 constexpr int kGroupRows = 8;                            // row tiles that are walked together
 
 struct Shared {
@@ -45,7 +48,7 @@ struct Shared {
     int abort;
 };
 
-constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + 2 * kChunkFloats * 4 + sizeof(Shared);
+constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kEpiWarps * kGiveFloats * 4 + sizeof(Shared);
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of the pair CTA");
 
 struct Tile {
@@ -87,19 +90,41 @@ __device__ __forceinline__ void give_up(const MmArgs &p, volatile int *abort_fla
     if (p.status) atomicOr(p.status, WZ_STATUS_WAIT_TIMEOUT);
 }
 
-// Barriers of the epilogue warps; the second says, to all alike, whether all came with `ok`.
-__device__ __forceinline__ void epilogue_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-__device__ __forceinline__ bool epilogue_all(bool ok) {
+// Barriers of two warps; the second says, to both alike, whether both came with `ok`.
+__device__ __forceinline__ void pair_barrier(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool pair_all(int id, bool ok) {
     uint32_t r;
     asm volatile(
         "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.u32 p, %1, 0;\n\t"
-        "bar.red.and.pred q, 1, 256, p;\n\t"
+        "setp.ne.u32 p, %2, 0;\n\t"
+        "bar.red.and.pred q, %1, 64, p;\n\t"
         "selp.u32 %0, 1, 0, q;\n\t}"
         : "=r"(r)
-        : "r"(ok ? 1u : 0u)
+        : "r"(id), "r"(ok ? 1u : 0u)
         : "memory");
     return r != 0;
+}
+
+// 16 values, `stride` apart, of which the first `count` are there; zeros for the others.
+__device__ __forceinline__ void fetch(const __nv_bfloat16 *p, int64_t stride, int count, float (&x)[kUnitRows]) {
+    if (count >= kUnitRows) {
+#pragma unroll
+        for (int j = 0; j < kUnitRows; ++j) x[j] = __bfloat162float(p[j * stride]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kUnitRows; ++j) x[j] = j < count ? __bfloat162float(p[j * stride]) : 0.f;
+    }
+}
+
+__device__ __forceinline__ void put(__nv_bfloat16 *p, int64_t stride, int count, const float (&x)[kUnitRows]) {
+    if (count >= kUnitRows) {
+#pragma unroll
+        for (int j = 0; j < kUnitRows; ++j) p[j * stride] = __float2bfloat16_rn(x[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kUnitRows; ++j)
+            if (j < count) p[j * stride] = __float2bfloat16_rn(x[j]);
+    }
 }
 
 }  // namespace
@@ -111,8 +136,8 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
     constexpr int kOwn = kBoth ? kOutputs / 2 : kOutputs;   // outputs of a CTA
     extern __shared__ uint8_t smem_raw[];
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    float *sums = reinterpret_cast<float *>(ring + (size_t)kStages * kStageBytes);
-    Shared *S = reinterpret_cast<Shared *>(sums + 2 * kChunkFloats);
+    float *gives = reinterpret_cast<float *>(ring + (size_t)kStages * kStageBytes);
+    Shared *S = reinterpret_cast<Shared *>(gives + kEpiWarps * kGiveFloats);
     volatile int *abort_flag = &S->abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = ptx::cluster_rank();
@@ -246,81 +271,132 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
         ptx::mbar_wait(&S->drain, 0, 2 * kMmTimeoutNs);   // the even CTA's last arrivals here
     } else if (warp >= 2) {
         // ---------------- epilogue of this CTA's outputs ----------------
-        constexpr int U = kBoth ? 2 : 4;          // rows of a lane in a chunk
-        const int quadrant = warp & 3, side = (warp - 2) >> 2, w8 = warp - 2;
-        const int own = kBoth ? lane & 15 : lane;
-        // the lane's rows of a chunk: first, first + every, ..
-        const int first = kBoth ? 4 * w8 + (lane >> 4) : 4 * w8, every = kBoth ? 2 : 1;
+        constexpr int kSides = kEpiWarps / 4;                   // warps of a quadrant
+        constexpr int kStride = kSides * kUnitRows * (kBoth ? 2 : 1);
+        const int quadrant = warp & 3, side = (warp - 2) >> 2;
+        const int kind = kBoth ? quadrant >> 1 : 0;             // 1: the up projection's sums
+        const int barrier = 1 + 2 * side + (quadrant & 1);      // of the two warps with the same outputs
+        float *give = gives + (4 * side + quadrant) * kGiveFloats + lane;
+        const float *take = gives + (4 * side + (quadrant ^ 2)) * kGiveFloats + lane;
         const uint32_t tempty[2] = {ptx::map_cluster(&S->tempty[0], 0), ptx::map_cluster(&S->tempty[1], 0)};
-        int it = 0, buffer = 0;
+        int it = 0;
         while (walk.next(t)) {
             const MmProblem &q = p.prob[t.prob];
             const int b = it & 1;
-            const int64_t end = t.row0 + t.rows < q.M ? t.row0 + t.rows : q.M;
-            MmOutputs o;
-            mm_outputs<kBoth>(p, q, o, (t.n * 2 + (int)rank) * kOwn + 4 * own);
-            const bool mine = o.left > 0;
-            float other[U][4];
-            if (mine) mm_fetch<EPI, U>(p, o, other, (int64_t)t.row0 + first, every, end);
-            // the warps leave together, on one verdict: their barriers count all of them
+            const int rows = q.M - t.row0 < t.rows ? q.M - t.row0 : t.rows;
+            const int i = (t.n * 2 + (int)rank) * kOwn + 32 * (kBoth ? quadrant & 1 : quadrant) + lane;
+            const int there = i < q.N ? rows : 0;               // of the lane's rows
+            const float bias = p.bias[kind] && i < q.N ? __ldg(p.bias[kind] + i) : 0.f;
+            // from this warp's first row on, which it is in a gated product when it has finished the exchange
+            const int first = side * (kStride / kSides), mine = first + kUnitRows * kind;
+            const int64_t row = t.row0 + mine;
+            const int64_t s_from = EPI == kMmStore ? p.residual_stride : p.dy_stride, s_out = q.out_stride;
+            const __nv_bfloat16 *from = EPI == kMmStore ? p.residual : EPI == kMmGated ? nullptr : p.dy;
+            if (from) from += row * s_from + i;
+            __nv_bfloat16 *out = q.out + row * s_out + i, *out2 = p.out2 + row * p.out2_stride + i;
+            __nv_bfloat16 *pre = p.pre[kind] ? p.pre[kind] + (t.row0 + first) * p.pre_stride[kind] + i : nullptr;
+            const int64_t s_pre = p.pre_stride[kind];
+            float other[kUnitRows];                             // the residual, or dy
+            if (from) fetch(from, s_from, there - mine, other);
+            float sum0 = 0.f, sum1 = 0.f;
             const bool full = ptx::mbar_wait(&S->tfull[b], (uint32_t)(it >> 1) & 1u, p.wait_ns);
             if (!full) give_up(p, abort_flag);
-            if (!epilogue_all(full)) break;
+            // (two warps that exchange sums leave on one verdict)
+            if (kBoth ? !pair_all(barrier, full) : !__all_sync(0xffffffffu, full)) break;
             ptx::tc_fence_after();
-            const uint32_t tbase = tmem + ((uint32_t)(quadrant * 32) << 16) + (uint32_t)(b * kAccCols);
+            const uint32_t tcol = tmem + ((uint32_t)(quadrant * 32) << 16) + (uint32_t)(b * kAccCols);
+            const auto read = [&](bool last) {   // the warp's sums of the tile are read
+                if (!last) return;
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive_cluster(b ? tempty[1] : tempty[0]);
+            };
+            read(first >= rows);
             mm_with_act(p.act, [&](auto act) {
                 constexpr int ACT = decltype(act)::value;
-                for (int c0 = 0; t.row0 + c0 < end; c0 += kChunk, buffer ^= 1) {
-                    float *at = sums + buffer * kChunkFloats;
-                    {
-                        float v[16];
-                        mm_read16(tbase + (uint32_t)(c0 + 16 * side), v);
-                        float *to = at + 16 * side * kOutputs + quadrant * 32 + lane;
+                for (int c = first; c < rows; c += kStride) {
+                    if constexpr (!kBoth) {
+                        float x[kUnitRows];
+                        mm_read16(tcol + (uint32_t)c, x);
+                        read(c + kStride >= rows);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) to[j * kOutputs] = v[j];
-                    }
-                    if (t.row0 + c0 + kChunk >= end) {   // the last of the tile's sums are read
-                        ptx::tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) ptx::mbar_arrive_cluster(b ? tempty[1] : tempty[0]);
-                    }
-                    epilogue_barrier();
-                    if (mine) {
-                        float v[U][4], u[U][4];
+                        for (int j = 0; j < kUnitRows; ++j) x[j] += bias;
+                        if (EPI == kMmStore && pre) {
+                            put(pre, s_pre, there - c, x);
+                            pre += kStride * s_pre;
+                        }
 #pragma unroll
-                        for (int k = 0; k < U; ++k) {
-                            const float *row = at + (first + k * every) * kOutputs + 4 * own;
-                            const float4 x = *reinterpret_cast<const float4 *>(row);
-                            v[k][0] = x.x, v[k][1] = x.y, v[k][2] = x.z, v[k][3] = x.w;
-                            if constexpr (kBoth) {
-                                const float4 y = *reinterpret_cast<const float4 *>(row + kOutputs / 2);
-                                u[k][0] = y.x, u[k][1] = y.y, u[k][2] = y.z, u[k][3] = y.w;
+                        for (int j = 0; j < kUnitRows; ++j) {
+                            if constexpr (EPI == kMmStore) {
+                                x[j] = mm_act1<ACT>(x[j]);
+                                if (from) x[j] += other[j];
+                            } else {
+                                float value, slope;
+                                mm_slope1<ACT>(x[j], value, slope);
+                                x[j] = other[j] * slope;
+                                sum0 += x[j];
                             }
                         }
-                        const int64_t r = (int64_t)t.row0 + c0 + first;
-                        mm_finish<EPI, ACT, U>(p, q, o, v, u, other, r, every, end);
-                        mm_fetch<EPI, U>(p, o, other, r + kChunk, every, end);
+                        if (from) {   // the next rows'
+                            from += kStride * s_from;
+                            fetch(from, s_from, there - c - kStride, other);
+                        }
+                        put(out, s_out, there - c, x);
+                        out += kStride * s_out;
+                    } else {
+                        // the gate's warp finishes the first 16 rows, the up projection's the others
+                        float x[kUnitRows], y[kUnitRows];   // g and u
+                        mm_read16(tcol + (uint32_t)c, x);
+                        mm_read16(tcol + (uint32_t)(c + kUnitRows), y);
+                        read(c + kStride >= rows);
+#pragma unroll
+                        for (int j = 0; j < kUnitRows; ++j) {
+                            x[j] += bias;
+                            y[j] += bias;
+                            give[j * 32] = kind ? x[j] : y[j];
+                        }
+                        if (EPI == kMmGated && pre) {
+                            put(pre, s_pre, there - c, x);
+                            put(pre + kUnitRows * s_pre, s_pre, there - c - kUnitRows, y);
+                            pre += kStride * s_pre;
+                        }
+                        pair_barrier(barrier);
+#pragma unroll
+                        for (int j = 0; j < kUnitRows; ++j) {
+                            const float partner = take[j * 32];
+                            if (kind) x[j] = partner;   // y: this warp's u of the second half
+                            else y[j] = partner;
+                        }
+                        pair_barrier(barrier);          // both have read
+                        const int count = there - c - kUnitRows * kind;
+                        if constexpr (EPI == kMmGated) {
+#pragma unroll
+                            for (int j = 0; j < kUnitRows; ++j) x[j] = mm_act1<ACT>(x[j]) * y[j];
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < kUnitRows; ++j) {
+                                float value, slope;
+                                mm_slope1<ACT>(x[j], value, slope);
+                                x[j] = other[j] * y[j] * slope;
+                                y[j] = other[j] * value;
+                                sum0 += x[j];
+                                sum1 += y[j];
+                            }
+                            from += kStride * s_from;
+                            fetch(from, s_from, count - kStride, other);
+                            put(out2, p.out2_stride, count, y);
+                            out2 += kStride * p.out2_stride;
+                        }
+                        put(out, s_out, count, x);
+                        out += kStride * s_out;
                     }
                 }
             });
             if constexpr (EPI == kMmSlope || EPI == kMmGatedSlope) {
-                // the warps' sums over their rows, in order; a buffer holds eight warps' of one kind,
-                // and in a gated product those of a warp's even and odd rows
-                constexpr int kHalves = kBoth ? 2 : 1;
-#pragma unroll
-                for (int w = 0; w < (kBoth ? 2 : 1); ++w) {
-                    float *at = sums + buffer * kChunkFloats;
-                    *reinterpret_cast<float4 *>(at + (w8 * kHalves + (kBoth ? lane >> 4 : 0)) * kOwn + 4 * own) =
-                        make_float4(o.sum[w][0], o.sum[w][1], o.sum[w][2], o.sum[w][3]);
-                    epilogue_barrier();
-                    const int i = (int)threadIdx.x - 64, out = (t.n * 2 + (int)rank) * kOwn + i;
-                    if (i < kOwn && out < q.N && p.part[w]) {
-                        float s = 0.f;
-                        for (int k = 0; k < kEpiWarps * kHalves; ++k) s += at[k * kOwn + i];
-                        p.part[w][(size_t)(t.row0 / q.tile_m) * q.N + out] = s;
-                    }
-                    buffer ^= 1;
-                }
+                // each warp's sums over its rows are a row of their own
+                const size_t at = (size_t)((t.row0 / q.tile_m) * kSides * (kBoth ? 2 : 1) + (kBoth ? 2 * side + kind : side)) * q.N + i;
+                if (i < q.N && p.part[0]) p.part[0][at] = sum0;
+                if (kBoth && i < q.N && p.part[1]) p.part[1][at] = sum1;
             }
             ++it;
         }
@@ -346,7 +422,7 @@ int MmMapList::add(const MmOperand &o, int box_rows) {
     auto enc = tmap_encode_fn();
     cuuint64_t dims[2] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows};
     cuuint64_t strides[1] = {(cuuint64_t)o.stride * 2};
-    cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    cuuint32_t box[2] = {(cuuint32_t)kStepK, (cuuint32_t)box_rows};
     cuuint32_t es[2] = {1, 1};
     ok = ok && enc && count < kMmMaps &&
          enc(&maps.m[count], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(o.base), dims, strides, box, es,
@@ -382,7 +458,7 @@ cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStr
     if (!list.ok) return cudaErrorInvalidValue;
     p.maps = list.count;
     if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
-    if (part_rows) *part_rows = p.prob[0].mt;
+    if (part_rows) *part_rows = (int64_t)p.prob[0].mt * (kEpiWarps / 4) * (mm_both(epi) ? 2 : 1);
     const void *fn = epi == kMmStore   ? (const void *)mm_pair_kernel<kMmStore>
                      : epi == kMmGated ? (const void *)mm_pair_kernel<kMmGated>
                      : epi == kMmSlope ? (const void *)mm_pair_kernel<kMmSlope>

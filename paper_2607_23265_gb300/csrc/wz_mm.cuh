@@ -214,27 +214,46 @@ __device__ __forceinline__ void mm_store4(__nv_bfloat16 *p, const float (&x)[4],
     }
 }
 
-// The residual, or dy, of U rows `step` apart from `row` on, of which those below `end` are there.
-template <int EPI, int U>
-__device__ __forceinline__ void mm_fetch(const MmArgs &p, const MmOutputs &o, float (&other)[U][4], int64_t row, int step,
-                                         int64_t end) {
-    const __nv_bfloat16 *from = EPI == kMmStore ? p.residual : p.dy;
-    const int64_t stride = EPI == kMmStore ? p.residual_stride : p.dy_stride;
-    if (EPI == kMmGated || !from) return;
+// Where the lane's outputs of a row are, in each array that the epilogue reads or writes.
+template <int EPI>
+struct MmAt {
+    const __nv_bfloat16 *from;   // the residual, or dy; null: none
+    __nv_bfloat16 *out, *out2, *pre0, *pre1;
+    int64_t s_from, s_out, s_out2, s_pre0, s_pre1;
+    __device__ __forceinline__ MmAt(const MmArgs &p, const MmProblem &q, int64_t row, int i) {
+        const __nv_bfloat16 *base = EPI == kMmStore ? p.residual : EPI == kMmGated ? nullptr : p.dy;
+        s_from = EPI == kMmStore ? p.residual_stride : p.dy_stride;
+        from = base ? base + row * s_from + i : nullptr;
+        s_out = q.out_stride, out = q.out + row * s_out + i;
+        s_out2 = p.out2_stride, out2 = p.out2 + row * s_out2 + i;
+        s_pre0 = p.pre_stride[0], pre0 = p.pre[0] ? p.pre[0] + row * s_pre0 + i : nullptr;
+        s_pre1 = p.pre_stride[1], pre1 = p.pre[1] + row * s_pre1 + i;
+    }
+    __device__ __forceinline__ void advance(int rows) {
+        if (from) from += rows * s_from;
+        if (pre0) pre0 += rows * s_pre0;
+        out += rows * s_out, out2 += rows * s_out2, pre1 += rows * s_pre1;
+    }
+};
+
+// The residual, or dy, of U rows `step` apart, of which the first `count` (in steps) are there.
+// FULL: all of them, and all four outputs.
+template <int EPI, int U, bool FULL>
+__device__ __forceinline__ void mm_fetch(const MmAt<EPI> &at, int left, float (&other)[U][4], int step, int count) {
+    if (EPI == kMmGated || !at.from) return;
 #pragma unroll
     for (int k = 0; k < U; ++k)
-        if (row + k * step < end) mm_load4(from + (row + k * step) * stride + o.i, other[k], o.left);
+        if (FULL || k < count) mm_load4(at.from + k * step * at.s_from, other[k], FULL ? 4 : left);
 }
 
 // Finishes and stores them: v holds the sums (g in a gated product, u its other ones).
-template <int EPI, int ACT, int U>
-__device__ __forceinline__ void mm_finish(const MmArgs &p, const MmProblem &q, MmOutputs &o, float (&v)[U][4],
-                                          float (&u)[U][4], const float (&other)[U][4], int64_t row, int step,
-                                          int64_t end) {
+template <int EPI, int ACT, int U, bool FULL>
+__device__ __forceinline__ void mm_finish(const MmAt<EPI> &at, MmOutputs &o, float (&v)[U][4], float (&u)[U][4],
+                                          const float (&other)[U][4], int step, int count) {
+    const int left = FULL ? 4 : o.left;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-        const int64_t r = row + k * step;
-        if (r >= end) break;
+        if (!FULL && k >= count) break;
         float y[4], z[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -242,7 +261,7 @@ __device__ __forceinline__ void mm_finish(const MmArgs &p, const MmProblem &q, M
             if constexpr (EPI == kMmStore) {
                 v[k][j] = x;
                 y[j] = mm_act1<ACT>(x);
-                if (p.residual) y[j] += other[k][j];
+                if (at.from) y[j] += other[k][j];
             } else if constexpr (EPI == kMmGated) {
                 v[k][j] = x;
                 u[k][j] += o.b[1][j];
@@ -261,11 +280,11 @@ __device__ __forceinline__ void mm_finish(const MmArgs &p, const MmProblem &q, M
             }
         }
         if constexpr (EPI == kMmStore || EPI == kMmGated)
-            if (p.pre[0]) mm_store4(p.pre[0] + r * p.pre_stride[0] + o.i, v[k], o.left);
+            if (at.pre0) mm_store4(at.pre0 + k * step * at.s_pre0, v[k], left);
         if constexpr (EPI == kMmGated)
-            if (p.pre[0]) mm_store4(p.pre[1] + r * p.pre_stride[1] + o.i, u[k], o.left);
-        mm_store4(q.out + r * q.out_stride + o.i, y, o.left);
-        if constexpr (EPI == kMmGatedSlope) mm_store4(p.out2 + r * p.out2_stride + o.i, z, o.left);
+            if (at.pre0) mm_store4(at.pre1 + k * step * at.s_pre1, u[k], left);
+        mm_store4(at.out + k * step * at.s_out, y, left);
+        if constexpr (EPI == kMmGatedSlope) mm_store4(at.out2 + k * step * at.s_out2, z, left);
     }
 }
 
