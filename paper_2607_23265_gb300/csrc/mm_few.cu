@@ -1,23 +1,24 @@
-// Matrix products with few rows, or few tiles: tiles of 128 outputs x 16 .. 256 rows on one SM,
+// Matrix products of few tiles: 128 outputs of a CTA x 16 .. 256 rows,
 //
-//   D^T[i][j] = sum_k B[i][k] A[j][k]     i: outputs (128 lanes of tensor memory), j: rows
+//   D^T[i][j] = sum_k B[i][k] A[j][k]     i: outputs (lanes of tensor memory), j: rows
 //
-// so that the number of rows is padded to 16 only.  Weights of few
-// rows are a stream that has to come from HBM as fast as it can: K is shared by the CTAs
-// of a cluster, each with a ring of up to twelve stages in flight, and their sums are
-// joined through distributed shared memory, in the order of their ranks, each CTA
+// on one SM each (row tiles in sixteens, for few rows) or on a pair of SMs (in thirty-twos; half
+// of the rows' tile a CTA).  What few rows need is a stream of weights that comes from HBM as
+// fast as it can, and what few tiles need is to be spread over all SMs: so K is shared by the
+// CTAs of a cluster, each with a ring of up to twelve stages in flight, and their sums
+// are joined through distributed shared memory, in the order of their ranks, each CTA
 // finishing its share of the rows.  No workspace, no second kernel, equal bits each time.
 //
-// A stage is 64 along K: 128 outputs' weights (16 KB; a gated product both projections',
-// whose sums lie beside one another in tensor memory) and the tile's rows, each K-major,
-// one box of 64 k of its rows, or MN-major, a box of 64 rows of its 64 k each, with
-// 128-byte swizzle.  What lies outside an operand arrives as zeros.
+// A stage is 64 along K: 128 weight rows (16 KB; in a gated product the gate's and the up
+// projection's of the same 64 outputs) and the rows' tile, each K-major, one box of 64 k of
+// its rows, or MN-major, a box of 64 rows of its 64 k each, with 128-byte swizzle.  What
+// lies outside an operand arrives as zeros.
 // Warps: 0 copies, 1 products, then all eight the epilogue.
 //
-// Tensor memory is taken by every CTA and held while it waits for its cluster.  So no two
-// such CTAs may share an SM unless both find room, or clusters could wait for one
-// another: a CTA of up to 256 columns asks for more than a third of an SM's shared
-// memory, one of 512 for more than two thirds, and the pairs of mm_pair.cu leave too little for either.
+// Two CTAs share an SM where there are enough of them, so that one's start and epilogue
+// overlap the other's products.  Tensor memory is taken by every CTA and held while it waits
+// for its cluster, so no CTA may be left without: all take 256 columns at most, and more than
+// a third of an SM's shared memory, and the pairs of mm_pair.cu leave too little for one.
 #include <algorithm>
 #include <cstring>
 #include <type_traits>
@@ -28,9 +29,10 @@ namespace wz {
 
 namespace {
 
-constexpr int kOutputs = 128, kStepK = 64;
-constexpr int kWeightBytes = kOutputs * kStepK * 2;   // 16 KB
+constexpr int kLanes = 128, kStepK = 64;
+constexpr int kWeightBytes = kLanes * kStepK * 2;     // 16 KB
 constexpr int kBoxBytes = kWeightBytes / 2;           // 64 x 64
+constexpr int kRowBytes = kLanes * 4;                 // sums of a row
 constexpr int kMaxStages = 12;
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
@@ -47,10 +49,9 @@ struct Shared {
 constexpr size_t kExtra = 1024 + sizeof(Shared);
 // an SM has 228 KB, of which a CTA's first kilobyte is the system's
 constexpr size_t kSmHas = 228 * 1024;
-constexpr size_t kSmemTwo = kSmHas / 2 - 1024;         // two CTAs an SM
+constexpr size_t kSmemTwo = kSmHas / 2 - 1024;        // two CTAs an SM
 constexpr size_t kSmemOne = 227 * 1024;
-constexpr size_t kSmemLeastTwo = kSmHas / 3;           // not three
-constexpr size_t kSmemLeastOne = kSmHas * 2 / 3;       // not beside one of the others
+constexpr size_t kSmemLeast = kSmHas / 3;             // not three
 
 __device__ __forceinline__ void give_up(const MmArgs &p, volatile int *abort_flag) {
     *abort_flag = 1;
@@ -71,11 +72,12 @@ __device__ __forceinline__ uint32_t tmem_columns(int n) { return n <= 32 ? 32u :
 
 }  // namespace
 
-template <int EPI>
+template <int EPI, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_constant__ MmMaps maps,
                                                              const __grid_constant__ MmArgs p) {
     constexpr bool kBoth = mm_both(EPI);
-    constexpr int kSums = kBoth ? 2 : 1;
+    constexpr int kOwn = kBoth ? kLanes / 2 : kLanes;     // outputs of a CTA
+    constexpr int kGroup = PAIR ? 2 : 1;                  // CTAs of a tile's K share
     extern __shared__ uint8_t smem_raw[];
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     Shared *S = reinterpret_cast<Shared *>(ring + p.ring_bytes);
@@ -83,52 +85,54 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     // this CTA's tile, and its share of K
-    const int cluster = p.cluster, id = (int)blockIdx.x / cluster, rank = (int)blockIdx.x - id * cluster;
+    const int id = (int)blockIdx.x / p.cluster, rank = (int)blockIdx.x - id * p.cluster;
+    const int side = rank % kGroup, group = rank / kGroup, groups = p.cluster / kGroup;
     int which = 0;
     while (which + 1 < p.problems && id >= p.prob[which + 1].first) ++which;
     const MmProblem &q = p.prob[which];
     const bool shared_k = q.split > 1;
-    const int tile = shared_k ? id - q.first : (id - q.first) * cluster + rank;
-    const int part = shared_k ? rank : 0;
+    const int tile = shared_k ? id - q.first : (id - q.first) * groups + group;
+    const int part = shared_k ? group : 0;
     const bool active = tile < q.mt * q.nt;
-    const int tn = tile / q.mt, tm = tile - tn * q.mt;
-    const int row0 = tm * q.tile_m, out0 = tn * kOutputs;
+    const int tn = tile / q.mt, row0 = (tile - tn * q.mt) * q.tile_m;
+    const int out0 = (tn * kGroup + side) * kOwn;
+    const int rows = q.M - row0 < q.tile_m ? q.M - row0 : q.tile_m;
+    const int columns = (rows + 16 * kGroup - 1) / (16 * kGroup) * (16 * kGroup);   // of the products
     const int total = q.segments * q.steps;
     const int step0 = (int)((int64_t)total * part / q.split), step1 = (int)((int64_t)total * (part + 1) / q.split);
-    const uint32_t columns = tmem_columns(kSums * q.tile_m);
+    const uint32_t allocated = tmem_columns(q.tile_m);
 
-    if (warp == 2 && lane < p.maps) ptx::prefetch_tmap(&maps.m[lane]);
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < p.stages; ++s) {
-            ptx::mbar_init(&S->full[s], 1);
-            ptx::mbar_init(&S->empty[s], 1);
+    if (warp == 0) {
+        if (ptx::elect_one()) {
+            for (int s = 0; s < p.stages; ++s) {
+                ptx::mbar_init(&S->full[s], 1);
+                ptx::mbar_init(&S->empty[s], 1);
+            }
+            ptx::mbar_init(&S->done, 1);
+            S->abort = 0;
+            ptx::fence_barrier_init();
+            ptx::fence_proxy_async_smem();
         }
-        ptx::mbar_init(&S->done, 1);
-        S->abort = 0;
-        ptx::fence_barrier_init();
-        ptx::fence_proxy_async_smem();
+        __syncwarp();
     }
-    if (warp == 1) {
-        ptx::tmem_alloc(&S->tmem_base, columns);
-        ptx::tmem_relinquish();
-    }
+    if (warp == 2 && lane < p.maps) ptx::prefetch_tmap(&maps.m[lane]);
     pdl_wait();   // an operand may be the previous grid's output
-    __syncthreads();
+    if constexpr (PAIR) ptx::cluster_sync();   // both CTAs' barriers are ready
+    else __syncthreads();
     pdl_trigger();
-    ptx::tc_fence_after();
-    const uint32_t tmem = S->tmem_base;
 
     if (active && warp == 0) {
         if (ptx::elect_one()) {
-            // ---------------- copies ----------------
+            // ---------------- copies: this CTA's weights, and its half of the rows ----------------
             // (a step's issue has to be short: a division for its segment and a look at the abort
             // word made it 390 cycles, more than its products take)
             const uint64_t once = ptx::policy_evict_first(), again = ptx::policy_evict_last();
             const uint64_t weights = q.mt > 1 ? again : once;   // row tiles share them in L2
-            // an operand K-major is one box, MN-major one for each 64 rows
             const bool a_mn = q.a_mn, b_mn = q.b_mn;
-            const int boxes = a_mn ? (q.tile_m + 63) / 64 : 1, steps = q.steps, stages = p.stages;
-            const uint32_t bytes = (uint32_t)(kSums * kWeightBytes + (a_mn ? boxes * kBoxBytes : q.tile_m * kStepK * 2));
+            const int r0 = row0 + side * (columns / 2);
+            const int boxes = a_mn ? (columns / kGroup + 63) / 64 : 1, steps = q.steps, stages = p.stages;
+            const uint32_t bytes = (uint32_t)kGroup * (uint32_t)(kWeightBytes + (a_mn ? boxes * kBoxBytes : q.box_rows * kStepK * 2));
+            const uint32_t full0 = PAIR ? ptx::map_cluster(&S->full[0], (uint32_t)(rank & ~1)) : 0;
             int seg = step0 / steps, k = (step0 - seg * steps) * kStepK, stage = 0;
             const CUtensorMap *a = &maps.m[q.a[seg]], *b = &maps.m[q.b[seg]], *b2 = &maps.m[q.b[1]];
             uint32_t phase = 1;
@@ -138,21 +142,25 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
                     break;
                 }
                 uint8_t *st = ring + stage * p.stage_bytes;
-                uint64_t *full = &S->full[stage];
-                ptx::mbar_arrive_expect_tx(full, bytes);
-                if (b_mn) {
-                    ptx::tma_load_2d(st, b, full, out0, k, weights);
-                    ptx::tma_load_2d(st + kBoxBytes, b, full, out0 + 64, k, weights);
+                const auto copy = [&](uint8_t *to, const CUtensorMap *m, int x, int y, uint64_t policy) {
+                    if constexpr (PAIR) ptx::tma_load_2d_pair(to, m, full0 + (uint32_t)stage * 8, x, y, policy);
+                    else ptx::tma_load_2d(to, m, &S->full[stage], x, y, policy);
+                };
+                if (side == 0) ptx::mbar_arrive_expect_tx(&S->full[stage], bytes);
+                if constexpr (kBoth) {
+                    copy(st, b, k, out0, weights);
+                    copy(st + kBoxBytes, b2, k, out0, weights);
+                } else if (b_mn) {
+                    copy(st, b, out0, k, weights);
+                    copy(st + kBoxBytes, b, out0 + 64, k, weights);
                 } else {
-                    ptx::tma_load_2d(st, b, full, k, out0, weights);
+                    copy(st, b, k, out0, weights);
                 }
-                if constexpr (kBoth) ptx::tma_load_2d(st + kWeightBytes, b2, full, k, out0, weights);
-                st += kSums * kWeightBytes;
+                st += kWeightBytes;
                 if (a_mn)
-                    for (int h = 0; h < boxes; ++h)
-                        ptx::tma_load_2d(st + h * kBoxBytes, a, full, row0 + 64 * h, k, again);
+                    for (int h = 0; h < boxes; ++h) copy(st + h * kBoxBytes, a, r0 + 64 * h, k, again);
                 else
-                    ptx::tma_load_2d(st, a, full, k, row0, again);
+                    copy(st, a, k, r0, again);
                 k += kStepK;
                 if (k == steps * kStepK && seg + 1 < q.segments) {
                     k = 0;
@@ -166,17 +174,27 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
                 }
             }
         }
-    } else if (active && warp == 1) {
-        if (ptx::elect_one()) {
+    } else if (warp == 1) {
+        // (tensor memory is taken while the first copies are under way)
+        if constexpr (PAIR) {
+            ptx::tmem_alloc_pair(&S->tmem_base, allocated);
+            ptx::tmem_relinquish_pair();
+        } else {
+            ptx::tmem_alloc(&S->tmem_base, allocated);
+            ptx::tmem_relinquish();
+        }
+        __syncwarp();
+        if (active && side == 0 && ptx::elect_one()) {
             // ---------------- products ----------------
             // K-major: rows of 128 bytes, 8 to a kilobyte; 16 k are 32 bytes.
             // MN-major: a kilobyte is 8 k of 64 rows, 64 rows on is the next box; 16 k are 2 KB.
-            const uint32_t ring32 = ptx::smem_u32(ring);
-            const uint32_t idesc = ptx::idesc_bf16(kOutputs, q.tile_m, q.b_mn, q.a_mn);
+            const uint32_t d = *(volatile uint32_t *)&S->tmem_base, ring32 = ptx::smem_u32(ring);
+            const uint32_t idesc = ptx::idesc_bf16(kGroup * kLanes, columns, q.b_mn, q.a_mn);
             const uint64_t w_base = ptx::smem_desc(ring32, q.b_mn ? kBoxBytes : 16, 1024, 2);
-            const uint64_t x_base = ptx::smem_desc(ring32 + kSums * kWeightBytes, q.a_mn ? kBoxBytes : 16, 1024, 2);
+            const uint64_t x_base = ptx::smem_desc(ring32 + kWeightBytes, q.a_mn ? kBoxBytes : 16, 1024, 2);
             const uint64_t w_step = q.b_mn ? 128 : 2, x_step = q.a_mn ? 128 : 2;
-            const int stages = p.stages, second = q.tile_m;
+            const int stages = p.stages;
+            const uint16_t both = (uint16_t)(3u << (rank & ~1));
             int stage = 0;
             uint32_t phase = 0, more = 0;
             for (int left = step1 - step0; left > 0; --left) {
@@ -187,38 +205,41 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
                 ptx::tc_fence_after();
                 const uint64_t so = (uint64_t)(stage * (p.stage_bytes >> 4));
 #pragma unroll
-                for (int w = 0; w < kSums; ++w)
-#pragma unroll
-                    for (int k = 0; k < kStepK / 16; ++k)
-                        ptx::mma_bf16(tmem + (uint32_t)(w * second),
-                                      w_base + so + (uint64_t)(w * (kWeightBytes >> 4)) + k * w_step,
-                                      x_base + so + k * x_step, idesc, k ? 1u : more);
+                for (int k = 0; k < kStepK / 16; ++k) {
+                    if constexpr (PAIR)
+                        ptx::mma_bf16_pair(d, w_base + so + k * w_step, x_base + so + k * x_step, idesc, k ? 1u : more);
+                    else
+                        ptx::mma_bf16(d, w_base + so + k * w_step, x_base + so + k * x_step, idesc, k ? 1u : more);
+                }
                 more = 1;
-                ptx::mma_commit(&S->empty[stage]);
+                if constexpr (PAIR) ptx::mma_commit_pair(&S->empty[stage], both);
+                else ptx::mma_commit(&S->empty[stage]);
                 if (++stage == stages) {
                     stage = 0;
                     phase ^= 1u;
                 }
             }
-            ptx::mma_commit(&S->done);
+            if constexpr (PAIR) ptx::mma_commit_pair(&S->done, both);
+            else ptx::mma_commit(&S->done);
         }
     }
     __syncwarp();
     // ---------------- epilogue ----------------
     // The sums go through shared memory, a warp writing 32 outputs of 16 rows, and then
-    // takes one row's 128 outputs after the other, four to a lane: 256 contiguous bytes.
-    const int quadrant = warp & 3, side = warp >> 2;
-    const int rows = q.M - row0 < q.tile_m ? q.M - row0 : q.tile_m;
+    // takes one row's outputs after the other (two rows' in a gated product), four to a lane.
+    constexpr int kLanesRow = kOwn / 4, kRowsWarp = 32 / kLanesRow, kRowsAll = kRowsWarp * kWarps;
+    const int quadrant = warp & 3, half = warp >> 2, own = lane % kLanesRow, sub = lane / kLanesRow;
     MmOutputs o;
-    mm_outputs<kBoth>(p, q, o, out0 + 4 * lane);
+    mm_outputs<kBoth>(p, q, o, out0 + 4 * own);
     // (a wait that gives up says so; the products under way are waited for all the same)
     if (active && !ptx::mbar_wait(&S->done, 0, p.wait_ns)) {
         give_up(p, abort_flag);
-        ptx::mbar_wait(&S->done, 0, kMmTimeoutNs);
+        ptx::mbar_wait(&S->done, 0, 2 * kMmTimeoutNs);
     }
     __syncthreads();
     const bool ok = active && !*abort_flag;
     ptx::tc_fence_after();
+    const uint32_t tmem = S->tmem_base;
     // the ring is free: every copy has been used, and every product is complete
     float *sums = reinterpret_cast<float *>(ring);
     const uint32_t tbase = tmem + ((uint32_t)(quadrant * 32) << 16);
@@ -226,65 +247,71 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     for (int c0 = 0; c0 < rows; c0 += chunk) {
         const int c1 = c0 + chunk < rows ? c0 + chunk : rows;
         if (ok)
-            for (int c = c0 + 16 * side; c < c1; c += 32)
+            for (int c = c0 + 16 * half; c < c1; c += 32) {
+                float v[16];
+                mm_read16(tbase + (uint32_t)c, v);
+                float *to = sums + (size_t)(c - c0) * kLanes + quadrant * 32 + lane;
 #pragma unroll
-                for (int w = 0; w < kSums; ++w) {
-                    float v[16];
-                    mm_read16(tbase + (uint32_t)(w * q.tile_m + c), v);
-                    float *to = sums + (size_t)(w * chunk + c - c0) * kOutputs + quadrant * 32 + lane;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) to[j * kOutputs] = v[j];
-                }
+                for (int j = 0; j < 16; ++j) to[j * kLanes] = v[j];
+            }
+        // this CTA's share of the rows
+        const int share = shared_k ? (rows + q.split - 1) / q.split : c1 - c0;
+        const int lo = shared_k ? part * share : c0, hi = lo + share < c1 ? lo + share : c1;
+        const int first = lo + warp * kRowsWarp + sub;   // the lane's first row
+        constexpr int U = 2;                              // rows in flight
+        MmAt<EPI> at(p, q, (int64_t)row0 + first, o.i);
+        float other[U][4];
+        if (ok && o.left > 0) mm_fetch<EPI, U, false>(at, o.left, other, kRowsAll, (hi - first + kRowsAll - 1) / kRowsAll);
         if (shared_k) ptx::cluster_sync();
         else __syncthreads();
         if (ok && o.left > 0)
             mm_with_act(p.act, [&](auto act) {
                 constexpr int ACT = decltype(act)::value;
-                constexpr int U = kBoth ? 1 : 2;   // rows in flight
-                // this CTA's share of the rows
-                const int share = shared_k ? (rows + q.split - 1) / q.split : c1 - c0;
-                const int lo = shared_k ? part * share : c0, hi = lo + share < c1 ? lo + share : c1;
-                MmAt<EPI> rows_at(p, q, (int64_t)row0 + lo + warp, o.i);
-                for (int c = lo + warp; c < hi; c += U * kWarps) {
-                    const int count = (hi - c + kWarps - 1) / kWarps;
-                    float v[U][4] = {}, u[U][4] = {}, other[U][4];
-                    mm_fetch<EPI, U, false>(rows_at, o.left, other, kWarps, count);
-                    const float *at = sums + (size_t)(c - c0) * kOutputs + 4 * lane;
+                for (int c = first; c < hi; c += U * kRowsAll) {
+                    const int count = (hi - c + kRowsAll - 1) / kRowsAll;
+                    float v[U][4] = {}, u[U][4] = {};
+                    const float *from = sums + (size_t)(c - c0) * kLanes + 4 * own;
+                    const auto add = [&](float (&d)[4], const float4 &t) {
+                        d[0] += t.x, d[1] += t.y, d[2] += t.z, d[3] += t.w;
+                    };
                     if (!shared_k) {
 #pragma unroll
                         for (int k = 0; k < U; ++k)
-                            if (c + k * kWarps < hi)
-#pragma unroll
-                                for (int w = 0; w < kSums; ++w) {
-                                    const float4 t = *reinterpret_cast<const float4 *>(
-                                        at + (size_t)(w * chunk + k * kWarps) * kOutputs);
-                                    float(&d)[4] = w ? u[k] : v[k];
-                                    d[0] = t.x, d[1] = t.y, d[2] = t.z, d[3] = t.w;
-                                }
+                            if (k < count) {
+                                add(v[k], *reinterpret_cast<const float4 *>(from + k * kRowsAll * kLanes));
+                                if constexpr (kBoth)
+                                    add(u[k], *reinterpret_cast<const float4 *>(from + k * kRowsAll * kLanes + kOwn));
+                            }
                     } else {
-                        for (int r0 = 0; r0 < q.split; r0 += 4) {
-                            float4 t[4][U * kSums];
+                        constexpr int kParts = kBoth ? 2 : 4;   // CTAs' sums on their way at a time
+                        for (int r0 = 0; r0 < q.split; r0 += kParts) {
+                            float4 t[kParts][U], s[kParts][U];
 #pragma unroll
-                            for (int r = 0; r < 4; ++r)
+                            for (int r = 0; r < kParts; ++r) {
+                                const uint32_t there =
+                                    ptx::map_cluster(from, (uint32_t)((r0 + r < q.split ? r0 + r : 0) * kGroup + side));
 #pragma unroll
-                                for (int x = 0; x < U * kSums; ++x) {
-                                    const int k = x / kSums, w = x % kSums;
-                                    t[r][x] = make_float4(0.f, 0.f, 0.f, 0.f);
-                                    if (r0 + r < q.split && c + k * kWarps < hi)
-                                        t[r][x] = ld_cluster4(ptx::map_cluster(
-                                            at + (size_t)(w * chunk + k * kWarps) * kOutputs, (uint32_t)(r0 + r)));
+                                for (int k = 0; k < U; ++k) {
+                                    t[r][k] = s[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                                    if (r0 + r < q.split && k < count) {
+                                        t[r][k] = ld_cluster4(there + (uint32_t)(k * kRowsAll * kRowBytes));
+                                        if constexpr (kBoth)
+                                            s[r][k] = ld_cluster4(there + (uint32_t)(k * kRowsAll * kRowBytes + kOwn * 4));
+                                    }
                                 }
+                            }
 #pragma unroll
-                            for (int r = 0; r < 4; ++r)
+                            for (int r = 0; r < kParts; ++r)
 #pragma unroll
-                                for (int x = 0; x < U * kSums; ++x) {
-                                    float(&d)[4] = x % kSums ? u[x / kSums] : v[x / kSums];
-                                    d[0] += t[r][x].x, d[1] += t[r][x].y, d[2] += t[r][x].z, d[3] += t[r][x].w;
+                                for (int k = 0; k < U; ++k) {
+                                    add(v[k], t[r][k]);
+                                    if constexpr (kBoth) add(u[k], s[r][k]);
                                 }
                         }
                     }
-                    mm_finish<EPI, ACT, U, false>(rows_at, o, v, u, other, kWarps, count);
-                    rows_at.advance(U * kWarps);
+                    mm_finish<EPI, ACT, U, false>(at, o, v, u, other, kRowsAll, count);
+                    at.advance(U * kRowsAll);
+                    mm_fetch<EPI, U, false>(at, o.left, other, kRowsAll, count - U);
                 }
             });
         if (c1 < rows) __syncthreads();
@@ -297,25 +324,28 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
         }
     }
     __syncthreads();
-    if (shared_k) ptx::cluster_sync();   // nobody reads this CTA's sums any more
+    // nobody reads this CTA's sums any more, and no arrival is under way
+    if (PAIR || shared_k) ptx::cluster_sync();
     if constexpr (EPI == kMmSlope || EPI == kMmGatedSlope) {
-        // the warps' sums over their rows, in order
+        // the lanes' sums over their rows, in order
+        constexpr int kSums = kBoth ? 2 : 1, kEach = kWarps * kRowsWarp;
 #pragma unroll
         for (int w = 0; w < kSums; ++w)
-            *reinterpret_cast<float4 *>(sums + (w * kWarps + warp) * kOutputs + 4 * lane) =
+            *reinterpret_cast<float4 *>(sums + (w * kEach + warp * kRowsWarp + sub) * kOwn + 4 * own) =
                 make_float4(o.sum[w][0], o.sum[w][1], o.sum[w][2], o.sum[w][3]);
         __syncthreads();
-        const int w = (int)threadIdx.x / kOutputs, i = (int)threadIdx.x % kOutputs;
+        const int w = (int)threadIdx.x / kOwn, i = (int)threadIdx.x % kOwn;
         if (ok && w < kSums && out0 + i < q.N && p.part[w]) {
             float s = 0.f;
 #pragma unroll
-            for (int k = 0; k < kWarps; ++k) s += sums[(w * kWarps + k) * kOutputs + i];
-            p.part[w][(size_t)(tm * q.split + part) * q.N + out0 + i] = s;
+            for (int k = 0; k < kEach; ++k) s += sums[(w * kEach + k) * kOwn + i];
+            p.part[w][(size_t)((row0 / q.tile_m) * q.split + part) * q.N + out0 + i] = s;
         }
     }
     if (warp == 1) {
         ptx::tc_fence_after();
-        ptx::tmem_dealloc(tmem, columns);
+        if constexpr (PAIR) ptx::tmem_dealloc_pair(tmem, allocated);
+        else ptx::tmem_dealloc(tmem, allocated);
     }
 }
 
@@ -324,24 +354,21 @@ namespace {
 int round_up(int x, int to) { return (x + to - 1) / to * to; }
 
 // A row tile's bytes of a stage.
-int row_bytes(const MmProblem &q, int tile_m) {
-    return (q.a_mn ? round_up(tile_m, 64) : tile_m) * kStepK * 2;
-}
+int row_bytes(const MmProblem &q, int rows) { return (q.a_mn ? round_up(rows, 64) : rows) * kStepK * 2; }
 
-// Whether a product can take tiles of tile_m rows and `split` CTAs a tile: the sums fit
-// into tensor memory and, where they are joined, into shared memory, no CTA is without
-// a step, and the sums over rows have a place.
-bool fits(MmEpilogue epi, const MmProblem &q, int tile_m, int split) {
-    const int sums = mm_both(epi) ? 2 : 1;
-    if (tile_m % 16 != 0 || tile_m < 16 || tile_m > 256 || sums * tile_m > 512) return false;
-    if (split > 1 && sums * tile_m * kOutputs * 4 + kExtra > kSmemOne) return false;
-    if (split > q.segments * q.steps) return false;
+// Whether a product can take tiles of tile_m rows and `split` shares of K a tile: its sums
+// fit into tensor memory and, where they are joined, into shared memory, no share is
+// empty, and the sums over rows have a place.
+bool fits(MmEpilogue epi, const MmProblem &q, bool pair, int tile_m, int split) {
+    const int even = pair ? 32 : 16;
+    if (tile_m % even != 0 || tile_m < even || tile_m > 256) return false;
+    if (split > q.segments * q.steps || split * (pair ? 2 : 1) > kMaxCluster) return false;
     const int64_t tiles = ((int64_t)q.M + tile_m - 1) / tile_m;
     return (epi != kMmSlope && epi != kMmGatedSlope) || tiles * split <= mm_part_rows(q.M);
 }
 
 #ifdef WZ_CHECKED
-int check_kind = 0, check_cluster = 1, check_tile = 64;
+int check_kind = 0, check_split = 1, check_tile = 64;
 #endif
 
 }  // namespace
@@ -350,88 +377,89 @@ bool plan_mm_few(MmEpilogue epi, const MmArgs &p, int sms, MmFewPlan *plan) {
 #ifdef WZ_CHECKED
     if (check_kind) {
         if (check_kind == 1) return false;
-        plan->cluster = check_cluster;
+        plan->pair = check_kind == 3;
+        plan->split = 1;
+        const int even = plan->pair ? 32 : 16;
         for (int i = 0; i < p.problems; ++i) {
             const MmProblem &q = p.prob[i];
-            plan->tile_m[i] = std::min(check_tile, round_up(q.M, 16));
-            plan->split[i] = fits(epi, q, plan->tile_m[i], check_cluster) ? check_cluster : 1;
-            if (!fits(epi, q, plan->tile_m[i], plan->split[i])) return false;
+            plan->tile_m[i] = std::min(round_up(check_tile, even), round_up(q.M, even));
+            plan->shared[i] = check_split > 1 && fits(epi, q, plan->pair, plan->tile_m[i], check_split);
+            if (plan->shared[i]) plan->split = check_split;
+            else if (!fits(epi, q, plan->pair, plan->tile_m[i], 1)) return false;
         }
         return true;
     }
 #endif
-    int cluster = 1;
-    for (int i = 0; i < p.problems; ++i) {
-        const MmProblem &q = p.prob[i];
-        plan->tile_m[i] = round_up(std::min(q.M, 64), 16);
-        plan->split[i] = 1;
-        if (q.M > 64 || !fits(epi, q, plan->tile_m[i], 1)) return false;
-        const int tiles = (q.N + kOutputs - 1) / kOutputs;
-        cluster = std::max(1, std::min({kMaxCluster, sms / tiles, q.segments * q.steps}));
-    }
     if (p.problems > 1) return false;
-    while (!fits(epi, p.prob[0], plan->tile_m[0], cluster)) --cluster;
-    plan->cluster = cluster;
-    plan->split[0] = cluster;
+    const MmProblem &q = p.prob[0];
+    if (q.M > 64) return false;
+    plan->pair = false;
+    plan->tile_m[0] = round_up(std::min(q.M, 64), 16);
+    const int own = mm_both(epi) ? kLanes / 2 : kLanes, tiles = (q.N + own - 1) / own;
+    plan->split = std::max(1, std::min({kMaxCluster, sms / tiles, q.segments * q.steps}));
+    while (!fits(epi, q, false, plan->tile_m[0], plan->split)) --plan->split;
+    plan->shared[0] = plan->split > 1;
     return true;
 }
 
 cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool pdl, cudaStream_t s,
                           int64_t *part_rows) {
-    const int sums = mm_both(epi) ? 2 : 1;
+    const int group = plan.pair ? 2 : 1, own = (mm_both(epi) ? kLanes / 2 : kLanes) * group;
     MmMapList list;
     int64_t clusters = 0;
-    int columns = 0, dump = 0, most_steps = 1;
-    p.cluster = plan.cluster;
+    int dump = 0, most_steps = 1;
+    p.cluster = plan.split * group;
     p.stage_bytes = 0;
     for (int i = 0; i < p.problems; ++i) {
         MmProblem &q = p.prob[i];
         q.tile_m = plan.tile_m[i];
-        q.split = plan.split[i];
+        q.box_rows = q.tile_m / group;
+        q.split = plan.shared[i] ? plan.split : 1;
         q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
-        q.nt = (q.N + kOutputs - 1) / kOutputs;
+        q.nt = (q.N + own - 1) / own;
         if ((int64_t)q.mt * q.nt > INT32_MAX / kMaxCluster) return cudaErrorInvalidValue;
         q.first = (int)clusters;
-        clusters += q.split > 1 ? q.mt * q.nt : (q.mt * q.nt + plan.cluster - 1) / plan.cluster;
-        p.stage_bytes = std::max(p.stage_bytes, sums * kWeightBytes + row_bytes(q, q.tile_m));
-        columns = std::max(columns, sums * q.tile_m);
-        if (q.split > 1) dump = std::max(dump, sums * q.tile_m * kOutputs * 4);
+        clusters += q.split > 1 ? q.mt * q.nt : (q.mt * q.nt + plan.split - 1) / plan.split;
+        p.stage_bytes = std::max(p.stage_bytes, kWeightBytes + row_bytes(q, q.box_rows));
+        if (q.split > 1) dump = std::max(dump, q.tile_m * kRowBytes);
         most_steps = std::max(most_steps, (q.segments * q.steps + q.split - 1) / q.split);
-        for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.a_mn ? 64 : q.tile_m);
-        for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j) q.b[j] = list.add(q.from_b[j], q.b_mn ? 64 : kOutputs);
+        for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.a_mn ? 64 : q.box_rows);
+        for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j)
+            q.b[j] = list.add(q.from_b[j], q.b_mn || mm_both(epi) ? 64 : kLanes);
     }
-    if (!list.ok || clusters * plan.cluster > INT32_MAX) return cudaErrorInvalidValue;
-    p.stage_bytes = round_up(p.stage_bytes, 1024);
+    if (!list.ok || clusters * p.cluster > INT32_MAX) return cudaErrorInvalidValue;
     p.maps = list.count;
-    // two CTAs an SM where their tensor memory, and joining sums, allow it
-    const bool two = columns <= 256 && dump + kExtra <= kSmemTwo && clusters * plan.cluster > sm_count();
+    p.stage_bytes = round_up(p.stage_bytes, 1024);
+    const bool two = dump + kExtra <= kSmemTwo && clusters * p.cluster > sm_count();
     const size_t most = (two ? kSmemTwo : kSmemOne) - kExtra;
-    p.stages = (int)std::min<size_t>({(size_t)kMaxStages, most / p.stage_bytes, (size_t)std::max(most_steps, 1)});
-    p.ring_bytes = std::max(p.stages * p.stage_bytes, dump);
+    p.stages = (int)std::min<size_t>({(size_t)kMaxStages, most / p.stage_bytes, (size_t)most_steps});
+    // (the slopes' sums over rows take 8 KB of the ring at the end)
+    p.ring_bytes = std::max({p.stages * p.stage_bytes, dump, kWarps * 1024});
     if (p.stages < 1 || (size_t)p.ring_bytes > most) return cudaErrorInvalidValue;
-    p.chunk = std::min(256, p.ring_bytes / (sums * kOutputs * 4) / 16 * 16);
-    const size_t smem = std::max(kExtra + (size_t)p.ring_bytes,
-                                 (columns <= 256 ? kSmemLeastTwo : kSmemLeastOne) + 1);
+    p.chunk = std::min(256, p.ring_bytes / kRowBytes / 16 * 16);
+    const size_t smem = std::max(kExtra + (size_t)p.ring_bytes, kSmemLeast + 1);
     if (part_rows) *part_rows = (int64_t)p.prob[0].mt * p.prob[0].split;
-    const void *fn = epi == kMmStore   ? (const void *)mm_few_kernel<kMmStore>
-                     : epi == kMmGated ? (const void *)mm_few_kernel<kMmGated>
-                     : epi == kMmSlope ? (const void *)mm_few_kernel<kMmSlope>
-                                       : (const void *)mm_few_kernel<kMmGatedSlope>;
+    const void *fns[4][2] = {
+        {(const void *)mm_few_kernel<kMmStore, false>, (const void *)mm_few_kernel<kMmStore, true>},
+        {(const void *)mm_few_kernel<kMmGated, false>, (const void *)mm_few_kernel<kMmGated, true>},
+        {(const void *)mm_few_kernel<kMmSlope, false>, (const void *)mm_few_kernel<kMmSlope, true>},
+        {(const void *)mm_few_kernel<kMmGatedSlope, false>, (const void *)mm_few_kernel<kMmGatedSlope, true>}};
+    const void *fn = fns[epi][plan.pair];
     const cudaError_t e = allow_smem(fn, smem);
     if (e != cudaSuccess) return e;
     void *args[] = {&list.maps, &p};
-    return launch_kernel(fn, dim3((unsigned)(clusters * plan.cluster)), dim3(kThreads), smem, s, args, pdl,
-                         (unsigned)plan.cluster);
+    return launch_kernel(fn, dim3((unsigned)(clusters * p.cluster)), dim3(kThreads), smem, s, args, pdl,
+                         (unsigned)p.cluster);
 }
 
 }  // namespace wz
 
 #ifdef WZ_CHECKED
-// Test hook: the kernel that products take. kind 0: by their sizes, 1: mm_pair.cu's, 2: this file's where it
-// can, with clusters and row tiles of these sizes.
-extern "C" __attribute__((visibility("default"))) void wz_check_mm_plan(int kind, int cluster, int tile_m) {
+// Test hook: the kernel that products take. kind 0: by their sizes, 1: mm_pair.cu's, 2 and 3: this file's on one SM
+// and on pairs, where it can, with K in `split` shares and row tiles of this size.
+extern "C" __attribute__((visibility("default"))) void wz_check_mm_plan(int kind, int split, int tile_m) {
     wz::check_kind = kind;
-    wz::check_cluster = cluster;
+    wz::check_split = split;
     wz::check_tile = tile_m;
 }
 #endif

@@ -54,8 +54,8 @@ struct MmProblem {
     int a[2], b[2];        // their tensor maps
     int mt, nt;            // tiles along M and N
     int tile_m;            // rows of a tile
-    int box_rows;          // pairs: a CTA's
-    int split;             // few-rows kernel: CTAs that share a tile's K,
+    int box_rows;          // a CTA's
+    int split;             // few-rows kernel: shares of a tile's K,
     int first;             //   first cluster
 };
 
@@ -310,10 +310,13 @@ cudaError_t launch_mm(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStream_t
 // Tiles of 256 x 256 on pairs of SMs (mm_pair.cu).
 cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStream_t s, int64_t *part_rows);
 
-// Tiles of 16 to 256 rows on one SM, K shared by a cluster (mm_few.cu).  False: they do not
-// suit it.
+// Tiles of 16 to 256 rows on one SM or a pair, K shared by a cluster (mm_few.cu).  False:
+// they do not suit it.
 struct MmFewPlan {
-    int cluster, tile_m[kMmProblems], split[kMmProblems];
+    bool pair;
+    int split;                                  // shares of K
+    int tile_m[kMmProblems];
+    bool shared[kMmProblems];                   // whether a product's K is shared
 };
 bool plan_mm_few(MmEpilogue epi, const MmArgs &p, int sms, MmFewPlan *plan);
 cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool pdl, cudaStream_t s,

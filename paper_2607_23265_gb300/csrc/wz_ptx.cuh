@@ -296,12 +296,12 @@ __device__ __forceinline__ void mma_bf16_pair(uint32_t d_tmem, uint64_t adesc, u
         : "memory");
 }
 
-// Arrive once on `bar` of both CTAs when the pair MMAs issued so far complete.
-__device__ __forceinline__ void mma_commit_pair(uint64_t *bar) {
+// Arrive once on `bar` of both CTAs (a bit of `ctas` each) when the pair MMAs issued so far complete.
+__device__ __forceinline__ void mma_commit_pair(uint64_t *bar, uint16_t ctas = 3) {
     asm volatile(
         "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
             smem_u32(bar)),
-        "h"((uint16_t)3)
+        "h"(ctas)
         : "memory");
 }
 

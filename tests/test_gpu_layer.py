@@ -139,8 +139,9 @@ def test_backward(wz, M, N, K, act, kept):
     gated_backward(wz, M, N, K, act, kept)
 
 
-# pairs of SMs; then clusters and row tiles of the few-rows kernel: one CTA, shared K, the widest tiles
-PLANS = [(1, 1, 64), (2, 1, 64), (2, 2, 16), (2, 3, 208), (2, 8, 48), (2, 5, 176), (2, 1, 256)]
+# persistent pairs of SMs; tiles on one SM and on pairs: one share of K, several, narrow and wide row tiles
+PLANS = [(1, 1, 64), (2, 1, 64), (2, 2, 16), (2, 3, 208), (2, 8, 48), (2, 5, 176), (2, 1, 256),
+         (3, 1, 96), (3, 2, 32), (3, 4, 192), (3, 3, 256)]
 
 
 @pytest.mark.parametrize("plan", PLANS)
