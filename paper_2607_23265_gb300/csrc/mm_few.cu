@@ -58,15 +58,16 @@ __device__ __forceinline__ void give_up(const MmArgs &p, volatile int *abort_fla
     if (p.status) atomicOr(p.status, WZ_STATUS_WAIT_TIMEOUT);
 }
 
-// Four floats of another CTA's shared memory (or of this one's).
-__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                 : "r"(addr)
-                 : "memory");
-    return v;
+__device__ __forceinline__ void st_cluster(uint32_t addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
+
+// The two halves of a cluster's barrier; the relaxed arrival does not wait for the thread's stores.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive_relaxed() {
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t tmem_columns(int n) { return n <= 32 ? 32u : 1u << (32 - __clz(n - 1)); }
 
@@ -103,16 +104,15 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     const uint32_t allocated = tmem_columns(q.tile_m);
 
     if (warp == 0) {
-        if (ptx::elect_one()) {
-            for (int s = 0; s < p.stages; ++s) {
-                ptx::mbar_init(&S->full[s], 1);
-                ptx::mbar_init(&S->empty[s], 1);
-            }
+        if (lane < p.stages) {
+            ptx::mbar_init(&S->full[lane], 1);
+            ptx::mbar_init(&S->empty[lane], 1);
+        }
+        if (lane == 31) {
             ptx::mbar_init(&S->done, 1);
             S->abort = 0;
-            ptx::fence_barrier_init();
-            ptx::fence_proxy_async_smem();
         }
+        ptx::fence_barrier_init();
         __syncwarp();
     }
     if (warp == 2 && lane < p.maps) ptx::prefetch_tmap(&maps.m[lane]);
@@ -120,6 +120,8 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     if constexpr (PAIR) ptx::cluster_sync();   // both CTAs' barriers are ready
     else __syncthreads();
     pdl_trigger();
+    // sums may come here from now on, unless the ring is in their place
+    if (shared_k && p.apart) cluster_arrive();
 
     if (active && warp == 0) {
         if (ptx::elect_one()) {
@@ -225,12 +227,15 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     }
     __syncwarp();
     // ---------------- epilogue ----------------
-    // The sums go through shared memory, a warp writing 32 outputs of 16 rows, and then
-    // takes one row's outputs after the other (two rows' in a gated product), four to a lane.
+    // The sums go through shared memory, a warp writing 32 outputs of 32 rows (those of a shared K
+    // to the CTA that finishes the row), and then takes one row's outputs after the other (two
+    // rows' in a gated product), four to a lane.
     constexpr int kLanesRow = kOwn / 4, kRowsWarp = 32 / kLanesRow, kRowsAll = kRowsWarp * kWarps;
     const int quadrant = warp & 3, half = warp >> 2, own = lane % kLanesRow, sub = lane / kLanesRow;
     MmOutputs o;
     mm_outputs<kBoth>(p, q, o, out0 + 4 * own);
+    // rows that are in shared memory at a time, of each share of K; a multiple of four
+    const int chunk = shared_k ? (rows + 4 * q.split - 1) / (4 * q.split) * 4 : p.chunk;
     // (a wait that gives up says so; the products under way are waited for all the same)
     if (active && !ptx::mbar_wait(&S->done, 0, p.wait_ns)) {
         give_up(p, abort_flag);
@@ -240,23 +245,42 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     const bool ok = active && !*abort_flag;
     ptx::tc_fence_after();
     const uint32_t tmem = S->tmem_base;
-    // the ring is free: every copy has been used, and every product is complete
-    float *sums = reinterpret_cast<float *>(ring);
+    // (the ring is free now: every copy has been used, and every product is complete)
+    float *sums = reinterpret_cast<float *>(ring + (shared_k && p.apart ? p.ring_bytes - p.sums_bytes : 0));
     const uint32_t tbase = tmem + ((uint32_t)(quadrant * 32) << 16);
-    const int chunk = shared_k ? q.tile_m : p.chunk;   // rows that are in shared memory at a time
+    if (shared_k) {
+        if (!p.apart) cluster_arrive();
+        cluster_wait();
+    }
     for (int c0 = 0; c0 < rows; c0 += chunk) {
-        const int c1 = c0 + chunk < rows ? c0 + chunk : rows;
+        // to shared memory: all of this CTA's sums, or a chunk of them
+        const int end = shared_k || c0 + chunk > rows ? rows : c0 + chunk;
         if (ok)
-            for (int c = c0 + 16 * half; c < c1; c += 32) {
-                float v[16];
-                mm_read16(tbase + (uint32_t)c, v);
-                float *to = sums + (size_t)(c - c0) * kLanes + quadrant * 32 + lane;
+            for (int c = c0 + 32 * half; c < end; c += 64) {
+                uint32_t raw[32];
+                ptx::tmem_ld_32x32b_x32(tbase + (uint32_t)c, raw);
+                int owner = shared_k ? c / chunk : 0, at = c - c0 - owner * chunk;
+                ptx::tmem_ld_wait();
+                ptx::reg_fence32(raw);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) to[j * kLanes] = v[j];
+                for (int j = 0; j < 32; j += 4) {
+                    if (c + j < end) {
+                        float *to = sums + (size_t)(part * chunk + at) * kLanes + quadrant * 32 + lane;
+                        if (shared_k) {
+                            const uint32_t there = ptx::map_cluster(to, (uint32_t)(owner * kGroup + side));
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) st_cluster(there + (uint32_t)(i * kRowBytes), __uint_as_float(raw[j + i]));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) to[i * kLanes] = __uint_as_float(raw[j + i]);
+                        }
+                    }
+                    at += 4;
+                    if (at >= chunk) at -= chunk, ++owner;
+                }
             }
-        // this CTA's share of the rows
-        const int share = shared_k ? (rows + q.split - 1) / q.split : c1 - c0;
-        const int lo = shared_k ? part * share : c0, hi = lo + share < c1 ? lo + share : c1;
+        // this CTA's rows
+        const int lo = shared_k ? part * chunk : c0, hi = lo + chunk < rows ? lo + chunk : rows;
         const int first = lo + warp * kRowsWarp + sub;   // the lane's first row
         constexpr int U = 2;                              // rows in flight
         MmAt<EPI> at(p, q, (int64_t)row0 + first, o.i);
@@ -270,51 +294,26 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
                 for (int c = first; c < hi; c += U * kRowsAll) {
                     const int count = (hi - c + kRowsAll - 1) / kRowsAll;
                     float v[U][4] = {}, u[U][4] = {};
-                    const float *from = sums + (size_t)(c - c0) * kLanes + 4 * own;
-                    const auto add = [&](float (&d)[4], const float4 &t) {
-                        d[0] += t.x, d[1] += t.y, d[2] += t.z, d[3] += t.w;
-                    };
-                    if (!shared_k) {
+                    const float *from = sums + (size_t)(c - lo) * kLanes + 4 * own;
+                    for (int r = 0; r < q.split; ++r, from += (size_t)chunk * kLanes) {
 #pragma unroll
                         for (int k = 0; k < U; ++k)
                             if (k < count) {
-                                add(v[k], *reinterpret_cast<const float4 *>(from + k * kRowsAll * kLanes));
-                                if constexpr (kBoth)
-                                    add(u[k], *reinterpret_cast<const float4 *>(from + k * kRowsAll * kLanes + kOwn));
-                            }
-                    } else {
-                        constexpr int kParts = kBoth ? 2 : 4;   // CTAs' sums on their way at a time
-                        for (int r0 = 0; r0 < q.split; r0 += kParts) {
-                            float4 t[kParts][U], s[kParts][U];
-#pragma unroll
-                            for (int r = 0; r < kParts; ++r) {
-                                const uint32_t there =
-                                    ptx::map_cluster(from, (uint32_t)((r0 + r < q.split ? r0 + r : 0) * kGroup + side));
-#pragma unroll
-                                for (int k = 0; k < U; ++k) {
-                                    t[r][k] = s[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                                    if (r0 + r < q.split && k < count) {
-                                        t[r][k] = ld_cluster4(there + (uint32_t)(k * kRowsAll * kRowBytes));
-                                        if constexpr (kBoth)
-                                            s[r][k] = ld_cluster4(there + (uint32_t)(k * kRowsAll * kRowBytes + kOwn * 4));
-                                    }
+                                const float4 x = *reinterpret_cast<const float4 *>(from + k * kRowsAll * kLanes);
+                                v[k][0] += x.x, v[k][1] += x.y, v[k][2] += x.z, v[k][3] += x.w;
+                                if constexpr (kBoth) {
+                                    const float4 y = *reinterpret_cast<const float4 *>(from + k * kRowsAll * kLanes + kOwn);
+                                    u[k][0] += y.x, u[k][1] += y.y, u[k][2] += y.z, u[k][3] += y.w;
                                 }
                             }
-#pragma unroll
-                            for (int r = 0; r < kParts; ++r)
-#pragma unroll
-                                for (int k = 0; k < U; ++k) {
-                                    add(v[k], t[r][k]);
-                                    if constexpr (kBoth) add(u[k], s[r][k]);
-                                }
-                        }
                     }
                     mm_finish<EPI, ACT, U, false>(at, o, v, u, other, kRowsAll, count);
                     at.advance(U * kRowsAll);
                     mm_fetch<EPI, U, false>(at, o.left, other, kRowsAll, count - U);
                 }
             });
-        if (c1 < rows) __syncthreads();
+        if (end == rows) break;
+        __syncthreads();
     }
     ptx::tc_fence_before();
     if (*abort_flag && threadIdx.x == 0) {
@@ -324,8 +323,6 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
         }
     }
     __syncthreads();
-    // nobody reads this CTA's sums any more, and no arrival is under way
-    if (PAIR || shared_k) ptx::cluster_sync();
     if constexpr (EPI == kMmSlope || EPI == kMmGatedSlope) {
         // the lanes' sums over their rows, in order
         constexpr int kSums = kBoth ? 2 : 1, kEach = kWarps * kRowsWarp;
@@ -342,6 +339,12 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
             p.part[w][(size_t)((row0 / q.tile_m) * q.split + part) * q.N + out0 + i] = s;
         }
     }
+    // a pair's arrivals have all come: the last is the one that says that its products are done,
+    // unless a wait ran out
+    if (PAIR) {
+        cluster_arrive_relaxed();
+        cluster_wait();
+    }
     if (warp == 1) {
         ptx::tc_fence_after();
         if constexpr (PAIR) ptx::tmem_dealloc_pair(tmem, allocated);
@@ -355,6 +358,9 @@ int round_up(int x, int to) { return (x + to - 1) / to * to; }
 
 // A row tile's bytes of a stage.
 int row_bytes(const MmProblem &q, int rows) { return (q.a_mn ? round_up(rows, 64) : rows) * kStepK * 2; }
+
+// The most rows of sums that come to a CTA of a shared K: a chunk from each share.
+int sums_rows(int tile_m, int split) { return (tile_m + 4 * split - 1) / (4 * split) * 4 * split; }
 
 // Whether a product can take tiles of tile_m rows and `split` shares of K a tile: its sums
 // fit into tensor memory and, where they are joined, into shared memory, no share is
@@ -421,7 +427,7 @@ cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool
         q.first = (int)clusters;
         clusters += q.split > 1 ? q.mt * q.nt : (q.mt * q.nt + plan.split - 1) / plan.split;
         p.stage_bytes = std::max(p.stage_bytes, kWeightBytes + row_bytes(q, q.box_rows));
-        if (q.split > 1) dump = std::max(dump, q.tile_m * kRowBytes);
+        if (q.split > 1) dump = std::max({dump, sums_rows(q.tile_m, q.split) * kRowBytes, kWarps * 1024});
         most_steps = std::max(most_steps, (q.segments * q.steps + q.split - 1) / q.split);
         for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.a_mn ? 64 : q.box_rows);
         for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j)
@@ -432,11 +438,15 @@ cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool
     p.stage_bytes = round_up(p.stage_bytes, 1024);
     const bool two = dump + kExtra <= kSmemTwo && clusters * p.cluster > sm_count();
     const size_t most = (two ? kSmemTwo : kSmemOne) - kExtra;
-    p.stages = (int)std::min<size_t>({(size_t)kMaxStages, most / p.stage_bytes, (size_t)most_steps});
-    // (the slopes' sums over rows take 8 KB of the ring at the end)
-    p.ring_bytes = std::max({p.stages * p.stage_bytes, dump, kWarps * 1024});
+    // joined sums have a place of their own where six stages are left, or as many as there are steps
+    p.apart = dump > 0 && (size_t)(std::min(most_steps, 6) * p.stage_bytes + dump) <= most;
+    p.sums_bytes = dump;
+    const size_t ring = most - (p.apart ? dump : 0);
+    p.stages = (int)std::min<size_t>({(size_t)kMaxStages, ring / p.stage_bytes, (size_t)most_steps});
+    // (the slopes' sums over rows take 8 KB at the end)
+    p.ring_bytes = p.apart ? p.stages * p.stage_bytes + dump : std::max({p.stages * p.stage_bytes, dump, kWarps * 1024});
     if (p.stages < 1 || (size_t)p.ring_bytes > most) return cudaErrorInvalidValue;
-    p.chunk = std::min(256, p.ring_bytes / kRowBytes / 16 * 16);
+    p.chunk = std::min(256, p.ring_bytes / kRowBytes / 32 * 32);   // (a warp reads 32 rows at a time)
     const size_t smem = std::max(kExtra + (size_t)p.ring_bytes, kSmemLeast + 1);
     if (part_rows) *part_rows = (int64_t)p.prob[0].mt * p.prob[0].split;
     const void *fns[4][2] = {

@@ -73,7 +73,9 @@ struct MmArgs {
     int maps;                               // tensor maps in use
     int cluster;                            // few-rows kernel: CTAs of a cluster, the ring,
     int stages, stage_bytes, ring_bytes;
-    int chunk;                              //   rows of its sums in shared memory at a time
+    int sums_bytes;                         //   joined sums, at its end where they are
+    int apart;                              //   apart from it,
+    int chunk;                              //   rows of sums in shared memory at a time
     int *status;
     uint64_t wait_ns;
 };
