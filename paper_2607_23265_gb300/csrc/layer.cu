@@ -44,34 +44,54 @@ __global__ void __launch_bounds__(32 * kDeltaWarps) mm_delta_kernel(const __grid
     if (left > 0) {
         mm_with_act(p.act, [&](auto act) {
             constexpr int ACT = decltype(act)::value;
-#pragma unroll 4
-            for (int r = warp; r < kDeltaRows; r += kDeltaWarps) {
-                const int64_t m = m0 + r;
-                if (m >= p.M) break;
-                float dy[8];
-                mm_load(p.dy + m * p.dy_stride + n, dy, left);
-                if constexpr (MODE == kDeltaSums) {
+            // (a batch of rows is on its way before the first of them is stored: the compiler keeps
+            // loads behind stores that might be to the same place)
+            constexpr int kBatch = 4, kArrays = MODE == kDeltaSums ? 1 : MODE == kDeltaSlope ? 2 : 3;
+            const __nv_bfloat16 *from[3] = {p.dy + n, p.pre[0] + n, p.pre[1] + n};
+            const int64_t strides[3] = {p.dy_stride, p.pre_stride[0], p.pre_stride[1]};
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) a0[j] += dy[j];
-                } else {
-                    float g[8], u[8];
-                    mm_load(p.pre[0] + m * p.pre_stride[0] + n, g, left);
-                    if constexpr (MODE == kDeltaGated) mm_load(p.pre[1] + m * p.pre_stride[1] + n, u, left);
+            for (int r0 = warp; r0 < kDeltaRows; r0 += kBatch * kDeltaWarps) {
+                uint4 raw[kArrays][kBatch];
+                const bool wide = left >= 8 && m0 + r0 + (kBatch - 1) * kDeltaWarps < p.M;
+                if (wide) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float value, slope;
-                        mm_slope1<ACT>(g[j], value, slope);
-                        if constexpr (MODE == kDeltaGated) {
-                            g[j] = dy[j] * u[j] * slope;
-                            u[j] = dy[j] * value;
-                            a1[j] += u[j];
-                        } else {
-                            g[j] = dy[j] * slope;
+                    for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+                        for (int a = 0; a < kArrays; ++a)
+                            raw[a][k] = *reinterpret_cast<const uint4 *>(from[a] + (m0 + r0 + k * kDeltaWarps) * strides[a]);
+                }
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    const int64_t m = m0 + r0 + k * kDeltaWarps;
+                    if (!wide && m >= p.M) break;
+                    float dy[8], g[8], u[8];
+                    const auto take = [&](int a, float (&x)[8]) {
+                        if (wide) unpack(raw[a < kArrays ? a : 0][k], x, (__nv_bfloat16 *)nullptr);
+                        else mm_load(from[a] + m * strides[a], x, left);
+                    };
+                    take(0, dy);
+                    if constexpr (MODE == kDeltaSums) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) a0[j] += dy[j];
+                    } else {
+                        take(1, g);
+                        if constexpr (MODE == kDeltaGated) take(2, u);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            float value, slope;
+                            mm_slope1<ACT>(g[j], value, slope);
+                            if constexpr (MODE == kDeltaGated) {
+                                g[j] = dy[j] * u[j] * slope;
+                                u[j] = dy[j] * value;
+                                a1[j] += u[j];
+                            } else {
+                                g[j] = dy[j] * slope;
+                            }
+                            a0[j] += g[j];
                         }
-                        a0[j] += g[j];
+                        mm_store(p.d[0] + m * p.d_stride + n, g, wide ? 8 : left);
+                        if constexpr (MODE == kDeltaGated) mm_store(p.d[1] + m * p.d_stride + n, u, wide ? 8 : left);
                     }
-                    mm_store(p.d[0] + m * p.d_stride + n, g, left);
-                    if constexpr (MODE == kDeltaGated) mm_store(p.d[1] + m * p.d_stride + n, u, left);
                 }
             }
         });

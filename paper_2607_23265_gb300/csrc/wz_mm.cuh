@@ -90,9 +90,32 @@ __device__ __forceinline__ float mm_sigmoid(float x) { return __fdividef(1.f, 1.
 // tanh z = 2 sigmoid(2z) - 1, so that gelu_tanh is x sigmoid(2z).
 __device__ __forceinline__ float mm_gelu_arg(float x) { return 1.5957691216057308f * x * (1.f + 0.044715f * x * x); }
 
+// The normal distribution's share below x, and exp(-x^2 / 2).  Below -|x| it is
+// exp(-x^2 / 2) erfcx(|x| / sqrt 2) / 2, and the last factor t P(t) with t = 1 / (1 + 0.21 |x|):
+// P was fitted for the least largest relative error over |x| <= 13 (2^-26; with fp32
+// coefficients and steps 2^-21, beside the exponential's).  One reciprocal and one
+// exponential, which the slope needs too: the slopes of 18,662 x 3584 products with
+// erfcf and the exponential apart took 211 us.
+__device__ __forceinline__ float mm_normal(float x, float &e) {
+    const float t = __fdividef(1.f, fmaf(0.21f, fabsf(x), 1.f));
+    float y = -7.219379397e-02f;
+    y = fmaf(y, t, 2.862429807e-01f);
+    y = fmaf(y, t, -3.358583682e-01f);
+    y = fmaf(y, t, 3.560014568e-01f);
+    y = fmaf(y, t, -9.866009608e-02f);
+    y = fmaf(y, t, 1.269889168e-01f);
+    y = fmaf(y, t, 6.861732179e-02f);
+    y = fmaf(y, t, 8.515556234e-02f);
+    y = fmaf(y, t, 8.370601885e-02f);
+    e = __expf(-0.5f * x * x);
+    y *= t * e;
+    return x > 0.f ? 1.f - y : y;
+}
+
 template <int ACT>
 __device__ __forceinline__ float mm_act1(float x) {
-    if constexpr (ACT == WZ_ACT_GELU) return 0.5f * x * erfcf(-0.70710678118654752f * x);
+    float e;
+    if constexpr (ACT == WZ_ACT_GELU) return x * mm_normal(x, e);
     if constexpr (ACT == WZ_ACT_GELU_TANH) return x * mm_sigmoid(mm_gelu_arg(x));
     if constexpr (ACT == WZ_ACT_SILU) return x * mm_sigmoid(x);
     return x;
@@ -106,10 +129,10 @@ __device__ __forceinline__ void mm_slope1(float x, float &value, float &slope) {
         value = x;
         slope = 1.f;
     } else if constexpr (ACT == WZ_ACT_GELU) {
-        const float phi = 0.5f * erfcf(-0.70710678118654752f * x);
-        const float e = 0.3989422804014327f * __expf(-0.5f * x * x);
+        float e;
+        const float phi = mm_normal(x, e);
         value = x * phi;
-        slope = phi + (e > 0.f ? x * e : 0.f);
+        slope = phi + (e > 0.f ? 0.3989422804014327f * x * e : 0.f);
     } else {
         const bool tanh_form = ACT == WZ_ACT_GELU_TANH;
         const float s = mm_sigmoid(tanh_form ? mm_gelu_arg(x) : x);
