@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     // this CTA's tile, and its share of K
-    const int id = (int)blockIdx.x / p.cluster, rank = (int)blockIdx.x - id * p.cluster;
+    const int id = p.by_cluster.divide((int)blockIdx.x), rank = (int)blockIdx.x - id * p.cluster;
     const int side = rank % kGroup, group = rank / kGroup, groups = p.cluster / kGroup;
     int which = 0;
     while (which + 1 < p.problems && id >= p.prob[which + 1].first) ++which;
@@ -94,13 +94,12 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     const bool shared_k = q.split > 1;
     const int tile = shared_k ? id - q.first : (id - q.first) * groups + group;
     const int part = shared_k ? group : 0;
-    const bool active = tile < q.mt * q.nt;
-    const int tn = tile / q.mt, row0 = (tile - tn * q.mt) * q.tile_m;
+    const bool active = tile < q.tiles;
+    const int tn = q.by_mt.divide(tile), row0 = (tile - tn * q.mt) * q.tile_m;
     const int out0 = (tn * kGroup + side) * kOwn;
     const int rows = q.M - row0 < q.tile_m ? q.M - row0 : q.tile_m;
     const int columns = (rows + 16 * kGroup - 1) / (16 * kGroup) * (16 * kGroup);   // of the products
-    const int total = q.segments * q.steps;
-    const int step0 = (int)((int64_t)total * part / q.split), step1 = (int)((int64_t)total * (part + 1) / q.split);
+    const int step0 = part * q.share + min(part, q.more), step1 = step0 + q.share + (part < q.more ? 1 : 0);
     const uint32_t allocated = tmem_columns(q.tile_m);
 
     if (warp == 0) {
@@ -415,6 +414,7 @@ cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool
     int64_t clusters = 0;
     int dump = 0, most_steps = 1;
     p.cluster = plan.split * group;
+    p.by_cluster.set((uint32_t)p.cluster);
     p.stage_bytes = 0;
     for (int i = 0; i < p.problems; ++i) {
         MmProblem &q = p.prob[i];
@@ -424,6 +424,10 @@ cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool
         q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
         q.nt = (q.N + own - 1) / own;
         if ((int64_t)q.mt * q.nt > INT32_MAX / kMaxCluster) return cudaErrorInvalidValue;
+        q.tiles = q.mt * q.nt;
+        q.by_mt.set((uint32_t)q.mt);
+        q.share = q.segments * q.steps / q.split;
+        q.more = q.segments * q.steps % q.split;
         q.first = (int)clusters;
         clusters += q.split > 1 ? q.mt * q.nt : (q.mt * q.nt + plan.split - 1) / plan.split;
         p.stage_bytes = std::max(p.stage_bytes, kWeightBytes + row_bytes(q, q.box_rows));

@@ -17,6 +17,7 @@
 // writes 64 contiguous bytes of a row, and waits for no other one (in a gated product the
 // two that have the gate's and the up projection's sums of the same outputs exchange
 // halves of 32 rows, and each finishes one).
+#include <algorithm>
 #include <cstring>
 #include <type_traits>
 
@@ -55,32 +56,49 @@ struct Tile {
     int prob, row0, rows, n;   // rows: a multiple of 32, those behind the last one among them
 };
 
-// The tiles of pair `pair` of `pairs`, in order: the first product's dealt in turn,
-// then the others'.
+// The tiles of a pair, product by product.  A product's first `head` tiles go to the pairs from
+// `from` on, in turn: those that had one of the longer tiles before it less than the
+// others.  The rest is dealt to all pairs.
 struct Walk {
     const MmArgs &p;
-    int pairs, t;
-    __device__ Walk(const MmArgs &args, int pair, int pairs_) : p(args), pairs(pairs_), t(pair) {}
+    int pair, pairs, i, x, end, stride;
+    bool rest;
+    __device__ Walk(const MmArgs &args, int pair_, int pairs_) : p(args), pair(pair_), pairs(pairs_), i(0) { begin(); }
+    __device__ void begin() {
+        const MmProblem &q = p.prob[i];
+        rest = pair < q.from || !q.head;
+        x = pair - q.from - q.skip;
+        if (rest) x = q.head + pair;
+        else if (x < 0) x += pairs - q.from;
+        end = rest ? q.tiles : q.head;
+        stride = rest ? pairs : pairs - q.from;
+    }
     __device__ bool next(Tile &tile) {
-        int x = t, i = 0;
-        for (; i < p.problems; ++i) {
-            const int tiles = p.prob[i].mt * p.prob[i].nt;
-            if (x < tiles) break;
-            x -= tiles;
+        while (x >= end) {
+            if (!rest) {
+                rest = true;
+                x = p.prob[i].head + pair;
+                end = p.prob[i].tiles;
+                stride = pairs;
+            } else {
+                if (++i == p.problems) {
+                    --i;
+                    return false;
+                }
+                begin();
+            }
         }
-        if (i == p.problems) return false;
-        t += pairs;
         // kGroupRows row tiles at a time, output tile by output tile: pairs that run
         // side by side share both operands' tiles in L2
         const MmProblem &q = p.prob[i];
-        const int group = x / (kGroupRows * q.nt), left = q.mt - group * kGroupRows;
-        const int rows = left < kGroupRows ? left : kGroupRows;
-        x -= group * kGroupRows * q.nt;
+        const int group = q.by_group.divide(x), m0 = group * kGroupRows, y = x - m0 * q.nt;
+        const bool last = q.mt - m0 < kGroupRows;
         tile.prob = i;
-        tile.n = x / rows;
-        tile.row0 = (group * kGroupRows + x - tile.n * rows) * q.tile_m;
+        tile.n = last ? q.by_last.divide(y) : y / kGroupRows;
+        tile.row0 = (m0 + y - tile.n * (last ? q.mt - m0 : kGroupRows)) * q.tile_m;
         const int r = q.M - tile.row0;
         tile.rows = r < q.tile_m ? (r + 31) / 32 * 32 : q.tile_m;
+        x += stride;
         return true;
     }
 };
@@ -309,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                 if (!last) return;
                 ptx::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive_cluster(b ? tempty[1] : tempty[0]);
+                if (lane == 0) ptx::mbar_arrive_cluster_local(b ? tempty[1] : tempty[0]);
             };
             read(first >= rows);
             mm_with_act(p.act, [&](auto act) {
@@ -439,6 +457,12 @@ int even_tile(int M) {
     return (int)(((int64_t)M + tiles * 32 - 1) / (tiles * 32) * 32);
 }
 
+// What a tile takes: a step is bound by its products, two cycles a row, or by what a CTA's
+// 128 outputs and half of the rows bring in, 64 bytes a cycle; the epilogue takes 5,000 cycles.
+int64_t tile_cost(const MmProblem &q) {
+    return std::max<int64_t>((int64_t)q.segments * q.steps * std::max(2 * q.tile_m, 256 + q.tile_m), 5000);
+}
+
 }  // namespace
 
 cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStream_t s, int64_t *part_rows) {
@@ -451,13 +475,16 @@ cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStr
         q.box_rows = q.tile_m / 2;   // a CTA's
         q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
         q.nt = (q.N + tile_n - 1) / tile_n;
-        tiles += (int64_t)q.mt * q.nt;
+        if ((int64_t)q.mt * q.nt > INT32_MAX / 4) return cudaErrorInvalidValue;
+        q.tiles = q.mt * q.nt;
+        tiles += q.tiles;
+        q.by_group.set((uint32_t)(kGroupRows * q.nt));
+        q.by_last.set((uint32_t)(q.mt % kGroupRows ? q.mt % kGroupRows : kGroupRows));
         for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.a_mn ? 64 : q.box_rows);
         for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j) q.b[j] = list.add(q.from_b[j], q.b_mn || mm_both(epi) ? 64 : kOutputs);
     }
     if (!list.ok) return cudaErrorInvalidValue;
     p.maps = list.count;
-    if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
     if (part_rows) *part_rows = (int64_t)p.prob[0].mt * (kEpiWarps / 4) * (mm_both(epi) ? 2 : 1);
     const void *fn = epi == kMmStore   ? (const void *)mm_pair_kernel<kMmStore>
                      : epi == kMmGated ? (const void *)mm_pair_kernel<kMmGated>
@@ -466,6 +493,26 @@ cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStr
     cudaError_t e = allow_smem(fn, kSmemBytes);
     if (e != cudaSuccess) return e;
     const int pairs = (int)(tiles < sms / 2 ? tiles : sms / 2);
+    // after a product that does not come out even, the pairs that had a tile less take as many
+    // tiles of the next ones first as make up for it
+    int behind = 0, skip = 0;   // the first of these pairs (0: none), and whose turn it is among them
+    int64_t lag = 0;            // what they have to make up for
+    for (int i = 0; i < p.problems; ++i) {
+        MmProblem &q = p.prob[i];
+        const int64_t cost = tile_cost(q), each = behind ? (lag + cost / 2) / cost : 0;
+        const int few = pairs - behind;
+        q.head = (int)std::min<int64_t>(q.tiles, each * few);
+        q.from = q.head ? behind : 0;
+        q.skip = q.head ? skip : 0;
+        if (q.head && q.head == q.tiles) {
+            lag -= (skip + q.head) / few * cost;
+            skip = (skip + q.head) % few;
+            continue;
+        }
+        behind = (q.tiles - q.head) % pairs;
+        lag = cost;
+        skip = 0;
+    }
     void *args[] = {&list.maps, &p};
     return launch_kernel(fn, dim3(2 * pairs), dim3(kThreads), kSmemBytes, s, args, pdl, 2);
 }

@@ -33,6 +33,20 @@ enum MmEpilogue : int {
 
 __host__ __device__ constexpr bool mm_both(int epi) { return epi == kMmGated || epi == kMmGatedSlope; }
 
+// Division of 0 .. 2^31 - 1 by a number that the host knows: n / d = (high(n mul) + n) >> shift with
+// 2^(shift - 1) < d <= 2^shift and mul = 2^32 (2^shift - d) / d + 1 (Granlund and Montgomery).
+struct MmDivisor {
+    uint32_t mul, shift;
+    void set(uint32_t d) {
+        shift = 0;
+        while (((uint64_t)1 << shift) < d) ++shift;
+        mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - d)) / d + 1);
+    }
+    __device__ __forceinline__ int divide(int n) const {
+        return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift);
+    }
+};
+
 // A matrix in memory: [rows][cols], rows `stride` elements apart.
 struct MmOperand {
     const void *base;
@@ -52,10 +66,14 @@ struct MmProblem {
     MmOperand from_a[2], from_b[2];   // host: the operands
     // set by the launch
     int a[2], b[2];        // their tensor maps
-    int mt, nt;            // tiles along M and N
+    int mt, nt, tiles;     // tiles along M and N, and all of them
     int tile_m;            // rows of a tile
+    MmDivisor by_mt;       // few-rows kernel
+    MmDivisor by_group, by_last;   // pairs: tiles of a group of row tiles, row tiles of the last one
+    int head, from, skip;  //   its first tiles, for the pairs from one on, the turn's first
     int box_rows;          // a CTA's
-    int split;             // few-rows kernel: shares of a tile's K,
+    int share, more;       // few-rows kernel: K steps of a share, shares that have one more
+    int split;             //   shares of a tile's K,
     int first;             //   first cluster
 };
 
@@ -72,6 +90,7 @@ struct MmArgs {
     int64_t residual_stride, dy_stride, pre_stride[2], out2_stride;
     int maps;                               // tensor maps in use
     int cluster;                            // few-rows kernel: CTAs of a cluster, the ring,
+    MmDivisor by_cluster;
     int stages, stage_bytes, ring_bytes;
     int sums_bytes;                         //   joined sums, at its end where they are
     int apart;                              //   apart from it,

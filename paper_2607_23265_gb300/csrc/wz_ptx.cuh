@@ -261,6 +261,12 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// The same without an order on other memory than this CTA sees: the release of a cluster waits until all of
+// the thread's stores to global memory are performed.
+__device__ __forceinline__ void mbar_arrive_cluster_local(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
 // 2D tile into this CTA's shared memory, counted on an mbarrier of either CTA
 // of the pair (a shared::cluster address).
 __device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *m, uint32_t bar, int x, int y,
