@@ -1008,7 +1008,7 @@ void wz_linear_backward_args_init(wz_linear_backward_args *a) {
 }
 
 size_t wz_linear_backward_workspace_size(int64_t M, int K, int N) {
-    return check_layer(M, N, K, WZ_ACT_NONE) == WZ_OK ? align_up(linear_backward_bytes(M, N)) : 0;
+    return check_layer(M, N, K, WZ_ACT_NONE) == WZ_OK ? align_up(linear_backward_bytes(M, N, K)) : 0;
 }
 
 int wz_linear_backward(const wz_linear_backward_args *a) {
@@ -1024,10 +1024,8 @@ int wz_linear_backward(const wz_linear_backward_args *a) {
         return WZ_ERR_INVALID_ARG;
     const cudaStream_t s = (cudaStream_t)a->stream;
     Scratch ws;
-    const size_t need = linear_backward_bytes(a->M, a->N);
-    // without an activation and db nothing is kept between kernels
-    const bool keeps = a->M > 0 && (a->act != WZ_ACT_NONE || a->db);
-    if ((a->workspace || keeps) && (st = ws.acquire(a->workspace, a->workspace_bytes, need, s)) != WZ_OK) return st;
+    const size_t need = linear_backward_bytes(a->M, a->N, a->K);
+    if ((a->workspace || a->M > 0) && (st = ws.acquire(a->workspace, a->workspace_bytes, need, s)) != WZ_OK) return st;
     Nvtx range("wz::linear_backward");
     WZ_CUDA(launch_linear_backward(*a, ws.ptr, s));
     return WZ_OK;
@@ -1062,7 +1060,7 @@ void wz_gated_backward_args_init(wz_gated_backward_args *a) {
 }
 
 size_t wz_gated_backward_workspace_size(int64_t M, int K, int N) {
-    return check_layer(M, N, K, WZ_ACT_NONE) == WZ_OK ? align_up(gated_backward_bytes(M, N)) : 0;
+    return check_layer(M, N, K, WZ_ACT_NONE) == WZ_OK ? align_up(gated_backward_bytes(M, N, K)) : 0;
 }
 
 int wz_gated_backward(const wz_gated_backward_args *a) {
@@ -1082,7 +1080,7 @@ int wz_gated_backward(const wz_gated_backward_args *a) {
     const cudaStream_t s = (cudaStream_t)a->stream;
     Scratch ws;
     if ((a->workspace || a->M > 0) &&
-        (st = ws.acquire(a->workspace, a->workspace_bytes, gated_backward_bytes(a->M, a->N), s)) != WZ_OK)
+        (st = ws.acquire(a->workspace, a->workspace_bytes, gated_backward_bytes(a->M, a->N, a->K), s)) != WZ_OK)
         return st;
     Nvtx range("wz::gated_backward");
     WZ_CUDA(launch_gated_backward(*a, ws.ptr, s));

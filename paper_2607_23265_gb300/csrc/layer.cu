@@ -3,7 +3,8 @@
 //
 //   mm_delta_kernel   d = dy act'(p), or dg = dout u act'(g) and du = dout act(g), from
 //                     kept products, with column sums over 64 rows; or the sums alone
-//   mm_sum_kernel     bias gradients from those sums
+//   mm_join_kernel    bias gradients from those sums, and products whose K was shared
+#include <algorithm>
 #include <cstring>
 #include <type_traits>
 
@@ -113,45 +114,110 @@ __global__ void __launch_bounds__(32 * kDeltaWarps) mm_delta_kernel(const __grid
     }
 }
 
-constexpr int kSumRows = 16;
+namespace {
 
-// out[n] = the sum of part[.][n]; blockIdx.y chooses one of two.
-__global__ void __launch_bounds__(32 * kSumRows) mm_sum_kernel(const float *part0, const float *part1, float *out0,
-                                                               float *out1, int64_t rows, int N) {
+constexpr int kSumRows = 16, kSumThreads = 32 * kSumRows;
+constexpr int kJoinRows = 4;   // rows that a thread of a join takes
+
+// What is left to add up when the products are done.
+struct JoinArgs {
+    // bias gradients: db[i][n] = the sum of part[i][.][n]
+    const float *part[2];
+    float *db[2];
+    int64_t part_rows;
+    int N;
+    // products whose K was shared: out = the sum of sums[split][M][cols]
+    struct {
+        const float *sums;
+        __nv_bfloat16 *out;
+        int64_t out_stride, M;
+        int cols, split;
+        unsigned first;        // its first block
+    } join[kMmProblems];
+    unsigned sum_blocks;       // of one bias gradient
+    int joins;
+};
+
+}  // namespace
+
+// The first blocks take 32 columns of a bias gradient each, 16 rows at a time; the others 512
+// outputs of four rows of a shared product, a thread four outputs, in the shares' order.
+__global__ void __launch_bounds__(kSumThreads) mm_join_kernel(const __grid_constant__ JoinArgs p) {
     __shared__ float sums[kSumRows][33];
     pdl_wait();
     pdl_trigger();
-    const float *part = blockIdx.y ? part1 : part0;
-    float *out = blockIdx.y ? out1 : out0;
-    const int c = (int)threadIdx.x & 31, r0 = (int)threadIdx.x >> 5, n = (int)blockIdx.x * 32 + c;
-    float s = 0.f;
-    if (n < N && out)
-        for (int64_t r = r0; r < rows; r += kSumRows) s += part[(size_t)r * N + n];
-    sums[r0][c] = s;
-    __syncthreads();
-    if (r0 == 0 && n < N && out) {
+    unsigned block = blockIdx.x;
+    if (block < 2 * p.sum_blocks) {
+        const int which = block >= p.sum_blocks;
+        const float *part = p.part[which];
+        float *out = p.db[which];
+        const int c = (int)threadIdx.x & 31, r0 = (int)threadIdx.x >> 5;
+        const int n = (int)(block - which * p.sum_blocks) * 32 + c;
+        float s = 0.f;
+        if (n < p.N && out)
+            for (int64_t r = r0; r < p.part_rows; r += kSumRows) s += part[(size_t)r * p.N + n];
+        sums[r0][c] = s;
+        __syncthreads();
+        if (r0 == 0 && n < p.N && out) {
 #pragma unroll
-        for (int i = 1; i < kSumRows; ++i) s += sums[i][c];
-        out[n] = s;
+            for (int i = 1; i < kSumRows; ++i) s += sums[i][c];
+            out[n] = s;
+        }
+        return;
+    }
+    int i = 0;
+    while (i + 1 < p.joins && block >= p.join[i + 1].first) ++i;
+    const auto &j = p.join[i];
+    const unsigned across = (unsigned)(j.cols + 511) / 512;
+    block -= j.first;
+    const int n = (int)(block % across) * 512 + 4 * (int)(threadIdx.x & 127), left = j.cols - n;
+    const int64_t m0 = (int64_t)(block / across) * (4 * kJoinRows) + (int)(threadIdx.x >> 7);
+    if (left <= 0) return;
+    const int64_t plane = j.M * j.cols;
+    const bool wide = left >= 4 && j.cols % 4 == 0;
+#pragma unroll
+    for (int r = 0; r < kJoinRows; ++r) {
+        const int64_t m = m0 + 4 * r;
+        if (m >= j.M) break;
+        const float *from = j.sums + m * j.cols + n;
+        float x[4] = {};
+        for (int k = 0; k < j.split; ++k, from += plane) {
+            if (wide) {
+                const float4 v = __ldcs(reinterpret_cast<const float4 *>(from));
+                x[0] += v.x, x[1] += v.y, x[2] += v.z, x[3] += v.w;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < left) x[e] += from[e];
+            }
+        }
+        mm_store4(j.out + m * j.out_stride + n, x, left);
     }
 }
 
 namespace {
 
-cudaError_t launch_delta(DeltaMode mode, DeltaArgs &p, bool pdl, cudaStream_t s) {
+cudaError_t launch_delta(DeltaMode mode, DeltaArgs &p, cudaStream_t s) {
     const dim3 grid((unsigned)((p.M + kDeltaRows - 1) / kDeltaRows), (unsigned)((p.N + kDeltaCols - 1) / kDeltaCols));
     const void *fn = mode == kDeltaSums    ? (const void *)mm_delta_kernel<kDeltaSums>
                      : mode == kDeltaSlope ? (const void *)mm_delta_kernel<kDeltaSlope>
                                            : (const void *)mm_delta_kernel<kDeltaGated>;
     void *args[] = {&p};
-    return launch_kernel(fn, grid, dim3(32 * kDeltaWarps), 0, s, args, pdl);
+    return launch_kernel(fn, grid, dim3(32 * kDeltaWarps), 0, s, args, true);
 }
 
-cudaError_t launch_sum(const float *part0, const float *part1, float *out0, float *out1, int64_t rows, int N, bool pdl,
-                       cudaStream_t s) {
-    void *args[] = {&part0, &part1, &out0, &out1, &rows, &N};
-    return launch_kernel((const void *)mm_sum_kernel, dim3((unsigned)((N + 31) / 32), out1 ? 2 : 1), dim3(32 * kSumRows),
-                         0, s, args, pdl);
+// Launches p's sums and joins, if there are any.
+cudaError_t launch_join(JoinArgs &p, cudaStream_t s) {
+    p.sum_blocks = p.db[0] || p.db[1] ? (unsigned)((p.N + 31) / 32) : 0;
+    int64_t blocks = 2 * (int64_t)p.sum_blocks;
+    for (int i = 0; i < p.joins; ++i) {
+        p.join[i].first = (unsigned)blocks;
+        blocks += (p.join[i].M + 4 * kJoinRows - 1) / (4 * kJoinRows) * ((p.join[i].cols + 511) / 512);
+    }
+    if (!blocks) return cudaSuccess;
+    if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+    void *args[] = {&p};
+    return launch_kernel((const void *)mm_join_kernel, dim3((unsigned)blocks), dim3(kSumThreads), 0, s, args, true);
 }
 
 __nv_bfloat16 *half(void *p) { return static_cast<__nv_bfloat16 *>(p); }
@@ -169,6 +235,14 @@ MmArgs mm_args(int act, int *status) {
 
 int64_t steps_of(int64_t k) { return (k + 63) / 64; }
 
+JoinArgs join_args(const float *part0, const float *part1, float *db0, float *db1, int64_t rows, int N) {
+    JoinArgs j;
+    memset(&j, 0, sizeof(j));
+    j.part[0] = part0, j.part[1] = part1, j.db[0] = db0, j.db[1] = db1;
+    j.part_rows = rows, j.N = N;
+    return j;
+}
+
 // One layer's gradients from d: dx = d W (+ d2 W2) and dW = d^T x (dW2 = d2^T x).
 struct Gradients {
     int both;                       // 1 or 2 products
@@ -179,7 +253,64 @@ struct Gradients {
     int N, K;
 };
 
-cudaError_t launch_gradients(const Gradients &g, int *status, int sms, bool pdl, cudaStream_t s) {
+// Into how many shares the K of dx and of dW is cut, where their tiles are too few or too long
+// to come out even on the pairs of SMs.
+struct GradientSplit {
+    int dx, dw;
+};
+
+constexpr int kPlanPairs = 76, kMostShares = 8;
+
+// Cycles of a launch with tx tiles of dx in sx shares and tw of dW in sw, each tile `cx` and `cw`
+// cycles long: the longest unit, or all of them evenly; shared ones are written, read again
+// and joined by a kernel (4,000 cycles and 2,600 bytes a cycle).
+int64_t split_cost(int64_t tx, int64_t cx, int64_t bx, int sx, int64_t tw, int64_t cw, int64_t bw, int sw) {
+    const int64_t ux = std::max<int64_t>(cx / sx, 5000), uw = std::max<int64_t>(cw / sw, 5000);
+    const int64_t nx = tx * sx, nw = tw * sw, all = (nx * ux + nw * uw) / kPlanPairs;
+    const auto rounds = [](int64_t n, int64_t u) { return (n + kPlanPairs - 1) / kPlanPairs * u; };
+    int64_t t;
+    if (!nx || !nw) t = rounds(nx, ux) + rounds(nw, uw);
+    else t = std::max({rounds(ux > uw ? nx : nw, std::max(ux, uw)), all + std::min(ux, uw) / 2});
+    if (sx > 1 || sw > 1) t += 4000 + ((sx > 1 ? sx * bx : 0) + (sw > 1 ? sw * bw : 0)) * 8 / 2600;
+    return t;
+}
+
+GradientSplit split_gradients(int64_t M, int N, int K, int both, bool dx, bool dw) {
+    const auto cost = [](int64_t rows) { return std::max<int64_t>(2 * mm_pair_tile(rows), 256 + mm_pair_tile(rows)); };
+    const auto tiles = [](int64_t rows, int64_t outs) { return (rows + mm_pair_tile(rows) - 1) / mm_pair_tile(rows) * ((outs + 255) / 256); };
+    const int64_t sx = both * steps_of(N), sw = steps_of(M);
+    const int64_t tx = dx ? tiles(M, K) : 0, tw = dw ? both * tiles(N, K) : 0, cx = sx * cost(M), cw = sw * cost(N);
+    GradientSplit best{1, 1};
+    int64_t least = split_cost(tx, cx, M * K, 1, tw, cw, (int64_t)both * N * K, 1);
+    for (int a = 1; a <= (dx ? kMostShares : 1); ++a)
+        for (int b = 1; b <= (dw ? kMostShares : 1); ++b) {
+            if ((a == 1 && b == 1) || (a > 1 && sx < 2 * a) || (b > 1 && sw < 2 * b)) continue;
+            // (something has to come of it: the model is not exact)
+            const int64_t t = split_cost(tx, cx, M * K, a, tw, cw, (int64_t)both * N * K, b) * 17 / 16;
+            if (t < least) {
+                least = t;
+                best = GradientSplit{a, b};
+            }
+        }
+    return best;
+}
+
+// The most floats of shares' sums that a call may need, whichever gradients it asks for.
+size_t shares_bytes(int64_t M, int N, int K, int both) {
+    size_t most = 0;
+    for (int need = 1; M > 0 && need < 4; ++need) {
+        const GradientSplit g = split_gradients(M, N, K, both, need & 1, need & 2);
+        size_t bytes = 0;
+        if ((need & 1) && g.dx > 1) bytes += pad256((size_t)g.dx * (size_t)M * (size_t)K * 4);
+        if ((need & 2) && g.dw > 1) bytes += both * pad256((size_t)g.dw * (size_t)N * (size_t)K * 4);
+        most = std::max(most, bytes);
+    }
+    return most;
+}
+
+// The products of both gradients in one launch; what they leave to be joined goes into `join`.
+cudaError_t launch_gradients(const Gradients &g, char *shares, JoinArgs &join, int *status, int sms,
+                             cudaStream_t s) {
     MmArgs p = mm_args(WZ_ACT_NONE, status);
     MmProblem in, weight[2];
     memset(&in, 0, sizeof(in));
@@ -198,14 +329,26 @@ cudaError_t launch_gradients(const Gradients &g, int *status, int sms, bool pdl,
         q.from_a[0] = d;
         q.from_b[0] = MmOperand{g.x, g.M, g.K, g.x_stride};
     }
+    const GradientSplit split = split_gradients(g.M, g.N, g.K, g.both, g.dx, g.dw[0]);
+    const auto add = [&](MmProblem &q, int shared) {
+        q.split = shared;
+        if (shared > 1) {
+            q.sums = reinterpret_cast<float *>(shares);
+            shares += pad256((size_t)shared * (size_t)q.M * (size_t)q.N * 4);
+            auto &j = join.join[join.joins++];
+            j.sums = q.sums, j.out = q.out, j.out_stride = q.out_stride, j.M = q.M, j.cols = q.N, j.split = shared;
+        }
+        p.prob[p.problems++] = q;
+    };
     // the longer tiles first, so that the shorter ones even out the ends
-    const bool weights_first = g.dw[0] && (!g.dx || weight[0].steps > in.steps * in.segments);
+    const bool weights_first = g.dw[0] && (!g.dx || weight[0].steps / split.dw > in.steps * in.segments / split.dx);
     p.problems = 0;
-    if (g.dx && !weights_first) p.prob[p.problems++] = in;
+    if (g.dx && !weights_first) add(in, split.dx);
     if (g.dw[0])
-        for (int i = 0; i < g.both; ++i) p.prob[p.problems++] = weight[i];
-    if (g.dx && weights_first) p.prob[p.problems++] = in;
-    return p.problems ? launch_mm(kMmStore, p, sms, pdl, s, nullptr) : cudaSuccess;
+        for (int i = 0; i < g.both; ++i) add(weight[i], split.dw);
+    if (g.dx && weights_first) add(in, split.dx);
+    if (!p.problems) return cudaSuccess;
+    return join.joins ? launch_mm_pair(kMmStore, p, sms, s, nullptr) : launch_mm(kMmStore, p, sms, s, nullptr);
 }
 
 cudaError_t zero_rows(void *p, int64_t stride, int rows, int cols, cudaStream_t s) {
@@ -242,10 +385,10 @@ uint64_t mm_wait_ns() {
 #endif
 }
 
-cudaError_t launch_mm(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStream_t s, int64_t *part_rows) {
+cudaError_t launch_mm(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_t *part_rows) {
     MmFewPlan plan;
-    if (plan_mm_few(epi, p, sms, &plan)) return launch_mm_few(epi, p, plan, pdl, s, part_rows);
-    return launch_mm_pair(epi, p, sms, pdl, s, part_rows);
+    if (plan_mm_few(epi, p, sms, &plan)) return launch_mm_few(epi, p, plan, s, part_rows);
+    return launch_mm_pair(epi, p, sms, s, part_rows);
 }
 
 cudaError_t launch_linear(const wz_linear_args &a, cudaStream_t s) {
@@ -257,7 +400,7 @@ cudaError_t launch_linear(const wz_linear_args &a, cudaStream_t s) {
     p.bias[0] = a.bias;
     p.residual = half(a.residual), p.residual_stride = a.residual_stride;
     p.pre[0] = half(a.pre), p.pre_stride[0] = a.pre_stride;
-    return launch_mm(kMmStore, p, sms, false, s, nullptr);
+    return launch_mm(kMmStore, p, sms, s, nullptr);
 }
 
 cudaError_t launch_gated(const wz_gated_args &a, cudaStream_t s) {
@@ -269,11 +412,16 @@ cudaError_t launch_gated(const wz_gated_args &a, cudaStream_t s) {
     p.bias[0] = a.b_gate, p.bias[1] = a.b_up;
     p.pre[0] = half(a.gate), p.pre_stride[0] = a.gate_stride;
     p.pre[1] = half(a.up), p.pre_stride[1] = a.up_stride;
-    return launch_mm(kMmGated, p, sms, false, s, nullptr);
+    return launch_mm(kMmGated, p, sms, s, nullptr);
 }
 
-size_t linear_backward_bytes(int64_t M, int N) { return delta_bytes(M, N) + part_bytes(M, N); }
-size_t gated_backward_bytes(int64_t M, int N) { return 2 * (delta_bytes(M, N) + part_bytes(M, N)); }
+// d, sums over rows, shares' sums, one after the other.
+size_t linear_backward_bytes(int64_t M, int N, int K) {
+    return delta_bytes(M, N) + part_bytes(M, N) + shares_bytes(M, N, K, 1);
+}
+size_t gated_backward_bytes(int64_t M, int N, int K) {
+    return 2 * (delta_bytes(M, N) + part_bytes(M, N)) + shares_bytes(M, N, K, 2);
+}
 
 #define MM_TRY(call)                              \
     do {                                          \
@@ -286,13 +434,13 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
     if (sms < 2) return cudaErrorInvalidDevice;
     if (a.M == 0) {
         MM_TRY(zero_rows(a.dw, a.dw_stride, a.N, a.K, s));
-        return a.db ? launch_sum(nullptr, nullptr, a.db, nullptr, 0, a.N, false, s) : cudaSuccess;
+        JoinArgs join = join_args(nullptr, nullptr, a.db, nullptr, 0, a.N);
+        return launch_join(join, s);
     }
     const int64_t d_stride = pad8(a.N);
     __nv_bfloat16 *d = half((void *)ws);
     float *part = a.db ? reinterpret_cast<float *>(ws + delta_bytes(a.M, a.N)) : nullptr;
     int64_t part_rows = (a.M + kDeltaRows - 1) / kDeltaRows;
-    bool pdl = false;   // a kernel of this call is before the next one
     if (a.act != WZ_ACT_NONE && !a.pre) {
         MmArgs p = mm_args(a.act, a.device_status);
         forward_product(p, a.M, a.N, a.K, a.x, a.x_stride, a.w, a.w_stride, nullptr, 0);
@@ -300,8 +448,7 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
         p.bias[0] = a.bias;
         p.dy = half(a.dy), p.dy_stride = a.dy_stride;
         p.part[0] = part;
-        MM_TRY(launch_mm(kMmSlope, p, sms, false, s, &part_rows));
-        pdl = true;
+        MM_TRY(launch_mm(kMmSlope, p, sms, s, &part_rows));
     } else if (a.act != WZ_ACT_NONE || part) {
         DeltaArgs p;
         memset(&p, 0, sizeof(p));
@@ -310,8 +457,7 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
         p.d[0] = d, p.d_stride = d_stride;
         p.part[0] = part;
         p.M = a.M, p.N = a.N, p.act = a.act;
-        MM_TRY(launch_delta(a.act == WZ_ACT_NONE ? kDeltaSums : kDeltaSlope, p, false, s));
-        pdl = true;
+        MM_TRY(launch_delta(a.act == WZ_ACT_NONE ? kDeltaSums : kDeltaSlope, p, s));
     }
     Gradients g;
     memset(&g, 0, sizeof(g));
@@ -323,8 +469,10 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
     g.dx = a.dx, g.dx_stride = a.dx_stride;
     g.dw[0] = a.dw, g.dw_stride[0] = a.dw_stride;
     g.M = a.M, g.N = a.N, g.K = a.K;
-    MM_TRY(launch_gradients(g, a.device_status, sms, pdl, s));
-    return part ? launch_sum(part, nullptr, a.db, nullptr, part_rows, a.N, true, s) : cudaSuccess;
+    JoinArgs join = join_args(part, nullptr, a.db, nullptr, part_rows, a.N);
+    char *shares = ws ? ws + delta_bytes(a.M, a.N) + part_bytes(a.M, a.N) : nullptr;
+    MM_TRY(launch_gradients(g, shares, join, a.device_status, sms, s));
+    return launch_join(join, s);
 }
 
 cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cudaStream_t s) {
@@ -334,7 +482,8 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
     if (a.M == 0) {
         MM_TRY(zero_rows(a.dw_gate, a.dw_gate_stride, a.N, a.K, s));
         MM_TRY(zero_rows(a.dw_up, a.dw_up_stride, a.N, a.K, s));
-        return db[0] || db[1] ? launch_sum(nullptr, nullptr, db[0], db[1], 0, a.N, false, s) : cudaSuccess;
+        JoinArgs join = join_args(nullptr, nullptr, db[0], db[1], 0, a.N);
+        return launch_join(join, s);
     }
     const int64_t d_stride = pad8(a.N);
     const size_t db_at = 2 * delta_bytes(a.M, a.N);
@@ -352,7 +501,7 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
         p.d[0] = d[0], p.d[1] = d[1], p.d_stride = d_stride;
         p.part[0] = part[0], p.part[1] = part[1];
         p.M = a.M, p.N = a.N, p.act = a.act;
-        MM_TRY(launch_delta(kDeltaGated, p, false, s));
+        MM_TRY(launch_delta(kDeltaGated, p, s));
     } else {
         MmArgs p = mm_args(a.act, a.device_status);
         forward_product(p, a.M, a.N, a.K, a.x, a.x_stride, a.w_gate, a.w_gate_stride, a.w_up, a.w_up_stride);
@@ -361,7 +510,7 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
         p.bias[0] = a.b_gate, p.bias[1] = a.b_up;
         p.dy = half(a.dout), p.dy_stride = a.dout_stride;
         p.part[0] = part[0], p.part[1] = part[1];
-        MM_TRY(launch_mm(kMmGatedSlope, p, sms, false, s, &part_rows));
+        MM_TRY(launch_mm(kMmGatedSlope, p, sms, s, &part_rows));
     }
     Gradients g;
     memset(&g, 0, sizeof(g));
@@ -373,8 +522,9 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
     g.dw[0] = a.dw_gate, g.dw[1] = a.dw_up;
     g.dw_stride[0] = a.dw_gate_stride, g.dw_stride[1] = a.dw_up_stride;
     g.M = a.M, g.N = a.N, g.K = a.K;
-    MM_TRY(launch_gradients(g, a.device_status, sms, true, s));
-    return part[0] || part[1] ? launch_sum(part[0], part[1], db[0], db[1], part_rows, a.N, true, s) : cudaSuccess;
+    JoinArgs join = join_args(part[0], part[1], db[0], db[1], part_rows, a.N);
+    MM_TRY(launch_gradients(g, ws + 2 * (delta_bytes(a.M, a.N) + part_bytes(a.M, a.N)), join, a.device_status, sms, s));
+    return launch_join(join, s);
 }
 
 }  // namespace wz

@@ -407,7 +407,7 @@ bool plan_mm_few(MmEpilogue epi, const MmArgs &p, int sms, MmFewPlan *plan) {
     return true;
 }
 
-cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool pdl, cudaStream_t s,
+cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, cudaStream_t s,
                           int64_t *part_rows) {
     const int group = plan.pair ? 2 : 1, own = (mm_both(epi) ? kLanes / 2 : kLanes) * group;
     MmMapList list;
@@ -462,7 +462,7 @@ cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool
     const cudaError_t e = allow_smem(fn, smem);
     if (e != cudaSuccess) return e;
     void *args[] = {&list.maps, &p};
-    return launch_kernel(fn, dim3((unsigned)(clusters * p.cluster)), dim3(kThreads), smem, s, args, pdl,
+    return launch_kernel(fn, dim3((unsigned)(clusters * p.cluster)), dim3(kThreads), smem, s, args, true,
                          (unsigned)p.cluster);
 }
 

@@ -54,6 +54,7 @@ static_assert(kSmemBytes <= 227 * 1024, "shared memory of the pair CTA");
 
 struct Tile {
     int prob, row0, rows, n;   // rows: a multiple of 32, those behind the last one among them
+    int part, step, steps;     // share of K: the first step and their number
 };
 
 // The tiles of a pair, product by product.  A product's first `head` tiles go to the pairs from
@@ -91,6 +92,12 @@ struct Walk {
         // kGroupRows row tiles at a time, output tile by output tile: pairs that run
         // side by side share both operands' tiles in L2
         const MmProblem &q = p.prob[i];
+        int x = this->x;
+        this->x += stride;
+        tile.part = 0;
+        for (const int each = q.mt * q.nt; x >= each; x -= each) ++tile.part;
+        tile.step = tile.part * q.share + min(tile.part, q.more);
+        tile.steps = q.share + (tile.part < q.more ? 1 : 0);
         const int group = q.by_group.divide(x), m0 = group * kGroupRows, y = x - m0 * q.nt;
         const bool last = q.mt - m0 < kGroupRows;
         tile.prob = i;
@@ -98,7 +105,6 @@ struct Walk {
         tile.row0 = (m0 + y - tile.n * (last ? q.mt - m0 : kGroupRows)) * q.tile_m;
         const int r = q.M - tile.row0;
         tile.rows = r < q.tile_m ? (r + 31) / 32 * 32 : q.tile_m;
-        x += stride;
         return true;
     }
 };
@@ -161,30 +167,31 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
     const uint32_t rank = ptx::cluster_rank();
 
     if (warp == 2 && lane < p.maps) ptx::prefetch_tmap(&maps.m[lane]);
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            ptx::mbar_init(&S->full[s], 1);
-            ptx::mbar_init(&S->empty[s], 1);
+    if (warp == 0) {
+        if (lane < kStages) {
+            ptx::mbar_init(&S->full[lane], 1);
+            ptx::mbar_init(&S->empty[lane], 1);
+        } else if (lane < kStages + 2) {
+            ptx::mbar_init(&S->tfull[lane - kStages], 1);
+            ptx::mbar_init(&S->tempty[lane - kStages], 2 * kEpiWarps);
+        } else if (lane == 31) {
+            ptx::mbar_init(&S->drain, 1);
+            S->abort = 0;
         }
-        for (int b = 0; b < 2; ++b) {
-            ptx::mbar_init(&S->tfull[b], 1);
-            ptx::mbar_init(&S->tempty[b], 2 * kEpiWarps);
-        }
-        ptx::mbar_init(&S->drain, 1);
-        S->abort = 0;
         ptx::fence_barrier_init();
-        ptx::fence_proxy_async_smem();
+        __syncwarp();
     }
+    pdl_wait();   // an operand may be the previous grid's output
+    ptx::cluster_sync();   // both CTAs' barriers are ready
+    pdl_trigger();
     if (warp == 1) {
+        // (tensor memory is taken while the first copies are under way)
         ptx::tmem_alloc_pair(&S->tmem_base, 2 * kAccCols);
         ptx::tmem_relinquish_pair();
     }
-    pdl_wait();   // an operand may be the previous grid's output
-    __syncthreads();
-    pdl_trigger();
-    ptx::cluster_sync();   // both CTAs' barriers are ready
+    if (warp != 0) asm volatile("bar.sync 15, %0;" ::"n"(kThreads - 32) : "memory");   // all but the copies' warp
     ptx::tc_fence_after();
-    const uint32_t tmem = S->tmem_base;
+    const uint32_t tmem = warp != 0 ? *(volatile uint32_t *)&S->tmem_base : 0;
     Walk walk(p, (int)blockIdx.x >> 1, (int)gridDim.x >> 1);
     Tile t;
 
@@ -203,10 +210,12 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                 // an operand K-major is one box (a gated product's weights two), MN-major one for each 64 rows
                 const int boxes = a_mn ? (t.rows / 2 + 63) / 64 : 1, ends = q.steps * kStepK;
                 const uint32_t bytes = 2u * (uint32_t)(kOperandBytes + (a_mn ? boxes * kBoxBytes : q.box_rows * kStepK * 2));
-                for (int seg = 0; ok && seg < q.segments; ++seg) {
+                int left = t.steps, k = t.step * kStepK;
+                for (int seg = 0; ok && left > 0; ++seg, k -= ends) {
+                    if (k >= ends) continue;   // the share begins in a later segment
                     const CUtensorMap *a = &maps.m[q.a[seg]], *b = &maps.m[q.b[kBoth ? 0 : seg]];
                     const CUtensorMap *b2 = &maps.m[q.b[1]];
-                    for (int k = 0; k < ends; k += kStepK) {
+                    for (; k < ends && left > 0; k += kStepK, --left) {
                         if (!ptx::mbar_wait(&S->empty[stage], phase, p.wait_ns)) {
                             give_up(p, abort_flag);
                             ok = false;
@@ -261,7 +270,7 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                 ptx::tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(b * kAccCols);
                 uint32_t more = 0;
-                for (int left = q.segments * q.steps; left > 0; --left) {
+                for (int left = t.steps; left > 0; --left) {
                     if (!ptx::mbar_wait(&S->full[stage], phase, p.wait_ns)) {
                         give_up(p, abort_flag);
                         ok = false;
@@ -337,6 +346,14 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                         float x[kUnitRows];
                         mm_read16(tcol + (uint32_t)c, x);
                         read(c + kStride >= rows);
+                        if (EPI == kMmStore && q.sums) {   // a share of K: the sums as they are
+                            float *to = q.sums + ((int64_t)t.part * q.M + t.row0 + c) * q.N + i;
+                            const int count = there - c;
+#pragma unroll
+                            for (int j = 0; j < kUnitRows; ++j)
+                                if (j < count) to[(int64_t)j * q.N] = x[j];
+                            continue;
+                        }
 #pragma unroll
                         for (int j = 0; j < kUnitRows; ++j) x[j] += bias;
                         if (EPI == kMmStore && pre) {
@@ -427,7 +444,8 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
         }
     }
     __syncthreads();
-    ptx::cluster_sync();   // no commit or arrival is under way to either CTA
+    // no commit or arrival is under way to either CTA (the arrival waits for no store)
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
     if (warp == 1) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc_pair(tmem, 2 * kAccCols);
@@ -451,32 +469,35 @@ int MmMapList::add(const MmOperand &o, int box_rows) {
 
 namespace {
 
-// Rows of a tile: 256, or the rows dealt evenly to as few tiles.
-int even_tile(int M) {
-    const int64_t tiles = ((int64_t)M + kAccCols - 1) / kAccCols;
-    return (int)(((int64_t)M + tiles * 32 - 1) / (tiles * 32) * 32);
-}
-
 // What a tile takes: a step is bound by its products, two cycles a row, or by what a CTA's
 // 128 outputs and half of the rows bring in, 64 bytes a cycle; the epilogue takes 5,000 cycles.
 int64_t tile_cost(const MmProblem &q) {
-    return std::max<int64_t>((int64_t)q.segments * q.steps * std::max(2 * q.tile_m, 256 + q.tile_m), 5000);
+    return std::max<int64_t>((int64_t)(q.share + 1) * std::max(2 * q.tile_m, 256 + q.tile_m), 5000);
 }
 
 }  // namespace
 
-cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStream_t s, int64_t *part_rows) {
+// Rows of a tile: 256, or the rows dealt evenly to as few tiles.
+int mm_pair_tile(int64_t M) {
+    const int64_t tiles = M > 0 ? (M + kAccCols - 1) / kAccCols : 1;
+    return (int)((M + tiles * 32 - 1) / (tiles * 32) * 32);
+}
+
+cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_t *part_rows) {
     const int tile_n = mm_both(epi) ? kOutputs : 2 * kOutputs;
     int64_t tiles = 0;
     MmMapList list;
     for (int i = 0; i < p.problems; ++i) {
         MmProblem &q = p.prob[i];
-        q.tile_m = even_tile(q.M);
+        q.tile_m = mm_pair_tile(q.M);
         q.box_rows = q.tile_m / 2;   // a CTA's
         q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
         q.nt = (q.N + tile_n - 1) / tile_n;
-        if ((int64_t)q.mt * q.nt > INT32_MAX / 4) return cudaErrorInvalidValue;
-        q.tiles = q.mt * q.nt;
+        if ((int64_t)q.mt * q.nt > INT32_MAX / 32) return cudaErrorInvalidValue;
+        q.split = q.sums ? q.split : 1;
+        q.share = q.segments * q.steps / q.split;
+        q.more = q.segments * q.steps % q.split;
+        q.tiles = q.mt * q.nt * q.split;
         tiles += q.tiles;
         q.by_group.set((uint32_t)(kGroupRows * q.nt));
         q.by_last.set((uint32_t)(q.mt % kGroupRows ? q.mt % kGroupRows : kGroupRows));
@@ -514,7 +535,7 @@ cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStr
         skip = 0;
     }
     void *args[] = {&list.maps, &p};
-    return launch_kernel(fn, dim3(2 * pairs), dim3(kThreads), kSmemBytes, s, args, pdl, 2);
+    return launch_kernel(fn, dim3(2 * pairs), dim3(kThreads), kSmemBytes, s, args, true, 2);
 }
 
 }  // namespace wz

@@ -358,8 +358,8 @@ cudaError_t launch_attend(const wz_attend_args &a, void *workspace, cudaStream_t
 // A layer's matrix products (layer.cu, mm_pair.cu); arguments checked.
 cudaError_t launch_linear(const wz_linear_args &a, cudaStream_t s);
 cudaError_t launch_gated(const wz_gated_args &a, cudaStream_t s);
-size_t linear_backward_bytes(int64_t M, int N);
-size_t gated_backward_bytes(int64_t M, int N);
+size_t linear_backward_bytes(int64_t M, int N, int K);
+size_t gated_backward_bytes(int64_t M, int N, int K);
 cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *workspace, cudaStream_t s);
 cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *workspace, cudaStream_t s);
 // Max-over-query relevance in one pass over the features (maxsim.cu): token

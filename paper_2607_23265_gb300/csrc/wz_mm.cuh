@@ -66,15 +66,16 @@ struct MmProblem {
     MmOperand from_a[2], from_b[2];   // host: the operands
     // set by the launch
     int a[2], b[2];        // their tensor maps
-    int mt, nt, tiles;     // tiles along M and N, and all of them
+    float *sums;           // pairs, K shared: [split][M][N] sums of the shares
+    int mt, nt, tiles;     // tiles along M and N, and all of them (with shared K, of all shares)
     int tile_m;            // rows of a tile
     MmDivisor by_mt;       // few-rows kernel
     MmDivisor by_group, by_last;   // pairs: tiles of a group of row tiles, row tiles of the last one
     int head, from, skip;  //   its first tiles, for the pairs from one on, the turn's first
     int box_rows;          // a CTA's
-    int share, more;       // few-rows kernel: K steps of a share, shares that have one more
-    int split;             //   shares of a tile's K,
-    int first;             //   first cluster
+    int split;             // shares of a tile's K
+    int share, more;       //   K steps of a share, shares that have one more
+    int first;             // few-rows kernel: first cluster
 };
 
 struct MmArgs {
@@ -343,16 +344,20 @@ __device__ __forceinline__ void mm_read16(uint32_t tcol, float (&x)[16]) {
 }
 
 // ---- launches (arguments checked) ------------------------------------------------
+// All with programmatic stream serialization, the first of a call too: each kernel waits for
+// the grid before it, whoever's it is, before it touches memory, so that only its start
+// overlaps that grid's end.
 
 // The most rows of sums over rows that a launch writes for M rows.
 __host__ __device__ inline int64_t mm_part_rows(int64_t M) { return (M + 31) / 32 + 16; }
 
 // The products with the kernel that suits their sizes; part_rows (nullable): the rows of
 // sums that it writes.
-cudaError_t launch_mm(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStream_t s, int64_t *part_rows);
+cudaError_t launch_mm(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_t *part_rows);
 
-// Tiles of 256 x 256 on pairs of SMs (mm_pair.cu).
-cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, bool pdl, cudaStream_t s, int64_t *part_rows);
+// Tiles of 256 outputs x up to 256 rows on pairs of SMs (mm_pair.cu).
+int mm_pair_tile(int64_t M);   // their rows
+cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_t *part_rows);
 
 // Tiles of 16 to 256 rows on one SM or a pair, K shared by a cluster (mm_few.cu).  False:
 // they do not suit it.
@@ -363,7 +368,7 @@ struct MmFewPlan {
     bool shared[kMmProblems];                   // whether a product's K is shared
 };
 bool plan_mm_few(MmEpilogue epi, const MmArgs &p, int sms, MmFewPlan *plan);
-cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, bool pdl, cudaStream_t s,
+cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, cudaStream_t s,
                           int64_t *part_rows);
 
 uint64_t mm_wait_ns();   // the limit of the products' waits
