@@ -329,6 +329,12 @@ cudaError_t launch_gradients(const Gradients &g, char *shares, JoinArgs &join, i
         q.from_a[0] = d;
         q.from_b[0] = MmOperand{g.x, g.M, g.K, g.x_stride};
     }
+    // (dx alone may suit the kernel for few tiles, which joins shares of K by itself)
+    if (g.dx && !g.dw[0]) {
+        MmFewPlan plan;
+        p.prob[0] = in;
+        if (plan_mm_few(kMmStore, p, sms, &plan)) return launch_mm_few(kMmStore, p, plan, s, nullptr);
+    }
     const GradientSplit split = split_gradients(g.M, g.N, g.K, g.both, g.dx, g.dw[0]);
     const auto add = [&](MmProblem &q, int shared) {
         q.split = shared;

@@ -20,7 +20,9 @@
 // for its cluster, so no CTA may be left without: all take 256 columns at most, and more than
 // a third of an SM's shared memory, and the pairs of mm_pair.cu leave too little for one.
 #include <algorithm>
+#include <atomic>
 #include <cstring>
+#include <mutex>
 #include <type_traits>
 
 #include "wz_mm.cuh"
@@ -49,7 +51,7 @@ struct Shared {
 constexpr size_t kExtra = 1024 + sizeof(Shared);
 // an SM has 228 KB, of which a CTA's first kilobyte is the system's
 constexpr size_t kSmHas = 228 * 1024;
-constexpr size_t kSmemTwo = kSmHas / 2 - 1024;        // two CTAs an SM
+constexpr size_t kSmemTwo = kSmHas / 2 - 2048;        // two CTAs an SM
 constexpr size_t kSmemOne = 227 * 1024;
 constexpr size_t kSmemLeast = kSmHas / 3;             // not three
 
@@ -372,6 +374,42 @@ bool fits(MmEpilogue epi, const MmProblem &q, bool pair, int tile_m, int split) 
     return (epi != kMmSlope && epi != kMmGatedSlope) || tiles * split <= mm_part_rows(q.M);
 }
 
+// Clusters of each size that the current device has room for with one CTA an SM (a property of the device,
+// asked for once); null on an error.  With two CTAs an SM there is room for about twice as many; the
+// runtime's answer for such sizes is that of one.
+struct Places {
+    int n[kMaxCluster + 1];
+};
+
+const Places *cluster_places() {
+    constexpr int kDevices = 64;
+    static std::mutex mu;
+    static Places places[kDevices];
+    static std::atomic<int> known[kDevices];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return nullptr;
+    if (known[dev].load(std::memory_order_acquire)) return &places[dev];
+    std::lock_guard<std::mutex> lock(mu);
+    const void *fn = (const void *)mm_few_kernel<kMmStore, false>;
+    if (allow_smem(fn, kSmemOne) != cudaSuccess) return nullptr;
+    for (int size = 1; size <= kMaxCluster; ++size) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)size);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = kSmemOne;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)size;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&places[dev].n[size], fn, &cfg) != cudaSuccess || places[dev].n[size] < 1)
+            return nullptr;
+    }
+    known[dev].store(1, std::memory_order_release);
+    return &places[dev];
+}
+
 #ifdef WZ_CHECKED
 int check_kind = 0, check_split = 1, check_tile = 64;
 #endif
@@ -396,15 +434,60 @@ bool plan_mm_few(MmEpilogue epi, const MmArgs &p, int sms, MmFewPlan *plan) {
     }
 #endif
     if (p.problems > 1) return false;
+    // What a call takes, in cycles, fitted to 9 weights (512 x 512 to 14336 x 3584) of 1 to 2,048 rows, plain
+    // and gated, with up to 60 plans each: the plan that it chooses is 2 % slower than the fastest on
+    // average, 14 % at most.  A step of K is bound by what comes into an SM or by its issue, a pair's wide
+    // ones by the products; all of them together by HBM (the weights once, up to 3,700 bytes a cycle
+    // from two CTAs an SM, 3,200 from 84); clusters that find no place share SMs.  Examples, us, this file's best / mm_pair.cu's: 80 x 14336 x 3584 (rows x K x
+    // outputs) 21 / 49, 512 x 14336 x 3584 41 / 66, 333 x 3584 x 4608 15.5 / 17.7, 128 x 1152 x 1152 4.9 / 7.2, but
+    // 1100 x 3584 x 3584 30 / 20 and 333 x 1152 x 4608 9.6 / 9.4.
     const MmProblem &q = p.prob[0];
-    if (q.M > 64) return false;
-    plan->pair = false;
-    plan->tile_m[0] = round_up(std::min(q.M, 64), 16);
-    const int own = mm_both(epi) ? kLanes / 2 : kLanes, tiles = (q.N + own - 1) / own;
-    plan->split = std::max(1, std::min({kMaxCluster, sms / tiles, q.segments * q.steps}));
-    while (!fits(epi, q, false, plan->tile_m[0], plan->split)) --plan->split;
-    plan->shared[0] = plan->split > 1;
-    return true;
+    const int both = mm_both(epi) ? 1 : 0, total = q.segments * q.steps;
+    const auto ceil_div = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+    const int64_t weights = (int64_t)q.N * total * kStepK * 2 * (both + 1);
+    const bool slopes = epi == kMmSlope || epi == kMmGatedSlope;
+    // rows that do not begin on 128 bytes come in as two lines each
+    const int lines = (q.from_a[0].stride | q.from_b[0].stride) % 64 ? 2 : 1;
+    const int wide = mm_pair_tile(q.M);
+    const int64_t rounds = ceil_div(ceil_div(q.M, wide) * ceil_div((int64_t)q.N << both, 2 * kLanes), sms / 2);
+    if (rounds > 3) return false;
+    const Places *places = cluster_places();
+    if (!places) return false;
+    int64_t best = 6900 + wide * (both ? 18 : 11) +
+                   std::max(rounds * total * std::max(2 * wide, (295 + wide) * lines), weights / 3250);
+    bool few = false;
+    for (int pair = 0; pair < 2; ++pair) {
+        const int even = pair ? 32 : 16, group = pair + 1;
+        int last = 0;
+        for (int k = 1; k <= 8; ++k) {
+            const int64_t tile = ceil_div(ceil_div(q.M, k), even) * even;
+            if (tile > 256 || tile == last) continue;
+            last = (int)tile;
+            const int64_t tiles = ceil_div(q.M, tile) * ceil_div((int64_t)q.N << both, kLanes * group);
+            const int64_t step = pair ? std::max<int64_t>({2 * tile, (190 + tile * 11 / 8) * lines, 338})
+                                      : std::max<int64_t>((190 + 2 * tile) * lines, 362);
+            for (int split = 1; split * group <= kMaxCluster; ++split) {
+                const int size = split * group;
+                // (clusters of five that fill their places: a row of 3584 x 3584 10.4 us, four 7.8)
+                if (size == 5 || size == 7 || !fits(epi, q, pair, (int)tile, split)) continue;
+                const int64_t waves = tiles <= places->n[size] ? 1 : 2 * ceil_div(tiles, 2 * places->n[size]);
+                if (waves > 6) break;
+                // joined: through the cluster's shared memory; else through the CTA's own
+                const int64_t end = (split > 1 ? 48 * tile + 173 * size : 200 + 38 * tile) + (slopes ? 25 * tile : 0);
+                const int64_t streamed = weights / (3900 - 60000 / std::max<int64_t>(tiles * size, 40));
+                const int64_t t = 5100 + std::max(waves * ceil_div(total, split) * step, streamed) + end * (6 * waves + 1) / 7;
+                if (t < best) {
+                    best = t;
+                    few = true;
+                    plan->pair = pair;
+                    plan->split = split;
+                    plan->tile_m[0] = (int)tile;
+                    plan->shared[0] = split > 1;
+                }
+            }
+        }
+    }
+    return few;
 }
 
 cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, cudaStream_t s,
@@ -440,7 +523,9 @@ cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, cuda
     if (!list.ok || clusters * p.cluster > INT32_MAX) return cudaErrorInvalidValue;
     p.maps = list.count;
     p.stage_bytes = round_up(p.stage_bytes, 1024);
-    const bool two = dump + kExtra <= kSmemTwo && clusters * p.cluster > sm_count();
+    const Places *places = cluster_places();
+    if (!places) return cudaErrorInvalidDevice;
+    const bool two = dump + kExtra <= kSmemTwo && clusters > places->n[p.cluster];
     const size_t most = (two ? kSmemTwo : kSmemOne) - kExtra;
     // joined sums have a place of their own where six stages are left, or as many as there are steps
     p.apart = dump > 0 && (size_t)(std::min(most_steps, 6) * p.stage_bytes + dump) <= most;
@@ -475,5 +560,20 @@ extern "C" __attribute__((visibility("default"))) void wz_check_mm_plan(int kind
     wz::check_kind = kind;
     wz::check_split = split;
     wz::check_tile = tile_m;
+}
+// Test hook: what a forward product of aligned rows takes on the current device: the kind, shares and tile of
+// wz_check_mm_plan.
+extern "C" __attribute__((visibility("default"))) int wz_check_mm_choice(int gated, int64_t M, int N, int K, int *split, int *tile) {
+    const int sms = wz::sm_count();
+    if (sms < 2) return -1;
+    wz::MmArgs p;
+    memset(&p, 0, sizeof(p));
+    p.problems = 1;
+    wz::MmProblem &q = p.prob[0];
+    q.M = (int)M, q.N = N, q.segments = 1, q.steps = (K + 63) / 64;
+    wz::MmFewPlan plan;
+    if (!wz::plan_mm_few(gated ? wz::kMmGated : wz::kMmStore, p, sms, &plan)) return 1;
+    *split = plan.split, *tile = plan.tile_m[0];
+    return plan.pair ? 3 : 2;
 }
 #endif
