@@ -118,13 +118,18 @@ namespace {
 
 constexpr int kSumRows = 16, kSumThreads = 32 * kSumRows;
 constexpr int kJoinRows = 4;   // rows that a thread of a join takes
+// Up to so many rows the last kernel adds dy's up by itself: a kernel less before the products (577 x 3584:
+// 3.7 us of 23).
+constexpr int64_t kSumsInJoin = 1024;
 
 // What is left to add up when the products are done.
 struct JoinArgs {
-    // bias gradients: db[i][n] = the sum of part[i][.][n]
+    // bias gradients: db[i][n] = the sum of part[i][.][n], or of dy's rows
     const float *part[2];
     float *db[2];
     int64_t part_rows;
+    const __nv_bfloat16 *dy;
+    int64_t dy_stride, dy_rows;
     int N;
     // products whose K was shared: out = the sum of sums[split][M][cols]
     struct {
@@ -154,8 +159,12 @@ __global__ void __launch_bounds__(kSumThreads) mm_join_kernel(const __grid_const
         const int c = (int)threadIdx.x & 31, r0 = (int)threadIdx.x >> 5;
         const int n = (int)(block - which * p.sum_blocks) * 32 + c;
         float s = 0.f;
-        if (n < p.N && out)
+        if (n < p.N && out) {
+#pragma unroll 8
             for (int64_t r = r0; r < p.part_rows; r += kSumRows) s += part[(size_t)r * p.N + n];
+#pragma unroll 8
+            for (int64_t r = r0; r < p.dy_rows; r += kSumRows) s += __bfloat162float(p.dy[r * p.dy_stride + n]);
+        }
         sums[r0][c] = s;
         __syncthreads();
         if (r0 == 0 && n < p.N && out) {
@@ -175,22 +184,30 @@ __global__ void __launch_bounds__(kSumThreads) mm_join_kernel(const __grid_const
     if (left <= 0) return;
     const int64_t plane = j.M * j.cols;
     const bool wide = left >= 4 && j.cols % 4 == 0;
+    if (wide && m0 + 4 * (kJoinRows - 1) < j.M) {
+        float x[kJoinRows][4] = {};
+        const float *from = j.sums + m0 * j.cols + n;
+#pragma unroll 2
+        for (int k = 0; k < j.split; ++k, from += plane) {
+            float4 v[kJoinRows];
 #pragma unroll
+            for (int r = 0; r < kJoinRows; ++r) v[r] = __ldcs(reinterpret_cast<const float4 *>(from + 4 * r * (int64_t)j.cols));
+#pragma unroll
+            for (int r = 0; r < kJoinRows; ++r) x[r][0] += v[r].x, x[r][1] += v[r].y, x[r][2] += v[r].z, x[r][3] += v[r].w;
+        }
+#pragma unroll
+        for (int r = 0; r < kJoinRows; ++r) mm_store4(j.out + (m0 + 4 * r) * j.out_stride + n, x[r], 4);
+        return;
+    }
     for (int r = 0; r < kJoinRows; ++r) {
         const int64_t m = m0 + 4 * r;
         if (m >= j.M) break;
         const float *from = j.sums + m * j.cols + n;
         float x[4] = {};
-        for (int k = 0; k < j.split; ++k, from += plane) {
-            if (wide) {
-                const float4 v = __ldcs(reinterpret_cast<const float4 *>(from));
-                x[0] += v.x, x[1] += v.y, x[2] += v.z, x[3] += v.w;
-            } else {
+        for (int k = 0; k < j.split; ++k, from += plane)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (e < left) x[e] += from[e];
-            }
-        }
+            for (int e = 0; e < 4; ++e)
+                if (e < left) x[e] += from[e];
         mm_store4(j.out + m * j.out_stride + n, x, left);
     }
 }
@@ -276,10 +293,16 @@ int64_t split_cost(int64_t tx, int64_t cx, int64_t bx, int sx, int64_t tw, int64
 }
 
 GradientSplit split_gradients(int64_t M, int N, int K, int both, bool dx, bool dw) {
-    const auto cost = [](int64_t rows) { return std::max<int64_t>(2 * mm_pair_tile(rows), 256 + mm_pair_tile(rows)); };
-    const auto tiles = [](int64_t rows, int64_t outs) { return (rows + mm_pair_tile(rows) - 1) / mm_pair_tile(rows) * ((outs + 255) / 256); };
+    const auto cost = [](int64_t rows, int64_t outs) {
+        const int t = mm_pair_tile(rows, (outs + 255) / 256);
+        return std::max<int64_t>(2 * t, 256 + t);
+    };
+    const auto tiles = [](int64_t rows, int64_t outs) {
+        const int t = mm_pair_tile(rows, (outs + 255) / 256);
+        return (rows + t - 1) / t * ((outs + 255) / 256);
+    };
     const int64_t sx = both * steps_of(N), sw = steps_of(M);
-    const int64_t tx = dx ? tiles(M, K) : 0, tw = dw ? both * tiles(N, K) : 0, cx = sx * cost(M), cw = sw * cost(N);
+    const int64_t tx = dx ? tiles(M, K) : 0, tw = dw ? both * tiles(N, K) : 0, cx = sx * cost(M, K), cw = sw * cost(N, K);
     GradientSplit best{1, 1};
     int64_t least = split_cost(tx, cx, M * K, 1, tw, cw, (int64_t)both * N * K, 1);
     for (int a = 1; a <= (dx ? kMostShares : 1); ++a)
@@ -361,9 +384,10 @@ cudaError_t zero_rows(void *p, int64_t stride, int rows, int cols, cudaStream_t 
     return p ? cudaMemset2DAsync(p, (size_t)stride * 2, 0, (size_t)cols * 2, (size_t)rows, s) : cudaSuccess;
 }
 
-int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
+// Rows of d begin on 128 bytes: what does not comes into an SM as two lines for each box row.
+int64_t delta_stride(int N) { return ((int64_t)N + 63) / 64 * 64; }
 
-size_t delta_bytes(int64_t M, int N) { return pad256((size_t)M * (size_t)pad8(N) * 2); }
+size_t delta_bytes(int64_t M, int N) { return pad256((size_t)M * (size_t)delta_stride(N) * 2); }
 
 size_t part_bytes(int64_t M, int N) { return pad256((size_t)mm_part_rows(M) * (size_t)N * 4); }
 
@@ -443,7 +467,7 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
         JoinArgs join = join_args(nullptr, nullptr, a.db, nullptr, 0, a.N);
         return launch_join(join, s);
     }
-    const int64_t d_stride = pad8(a.N);
+    const int64_t d_stride = delta_stride(a.N);
     __nv_bfloat16 *d = half((void *)ws);
     float *part = a.db ? reinterpret_cast<float *>(ws + delta_bytes(a.M, a.N)) : nullptr;
     int64_t part_rows = (a.M + kDeltaRows - 1) / kDeltaRows;
@@ -455,7 +479,7 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
         p.dy = half(a.dy), p.dy_stride = a.dy_stride;
         p.part[0] = part;
         MM_TRY(launch_mm(kMmSlope, p, sms, s, &part_rows));
-    } else if (a.act != WZ_ACT_NONE || part) {
+    } else if (a.act != WZ_ACT_NONE || (part && a.M > kSumsInJoin)) {
         DeltaArgs p;
         memset(&p, 0, sizeof(p));
         p.dy = half(a.dy), p.dy_stride = a.dy_stride;
@@ -476,6 +500,10 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
     g.dw[0] = a.dw, g.dw_stride[0] = a.dw_stride;
     g.M = a.M, g.N = a.N, g.K = a.K;
     JoinArgs join = join_args(part, nullptr, a.db, nullptr, part_rows, a.N);
+    if (a.act == WZ_ACT_NONE && a.M <= kSumsInJoin) {
+        join.part_rows = 0;
+        join.dy = half(a.dy), join.dy_stride = a.dy_stride, join.dy_rows = a.M;
+    }
     char *shares = ws ? ws + delta_bytes(a.M, a.N) + part_bytes(a.M, a.N) : nullptr;
     MM_TRY(launch_gradients(g, shares, join, a.device_status, sms, s));
     return launch_join(join, s);
@@ -491,7 +519,7 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
         JoinArgs join = join_args(nullptr, nullptr, db[0], db[1], 0, a.N);
         return launch_join(join, s);
     }
-    const int64_t d_stride = pad8(a.N);
+    const int64_t d_stride = delta_stride(a.N);
     const size_t db_at = 2 * delta_bytes(a.M, a.N);
     __nv_bfloat16 *d[2] = {half((void *)ws), half((void *)(ws + delta_bytes(a.M, a.N)))};
     float *part[2];

@@ -448,8 +448,9 @@ bool plan_mm_few(MmEpilogue epi, const MmArgs &p, int sms, MmFewPlan *plan) {
     const bool slopes = epi == kMmSlope || epi == kMmGatedSlope;
     // rows that do not begin on 128 bytes come in as two lines each
     const int lines = (q.from_a[0].stride | q.from_b[0].stride) % 64 ? 2 : 1;
-    const int wide = mm_pair_tile(q.M);
-    const int64_t rounds = ceil_div(ceil_div(q.M, wide) * ceil_div((int64_t)q.N << both, 2 * kLanes), sms / 2);
+    const int64_t outputs = ceil_div((int64_t)q.N << both, 2 * kLanes);
+    const int wide = mm_pair_tile(q.M, outputs);
+    const int64_t rounds = ceil_div(ceil_div(q.M, wide) * outputs, sms / 2);
     if (rounds > 3) return false;
     const Places *places = cluster_places();
     if (!places) return false;

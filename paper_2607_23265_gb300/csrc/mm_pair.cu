@@ -37,6 +37,7 @@ constexpr int kThreads = (2 + kEpiWarps) * 32;
 constexpr int kAccCols = 256;                            // the most rows of a tile
 constexpr int kUnitRows = 16;                            // rows that an epilogue warp takes at a time
 constexpr int kGiveFloats = kUnitRows * 32;              // sums that a warp of a gated product gives away
+constexpr int kPlanPairs = 76;                           // pairs of SMs that tiles are planned for
 constexpr int kGroupRows = 8;                            // row tiles that are walked together
 
 struct Shared {
@@ -477,10 +478,23 @@ int64_t tile_cost(const MmProblem &q) {
 
 }  // namespace
 
-// Rows of a tile: 256, or the rows dealt evenly to as few tiles.
-int mm_pair_tile(int64_t M) {
-    const int64_t tiles = M > 0 ? (M + kAccCols - 1) / kAccCols : 1;
-    return (int)((M + tiles * 32 - 1) / (tiles * 32) * 32);
+// Rows of a tile: the rows dealt evenly to as few tiles as hold them, or to one or two more where that
+// makes the rounds of tiles on the pairs cheaper (741 rows x 37 output tiles: 148 tiles of 192 rows are two
+// rounds as 111 of 256 are).
+int mm_pair_tile(int64_t M, int64_t output_tiles) {
+    const int64_t least = M > 0 ? (M + kAccCols - 1) / kAccCols : 1;
+    int best = 0;
+    int64_t cost = 0;
+    for (int64_t k = least; k <= least + (least <= 8 ? 2 : 0); ++k) {
+        const int64_t tile = (std::max<int64_t>(M, 1) + k * 32 - 1) / (k * 32) * 32;
+        const int64_t tiles = (std::max<int64_t>(M, 1) + tile - 1) / tile * output_tiles;
+        const int64_t t = (tiles + kPlanPairs - 1) / kPlanPairs * std::max<int64_t>(2 * tile, 256 + tile);
+        if (!best || t < cost) {
+            best = (int)tile;
+            cost = t;
+        }
+    }
+    return best;
 }
 
 cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_t *part_rows) {
@@ -489,10 +503,10 @@ cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, i
     MmMapList list;
     for (int i = 0; i < p.problems; ++i) {
         MmProblem &q = p.prob[i];
-        q.tile_m = mm_pair_tile(q.M);
+        q.nt = (q.N + tile_n - 1) / tile_n;
+        q.tile_m = mm_pair_tile(q.M, q.nt);
         q.box_rows = q.tile_m / 2;   // a CTA's
         q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
-        q.nt = (q.N + tile_n - 1) / tile_n;
         if ((int64_t)q.mt * q.nt > INT32_MAX / 32) return cudaErrorInvalidValue;
         q.split = q.sums ? q.split : 1;
         q.share = q.segments * q.steps / q.split;

@@ -348,15 +348,16 @@ __device__ __forceinline__ void mm_read16(uint32_t tcol, float (&x)[16]) {
 // the grid before it, whoever's it is, before it touches memory, so that only its start
 // overlaps that grid's end.
 
-// The most rows of sums over rows that a launch writes for M rows.
-__host__ __device__ inline int64_t mm_part_rows(int64_t M) { return (M + 31) / 32 + 16; }
+// The most rows of sums over rows that a launch writes for M rows: mm_pair.cu's up to eight for each of at most
+// M / 256 + 3 row tiles.
+__host__ __device__ inline int64_t mm_part_rows(int64_t M) { return (M + 31) / 32 + 32; }
 
 // The products with the kernel that suits their sizes; part_rows (nullable): the rows of
 // sums that it writes.
 cudaError_t launch_mm(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_t *part_rows);
 
 // Tiles of 256 outputs x up to 256 rows on pairs of SMs (mm_pair.cu).
-int mm_pair_tile(int64_t M);   // their rows
+int mm_pair_tile(int64_t M, int64_t output_tiles);   // their rows
 cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_t *part_rows);
 
 // Tiles of 16 to 256 rows on one SM or a pair, K shared by a cluster (mm_few.cu).  False:
