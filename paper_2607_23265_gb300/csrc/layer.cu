@@ -460,13 +460,13 @@ size_t gated_backward_bytes(int64_t M, int N, int K) {
     } while (0)
 
 cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, cudaStream_t s) {
-    const int sms = sm_count();
-    if (sms < 2) return cudaErrorInvalidDevice;
     if (a.M == 0) {
         MM_TRY(zero_rows(a.dw, a.dw_stride, a.N, a.K, s));
         JoinArgs join = join_args(nullptr, nullptr, a.db, nullptr, 0, a.N);
         return launch_join(join, s);
     }
+    const int sms = sm_count();
+    if (sms < 2) return cudaErrorInvalidDevice;
     const int64_t d_stride = delta_stride(a.N);
     __nv_bfloat16 *d = half((void *)ws);
     float *part = a.db ? reinterpret_cast<float *>(ws + delta_bytes(a.M, a.N)) : nullptr;
@@ -510,8 +510,6 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
 }
 
 cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cudaStream_t s) {
-    const int sms = sm_count();
-    if (sms < 2) return cudaErrorInvalidDevice;
     float *db[2] = {a.db_gate, a.db_up};
     if (a.M == 0) {
         MM_TRY(zero_rows(a.dw_gate, a.dw_gate_stride, a.N, a.K, s));
@@ -519,6 +517,8 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
         JoinArgs join = join_args(nullptr, nullptr, db[0], db[1], 0, a.N);
         return launch_join(join, s);
     }
+    const int sms = sm_count();
+    if (sms < 2) return cudaErrorInvalidDevice;
     const int64_t d_stride = delta_stride(a.N);
     const size_t db_at = 2 * delta_bytes(a.M, a.N);
     __nv_bfloat16 *d[2] = {half((void *)ws), half((void *)(ws + delta_bytes(a.M, a.N)))};
