@@ -365,13 +365,14 @@ int sums_rows(int tile_m, int split) { return (tile_m + 4 * split - 1) / (4 * sp
 
 // Whether a product can take tiles of tile_m rows and `split` shares of K a tile: its sums
 // fit into tensor memory and, where they are joined, into shared memory, no share is
-// empty, and the sums over rows have a place.
+// empty, and the sums over rows have a place and a short enough share (kLongSteps).
 bool fits(MmEpilogue epi, const MmProblem &q, bool pair, int tile_m, int split) {
     const int even = pair ? 32 : 16;
     if (tile_m % even != 0 || tile_m < even || tile_m > 256) return false;
     if (split > q.segments * q.steps || split * (pair ? 2 : 1) > kMaxCluster) return false;
     const int64_t tiles = ((int64_t)q.M + tile_m - 1) / tile_m;
-    return (epi != kMmSlope && epi != kMmGatedSlope) || tiles * split <= mm_part_rows(q.M);
+    return (epi != kMmSlope && epi != kMmGatedSlope) ||
+           (tiles * split <= mm_part_rows(q.M) && q.steps <= kLongSteps * split);
 }
 
 // Clusters of each size that the current device has room for with one CTA an SM (a property of the device,

@@ -38,6 +38,11 @@ constexpr int kAccCols = 256;                            // the most rows of a t
 constexpr int kUnitRows = 16;                            // rows that an epilogue warp takes at a time
 constexpr int kGiveFloats = kUnitRows * 32;              // sums that a warp of a gated product gives away
 constexpr int kPlanPairs = 76;                           // pairs of SMs that tiles are planned for
+// The tensor cores cut off what a sum cannot hold each time that 16 products are added to it, so that long sums
+// come out a little too small: bias gradients, which are f32 and made of slopes at such sums, are 1.3e-6 off in norm
+// with K = 1,152, 4.6e-6 with 3,584 and 9.4e-6 with 14,336 (bf16 results do not notice).  Products that are formed
+// again for their slopes keep two sums when they have more steps than kLongSteps, of the even and of the odd ones, in
+// tiles of half the rows: 4.6e-6 with 14,336.  (mm_few.cu: a share of K for each as many steps.)
 constexpr int kGroupRows = 8;                            // row tiles that are walked together
 
 struct Shared {
@@ -271,7 +276,9 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                 ptx::tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(b * kAccCols);
                 uint32_t more = 0;
-                for (int left = t.steps; left > 0; --left) {
+                // (two sums, of the even and of the odd steps: see kLongSteps)
+                const int second = EPI == kMmSlope || EPI == kMmGatedSlope ? p.second : 0;
+                for (int left = t.steps, odd = 0; left > 0; --left, odd ^= 1) {
                     if (!ptx::mbar_wait(&S->full[stage], phase, p.wait_ns)) {
                         give_up(p, abort_flag);
                         ok = false;
@@ -281,8 +288,9 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                     const uint64_t so = (uint64_t)(stage * (kStageBytes >> 4));
 #pragma unroll
                     for (int k = 0; k < kStepK / 16; ++k)
-                        ptx::mma_bf16_pair(d, w_base + so + k * w_step, x_base + so + k * x_step, idesc, k ? 1u : more);
-                    more = 1;
+                        ptx::mma_bf16_pair(odd ? d + (uint32_t)second : d, w_base + so + k * w_step,
+                                           x_base + so + k * x_step, idesc, k ? 1u : more);
+                    if (!second || odd) more = 1;
                     ptx::mma_commit_pair(&S->empty[stage]);
                     if (++stage == kStages) {
                         stage = 0;
@@ -333,6 +341,15 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
             if (kBoth ? !pair_all(barrier, full) : !__all_sync(0xffffffffu, full)) break;
             ptx::tc_fence_after();
             const uint32_t tcol = tmem + ((uint32_t)(quadrant * 32) << 16) + (uint32_t)(b * kAccCols);
+            const auto sums = [&](int c, float (&x)[kUnitRows]) {
+                mm_read16(tcol + (uint32_t)c, x);
+                if ((EPI == kMmSlope || EPI == kMmGatedSlope) && p.second) {
+                    float y[kUnitRows];
+                    mm_read16(tcol + (uint32_t)(p.second + c), y);
+#pragma unroll
+                    for (int j = 0; j < kUnitRows; ++j) x[j] += y[j];
+                }
+            };
             const auto read = [&](bool last) {   // the warp's sums of the tile are read
                 if (!last) return;
                 ptx::tc_fence_before();
@@ -345,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                 for (int c = first; c < rows; c += kStride) {
                     if constexpr (!kBoth) {
                         float x[kUnitRows];
-                        mm_read16(tcol + (uint32_t)c, x);
+                        sums(c, x);
                         read(c + kStride >= rows);
                         if (EPI == kMmStore && q.sums) {   // a share of K: the sums as they are
                             float *to = q.sums + ((int64_t)t.part * q.M + t.row0 + c) * q.N + i;
@@ -382,8 +399,8 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                     } else {
                         // the gate's warp finishes the first 16 rows, the up projection's the others
                         float x[kUnitRows], y[kUnitRows];   // g and u
-                        mm_read16(tcol + (uint32_t)c, x);
-                        mm_read16(tcol + (uint32_t)(c + kUnitRows), y);
+                        sums(c, x);
+                        sums(c + kUnitRows, y);
                         read(c + kStride >= rows);
 #pragma unroll
                         for (int j = 0; j < kUnitRows; ++j) {
@@ -478,9 +495,15 @@ int64_t tile_cost(const MmProblem &q) {
 
 }  // namespace
 
-// Rows of a tile: the rows dealt evenly to as few tiles as hold them, or to one or two more where that
-// makes the rounds of tiles on the pairs cheaper (741 rows x 37 output tiles: 148 tiles of 192 rows are two
-// rounds as 111 of 256 are).
+// The rows dealt evenly to as few tiles of at most `most` rows as hold them.
+static int even_tile(int64_t M, int most) {
+    const int64_t k = (M + most - 1) / most;
+    return (int)((M + k * 32 - 1) / (k * 32) * 32);
+}
+
+// Rows of a tile: dealt evenly to as few tiles as hold them, or to one or two more where that makes the
+// rounds of tiles on the pairs cheaper (741 rows x 37 output tiles: 148 tiles of 192 rows are two rounds as
+// 111 of 256 are).
 int mm_pair_tile(int64_t M, int64_t output_tiles) {
     const int64_t least = M > 0 ? (M + kAccCols - 1) / kAccCols : 1;
     int best = 0;
@@ -505,6 +528,11 @@ cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, i
         MmProblem &q = p.prob[i];
         q.nt = (q.N + tile_n - 1) / tile_n;
         q.tile_m = mm_pair_tile(q.M, q.nt);
+        if (i == 0) {
+            const bool longs = (epi == kMmSlope || epi == kMmGatedSlope) && q.steps > kLongSteps;
+            p.second = longs ? kAccCols / 2 : 0;
+            if (longs && q.tile_m > kAccCols / 2) q.tile_m = even_tile(q.M, kAccCols / 2);
+        }
         q.box_rows = q.tile_m / 2;   // a CTA's
         q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
         if ((int64_t)q.mt * q.nt > INT32_MAX / 32) return cudaErrorInvalidValue;

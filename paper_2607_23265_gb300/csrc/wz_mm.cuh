@@ -18,6 +18,7 @@ namespace wz {
 constexpr int kMmMaps = 8;
 constexpr int kMmProblems = 3;
 constexpr uint64_t kMmTimeoutNs = 2000000000ull;
+constexpr int kLongSteps = 64;   // see mm_pair.cu
 
 struct MmMaps {
     CUtensorMap m[kMmMaps];   // 2D, boxes 64 wide with 128-byte swizzle
@@ -90,6 +91,7 @@ struct MmArgs {
     float *part[2];                         // [some rows][N] sums over rows; null: none
     int64_t residual_stride, dy_stride, pre_stride[2], out2_stride;
     int maps;                               // tensor maps in use
+    int second;                             // pairs: columns from the even steps' sums to the odd ones'; 0: one
     int cluster;                            // few-rows kernel: CTAs of a cluster, the ring,
     MmDivisor by_cluster;
     int stages, stage_bytes, ring_bytes;
@@ -349,8 +351,8 @@ __device__ __forceinline__ void mm_read16(uint32_t tcol, float (&x)[16]) {
 // overlaps that grid's end.
 
 // The most rows of sums over rows that a launch writes for M rows: mm_pair.cu's up to eight for each of at most
-// M / 256 + 3 row tiles.
-__host__ __device__ inline int64_t mm_part_rows(int64_t M) { return (M + 31) / 32 + 32; }
+// M / 128 + 3 row tiles.
+__host__ __device__ inline int64_t mm_part_rows(int64_t M) { return (M + 15) / 16 + 32; }
 
 // The products with the kernel that suits their sizes; part_rows (nullable): the rows of
 // sums that it writes.

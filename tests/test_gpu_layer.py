@@ -139,6 +139,19 @@ def test_backward(wz, M, N, K, act, kept):
     gated_backward(wz, M, N, K, act, kept)
 
 
+@pytest.mark.parametrize("M,N,K", [(5, 200, 4200), (150, 130, 4099), (300, 520, 5000), (700, 300, 14336)])
+def test_long_sums_formed_again(wz, M, N, K):
+    """Products of more than 4,096 terms for their slopes: a bias gradient, a sum of M slopes of them in fp32, within 1e-5 of
+    64 bits in norm (what 16 products cut off, 2^-24 of the sum at most, K / 16 times over half of K, stays below)."""
+    act = "silu"
+    s = Layer(M, N, K, 2, bias=True, pad=0, seed=K)
+    linear_backward(wz, M, N, K, act, False)
+    gated_backward(wz, M, N, K, act, False)
+    got = wz.wz_gated_backward(s.dy, s.x, *s.w, act=act, b_gate=s.b[0], b_up=s.b[1], need_b=True, need_x=False, need_w=False)
+    for (d, _), db in zip(ref.gated_delta(s.dy, s.x, *s.w, *s.b, None, None, act), got[3:]):
+        assert float((db.double() - d.sum(0)).norm() / d.sum(0).norm()) < 1e-5
+
+
 # persistent pairs of SMs; tiles on one SM and on pairs: one share of K, several, narrow and wide row tiles
 PLANS = [(1, 1, 64), (2, 1, 64), (2, 2, 16), (2, 3, 208), (2, 8, 48), (2, 5, 176), (2, 1, 256),
          (3, 1, 96), (3, 2, 32), (3, 4, 192), (3, 3, 256)]
