@@ -270,50 +270,63 @@ struct Gradients {
     int N, K;
 };
 
-// Into how many shares the K of dx and of dW is cut, where their tiles are too few or too long
-// to come out even on the pairs of SMs.
+// How the gradients' products are cut: row tiles, and shares of K where tiles are too few or too long to come out even
+// on the pairs of SMs.
 struct GradientSplit {
-    int dx, dw;
+    int dx, dw;              // shares
+    int tile_x, tile_w;      // rows of a tile
 };
 
 constexpr int kPlanPairs = 76, kMostShares = 8;
 
-// Cycles of a launch with tx tiles of dx in sx shares and tw of dW in sw, each tile `cx` and `cw`
-// cycles long: the longest unit, or all of them evenly; shared ones are written, read again
-// and joined by a kernel (4,000 cycles and 2,600 bytes a cycle).
-int64_t split_cost(int64_t tx, int64_t cx, int64_t bx, int sx, int64_t tw, int64_t cw, int64_t bw, int sw) {
-    const int64_t ux = std::max<int64_t>(cx / sx, 5000), uw = std::max<int64_t>(cw / sw, 5000);
-    const int64_t nx = tx * sx, nw = tw * sw, all = (nx * ux + nw * uw) / kPlanPairs;
-    const auto rounds = [](int64_t n, int64_t u) { return (n + kPlanPairs - 1) / kPlanPairs * u; };
-    int64_t t;
-    if (!nx || !nw) t = rounds(nx, ux) + rounds(nw, uw);
-    else t = std::max({rounds(ux > uw ? nx : nw, std::max(ux, uw)), all + std::min(ux, uw) / 2});
-    if (sx > 1 || sw > 1) t += 4000 + ((sx > 1 ? sx * bx : 0) + (sw > 1 ? sw * bw : 0)) * 8 / 2600;
-    return t;
+// Units of one gradient's products: tiles times shares, and the cycles of one.
+struct Units {
+    int64_t n, cycles;
+};
+
+Units units(int64_t rows, int64_t outs, int64_t products, int64_t steps, int tile, int shares) {
+    return Units{products * ((rows + tile - 1) / tile) * ((outs + 255) / 256) * shares,
+                 std::max<int64_t>((steps + shares - 1) / shares * std::max(2 * tile, 256 + tile), 5000)};
+}
+
+// Cycles of a launch of both: the longest unit's, or all of them evenly.
+int64_t launch_cycles(const Units &x, const Units &w) {
+    const auto rounds = [](const Units &u) { return (u.n + kPlanPairs - 1) / kPlanPairs * u.cycles; };
+    if (!x.n || !w.n) return rounds(x) + rounds(w);
+    const Units &longer = x.cycles > w.cycles ? x : w;
+    return std::max(rounds(longer), (x.n * x.cycles + w.n * w.cycles) / kPlanPairs + std::min(x.cycles, w.cycles) / 2);
+}
+
+// The rows dealt evenly to k tiles of at most 256, in thirty-twos; 0: they do not fit.
+int tile_of(int64_t rows, int64_t k) {
+    const int64_t tile = (rows + k * 32 - 1) / (k * 32) * 32;
+    return tile <= 256 ? (int)tile : 0;
 }
 
 GradientSplit split_gradients(int64_t M, int N, int K, int both, bool dx, bool dw) {
-    const auto cost = [](int64_t rows, int64_t outs) {
-        const int t = mm_pair_tile(rows, (outs + 255) / 256);
-        return std::max<int64_t>(2 * t, 256 + t);
-    };
-    const auto tiles = [](int64_t rows, int64_t outs) {
-        const int t = mm_pair_tile(rows, (outs + 255) / 256);
-        return (rows + t - 1) / t * ((outs + 255) / 256);
-    };
     const int64_t sx = both * steps_of(N), sw = steps_of(M);
-    const int64_t tx = dx ? tiles(M, K) : 0, tw = dw ? both * tiles(N, K) : 0, cx = sx * cost(M, K), cw = sw * cost(N, K);
-    GradientSplit best{1, 1};
-    int64_t least = split_cost(tx, cx, M * K, 1, tw, cw, (int64_t)both * N * K, 1);
-    for (int a = 1; a <= (dx ? kMostShares : 1); ++a)
-        for (int b = 1; b <= (dw ? kMostShares : 1); ++b) {
-            if ((a == 1 && b == 1) || (a > 1 && sx < 2 * a) || (b > 1 && sw < 2 * b)) continue;
-            // (something has to come of it: the model is not exact)
-            const int64_t t = split_cost(tx, cx, M * K, a, tw, cw, (int64_t)both * N * K, b) * 17 / 16;
-            if (t < least) {
-                least = t;
-                best = GradientSplit{a, b};
-            }
+    const int64_t kx = (M + 255) / 256, kw = ((int64_t)N + 255) / 256;
+    GradientSplit best{1, 1, tile_of(M, kx), tile_of(N, kw)};
+    int64_t least = INT64_MAX;
+    // as few row tiles as hold the rows, or one or two more
+    for (int64_t i = kx; i <= kx + (dx && kx <= 8 ? 2 : 0); ++i)
+        for (int64_t j = kw; j <= kw + (dw && kw <= 8 ? 2 : 0); ++j) {
+            const int tx = tile_of(M, i), tw = tile_of(N, j);
+            for (int a = 1; a <= (dx ? kMostShares : 1); ++a)
+                for (int b = 1; b <= (dw ? kMostShares : 1); ++b) {
+                    if ((a > 1 && sx < 2 * a) || (b > 1 && sw < 2 * b)) continue;
+                    const Units none{0, 0};
+                    int64_t t = launch_cycles(dx ? units(M, K, 1, sx, tx, a) : none,
+                                              dw ? units(N, K, both, sw, tw, b) : none);
+                    // shares are written, read again and joined by a kernel (4,000 cycles and 2,600 bytes a cycle),
+                    // and something has to come of it: the model is not exact
+                    if (a > 1 || b > 1)
+                        t = (t + 4000 + ((a > 1 ? a * M : 0) + (b > 1 ? b * (int64_t)both * N : 0)) * K * 8 / 2600) * 17 / 16;
+                    if (t < least) {
+                        least = t;
+                        best = GradientSplit{a, b, tx, tw};
+                    }
+                }
         }
     return best;
 }
@@ -359,6 +372,8 @@ cudaError_t launch_gradients(const Gradients &g, char *shares, JoinArgs &join, i
         if (plan_mm_few(kMmStore, p, sms, &plan)) return launch_mm_few(kMmStore, p, plan, s, nullptr);
     }
     const GradientSplit split = split_gradients(g.M, g.N, g.K, g.both, g.dx, g.dw[0]);
+    in.tile_m = split.tile_x;
+    weight[0].tile_m = weight[1].tile_m = split.tile_w;
     const auto add = [&](MmProblem &q, int shared) {
         q.split = shared;
         if (shared > 1) {
@@ -377,7 +392,7 @@ cudaError_t launch_gradients(const Gradients &g, char *shares, JoinArgs &join, i
         for (int i = 0; i < g.both; ++i) add(weight[i], split.dw);
     if (g.dx && weights_first) add(in, split.dx);
     if (!p.problems) return cudaSuccess;
-    return join.joins ? launch_mm_pair(kMmStore, p, sms, s, nullptr) : launch_mm(kMmStore, p, sms, s, nullptr);
+    return launch_mm_pair(kMmStore, p, sms, s, nullptr);
 }
 
 cudaError_t zero_rows(void *p, int64_t stride, int rows, int cols, cudaStream_t s) {

@@ -88,15 +88,10 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     // this CTA's tile, and its share of K
-    const int id = p.by_cluster.divide((int)blockIdx.x), rank = (int)blockIdx.x - id * p.cluster;
-    const int side = rank % kGroup, group = rank / kGroup, groups = p.cluster / kGroup;
-    int which = 0;
-    while (which + 1 < p.problems && id >= p.prob[which + 1].first) ++which;
-    const MmProblem &q = p.prob[which];
+    const MmProblem &q = p.prob[0];
+    const int tile = p.by_cluster.divide((int)blockIdx.x), rank = (int)blockIdx.x - tile * p.cluster;
+    const int side = rank % kGroup, part = rank / kGroup;
     const bool shared_k = q.split > 1;
-    const int tile = shared_k ? id - q.first : (id - q.first) * groups + group;
-    const int part = shared_k ? group : 0;
-    const bool active = tile < q.tiles;
     const int tn = q.by_mt.divide(tile), row0 = (tile - tn * q.mt) * q.tile_m;
     const int out0 = (tn * kGroup + side) * kOwn;
     const int rows = q.M - row0 < q.tile_m ? q.M - row0 : q.tile_m;
@@ -124,7 +119,7 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     // sums may come here from now on, unless the ring is in their place
     if (shared_k && p.apart) cluster_arrive();
 
-    if (active && warp == 0) {
+    if (warp == 0) {
         if (ptx::elect_one()) {
             // ---------------- copies: this CTA's weights, and its half of the rows ----------------
             // (a step's issue has to be short: a division for its segment and a look at the abort
@@ -187,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
             ptx::tmem_relinquish();
         }
         __syncwarp();
-        if (active && side == 0 && ptx::elect_one()) {
+        if (side == 0 && ptx::elect_one()) {
             // ---------------- products ----------------
             // K-major: rows of 128 bytes, 8 to a kilobyte; 16 k are 32 bytes.
             // MN-major: a kilobyte is 8 k of 64 rows, 64 rows on is the next box; 16 k are 2 KB.
@@ -238,12 +233,12 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     // rows that are in shared memory at a time, of each share of K; a multiple of four
     const int chunk = shared_k ? (rows + 4 * q.split - 1) / (4 * q.split) * 4 : p.chunk;
     // (a wait that gives up says so; the products under way are waited for all the same)
-    if (active && !ptx::mbar_wait(&S->done, 0, p.wait_ns)) {
+    if (!ptx::mbar_wait(&S->done, 0, p.wait_ns)) {
         give_up(p, abort_flag);
         ptx::mbar_wait(&S->done, 0, 2 * kMmTimeoutNs);
     }
     __syncthreads();
-    const bool ok = active && !*abort_flag;
+    const bool ok = !*abort_flag;
     ptx::tc_fence_after();
     const uint32_t tmem = S->tmem_base;
     // (the ring is free now: every copy has been used, and every product is complete)
@@ -422,19 +417,12 @@ bool plan_mm_few(MmEpilogue epi, const MmArgs &p, int sms, MmFewPlan *plan) {
     if (check_kind) {
         if (check_kind == 1) return false;
         plan->pair = check_kind == 3;
-        plan->split = 1;
         const int even = plan->pair ? 32 : 16;
-        for (int i = 0; i < p.problems; ++i) {
-            const MmProblem &q = p.prob[i];
-            plan->tile_m[i] = std::min(round_up(check_tile, even), round_up(q.M, even));
-            plan->shared[i] = check_split > 1 && fits(epi, q, plan->pair, plan->tile_m[i], check_split);
-            if (plan->shared[i]) plan->split = check_split;
-            else if (!fits(epi, q, plan->pair, plan->tile_m[i], 1)) return false;
-        }
-        return true;
+        plan->tile_m = std::min(round_up(check_tile, even), round_up(p.prob[0].M, even));
+        plan->split = fits(epi, p.prob[0], plan->pair, plan->tile_m, check_split) ? check_split : 1;
+        return fits(epi, p.prob[0], plan->pair, plan->tile_m, plan->split);
     }
 #endif
-    if (p.problems > 1) return false;
     // What a call takes, in cycles, fitted to 9 weights (512 x 512 to 14336 x 3584) of 1 to 2,048 rows, plain
     // and gated, with up to 60 plans each: the plan that it chooses is 2 % slower than the fastest on
     // average, 14 % at most.  A step of K is bound by what comes into an SM or by its issue, a pair's wide
@@ -483,8 +471,7 @@ bool plan_mm_few(MmEpilogue epi, const MmArgs &p, int sms, MmFewPlan *plan) {
                     few = true;
                     plan->pair = pair;
                     plan->split = split;
-                    plan->tile_m[0] = (int)tile;
-                    plan->shared[0] = split > 1;
+                    plan->tile_m = (int)tile;
                 }
             }
         }
@@ -496,32 +483,26 @@ cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, cuda
                           int64_t *part_rows) {
     const int group = plan.pair ? 2 : 1, own = (mm_both(epi) ? kLanes / 2 : kLanes) * group;
     MmMapList list;
-    int64_t clusters = 0;
-    int dump = 0, most_steps = 1;
+    MmProblem &q = p.prob[0];
     p.cluster = plan.split * group;
     p.by_cluster.set((uint32_t)p.cluster);
-    p.stage_bytes = 0;
-    for (int i = 0; i < p.problems; ++i) {
-        MmProblem &q = p.prob[i];
-        q.tile_m = plan.tile_m[i];
-        q.box_rows = q.tile_m / group;
-        q.split = plan.shared[i] ? plan.split : 1;
-        q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
-        q.nt = (q.N + own - 1) / own;
-        if ((int64_t)q.mt * q.nt > INT32_MAX / kMaxCluster) return cudaErrorInvalidValue;
-        q.tiles = q.mt * q.nt;
-        q.by_mt.set((uint32_t)q.mt);
-        q.share = q.segments * q.steps / q.split;
-        q.more = q.segments * q.steps % q.split;
-        q.first = (int)clusters;
-        clusters += q.split > 1 ? q.mt * q.nt : (q.mt * q.nt + plan.split - 1) / plan.split;
-        p.stage_bytes = std::max(p.stage_bytes, kWeightBytes + row_bytes(q, q.box_rows));
-        if (q.split > 1) dump = std::max({dump, sums_rows(q.tile_m, q.split) * kRowBytes, kWarps * 1024});
-        most_steps = std::max(most_steps, (q.segments * q.steps + q.split - 1) / q.split);
-        for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.a_mn ? 64 : q.box_rows);
-        for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j)
-            q.b[j] = list.add(q.from_b[j], q.b_mn || mm_both(epi) ? 64 : kLanes);
-    }
+    q.tile_m = plan.tile_m;
+    q.box_rows = q.tile_m / group;
+    q.split = plan.split;
+    q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
+    q.nt = (q.N + own - 1) / own;
+    if ((int64_t)q.mt * q.nt > INT32_MAX / kMaxCluster) return cudaErrorInvalidValue;
+    q.tiles = q.mt * q.nt;
+    q.by_mt.set((uint32_t)q.mt);
+    q.share = q.segments * q.steps / q.split;
+    q.more = q.segments * q.steps % q.split;
+    const int64_t clusters = q.tiles;
+    const int dump = q.split > 1 ? std::max(sums_rows(q.tile_m, q.split) * kRowBytes, kWarps * 1024) : 0;
+    const int most_steps = q.share + (q.more ? 1 : 0);
+    p.stage_bytes = kWeightBytes + row_bytes(q, q.box_rows);
+    for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.a_mn ? 64 : q.box_rows);
+    for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j)
+        q.b[j] = list.add(q.from_b[j], q.b_mn || mm_both(epi) ? 64 : kLanes);
     if (!list.ok || clusters * p.cluster > INT32_MAX) return cudaErrorInvalidValue;
     p.maps = list.count;
     p.stage_bytes = round_up(p.stage_bytes, 1024);
@@ -539,7 +520,7 @@ cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, cuda
     if (p.stages < 1 || (size_t)p.ring_bytes > most) return cudaErrorInvalidValue;
     p.chunk = std::min(256, p.ring_bytes / kRowBytes / 32 * 32);   // (a warp reads 32 rows at a time)
     const size_t smem = std::max(kExtra + (size_t)p.ring_bytes, kSmemLeast + 1);
-    if (part_rows) *part_rows = (int64_t)p.prob[0].mt * p.prob[0].split;
+    if (part_rows) *part_rows = (int64_t)q.mt * q.split;
     const void *fns[4][2] = {
         {(const void *)mm_few_kernel<kMmStore, false>, (const void *)mm_few_kernel<kMmStore, true>},
         {(const void *)mm_few_kernel<kMmGated, false>, (const void *)mm_few_kernel<kMmGated, true>},
@@ -575,7 +556,7 @@ extern "C" __attribute__((visibility("default"))) int wz_check_mm_choice(int gat
     q.M = (int)M, q.N = N, q.segments = 1, q.steps = (K + 63) / 64;
     wz::MmFewPlan plan;
     if (!wz::plan_mm_few(gated ? wz::kMmGated : wz::kMmStore, p, sms, &plan)) return 1;
-    *split = plan.split, *tile = plan.tile_m[0];
+    *split = plan.split, *tile = plan.tile_m;
     return plan.pair ? 3 : 2;
 }
 #endif

@@ -527,7 +527,7 @@ cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, i
     for (int i = 0; i < p.problems; ++i) {
         MmProblem &q = p.prob[i];
         q.nt = (q.N + tile_n - 1) / tile_n;
-        q.tile_m = mm_pair_tile(q.M, q.nt);
+        if (!q.tile_m) q.tile_m = mm_pair_tile(q.M, q.nt);
         if (i == 0) {
             const bool longs = (epi == kMmSlope || epi == kMmGatedSlope) && q.steps > kLongSteps;
             p.second = longs ? kAccCols / 2 : 0;

@@ -68,15 +68,14 @@ struct MmProblem {
     // set by the launch
     int a[2], b[2];        // their tensor maps
     float *sums;           // pairs, K shared: [split][M][N] sums of the shares
+    int tile_m;            // rows of a tile; pairs: 0 lets the launch choose them
     int mt, nt, tiles;     // tiles along M and N, and all of them (with shared K, of all shares)
-    int tile_m;            // rows of a tile
     MmDivisor by_mt;       // few-rows kernel
     MmDivisor by_group, by_last;   // pairs: tiles of a group of row tiles, row tiles of the last one
     int head, from, skip;  //   its first tiles, for the pairs from one on, the turn's first
     int box_rows;          // a CTA's
     int split;             // shares of a tile's K
     int share, more;       //   K steps of a share, shares that have one more
-    int first;             // few-rows kernel: first cluster
 };
 
 struct MmArgs {
@@ -362,13 +361,11 @@ cudaError_t launch_mm(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_
 int mm_pair_tile(int64_t M, int64_t output_tiles);   // their rows
 cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_t *part_rows);
 
-// Tiles of 16 to 256 rows on one SM or a pair, K shared by a cluster (mm_few.cu).  False:
-// they do not suit it.
+// One product in tiles of 16 to 256 rows on one SM or a pair, K shared by a cluster (mm_few.cu).
+// False: it does not suit it.
 struct MmFewPlan {
     bool pair;
-    int split;                                  // shares of K
-    int tile_m[kMmProblems];
-    bool shared[kMmProblems];                   // whether a product's K is shared
+    int split, tile_m;   // shares of K, rows of a tile
 };
 bool plan_mm_few(MmEpilogue epi, const MmArgs &p, int sms, MmFewPlan *plan);
 cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, cudaStream_t s,
