@@ -1,10 +1,11 @@
-"""Condense a video, put its tokens in a decoder's 8-bit cache, and attend to them.
+"""Condense a video, put its tokens in a decoder's 8-bit cache, attend to them, and run a layer.
 
-What a serving program does around one attention layer of an LLM: the condensed and projected
-tokens take positions from the index map (frame, row, column), the question's tokens follow with
-all three axes alike, one layer's projections give queries, keys and values, the prompt attends to
-itself causally, and then single tokens are appended and answered one by one.  Weights and inputs
-are random: the program shows the calls and checks them against plain attention in fp32.
+What a serving program does around one layer of an LLM: the condensed and projected tokens take
+positions from the index map (frame, row, column), the question's tokens follow with all three axes
+alike, one product gives queries, keys and values, the prompt attends to itself causally, the
+attention's output goes back into the residual stream and through a gated feed-forward block,
+and then single tokens are appended and answered one by one.  Weights and inputs are random: the program
+shows the calls and checks them against plain attention and plain products in fp32.
 
     python examples/answer_from_cache.py
 """
@@ -33,6 +34,13 @@ def plain_attention(q, cache, pages, kv_len, causal):
     return torch.einsum("hgnt,htd->nhgd", w.softmax(-1), v).reshape(n, Hq, D)
 
 
+def plain_layer(rows, o, w_o, w_gate, w_up, w_down):
+    """What follows the attention's output o of a layer's rows, in fp32."""
+    x = rows.float() + o.float() @ w_o.float().T
+    g = x @ w_gate.float().T
+    return x + (g * torch.sigmoid(g) * (x @ w_up.float().T)) @ w_down.float().T
+
+
 def main(T=16, H=13, W=13, D=512, Hq=8, heads=2, head_dim=64, page=64, question=21, answer=5, seed=0):
     dev = torch.device("cuda")
     g = torch.Generator(device=dev).manual_seed(seed)
@@ -49,7 +57,10 @@ def main(T=16, H=13, W=13, D=512, Hq=8, heads=2, head_dim=64, page=64, question=
     prompt = torch.cat([tokens, query])
     last = T + torch.arange(question, device=dev, dtype=torch.int32)
     positions = torch.cat([out["index"][:n], last[:, None].expand(-1, 3)]).contiguous()
-    w_qkv = (rand((Hq + 2 * heads) * head_dim, D) / math.sqrt(D)).bfloat16()
+    wide = Hq * head_dim
+    weight = lambda outs, ins: (rand(outs, ins) / math.sqrt(ins)).bfloat16()  # noqa: E731
+    w_qkv, b_qkv = weight(wide + 2 * heads * head_dim, D), 0.1 * rand(wide + 2 * heads * head_dim)
+    w_o, w_gate, w_up, w_down = weight(D, wide), weight(4 * D, D), weight(4 * D, D), weight(D, 4 * D)
 
     # a cache with room for the answer; this sequence's pages lie anywhere in it
     length = prompt.shape[0]
@@ -67,7 +78,7 @@ def main(T=16, H=13, W=13, D=512, Hq=8, heads=2, head_dim=64, page=64, question=
     rows = prompt
     for step in range(1 + answer):
         new = rows.shape[0]
-        qkv = (rows @ w_qkv.T).view(new, Hq + 2 * heads, head_dim)
+        qkv = wz.wz_linear(rows, w_qkv, b_qkv).view(new, Hq + 2 * heads, head_dim)
         q = wz.wz_kv_append(qkv[:, Hq:Hq + heads], qkv[:, Hq + heads:], cache, table, i32(0, new), i32(held), max_new=new,
                             q=qkv[:, :Hq], rotation=rotation, positions=positions, sections=sections,
                             device_status=status)
@@ -75,11 +86,16 @@ def main(T=16, H=13, W=13, D=512, Hq=8, heads=2, head_dim=64, page=64, question=
         o = wz.wz_attend(q, cache, table, i32(0, new), i32(held), max_new=new, workspace=workspace, device_status=status)
         want = plain_attention(q, cache, table[0], held, True)
         worst = max(worst, float((o.float() - want).norm() / want.norm()))
-        rows = (o[-1:].reshape(1, -1) @ (rand(Hq * head_dim, D) / math.sqrt(D)).bfloat16())   # the next token's input
+        o = o.view(new, wide)
+        x = wz.wz_linear(o, w_o, residual=rows)
+        y = wz.wz_linear(wz.wz_gated(x, w_gate, w_up), w_down, residual=x)
+        want = plain_layer(rows, o, w_o, w_gate, w_up, w_down)
+        worst = max(worst, float((y.float() - want).norm() / want.norm()))
+        rows = y[-1:] / y[-1:].float().std().bfloat16()                                     # the next token's input
         positions = (last[-1] + 1 + i32(step))[:, None].expand(1, 3).contiguous()
     assert int(status) == 0, f"status {int(status):#x}"
     print(f"{n} condensed tokens and {question} of the question cached, {answer} tokens answered: "
-          f"outputs within {worst:.1e} of plain attention")
+          f"outputs within {worst:.1e} of plain attention and products")
     return worst
 
 

@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
                 for (int j = 0; j < 32; j += 4) {
                     if (c + j < end) {
                         float *to = sums + (size_t)(part * chunk + at) * kLanes + quadrant * 32 + lane;
-                        if (shared_k) {
+                        if (shared_k && owner != part) {
                             const uint32_t there = ptx::map_cluster(to, (uint32_t)(owner * kGroup + side));
 #pragma unroll
                             for (int i = 0; i < 4; ++i) st_cluster(there + (uint32_t)(i * kRowBytes), __uint_as_float(raw[j + i]));
