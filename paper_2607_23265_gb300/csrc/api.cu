@@ -1024,8 +1024,8 @@ int wz_linear_backward(const wz_linear_backward_args *a) {
         return WZ_ERR_INVALID_ARG;
     const cudaStream_t s = (cudaStream_t)a->stream;
     Scratch ws;
-    const size_t need = linear_backward_bytes(a->M, a->N, a->K);
-    if ((a->workspace || a->M > 0) && (st = ws.acquire(a->workspace, a->workspace_bytes, need, s)) != WZ_OK) return st;
+    const size_t need = a->workspace ? linear_backward_bytes(a->M, a->N, a->K) : linear_backward_need(*a);
+    if (need && (st = ws.acquire(a->workspace, a->workspace_bytes, need, s)) != WZ_OK) return st;
     Nvtx range("wz::linear_backward");
     WZ_CUDA(launch_linear_backward(*a, ws.ptr, s));
     return WZ_OK;
@@ -1079,9 +1079,8 @@ int wz_gated_backward(const wz_gated_backward_args *a) {
         return WZ_ERR_INVALID_ARG;
     const cudaStream_t s = (cudaStream_t)a->stream;
     Scratch ws;
-    if ((a->workspace || a->M > 0) &&
-        (st = ws.acquire(a->workspace, a->workspace_bytes, gated_backward_bytes(a->M, a->N, a->K), s)) != WZ_OK)
-        return st;
+    const size_t need = a->workspace ? gated_backward_bytes(a->M, a->N, a->K) : gated_backward_need(*a);
+    if (need && (st = ws.acquire(a->workspace, a->workspace_bytes, need, s)) != WZ_OK) return st;
     Nvtx range("wz::gated_backward");
     WZ_CUDA(launch_gated_backward(*a, ws.ptr, s));
     return WZ_OK;

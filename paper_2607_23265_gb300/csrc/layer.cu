@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(32 * kDeltaWarps) mm_delta_kernel(const __grid
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int n = (int)blockIdx.y * kDeltaCols + 8 * lane, left = p.N - n;
     const int64_t m0 = (int64_t)blockIdx.x * kDeltaRows;
-    float a0[8] = {}, a1[8] = {};
+    f2_t a0[4] = {}, a1[4] = {};   // (zero bits are zeros)
     if (left > 0) {
         mm_with_act(p.act, [&](auto act) {
             constexpr int ACT = decltype(act)::value;
@@ -65,33 +65,49 @@ __global__ void __launch_bounds__(32 * kDeltaWarps) mm_delta_kernel(const __grid
                 for (int k = 0; k < kBatch; ++k) {
                     const int64_t m = m0 + r0 + k * kDeltaWarps;
                     if (!wide && m >= p.M) break;
-                    float dy[8], g[8], u[8];
-                    const auto take = [&](int a, float (&x)[8]) {
-                        if (wide) unpack(raw[a < kArrays ? a : 0][k], x, (__nv_bfloat16 *)nullptr);
-                        else mm_load(from[a] + m * strides[a], x, left);
+                    f2_t dy[4], g[4], u[4];
+                    const auto take = [&](int a, f2_t (&x)[4]) {
+                        if (wide) {
+                            unpack_pairs(raw[a < kArrays ? a : 0][k], x, (__nv_bfloat16 *)nullptr);
+                        } else {
+                            float y[8];
+                            mm_load(from[a] + m * strides[a], y, left);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) x[j] = pack2(y[2 * j], y[2 * j + 1]);
+                        }
+                    };
+                    const auto put = [&](__nv_bfloat16 *to, const f2_t (&x)[4]) {
+                        float y[8];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 v = unpack2(x[j]);
+                            y[2 * j] = v.x;
+                            y[2 * j + 1] = v.y;
+                        }
+                        mm_store(to, y, wide ? 8 : left);
                     };
                     take(0, dy);
                     if constexpr (MODE == kDeltaSums) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) a0[j] += dy[j];
+                        for (int j = 0; j < 4; ++j) a0[j] = add2(a0[j], dy[j]);
                     } else {
                         take(1, g);
                         if constexpr (MODE == kDeltaGated) take(2, u);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            float value, slope;
-                            mm_slope1<ACT>(g[j], value, slope);
+                        for (int j = 0; j < 4; ++j) {
+                            f2_t value, slope;
+                            mm_slope2<ACT, MODE == kDeltaGated>(g[j], value, slope);
                             if constexpr (MODE == kDeltaGated) {
-                                g[j] = dy[j] * u[j] * slope;
-                                u[j] = dy[j] * value;
-                                a1[j] += u[j];
+                                g[j] = mul2(mul2(dy[j], u[j]), slope);
+                                u[j] = mul2(dy[j], value);
+                                a1[j] = add2(a1[j], u[j]);
                             } else {
-                                g[j] = dy[j] * slope;
+                                g[j] = mul2(dy[j], slope);
                             }
-                            a0[j] += g[j];
+                            a0[j] = add2(a0[j], g[j]);
                         }
-                        mm_store(p.d[0] + m * p.d_stride + n, g, wide ? 8 : left);
-                        if constexpr (MODE == kDeltaGated) mm_store(p.d[1] + m * p.d_stride + n, u, wide ? 8 : left);
+                        put(p.d[0] + m * p.d_stride + n, g);
+                        if constexpr (MODE == kDeltaGated) put(p.d[1] + m * p.d_stride + n, u);
                     }
                 }
             }
@@ -102,7 +118,11 @@ __global__ void __launch_bounds__(32 * kDeltaWarps) mm_delta_kernel(const __grid
         if (!p.part[i]) continue;
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sums[warp][8 * lane + j] = i ? a1[j] : a0[j];
+        for (int j = 0; j < 4; ++j) {
+            const float2 v = unpack2(i ? a1[j] : a0[j]);
+            sums[warp][8 * lane + 2 * j] = v.x;
+            sums[warp][8 * lane + 2 * j + 1] = v.y;
+        }
         __syncthreads();
         const int c = (int)blockIdx.y * kDeltaCols + (int)threadIdx.x;
         if (c < p.N) {
@@ -277,7 +297,7 @@ struct GradientSplit {
     int tile_x, tile_w;      // rows of a tile
 };
 
-constexpr int kPlanPairs = 76, kMostShares = 8;
+constexpr int kPlanPairs = 76;
 
 // Units of one gradient's products: tiles times shares, and the cycles of one.
 struct Units {
@@ -303,50 +323,51 @@ int tile_of(int64_t rows, int64_t k) {
     return tile <= 256 ? (int)tile : 0;
 }
 
+// Bytes of the shares' sums.
+size_t shares_bytes(int64_t M, int N, int K, int both, int dx, int dw) {
+    return (dx > 1 ? pad256((size_t)dx * (size_t)M * (size_t)K * 4) : 0) +
+           (dw > 1 ? both * pad256((size_t)dw * (size_t)N * (size_t)K * 4) : 0);
+}
+constexpr size_t kMostSharesBytes = 48u << 20;
+
 GradientSplit split_gradients(int64_t M, int N, int K, int both, bool dx, bool dw) {
     const int64_t sx = both * steps_of(N), sw = steps_of(M);
     const int64_t kx = (M + 255) / 256, kw = ((int64_t)N + 255) / 256;
     GradientSplit best{1, 1, tile_of(M, kx), tile_of(N, kw)};
     int64_t least = INT64_MAX;
+    const auto consider = [&](int tx, int tw, int a, int b) {
+        if (!tx || !tw) return;
+        const Units none{0, 0};
+        int64_t t = launch_cycles(dx ? units(M, K, 1, sx, tx, a) : none, dw ? units(N, K, both, sw, tw, b) : none);
+        // shares are written, read again and joined by a kernel (4,000 cycles and 2,600 bytes a cycle), and
+        // something has to come of it: the model is not exact
+        if (a > 1 || b > 1)
+            t = (t + 4000 + ((a > 1 ? a * M : 0) + (b > 1 ? b * (int64_t)both * N : 0)) * K * 8 / 2600) * 17 / 16;
+        if (t < least) {
+            least = t;
+            best = GradientSplit{a, b, tx, tw};
+        }
+    };
     // as few row tiles as hold the rows, or one or two more
     for (int64_t i = kx; i <= kx + (dx && kx <= 8 ? 2 : 0); ++i)
-        for (int64_t j = kw; j <= kw + (dw && kw <= 8 ? 2 : 0); ++j) {
-            const int tx = tile_of(M, i), tw = tile_of(N, j);
-            for (int a = 1; a <= (dx ? kMostShares : 1); ++a)
-                for (int b = 1; b <= (dw ? kMostShares : 1); ++b) {
-                    if ((a > 1 && sx < 2 * a) || (b > 1 && sw < 2 * b)) continue;
-                    const Units none{0, 0};
-                    int64_t t = launch_cycles(dx ? units(M, K, 1, sx, tx, a) : none,
-                                              dw ? units(N, K, both, sw, tw, b) : none);
-                    // shares are written, read again and joined by a kernel (4,000 cycles and 2,600 bytes a cycle),
-                    // and something has to come of it: the model is not exact
-                    if (a > 1 || b > 1)
-                        t = (t + 4000 + ((a > 1 ? a * M : 0) + (b > 1 ? b * (int64_t)both * N : 0)) * K * 8 / 2600) * 17 / 16;
-                    if (t < least) {
-                        least = t;
-                        best = GradientSplit{a, b, tx, tw};
-                    }
-                }
-        }
+        for (int64_t j = kw; j <= kw + (dw && kw <= 8 ? 2 : 0); ++j) consider(tile_of(M, i), tile_of(N, j), 1, 1);
+    // and shares, unless the pairs have no less to do on the whole
+    const Units x = dx ? units(M, K, 1, sx, best.tile_x, 1) : Units{0, 0}, w = dw ? units(N, K, both, sw, best.tile_w, 1) : Units{0, 0};
+    if (least <= (x.n * x.cycles + w.n * w.cycles) / kPlanPairs * 9 / 8) return best;
+    const int tiles[2][2] = {{best.tile_x, best.tile_w}, {tile_of(M, kx), tile_of(N, kw)}};
+    constexpr int kShares[] = {1, 2, 3, 4, 6, 8};
+    for (const auto &t : tiles)
+        for (int a : kShares)
+            for (int b : kShares) {
+                if ((a > 1 && (!dx || sx < 2 * a)) || (b > 1 && (!dw || sw < 2 * b)) || (a == 1 && b == 1)) continue;
+                if (shares_bytes(M, N, K, both, a, b) <= kMostSharesBytes) consider(t[0], t[1], a, b);
+            }
     return best;
 }
 
-// The most floats of shares' sums that a call may need, whichever gradients it asks for.
-size_t shares_bytes(int64_t M, int N, int K, int both) {
-    size_t most = 0;
-    for (int need = 1; M > 0 && need < 4; ++need) {
-        const GradientSplit g = split_gradients(M, N, K, both, need & 1, need & 2);
-        size_t bytes = 0;
-        if ((need & 1) && g.dx > 1) bytes += pad256((size_t)g.dx * (size_t)M * (size_t)K * 4);
-        if ((need & 2) && g.dw > 1) bytes += both * pad256((size_t)g.dw * (size_t)N * (size_t)K * 4);
-        most = std::max(most, bytes);
-    }
-    return most;
-}
-
 // The products of both gradients in one launch; what they leave to be joined goes into `join`.
-cudaError_t launch_gradients(const Gradients &g, char *shares, JoinArgs &join, int *status, int sms,
-                             cudaStream_t s) {
+cudaError_t launch_gradients(const Gradients &g, const GradientSplit &split, char *shares, JoinArgs &join, int *status,
+                             int sms, cudaStream_t s) {
     MmArgs p = mm_args(WZ_ACT_NONE, status);
     MmProblem in, weight[2];
     memset(&in, 0, sizeof(in));
@@ -371,7 +392,6 @@ cudaError_t launch_gradients(const Gradients &g, char *shares, JoinArgs &join, i
         p.prob[0] = in;
         if (plan_mm_few(kMmStore, p, sms, &plan)) return launch_mm_few(kMmStore, p, plan, s, nullptr);
     }
-    const GradientSplit split = split_gradients(g.M, g.N, g.K, g.both, g.dx, g.dw[0]);
     in.tile_m = split.tile_x;
     weight[0].tile_m = weight[1].tile_m = split.tile_w;
     const auto add = [&](MmProblem &q, int shared) {
@@ -460,13 +480,48 @@ cudaError_t launch_gated(const wz_gated_args &a, cudaStream_t s) {
     return launch_mm(kMmGated, p, sms, s, nullptr);
 }
 
-// d, sums over rows, shares' sums, one after the other.
-size_t linear_backward_bytes(int64_t M, int N, int K) {
-    return delta_bytes(M, N) + part_bytes(M, N) + shares_bytes(M, N, K, 1);
+namespace {
+
+// How a backward call is cut, and where its parts are in its workspace: d, sums over rows, shares' sums, as
+// many as it needs.
+struct BackwardLayout {
+    GradientSplit split;
+    size_t d[2], part[2], shares, total;
+    BackwardLayout(int64_t M, int N, int K, int both, bool with_d, const bool (&with_part)[2], bool dx, bool dw)
+        : split(split_gradients(M, N, K, both, dx, dw)), total(0) {
+        const auto take = [&](size_t bytes) {
+            const size_t at = total;
+            total += bytes;
+            return at;
+        };
+        for (int i = 0; i < 2; ++i) d[i] = take(with_d && i < both ? delta_bytes(M, N) : 0);
+        for (int i = 0; i < 2; ++i) part[i] = take(with_part[i] ? part_bytes(M, N) : 0);
+        shares = take(shares_bytes(M, N, K, both, split.dx, split.dw));
+    }
+};
+
+// Whether the last kernel adds dy up by itself.
+bool sums_in_join(const wz_linear_backward_args &a) { return a.act == WZ_ACT_NONE && a.M <= kSumsInJoin; }
+
+BackwardLayout layout_of(const wz_linear_backward_args &a) {
+    return BackwardLayout(a.M, a.N, a.K, 1, a.act != WZ_ACT_NONE, {a.db && !sums_in_join(a), false}, a.dx, a.dw);
 }
-size_t gated_backward_bytes(int64_t M, int N, int K) {
-    return 2 * (delta_bytes(M, N) + part_bytes(M, N)) + shares_bytes(M, N, K, 2);
+
+BackwardLayout layout_of(const wz_gated_backward_args &a) {
+    return BackwardLayout(a.M, a.N, a.K, 2, true, {a.db_gate != nullptr, a.db_up != nullptr}, a.dx, a.dw_gate);
 }
+
+// The most that a call of these sizes needs, whichever gradients it asks for.
+size_t most_bytes(int64_t M, int N, int K, int both) {
+    return both * (delta_bytes(M, N) + part_bytes(M, N)) + std::min(kMostSharesBytes, shares_bytes(M, N, K, both, 8, 8));
+}
+
+}  // namespace
+
+size_t linear_backward_bytes(int64_t M, int N, int K) { return most_bytes(M, N, K, 1); }
+size_t gated_backward_bytes(int64_t M, int N, int K) { return most_bytes(M, N, K, 2); }
+size_t linear_backward_need(const wz_linear_backward_args &a) { return a.M > 0 ? layout_of(a).total : 0; }
+size_t gated_backward_need(const wz_gated_backward_args &a) { return a.M > 0 ? layout_of(a).total : 0; }
 
 #define MM_TRY(call)                              \
     do {                                          \
@@ -483,8 +538,9 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
     const int sms = sm_count();
     if (sms < 2) return cudaErrorInvalidDevice;
     const int64_t d_stride = delta_stride(a.N);
-    __nv_bfloat16 *d = half((void *)ws);
-    float *part = a.db ? reinterpret_cast<float *>(ws + delta_bytes(a.M, a.N)) : nullptr;
+    const BackwardLayout at = layout_of(a);
+    __nv_bfloat16 *d = half((void *)(ws + at.d[0]));
+    float *part = a.db && !sums_in_join(a) ? reinterpret_cast<float *>(ws + at.part[0]) : nullptr;
     int64_t part_rows = (a.M + kDeltaRows - 1) / kDeltaRows;
     if (a.act != WZ_ACT_NONE && !a.pre) {
         MmArgs p = mm_args(a.act, a.device_status);
@@ -494,7 +550,7 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
         p.dy = half(a.dy), p.dy_stride = a.dy_stride;
         p.part[0] = part;
         MM_TRY(launch_mm(kMmSlope, p, sms, s, &part_rows));
-    } else if (a.act != WZ_ACT_NONE || (part && a.M > kSumsInJoin)) {
+    } else if (a.act != WZ_ACT_NONE || part) {
         DeltaArgs p;
         memset(&p, 0, sizeof(p));
         p.dy = half(a.dy), p.dy_stride = a.dy_stride;
@@ -515,12 +571,11 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
     g.dw[0] = a.dw, g.dw_stride[0] = a.dw_stride;
     g.M = a.M, g.N = a.N, g.K = a.K;
     JoinArgs join = join_args(part, nullptr, a.db, nullptr, part_rows, a.N);
-    if (a.act == WZ_ACT_NONE && a.M <= kSumsInJoin) {
+    if (sums_in_join(a)) {
         join.part_rows = 0;
         join.dy = half(a.dy), join.dy_stride = a.dy_stride, join.dy_rows = a.M;
     }
-    char *shares = ws ? ws + delta_bytes(a.M, a.N) + part_bytes(a.M, a.N) : nullptr;
-    MM_TRY(launch_gradients(g, shares, join, a.device_status, sms, s));
+    MM_TRY(launch_gradients(g, at.split, ws + at.shares, join, a.device_status, sms, s));
     return launch_join(join, s);
 }
 
@@ -535,11 +590,13 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
     const int sms = sm_count();
     if (sms < 2) return cudaErrorInvalidDevice;
     const int64_t d_stride = delta_stride(a.N);
-    const size_t db_at = 2 * delta_bytes(a.M, a.N);
-    __nv_bfloat16 *d[2] = {half((void *)ws), half((void *)(ws + delta_bytes(a.M, a.N)))};
+    const BackwardLayout at = layout_of(a);
+    __nv_bfloat16 *d[2];
     float *part[2];
-    for (int i = 0; i < 2; ++i)
-        part[i] = db[i] ? reinterpret_cast<float *>(ws + db_at + i * part_bytes(a.M, a.N)) : nullptr;
+    for (int i = 0; i < 2; ++i) {
+        d[i] = half((void *)(ws + at.d[i]));
+        part[i] = db[i] ? reinterpret_cast<float *>(ws + at.part[i]) : nullptr;
+    }
     int64_t part_rows = (a.M + kDeltaRows - 1) / kDeltaRows;
     if (a.gate) {
         DeltaArgs p;
@@ -572,7 +629,7 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
     g.dw_stride[0] = a.dw_gate_stride, g.dw_stride[1] = a.dw_up_stride;
     g.M = a.M, g.N = a.N, g.K = a.K;
     JoinArgs join = join_args(part[0], part[1], db[0], db[1], part_rows, a.N);
-    MM_TRY(launch_gradients(g, ws + 2 * (delta_bytes(a.M, a.N) + part_bytes(a.M, a.N)), join, a.device_status, sms, s));
+    MM_TRY(launch_gradients(g, at.split, ws + at.shares, join, a.device_status, sms, s));
     return launch_join(join, s);
 }
 

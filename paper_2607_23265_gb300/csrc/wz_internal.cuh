@@ -269,6 +269,12 @@ __device__ __forceinline__ f2_t add2(f2_t a, f2_t b) {
     return d;
 }
 
+__device__ __forceinline__ f2_t mul2(f2_t a, f2_t b) {
+    f2_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 // A 16-byte vector as VEC/2 packed pairs of consecutive elements.
 __device__ __forceinline__ void unpack_pairs(const uint4 &v, f2_t (&p)[4], __nv_bfloat16 *) {
     p[0] = pack2(bf16_lo(v.x), bf16_hi(v.x));
@@ -358,8 +364,10 @@ cudaError_t launch_attend(const wz_attend_args &a, void *workspace, cudaStream_t
 // A layer's matrix products (layer.cu, mm_pair.cu); arguments checked.
 cudaError_t launch_linear(const wz_linear_args &a, cudaStream_t s);
 cudaError_t launch_gated(const wz_gated_args &a, cudaStream_t s);
-size_t linear_backward_bytes(int64_t M, int N, int K);
+size_t linear_backward_bytes(int64_t M, int N, int K);             // the most that calls of these sizes need
 size_t gated_backward_bytes(int64_t M, int N, int K);
+size_t linear_backward_need(const wz_linear_backward_args &a);      // what this call needs; 0: none
+size_t gated_backward_need(const wz_gated_backward_args &a);
 cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *workspace, cudaStream_t s);
 cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *workspace, cudaStream_t s);
 // Max-over-query relevance in one pass over the features (maxsim.cu): token

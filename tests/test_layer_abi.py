@@ -119,8 +119,10 @@ def test_workspace_sizes(wz):
         assert f(-1, 64, 64) == 0 and f(1, 0, 64) == 0 and f(1, 64, 65537) == 0 and f(1 << 31, 64, 64) == 0
         assert 0 < f(1, 64, 64) < f(1000, 64, 64) < f(100000, 64, 64)
         assert f(0, 64, 64) >= 0 and f(0, 65536, 65536) < 1 << 30
-        # d, once or twice, and little beside it
-        assert f(18662, 3584, 3584) < 2.5 * 18662 * 3584 * 2
+    # d, once or twice, an eighth of it for sums over 16 rows in fp32, and at most 48 MB of shares' sums
+    for f, both in ((wz.wz_linear_backward_workspace_size, 1), (wz.wz_gated_backward_workspace_size, 2)):
+        d = 18662 * 3584 * 2
+        assert both * d <= f(18662, 3584, 3584) <= both * (d + d // 8 + 40 * 3584 * 4) + (48 << 20)
     assert wz.wz_gated_backward_workspace_size(4103, 3584, 14336) >= 2 * 4103 * 14336 * 2
 
 
