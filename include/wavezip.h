@@ -550,8 +550,8 @@ WZ_API int wz_attend(const wz_attend_args *a);
  * what lies between a row's end and the next row is neither read nor written.
  * Every bf16 array 16-byte aligned, f32 arrays 4-byte.  Results do not depend
  * on the order in which blocks run: equal calls give equal bits.
- *   Outputs must not overlap inputs, but for `out` of wz_linear, which may be
- * `residual` itself (same address and stride).
+ *   Outputs must not overlap inputs or one another, but for `out` of wz_linear, which
+ * may be `residual` itself (same address and stride).
  * Errors of all four: WZ_ERR_INVALID_ARG (null, misaligned, bad size or enum),
  * WZ_ERR_UNSUPPORTED (M past 2^31 - 513, N or K past 65536, M N or M K past 2^40),
  * WZ_ERR_WORKSPACE, WZ_ERR_NO_MEMORY, WZ_ERR_CUDA; nothing is launched on an

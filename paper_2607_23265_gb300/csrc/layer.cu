@@ -297,8 +297,6 @@ struct GradientSplit {
     int tile_x, tile_w;      // rows of a tile
 };
 
-constexpr int kPlanPairs = 76;
-
 // Units of one gradient's products: tiles times shares, and the cycles of one.
 struct Units {
     int64_t n, cycles;
@@ -436,6 +434,13 @@ void forward_product(MmArgs &p, int64_t M, int N, int K, const void *x, int64_t 
     q.from_b[1] = MmOperand{w1, N, K, stride1};
 }
 
+// The products of a forward call, or of the slopes, with the kernel that suits their sizes.
+cudaError_t launch_mm(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_t *part_rows) {
+    MmFewPlan plan;
+    if (plan_mm_few(epi, p, sms, &plan)) return launch_mm_few(epi, p, plan, s, part_rows);
+    return launch_mm_pair(epi, p, sms, s, part_rows);
+}
+
 #ifdef WZ_CHECKED
 uint64_t check_mm_wait_ns = kMmTimeoutNs;
 #endif
@@ -448,12 +453,6 @@ uint64_t mm_wait_ns() {
 #else
     return kMmTimeoutNs;
 #endif
-}
-
-cudaError_t launch_mm(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_t *part_rows) {
-    MmFewPlan plan;
-    if (plan_mm_few(epi, p, sms, &plan)) return launch_mm_few(epi, p, plan, s, part_rows);
-    return launch_mm_pair(epi, p, sms, s, part_rows);
 }
 
 cudaError_t launch_linear(const wz_linear_args &a, cudaStream_t s) {

@@ -10,15 +10,17 @@
 // finishing its share of the rows.  No workspace, no second kernel, equal bits each time.
 //
 // A stage is 64 along K: 128 weight rows (16 KB; in a gated product the gate's and the up
-// projection's of the same 64 outputs) and the rows' tile, each K-major, one box of 64 k of
-// its rows, or MN-major, a box of 64 rows of its 64 k each, with 128-byte swizzle.  What
-// lies outside an operand arrives as zeros.
+// projection's of the same 64 outputs), K-major, one box of 64 k, or, for the gradient of x,
+// MN-major, a box of 64 rows of its 64 k each; and the rows' tile, K-major.  128-byte
+// swizzle; what lies outside an operand arrives as zeros.
 // Warps: 0 copies, 1 products, then all eight the epilogue.
 //
 // Two CTAs share an SM where there are enough of them, so that one's start and epilogue
 // overlap the other's products.  Tensor memory is taken by every CTA and held while it waits
 // for its cluster, so no CTA may be left without: all take 256 columns at most, and more than
-// a third of an SM's shared memory, and the pairs of mm_pair.cu leave too little for one.
+// a third of an SM's shared memory, and the pairs of mm_pair.cu leave too little for one.  Nor
+// may the next grid's CTAs come before: some kernels take tensor memory before they wait for
+// the grid in front of them.
 #include <algorithm>
 #include <atomic>
 #include <cstring>
@@ -115,7 +117,6 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     pdl_wait();   // an operand may be the previous grid's output
     if constexpr (PAIR) ptx::cluster_sync();   // both CTAs' barriers are ready
     else __syncthreads();
-    pdl_trigger();
     // sums may come here from now on, unless the ring is in their place
     if (shared_k && p.apart) cluster_arrive();
 
@@ -126,10 +127,9 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
             // word made it 390 cycles, more than its products take)
             const uint64_t once = ptx::policy_evict_first(), again = ptx::policy_evict_last();
             const uint64_t weights = q.mt > 1 ? again : once;   // row tiles share them in L2
-            const bool a_mn = q.a_mn, b_mn = q.b_mn;
-            const int r0 = row0 + side * (columns / 2);
-            const int boxes = a_mn ? (columns / kGroup + 63) / 64 : 1, steps = q.steps, stages = p.stages;
-            const uint32_t bytes = (uint32_t)kGroup * (uint32_t)(kWeightBytes + (a_mn ? boxes * kBoxBytes : q.box_rows * kStepK * 2));
+            const bool b_mn = q.b_mn;
+            const int r0 = row0 + side * (columns / 2), steps = q.steps, stages = p.stages;
+            const uint32_t bytes = (uint32_t)kGroup * (uint32_t)(kWeightBytes + q.box_rows * kStepK * 2);
             const uint32_t full0 = PAIR ? ptx::map_cluster(&S->full[0], (uint32_t)(rank & ~1)) : 0;
             int seg = step0 / steps, k = (step0 - seg * steps) * kStepK, stage = 0;
             const CUtensorMap *a = &maps.m[q.a[seg]], *b = &maps.m[q.b[seg]], *b2 = &maps.m[q.b[1]];
@@ -154,11 +154,7 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
                 } else {
                     copy(st, b, k, out0, weights);
                 }
-                st += kWeightBytes;
-                if (a_mn)
-                    for (int h = 0; h < boxes; ++h) copy(st + h * kBoxBytes, a, r0 + 64 * h, k, again);
-                else
-                    copy(st, a, k, r0, again);
+                copy(st + kWeightBytes, a, k, r0, again);
                 k += kStepK;
                 if (k == steps * kStepK && seg + 1 < q.segments) {
                     k = 0;
@@ -182,15 +178,15 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
             ptx::tmem_relinquish();
         }
         __syncwarp();
+        pdl_trigger();   // not before: see the top
         if (side == 0 && ptx::elect_one()) {
             // ---------------- products ----------------
-            // K-major: rows of 128 bytes, 8 to a kilobyte; 16 k are 32 bytes.
-            // MN-major: a kilobyte is 8 k of 64 rows, 64 rows on is the next box; 16 k are 2 KB.
+            // (layouts: mm_pair.cu)
             const uint32_t d = *(volatile uint32_t *)&S->tmem_base, ring32 = ptx::smem_u32(ring);
-            const uint32_t idesc = ptx::idesc_bf16(kGroup * kLanes, columns, q.b_mn, q.a_mn);
+            const uint32_t idesc = ptx::idesc_bf16(kGroup * kLanes, columns, q.b_mn, 0);
             const uint64_t w_base = ptx::smem_desc(ring32, q.b_mn ? kBoxBytes : 16, 1024, 2);
-            const uint64_t x_base = ptx::smem_desc(ring32 + kWeightBytes, q.a_mn ? kBoxBytes : 16, 1024, 2);
-            const uint64_t w_step = q.b_mn ? 128 : 2, x_step = q.a_mn ? 128 : 2;
+            const uint64_t x_base = ptx::smem_desc(ring32 + kWeightBytes, 16, 1024, 2);
+            const uint64_t w_step = q.b_mn ? 128 : 2, x_step = 2;
             const int stages = p.stages;
             const uint16_t both = (uint16_t)(3u << (rank & ~1));
             int stage = 0;
@@ -281,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
         constexpr int U = 2;                              // rows in flight
         MmAt<EPI> at(p, q, (int64_t)row0 + first, o.i);
         float other[U][4];
-        if (ok && o.left > 0) mm_fetch<EPI, U, false>(at, o.left, other, kRowsAll, (hi - first + kRowsAll - 1) / kRowsAll);
+        if (ok && o.left > 0) mm_fetch<EPI, U>(at, o.left, other, kRowsAll, (hi - first + kRowsAll - 1) / kRowsAll);
         if (shared_k) ptx::cluster_sync();
         else __syncthreads();
         if (ok && o.left > 0)
@@ -303,9 +299,9 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
                                 }
                             }
                     }
-                    mm_finish<EPI, ACT, U, false>(at, o, v, u, other, kRowsAll, count);
+                    mm_finish<EPI, ACT, U>(at, o, v, u, other, kRowsAll, count);
                     at.advance(U * kRowsAll);
-                    mm_fetch<EPI, U, false>(at, o.left, other, kRowsAll, count - U);
+                    mm_fetch<EPI, U>(at, o.left, other, kRowsAll, count - U);
                 }
             });
         if (end == rows) break;
@@ -352,9 +348,6 @@ namespace {
 
 int round_up(int x, int to) { return (x + to - 1) / to * to; }
 
-// A row tile's bytes of a stage.
-int row_bytes(const MmProblem &q, int rows) { return (q.a_mn ? round_up(rows, 64) : rows) * kStepK * 2; }
-
 // The most rows of sums that come to a CTA of a shared K: a chunk from each share.
 int sums_rows(int tile_m, int split) { return (tile_m + 4 * split - 1) / (4 * split) * 4 * split; }
 
@@ -386,6 +379,7 @@ const Places *cluster_places() {
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return nullptr;
     if (known[dev].load(std::memory_order_acquire)) return &places[dev];
     std::lock_guard<std::mutex> lock(mu);
+    if (known[dev].load(std::memory_order_relaxed)) return &places[dev];
     const void *fn = (const void *)mm_few_kernel<kMmStore, false>;
     if (allow_smem(fn, kSmemOne) != cudaSuccess) return nullptr;
     for (int size = 1; size <= kMaxCluster; ++size) {
@@ -499,13 +493,12 @@ cudaError_t launch_mm_few(MmEpilogue epi, MmArgs &p, const MmFewPlan &plan, cuda
     const int64_t clusters = q.tiles;
     const int dump = q.split > 1 ? std::max(sums_rows(q.tile_m, q.split) * kRowBytes, kWarps * 1024) : 0;
     const int most_steps = q.share + (q.more ? 1 : 0);
-    p.stage_bytes = kWeightBytes + row_bytes(q, q.box_rows);
-    for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.a_mn ? 64 : q.box_rows);
+    p.stage_bytes = round_up(kWeightBytes + q.box_rows * kStepK * 2, 1024);
+    for (int j = 0; j < q.segments; ++j) q.a[j] = list.add(q.from_a[j], q.box_rows);
     for (int j = 0; j < (mm_both(epi) ? 2 : q.segments); ++j)
         q.b[j] = list.add(q.from_b[j], q.b_mn || mm_both(epi) ? 64 : kLanes);
     if (!list.ok || clusters * p.cluster > INT32_MAX) return cudaErrorInvalidValue;
     p.maps = list.count;
-    p.stage_bytes = round_up(p.stage_bytes, 1024);
     const Places *places = cluster_places();
     if (!places) return cudaErrorInvalidDevice;
     const bool two = dump + kExtra <= kSmemTwo && clusters > places->n[p.cluster];
@@ -543,20 +536,5 @@ extern "C" __attribute__((visibility("default"))) void wz_check_mm_plan(int kind
     wz::check_kind = kind;
     wz::check_split = split;
     wz::check_tile = tile_m;
-}
-// Test hook: what a forward product of aligned rows takes on the current device: the kind, shares and tile of
-// wz_check_mm_plan.
-extern "C" __attribute__((visibility("default"))) int wz_check_mm_choice(int gated, int64_t M, int N, int K, int *split, int *tile) {
-    const int sms = wz::sm_count();
-    if (sms < 2) return -1;
-    wz::MmArgs p;
-    memset(&p, 0, sizeof(p));
-    p.problems = 1;
-    wz::MmProblem &q = p.prob[0];
-    q.M = (int)M, q.N = N, q.segments = 1, q.steps = (K + 63) / 64;
-    wz::MmFewPlan plan;
-    if (!wz::plan_mm_few(gated ? wz::kMmGated : wz::kMmStore, p, sms, &plan)) return 1;
-    *split = plan.split, *tile = plan.tile_m;
-    return plan.pair ? 3 : 2;
 }
 #endif

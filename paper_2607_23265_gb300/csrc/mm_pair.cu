@@ -37,12 +37,6 @@ constexpr int kThreads = (2 + kEpiWarps) * 32;
 constexpr int kAccCols = 256;                            // the most rows of a tile
 constexpr int kUnitRows = 16;                            // rows that an epilogue warp takes at a time
 constexpr int kGiveFloats = kUnitRows * 32;              // sums that a warp of a gated product gives away
-constexpr int kPlanPairs = 76;                           // pairs of SMs that tiles are planned for
-// The tensor cores cut off what a sum cannot hold each time that 16 products are added to it, so that long sums
-// come out a little too small: bias gradients, which are f32 and made of slopes at such sums, are 1.3e-6 off in norm
-// with K = 1,152, 4.6e-6 with 3,584 and 9.4e-6 with 14,336 (bf16 results do not notice).  Products that are formed
-// again for their slopes keep two sums when they have more steps than kLongSteps, of the even and of the odd ones, in
-// tiles of half the rows: 4.6e-6 with 14,336.  (mm_few.cu: a share of K for each as many steps.)
 constexpr int kGroupRows = 8;                            // row tiles that are walked together
 
 struct Shared {
@@ -387,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                                 float value, slope;
                                 mm_slope1<ACT>(x[j], value, slope);
                                 x[j] = other[j] * slope;
-                                sum0 += x[j];
+                                sum0 += c + j < there ? x[j] : 0.f;   // (rows behind the last have no finite product where a weight has none)
                             }
                         }
                         if (from) {   // the next rows'
@@ -432,8 +426,8 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                                 mm_slope1<ACT>(x[j], value, slope);
                                 x[j] = other[j] * y[j] * slope;
                                 y[j] = other[j] * value;
-                                sum0 += x[j];
-                                sum1 += y[j];
+                                sum0 += j < count ? x[j] : 0.f;
+                                sum1 += j < count ? y[j] : 0.f;
                             }
                             from += kStride * s_from;
                             fetch(from, s_from, count - kStride, other);

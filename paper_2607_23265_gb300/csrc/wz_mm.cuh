@@ -18,7 +18,14 @@ namespace wz {
 constexpr int kMmMaps = 8;
 constexpr int kMmProblems = 3;
 constexpr uint64_t kMmTimeoutNs = 2000000000ull;
-constexpr int kLongSteps = 64;   // see mm_pair.cu
+// The tensor cores cut off what a sum cannot hold each time that 16 products are added to it, so that long sums
+// come out a little too small: bias gradients, which are f32 and made of slopes at such sums, are 1.3e-6 off in norm
+// with K = 1,152, 4.6e-6 with 3,584 and 9.4e-6 with 14,336 (bf16 results do not notice).  Products that are formed
+// again for their slopes keep two sums when they have more steps of 64 than this, of the even and of the odd ones, in
+// tiles of half the rows (mm_pair.cu), or a share of K for each as many steps (mm_few.cu): 4.6e-6 with 14,336.
+constexpr int kLongSteps = 64;
+// Pairs of SMs that tiles are planned for: a constant, so that workspace sizes and results do not depend on the device.
+constexpr int kPlanPairs = 76;
 
 struct MmMaps {
     CUtensorMap m[kMmMaps];   // 2D, boxes 64 wide with 128-byte swizzle
@@ -70,7 +77,7 @@ struct MmProblem {
     float *sums;           // pairs, K shared: [split][M][N] sums of the shares
     int tile_m;            // rows of a tile; pairs: 0 lets the launch choose them
     int mt, nt, tiles;     // tiles along M and N, and all of them (with shared K, of all shares)
-    MmDivisor by_mt;       // few-rows kernel
+    MmDivisor by_mt;       // mm_few.cu
     MmDivisor by_group, by_last;   // pairs: tiles of a group of row tiles, row tiles of the last one
     int head, from, skip;  //   its first tiles, for the pairs from one on, the turn's first
     int box_rows;          // a CTA's
@@ -91,7 +98,7 @@ struct MmArgs {
     int64_t residual_stride, dy_stride, pre_stride[2], out2_stride;
     int maps;                               // tensor maps in use
     int second;                             // pairs: columns from the even steps' sums to the odd ones'; 0: one
-    int cluster;                            // few-rows kernel: CTAs of a cluster, the ring,
+    int cluster;                            // mm_few.cu: CTAs of a cluster, the ring,
     MmDivisor by_cluster;
     int stages, stage_bytes, ring_bytes;
     int sums_bytes;                         //   joined sums, at its end where they are
@@ -281,8 +288,9 @@ __device__ __forceinline__ void mm_load(const __nv_bfloat16 *p, float (&x)[C], i
 }
 
 // ---- finishing -------------------------------------------------------------------
-// The sums D^T of a tile go through shared memory, [row][output], and are finished row by
-// row, four outputs to a lane: a warp reads and writes 256 (or 128) contiguous bytes.
+// How mm_few.cu finishes sums: they go through shared memory, [row][output], and are finished row
+// by row, four outputs to a lane: a warp reads and writes 256 (or 128) contiguous bytes.
+// (mm_pair.cu finishes them where they are read.)
 
 struct MmOutputs {
     int i, left;        // the lane's first output; how many there are from it on
@@ -346,23 +354,22 @@ struct MmAt {
 };
 
 // The residual, or dy, of U rows `step` apart, of which the first `count` (in steps) are there.
-// FULL: all of them, and all four outputs.
-template <int EPI, int U, bool FULL>
+template <int EPI, int U>
 __device__ __forceinline__ void mm_fetch(const MmAt<EPI> &at, int left, float (&other)[U][4], int step, int count) {
     if (EPI == kMmGated || !at.from) return;
 #pragma unroll
     for (int k = 0; k < U; ++k)
-        if (FULL || k < count) mm_load4(at.from + k * step * at.s_from, other[k], FULL ? 4 : left);
+        if (k < count) mm_load4(at.from + k * step * at.s_from, other[k], left);
 }
 
 // Finishes and stores them: v holds the sums (g in a gated product, u its other ones).
-template <int EPI, int ACT, int U, bool FULL>
+template <int EPI, int ACT, int U>
 __device__ __forceinline__ void mm_finish(const MmAt<EPI> &at, MmOutputs &o, float (&v)[U][4], float (&u)[U][4],
                                           const float (&other)[U][4], int step, int count) {
-    const int left = FULL ? 4 : o.left;
+    const int left = o.left;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-        if (!FULL && k >= count) break;
+        if (k >= count) break;
         float y[4], z[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -416,11 +423,8 @@ __device__ __forceinline__ void mm_read16(uint32_t tcol, float (&x)[16]) {
 // M / 128 + 3 row tiles.
 __host__ __device__ inline int64_t mm_part_rows(int64_t M) { return (M + 15) / 16 + 32; }
 
-// The products with the kernel that suits their sizes; part_rows (nullable): the rows of
-// sums that it writes.
-cudaError_t launch_mm(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_t *part_rows);
-
-// Tiles of 256 outputs x up to 256 rows on pairs of SMs (mm_pair.cu).
+// Tiles of 256 outputs x up to 256 rows on pairs of SMs (mm_pair.cu).  part_rows (nullable), here and
+// below: the rows of sums that the launch writes.
 int mm_pair_tile(int64_t M, int64_t output_tiles);   // their rows
 cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, int64_t *part_rows);
 

@@ -167,3 +167,32 @@ def test_every_kernel(wz, forced, M, N, K, plan):
     for kept in (True, False):
         linear_backward(wz, M, N, K, act, kept)
         gated_backward(wz, M, N, K, act, kept)
+
+
+@pytest.mark.parametrize("plan", [(0, 1, 64), (1, 1, 64), (2, 2, 64), (3, 1, 96)])
+@pytest.mark.parametrize("M", [1, 33, 70])
+def test_bias_gradients_of_infinite_products(wz, forced, M, plan):
+    """A weight that is infinite: the products are, and GELU's slope there is 1.  A tile's rows behind the last one, whose
+    products with it are not numbers, have no part in the sums."""
+    forced(*plan)
+    g = gen(M)
+    N, K, bad = 130, 64, 5
+    x, (w, wu), dy = ref.random_rows(M, K, 1.0, g), (ref.random_rows(N, K, 0.2, g) for _ in range(2)), ref.random_rows(M, N, 0.1, g)
+    x[:, 3] = 1.0
+    dy[:, bad] = dy[:, bad].abs()
+    w[bad, 3] = float("inf")
+    large = w.clone()
+    large[bad, 3] = 2.0 ** 60   # the same slopes
+    db = wz.wz_linear_backward(dy, x, w, act="gelu", need_x=False, need_w=False, need_b=True)[2]
+    d, e = ref.linear_delta(dy, x, large, None, None, "gelu")
+    e[:, bad] = ref.FORM * dy[:, bad].double().abs()
+    ref.check(db, ref.gradients(x, [(d, e)], [large])[2][0], "db")
+    got = wz.wz_gated_backward(dy, x, w, wu, act="gelu", need_x=False, need_w=False, need_b=True)[3:]
+    (dg, eg), (du, eu) = ref.gated_delta(dy, x, large, wu, None, None, None, None, "gelu")
+    u, err = ref.product(x, wu)
+    eg[:, bad] = (dy.double().abs() * (err + 2 * ref.FORM * u.abs()))[:, bad]
+    ref.check(got[0], ref.gradients(x, [(dg, eg)], [large])[2][0], "db_gate")
+    keep = torch.arange(N, device="cuda") != bad
+    want, bound = ref.gradients(x, [(du, eu)], [large])[2][0]
+    ref.check(got[1][keep], (want[keep], bound[keep]), "db_up")
+    assert float(got[1][bad]) == float("inf")
