@@ -41,6 +41,9 @@ constexpr int kMaxStages = 12;
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kMaxCluster = 8;
+// Steps whose weights are sent for before the grid in front has ended: 1 x 3584 x 2 x 14336 (rows x K x outputs) 32.2 us
+// without, 30.8 with; 64 x 14336 x 3584 20.0 and 19.5; 32 steps: 36.7 and 20.6.  (Nothing gained in mm_pair.cu.)
+constexpr int kAhead = 12;
 
 struct Shared {
     uint64_t full[kMaxStages];
@@ -114,6 +117,17 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
         __syncwarp();
     }
     if (warp == 2 && lane < p.maps) ptx::prefetch_tmap(&maps.m[lane]);
+    // the first weights come to L2 while the grid before this one ends
+    if (warp == 3 && row0 == 0 && lane < kAhead && step0 + lane < step1) {
+        const int seg = (step0 + lane) / q.steps, k = (step0 + lane - seg * q.steps) * kStepK;
+        if (kBoth || !q.b_mn) {
+            ptx::tma_prefetch_2d(&maps.m[q.b[seg]], k, out0);
+            if constexpr (kBoth) ptx::tma_prefetch_2d(&maps.m[q.b[1]], k, out0);
+        } else {
+            ptx::tma_prefetch_2d(&maps.m[q.b[seg]], out0, k);
+            ptx::tma_prefetch_2d(&maps.m[q.b[seg]], out0 + 64, k);
+        }
+    }
     pdl_wait();   // an operand may be the previous grid's output
     if constexpr (PAIR) ptx::cluster_sync();   // both CTAs' barriers are ready
     else __syncthreads();
