@@ -136,21 +136,22 @@ __global__ void __launch_bounds__(32 * kDeltaWarps) mm_delta_kernel(const __grid
 
 namespace {
 
-constexpr int kSumRows = 16, kSumThreads = 32 * kSumRows;
+constexpr int kSumThreads = 32 * kSumRows;
 constexpr int kJoinRows = 4;   // rows that a thread of a join takes
-// Up to so many rows the last kernel adds dy's up by itself: a kernel less before the products (577 x 3584:
-// 3.7 us of 23).
-constexpr int64_t kSumsInJoin = 1024;
+// Up to so many rows of dy are added up as they are, if need be by the last kernel, which is a kernel less before the
+// products.
+constexpr int64_t kFewSumRows = 1024;
+// A CTA of the products adds up to so many blocks of 32 columns of them, or of sums over some rows, before its first
+// tile; more are left to the last kernel (577 x 1152 x 3584 (M x K x N) 19.5 us with it, 15.8 without).
+constexpr int kSumBlocksEach = 4;
+// And of more rows where the first tile's products take longer: 13 / 2 cycles a row of a block.  4,096 rows of
+// 3584 x 14336 (K x N) 434 us, with a kernel for sums over 64 rows before 460; 18,662 of 3584 x 3584 500 and 523;
+// but 4,096 of 256 x 4608, whose tiles are short, 68 and 34.
+constexpr int64_t kSumRowCycles2 = 13;
 
 // What is left to add up when the products are done.
 struct JoinArgs {
-    // bias gradients: db[i][n] = the sum of part[i][.][n], or of dy's rows
-    const float *part[2];
-    float *db[2];
-    int64_t part_rows;
-    const __nv_bfloat16 *dy;
-    int64_t dy_stride, dy_rows;
-    int N;
+    MmSums sums;
     // products whose K was shared: out = the sum of sums[split][M][cols]
     struct {
         const float *sums;
@@ -159,39 +160,20 @@ struct JoinArgs {
         int cols, split;
         unsigned first;        // its first block
     } join[kMmProblems];
-    unsigned sum_blocks;       // of one bias gradient
     int joins;
 };
 
 }  // namespace
 
-// The first blocks take 32 columns of a bias gradient each, 16 rows at a time; the others 512
-// outputs of four rows of a shared product, a thread four outputs, in the shares' order.
+// The first blocks take 32 columns of a bias gradient each; the others 512 outputs of four rows of a
+// shared product, a thread four outputs, in the shares' order.
 __global__ void __launch_bounds__(kSumThreads) mm_join_kernel(const __grid_constant__ JoinArgs p) {
     __shared__ float sums[kSumRows][33];
     pdl_wait();
     pdl_trigger();
     unsigned block = blockIdx.x;
-    if (block < 2 * p.sum_blocks) {
-        const int which = block >= p.sum_blocks;
-        const float *part = p.part[which];
-        float *out = p.db[which];
-        const int c = (int)threadIdx.x & 31, r0 = (int)threadIdx.x >> 5;
-        const int n = (int)(block - which * p.sum_blocks) * 32 + c;
-        float s = 0.f;
-        if (n < p.N && out) {
-#pragma unroll 8
-            for (int64_t r = r0; r < p.part_rows; r += kSumRows) s += part[(size_t)r * p.N + n];
-#pragma unroll 8
-            for (int64_t r = r0; r < p.dy_rows; r += kSumRows) s += __bfloat162float(p.dy[r * p.dy_stride + n]);
-        }
-        sums[r0][c] = s;
-        __syncthreads();
-        if (r0 == 0 && n < p.N && out) {
-#pragma unroll
-            for (int i = 1; i < kSumRows; ++i) s += sums[i][c];
-            out[n] = s;
-        }
+    if ((int)block < p.sums.blocks) {
+        mm_column_sums(p.sums, (int)block, (int)threadIdx.x, sums, [] { __syncthreads(); });
         return;
     }
     int i = 0;
@@ -245,8 +227,7 @@ cudaError_t launch_delta(DeltaMode mode, DeltaArgs &p, cudaStream_t s) {
 
 // Launches p's sums and joins, if there are any.
 cudaError_t launch_join(JoinArgs &p, cudaStream_t s) {
-    p.sum_blocks = p.db[0] || p.db[1] ? (unsigned)((p.N + 31) / 32) : 0;
-    int64_t blocks = 2 * (int64_t)p.sum_blocks;
+    int64_t blocks = p.sums.blocks;
     for (int i = 0; i < p.joins; ++i) {
         p.join[i].first = (unsigned)blocks;
         blocks += (p.join[i].M + 4 * kJoinRows - 1) / (4 * kJoinRows) * ((p.join[i].cols + 511) / 512);
@@ -275,8 +256,10 @@ int64_t steps_of(int64_t k) { return (k + 63) / 64; }
 JoinArgs join_args(const float *part0, const float *part1, float *db0, float *db1, int64_t rows, int N) {
     JoinArgs j;
     memset(&j, 0, sizeof(j));
-    j.part[0] = part0, j.part[1] = part1, j.db[0] = db0, j.db[1] = db1;
-    j.part_rows = rows, j.N = N;
+    MmSums &p = j.sums;
+    p.part[0] = part0, p.part[1] = part1, p.db[0] = db0, p.db[1] = db1;
+    p.part_rows = rows, p.N = N;
+    p.blocks = ((db0 ? 1 : 0) + (db1 ? 1 : 0)) * ((N + 31) / 32);
     return j;
 }
 
@@ -363,9 +346,10 @@ GradientSplit split_gradients(int64_t M, int N, int K, int both, bool dx, bool d
     return best;
 }
 
-// The products of both gradients in one launch; what they leave to be joined goes into `join`.
-cudaError_t launch_gradients(const Gradients &g, const GradientSplit &split, char *shares, JoinArgs &join, int *status,
-                             int sms, cudaStream_t s) {
+// The products of both gradients in one launch, with the bias gradients of `join` where they are few enough; what
+// they leave to be joined goes into `join`.
+cudaError_t launch_gradients(const Gradients &g, const GradientSplit &split, bool beside, char *shares, JoinArgs &join,
+                             int *status, int sms, cudaStream_t s) {
     MmArgs p = mm_args(WZ_ACT_NONE, status);
     MmProblem in, weight[2];
     memset(&in, 0, sizeof(in));
@@ -410,6 +394,10 @@ cudaError_t launch_gradients(const Gradients &g, const GradientSplit &split, cha
         for (int i = 0; i < g.both; ++i) add(weight[i], split.dw);
     if (g.dx && weights_first) add(in, split.dx);
     if (!p.problems) return cudaSuccess;
+    if (beside || join.sums.blocks <= kSumBlocksEach * sms) {
+        p.sums = join.sums;
+        join.sums.blocks = 0;
+    }
     return launch_mm_pair(kMmStore, p, sms, s, nullptr);
 }
 
@@ -481,33 +469,46 @@ cudaError_t launch_gated(const wz_gated_args &a, cudaStream_t s) {
 
 namespace {
 
+// Whether dy's sums are ready before the products of the first tiles.
+bool sums_beside(int64_t M, int N, int K, const GradientSplit &split, bool dx, bool dw) {
+    const Units none{0, 0}, x = dx ? units(M, K, 1, steps_of(N), split.tile_x, split.dx) : none,
+                            w = dw ? units(N, K, 1, steps_of(M), split.tile_w, split.dw) : none;
+    const int64_t ctas = 2 * std::min<int64_t>(kPlanPairs, x.n + w.n);
+    return dw && M * (((N + 31) / 32 + ctas - 1) / ctas) * kSumRowCycles2 <= 2 * std::max(x.cycles, w.cycles);
+}
+
 // How a backward call is cut, and where its parts are in its workspace: d, sums over rows, shares' sums, as
 // many as it needs.
 struct BackwardLayout {
     GradientSplit split;
-    size_t d[2], part[2], shares, total;
-    BackwardLayout(int64_t M, int N, int K, int both, bool with_d, const bool (&with_part)[2], bool dx, bool dw)
-        : split(split_gradients(M, N, K, both, dx, dw)), total(0) {
-        const auto take = [&](size_t bytes) {
-            const size_t at = total;
-            total += bytes;
-            return at;
-        };
+    bool beside = false, of_dy = false;   // dy is added up beside the products; without sums over some rows before
+    size_t d[2], part[2] = {}, shares, total = 0;
+    BackwardLayout(int64_t M, int N, int K, int both, bool dx, bool dw) : split(split_gradients(M, N, K, both, dx, dw)) {}
+    size_t take(size_t bytes) {
+        const size_t at = total;
+        total += bytes;
+        return at;
+    }
+    void place(int64_t M, int N, int K, int both, bool with_d, bool part0, bool part1) {
         for (int i = 0; i < 2; ++i) d[i] = take(with_d && i < both ? delta_bytes(M, N) : 0);
-        for (int i = 0; i < 2; ++i) part[i] = take(with_part[i] ? part_bytes(M, N) : 0);
+        part[0] = take(part0 ? part_bytes(M, N) : 0);
+        part[1] = take(part1 ? part_bytes(M, N) : 0);
         shares = take(shares_bytes(M, N, K, both, split.dx, split.dw));
     }
 };
 
-// Whether the last kernel adds dy up by itself.
-bool sums_in_join(const wz_linear_backward_args &a) { return a.act == WZ_ACT_NONE && a.M <= kSumsInJoin; }
-
 BackwardLayout layout_of(const wz_linear_backward_args &a) {
-    return BackwardLayout(a.M, a.N, a.K, 1, a.act != WZ_ACT_NONE, {a.db && !sums_in_join(a), false}, a.dx, a.dw);
+    BackwardLayout at(a.M, a.N, a.K, 1, a.dx, a.dw);
+    at.beside = a.act == WZ_ACT_NONE && sums_beside(a.M, a.N, a.K, at.split, a.dx, a.dw);
+    at.of_dy = at.beside || (a.act == WZ_ACT_NONE && a.M <= kFewSumRows);
+    at.place(a.M, a.N, a.K, 1, a.act != WZ_ACT_NONE, a.db && !at.of_dy, false);
+    return at;
 }
 
 BackwardLayout layout_of(const wz_gated_backward_args &a) {
-    return BackwardLayout(a.M, a.N, a.K, 2, true, {a.db_gate != nullptr, a.db_up != nullptr}, a.dx, a.dw_gate);
+    BackwardLayout at(a.M, a.N, a.K, 2, a.dx, a.dw_gate);
+    at.place(a.M, a.N, a.K, 2, true, a.db_gate, a.db_up);
+    return at;
 }
 
 // The most that a call of these sizes needs, whichever gradients it asks for.
@@ -539,7 +540,7 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
     const int64_t d_stride = delta_stride(a.N);
     const BackwardLayout at = layout_of(a);
     __nv_bfloat16 *d = half((void *)(ws + at.d[0]));
-    float *part = a.db && !sums_in_join(a) ? reinterpret_cast<float *>(ws + at.part[0]) : nullptr;
+    float *part = a.db && !at.of_dy ? reinterpret_cast<float *>(ws + at.part[0]) : nullptr;
     int64_t part_rows = (a.M + kDeltaRows - 1) / kDeltaRows;
     if (a.act != WZ_ACT_NONE && !a.pre) {
         MmArgs p = mm_args(a.act, a.device_status);
@@ -570,11 +571,11 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
     g.dw[0] = a.dw, g.dw_stride[0] = a.dw_stride;
     g.M = a.M, g.N = a.N, g.K = a.K;
     JoinArgs join = join_args(part, nullptr, a.db, nullptr, part_rows, a.N);
-    if (sums_in_join(a)) {
-        join.part_rows = 0;
-        join.dy = half(a.dy), join.dy_stride = a.dy_stride, join.dy_rows = a.M;
+    if (at.of_dy) {
+        join.sums.part_rows = 0;
+        join.sums.dy = half(a.dy), join.sums.dy_stride = a.dy_stride, join.sums.dy_rows = a.M;
     }
-    MM_TRY(launch_gradients(g, at.split, ws + at.shares, join, a.device_status, sms, s));
+    MM_TRY(launch_gradients(g, at.split, at.beside, ws + at.shares, join, a.device_status, sms, s));
     return launch_join(join, s);
 }
 
@@ -628,7 +629,7 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
     g.dw_stride[0] = a.dw_gate_stride, g.dw_stride[1] = a.dw_up_stride;
     g.M = a.M, g.N = a.N, g.K = a.K;
     JoinArgs join = join_args(part[0], part[1], db[0], db[1], part_rows, a.N);
-    MM_TRY(launch_gradients(g, at.split, ws + at.shares, join, a.device_status, sms, s));
+    MM_TRY(launch_gradients(g, at.split, at.beside, ws + at.shares, join, a.device_status, sms, s));
     return launch_join(join, s);
 }
 

@@ -49,6 +49,8 @@ struct Shared {
     int abort;
 };
 
+static_assert(kEpiWarps == kSumRows && kGiveFloats >= 33, "mm_column_sums");
+
 constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kEpiWarps * kGiveFloats * 4 + sizeof(Shared);
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of the pair CTA");
 
@@ -309,6 +311,14 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
         float *give = gives + (4 * side + quadrant) * kGiveFloats + lane;
         const float *take = gives + (4 * side + (quadrant ^ 2)) * kGiveFloats + lane;
         const uint32_t tempty[2] = {ptx::map_cluster(&S->tempty[0], 0), ptx::map_cluster(&S->tempty[1], 0)};
+        if constexpr (EPI == kMmStore) {
+            // bias gradients, while the first products are on their way
+            const auto barrier = [] { asm volatile("bar.sync 14, %0;" ::"n"(kEpiWarps * 32) : "memory"); };
+            for (int x = (int)blockIdx.x; x < p.sums.blocks; x += (int)gridDim.x) {
+                mm_column_sums(p.sums, x, (int)threadIdx.x - 64, reinterpret_cast<float (*)[33]>(gives), barrier);
+                barrier();
+            }
+        }
         int it = 0;
         while (walk.next(t)) {
             const MmProblem &q = p.prob[t.prob];

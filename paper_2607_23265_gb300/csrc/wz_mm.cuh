@@ -85,8 +85,20 @@ struct MmProblem {
     int share, more;       //   K steps of a share, shares that have one more
 };
 
+// Bias gradients: db[i][n] = the sum of part[i][.][n], or of dy's rows.
+struct MmSums {
+    const float *part[2];
+    float *db[2];                           // null: not wanted
+    int64_t part_rows;
+    const __nv_bfloat16 *dy;
+    int64_t dy_stride, dy_rows;
+    int N;
+    int blocks;                             // of 32 columns of either, all together; 0: none
+};
+
 struct MmArgs {
     MmProblem prob[kMmProblems];
+    MmSums sums;                            // mm_pair.cu, kMmStore: added up before a CTA's first tile
     int problems;
     int act;                                // WZ_ACT_*
     const float *bias[2];                   // [N]; null: none
@@ -401,6 +413,42 @@ __device__ __forceinline__ void mm_finish(const MmAt<EPI> &at, MmOutputs &o, flo
             if (at.pre0) mm_store4(at.pre1 + k * step * at.s_pre1, u[k], left);
         mm_store4(at.out + k * step * at.s_out, y, left);
         if constexpr (EPI == kMmGatedSlope) mm_store4(at.out2 + k * step * at.s_out2, z, left);
+    }
+}
+
+// 32 columns of a bias gradient, by 16 warps: a lane has a column, a warp every 16th row, 16 of them
+// on their way at a time; then the warps' sums in order.  barrier(): of the 16 warps.
+constexpr int kSumRows = 16;
+
+template <typename F>
+__device__ __forceinline__ void mm_column_sums(const MmSums &p, int block, int thread, float (*sums)[33], F barrier) {
+    const int columns = (p.N + 31) / 32, which = p.db[0] && block < columns ? 0 : 1;
+    const float *part = p.part[which];
+    const int c = thread & 31, r0 = thread >> 5;
+    const int n = (which && p.db[0] ? block - columns : block) * 32 + c;
+    float s = 0.f;
+    if (n < p.N) {
+        const auto add = [&](int64_t rows, auto value) {
+            for (int64_t r = r0; r < rows; r += 16 * kSumRows) {
+                float x[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) x[k] = r + k * kSumRows < rows ? value(r + k * kSumRows) : 0.f;
+#pragma unroll
+                for (int d = 1; d < 16; d *= 2)
+#pragma unroll
+                    for (int k = 0; k < 16; k += 2 * d) x[k] += x[k + d];
+                s += x[0];
+            }
+        };
+        add(p.part_rows, [&](int64_t r) { return part[r * p.N + n]; });
+        add(p.dy_rows, [&](int64_t r) { return __bfloat162float(p.dy[r * p.dy_stride + n]); });
+    }
+    sums[r0][c] = s;
+    barrier();
+    if (r0 == 0 && n < p.N) {
+#pragma unroll
+        for (int i = 1; i < kSumRows; ++i) s += sums[i][c];
+        p.db[which][n] = s;
     }
 }
 

@@ -196,3 +196,15 @@ def test_bias_gradients_of_infinite_products(wz, forced, M, plan):
     want, bound = ref.gradients(x, [(du, eu)], [large])[2][0]
     ref.check(got[1][keep], (want[keep], bound[keep]), "db_up")
     assert float(got[1][bad]) == float("inf")
+
+
+@pytest.mark.parametrize("M,N,K", [(3001, 700, 320), (500, 20000, 40), (1100, 20000, 40), (2500, 130, 1000), (1024, 97, 8), (1500, 96, 9)])
+def test_where_bias_gradients_are_added_up(wz, M, N, K):
+    """Beside the products, by a kernel of their own, and from sums over some rows: more rows and columns of dy than fit
+    into one of them."""
+    linear_backward(wz, M, N, K, "none", False)
+    linear_backward(wz, M, N, K, "silu", True)
+    s = Layer(M, N, K, 1, bias=False, pad=8, seed=M)
+    for kw in (dict(need_x=False), dict(need_w=False), dict(need_x=False, need_w=False)):
+        db = wz.wz_linear_backward(s.dy, s.x, s.w[0], need_b=True, **kw)[2]
+        ref.check(db, ref.gradients(s.x, [(s.dy.double(), torch.zeros_like(s.dy).double())], s.w, True)[2][0], str(kw))
