@@ -9,9 +9,17 @@
 // 256: 333 rows are tiles of 192 and 160.  An operand tile is K-major, one box of
 // 64 k of its rows, or MN-major, a box of 64 rows of its 64 k each, both with 128-byte
 // swizzle; what lies outside an operand arrives as zeros, so any size works.  (A thread
-// issues a copy every 55 cycles: with boxes of 64 x 64 and 32 x 64 a step of 192 rows took 0.32 us.)  In a gated product a CTA's 128 lanes are the
-// gate's weights of 64 outputs and the up projection's of the same 64.
-//   Persistent pairs walk the tiles of up to three products.
+// issues a copy every 55 cycles: with boxes of 64 x 64 and 32 x 64 a step of 192 rows took
+// 0.32 us.)  In a gated product a CTA's 128 lanes are the gate's weights of 64 outputs and
+// the up projection's of the same 64.
+//   Persistent pairs walk the tiles of up to three products: both gradients of a layer are
+// one launch, whose rounds of tiles even out together.
+//   What bounds it: a step of 64 along K is max(2 rows, 256 + rows) cycles, products against
+// the 64 bytes a cycle that come into an SM, so tiles of 256 rows are bound by the tensor
+// cores: 18,662 x 3584 x 3584 253 us (1,892 TFLOP/s), 18,699 x 14336 x 3584 1,155 to 1,196 under
+// the power limit, the pipe 96 % busy.  An epilogue takes 4,900 cycles, 64-byte stores at
+// 4.8 cycles, which fewer than ten steps do not hide; staging them in shared memory, by rows or for
+// TMA stores, was not faster, and TMA writes a whole word where a row ends inside one.
 // Warps: 0 copies, 1 products (the even CTA's), 2-17 epilogue, four a TMEM lane quadrant.  A
 // lane of the epilogue has an output and takes 16 of its rows at a time: a warp reads and
 // writes 64 contiguous bytes of a row, and waits for no other one (in a gated product the
@@ -391,7 +399,8 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                                 float value, slope;
                                 mm_slope1<ACT>(x[j], value, slope);
                                 x[j] = other[j] * slope;
-                                sum0 += c + j < there ? x[j] : 0.f;   // (rows behind the last have no finite product where a weight has none)
+                                // (rows behind the last have no finite product where a weight has none)
+                                sum0 += c + j < there ? x[j] : 0.f;
                             }
                         }
                         if (from) {   // the next rows'
