@@ -16,9 +16,9 @@
 // Warps: 0 copies, 1 products, then all eight the epilogue.
 //
 // Measured: 1 x 3584 x 2 x 14336 (rows x K x outputs) 31.0 us (6.6 TB/s; HBM bounds it), 64 x 14336 x 3584
-// 19.8 (5.3 TB/s), 333 x 3584 x 4608 15.5, of which 2.1 us are the start, 6.7 the products, at 64
-// bytes a cycle into an SM, 3.1 the way of the sums to the CTA that finishes a row (9 bytes a cycle
-// from each CTA: 16-byte stores take as long as 4-byte ones) and 1.8 the finish.
+// 19.8 (5.3 TB/s), 333 x 3584 x 4608 15.4, of which 2.1 us are the start, 6.7 the products, at 64
+// bytes a cycle into an SM, 3.2 the wait for the cluster's other CTAs and the way of the sums (16-byte
+// stores took as long, bulk copies between the CTAs 0.8 us longer) and 1.8 the finish.
 //
 // Two CTAs share an SM where there are enough of them, so that one's start and epilogue
 // overlap the other's products.  Tensor memory is taken by every CTA and held while it waits
