@@ -257,6 +257,30 @@ def test_the_checked_build_agrees(wz, M, K, N):
     assert int(status) == 0
 
 
+@pytest.mark.parametrize("M,K,N", [(1, 512, 1024), (40, 320, 700), (700, 256, 384)])
+def test_weights_that_the_call_before_has_just_written(wz, M, K, N):
+    """The first weights are sent for early; what a product takes is what the grid in front of it has left there."""
+    g = gen(N)
+    x, left = rows(M, K, 1.0, g), [rows(N, 64, 0.4, g) for _ in range(6)]
+    right = rows(K, 64, 0.3, g)
+    w, first = torch.zeros((N, K), dtype=torch.bfloat16, device="cuda"), rows(M, N, 1.0, g)
+    dy, out = first, []
+    for a in left:
+        wz.wz_linear(a, right, out=w)
+        y, h = wz.wz_linear(x, w), wz.wz_gated(x, w, w)
+        wz.wz_linear(a, right, out=w)
+        out.append((y, h, wz.wz_linear_backward(dy, x, w, need_w=False)[0]))
+        dy = y
+    torch.cuda.synchronize()
+    dy = first
+    for a, (y, h, dx) in zip(left, out):
+        w = wz.wz_linear(a, right)
+        torch.cuda.synchronize()
+        assert torch.equal(y, wz.wz_linear(x, w)) and torch.equal(h, wz.wz_gated(x, w, w))
+        assert torch.equal(dx, wz.wz_linear_backward(dy, x, w, need_w=False)[0])
+        dy = y
+
+
 @pytest.mark.parametrize("M,K,N", SHAPES)
 def test_captured_and_replayed(wz, M, K, N):
     """Two graphs that share a workspace, each replayed on new contents, in turn."""
