@@ -20,9 +20,10 @@ constexpr int kMmProblems = 3;
 constexpr uint64_t kMmTimeoutNs = 2000000000ull;
 // The tensor cores cut off what a sum cannot hold each time that 16 products are added to it, so that long sums
 // come out a little too small: bias gradients, which are f32 and made of slopes at such sums, are 1.3e-6 off in norm
-// with K = 1,152, 4.6e-6 with 3,584 and 9.4e-6 with 14,336 (bf16 results do not notice).  Products that are formed
-// again for their slopes keep two sums when they have more steps of 64 than this, of the even and of the odd ones, in
-// tiles of half the rows (mm_pair.cu), or a share of K for each as many steps (mm_few.cu): 4.6e-6 with 14,336.
+// with K = 1,152, 4.6e-6 with 3,584 and 9.4e-6 with 14,336 (bf16 results do not notice).  Two sums, of the even and of the
+// odd steps of 64 along K, halve that (6.5e-7 with 1,152, 4.6e-6 with 14,336).  Products that are formed again for their
+// slopes keep two in mm_pair.cu, in tiles of half the rows, when they have more steps than this or it costs next to
+// nothing, and have a share of K for each as many steps in mm_few.cu.
 constexpr int kLongSteps = 64;
 // Pairs of SMs that tiles are planned for: a constant, so that workspace sizes and results do not depend on the device.
 constexpr int kPlanPairs = 76;
