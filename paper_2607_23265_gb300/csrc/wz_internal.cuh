@@ -361,7 +361,7 @@ cudaError_t launch_kv_append(const wz_kv_append_args &a, cudaStream_t s);
 size_t attend_workspace_bytes(int64_t T, int Hq);        // the most that a call of these sizes needs
 size_t attend_workspace_need(const wz_attend_args &a);   // what this call needs; 0: none
 cudaError_t launch_attend(const wz_attend_args &a, void *workspace, cudaStream_t s);
-// A layer's matrix products (layer.cu, mm_pair.cu); arguments checked.
+// A layer's matrix products (layer.cu, with mm_pair.cu and mm_few.cu); arguments checked.
 cudaError_t launch_linear(const wz_linear_args &a, cudaStream_t s);
 cudaError_t launch_gated(const wz_gated_args &a, cudaStream_t s);
 size_t linear_backward_bytes(int64_t M, int N, int K);             // the most that calls of these sizes need
