@@ -390,12 +390,18 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                             put(pre, s_pre, there - c, x);
                             pre += kStride * s_pre;
                         }
+                        if constexpr (EPI == kMmStore) {
+                            float far_there[kUnitRows];
+                            const bool far = mm_far<ACT>(x, far_there);
 #pragma unroll
-                        for (int j = 0; j < kUnitRows; ++j) {
-                            if constexpr (EPI == kMmStore) {
-                                x[j] = mm_act1<ACT>(x[j]);
+                            for (int j = 0; j < kUnitRows; ++j) x[j] = mm_act1<ACT>(x[j]);
+                            mm_put_far<false>(far, far_there, x);
+#pragma unroll
+                            for (int j = 0; j < kUnitRows; ++j)
                                 if (from) x[j] += other[j];
-                            } else {
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < kUnitRows; ++j) {
                                 float value, slope;
                                 mm_slope1<ACT>(x[j], value, slope);
                                 x[j] = other[j] * slope;
@@ -435,10 +441,16 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                         }
                         pair_barrier(barrier);          // both have read
                         const int count = there - c - kUnitRows * kind;
+                        float far_there[kUnitRows];
                         if constexpr (EPI == kMmGated) {
+                            const bool far = mm_far<ACT>(x, far_there);
+                            mm_far_times(far, far_there, y);
 #pragma unroll
                             for (int j = 0; j < kUnitRows; ++j) x[j] = mm_act1<ACT>(x[j]) * y[j];
+                            mm_put_far<true>(far, far_there, x);
                         } else {
+                            const bool far = mm_far<ACT>(x, far_there);
+                            mm_far_times(far, far_there, other);
 #pragma unroll
                             for (int j = 0; j < kUnitRows; ++j) {
                                 float value, slope;
@@ -446,8 +458,10 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                                 x[j] = other[j] * y[j] * slope;
                                 y[j] = other[j] * value;
                                 sum0 += j < count ? x[j] : 0.f;
-                                sum1 += j < count ? y[j] : 0.f;
                             }
+                            mm_put_far<true>(far, far_there, y);
+#pragma unroll
+                            for (int j = 0; j < kUnitRows; ++j) sum1 += j < count ? y[j] : 0.f;
                             from += kStride * s_from;
                             fetch(from, s_from, count - kStride, other);
                             put(out2, p.out2_stride, count, y);

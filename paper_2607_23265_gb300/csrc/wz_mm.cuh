@@ -122,14 +122,25 @@ struct MmArgs {
 };
 
 // ---- activations -------------------------------------------------------------
-// The logistic function and what follows from it are within a few 2^-22 of the
-// value: far below the bf16 rounding of what they go into, and of the order of the
-// f32 rounding of a bias gradient's terms.
+// An exponential is off by about 2^-23 for each unit of its argument (which carries 2^-24 itself), and so are the
+// logistic function and what follows from it, far below 0: 2^-22 around 0, up to 2^-15 near -90.  Values in bf16
+// do not notice; of a bias gradient's terms it is those of little weight.
 
 __device__ __forceinline__ float mm_sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 
 // tanh z = 2 sigmoid(2z) - 1, so that gelu_tanh is x sigmoid(2z).
 __device__ __forceinline__ float mm_gelu_arg(float x) { return 1.5957691216057308f * x * (1.f + 0.044715f * x * x); }
+
+// x sigmoid(z).  Below z = -87 the logistic function comes near the least normal number, where its reciprocal is cut to 0;
+// it is exp(z) there, and its product with x, which stays normal down to -91, is exp(z + 32) times x exp(-32).
+template <int ACT>
+__device__ __forceinline__ bool mm_far1(float x) {
+    return x < (ACT == WZ_ACT_SILU ? -87.f : -9.98f);   // z: x, or mm_gelu_arg(x)
+}
+template <int ACT>
+__device__ __forceinline__ float mm_far_value(float x) {
+    return x * 1.2664165549e-14f * __expf((ACT == WZ_ACT_SILU ? x : mm_gelu_arg(x)) + 32.f);
+}
 
 // The normal distribution's share below x, and exp(-x^2 / 2).  Below -|x| it is
 // exp(-x^2 / 2) erfcx(|x| / sqrt 2) / 2, and the last factor t P(t) with t = 1 / (1 + 0.21 |x|):
@@ -160,6 +171,44 @@ __device__ __forceinline__ float mm_act1(float x) {
     if constexpr (ACT == WZ_ACT_GELU_TANH) return x * mm_sigmoid(mm_gelu_arg(x));
     if constexpr (ACT == WZ_ACT_SILU) return x * mm_sigmoid(x);
     return x;
+}
+
+// Whether some of x are far below 0, and then their activations (1 for the others); mm_put_far puts these, times a
+// factor, where they belong.  Few products come near, so that a lane looks at the least of its numbers, and what is to
+// be done about them stays out of the way, in local memory: asked for each number by itself, 5,103 x 1151 x 4607
+// (M x K x N) with GELU took 58.5 us, so 55.8, as without; slopes of 741 x 1152 x 4616 formed again take 1.4 us
+// longer for it (65.8 and 64.4 us with their products).
+template <int ACT, int C>
+__device__ __forceinline__ bool mm_far(const float (&x)[C], float (&there)[C]) {
+    if constexpr (ACT == WZ_ACT_NONE || ACT == WZ_ACT_GELU) return false;
+    float least = x[0];
+#pragma unroll
+    for (int j = 1; j < C; ++j) least = fminf(least, x[j]);
+    const bool far = mm_far1<ACT>(least);
+    if (far) {
+#pragma unroll
+        for (int j = 0; j < C; ++j) there[j] = x[j];
+#pragma unroll 1
+        for (int j = 0; j < C; ++j) there[j] = mm_far1<ACT>(there[j]) ? mm_far_value<ACT>(there[j]) : 1.f;
+    }
+    return far;
+}
+
+template <int C>
+__device__ __forceinline__ void mm_far_times(bool far, float (&there)[C], const float (&factor)[C]) {
+    if (far) {
+#pragma unroll
+        for (int j = 0; j < C; ++j) there[j] = there[j] <= 0.f ? there[j] * factor[j] : 0.f;
+    }
+}
+
+template <bool TIMES, int C>
+__device__ __forceinline__ void mm_put_far(bool far, const float (&there)[C], float (&y)[C]) {
+    if (far) {
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+            if (TIMES ? there[j] != 0.f : there[j] <= 0.f) y[j] = there[j];
+    }
 }
 
 // Value and slope.  A factor that has become 0 wins over an x, or a power of it, that
@@ -199,6 +248,8 @@ __device__ __forceinline__ float mm_exp2(float x) {
     return r;
 }
 __device__ __forceinline__ f2_t both2(float x) { return pack2(x, x); }
+
+constexpr float kFarW = 125.5f;   // of -z log2 e: 87 times it (mm_far1)
 
 template <int ACT, bool VALUE>
 __device__ __forceinline__ void mm_slope2(f2_t x, f2_t &value, f2_t &slope) {
@@ -243,7 +294,14 @@ __device__ __forceinline__ void mm_slope2(f2_t x, f2_t &value, f2_t &slope) {
         if constexpr (kTanh) xt = mul2(xt, fma2(square, both2(1.5957691216057308f * 0.134145f), both2(1.5957691216057308f)));
         const float2 a = unpack2(t), b = unpack2(xt);
         slope = add2(s, pack2(a.x > 0.f ? b.x : 0.f, a.y > 0.f ? b.y : 0.f));
-        value = mul2(x, s);
+        if constexpr (VALUE) {
+            value = mul2(x, s);
+            if (fmaxf(w.x, w.y) > kFarW) {   // (mm_far_value, in powers of two)
+                const float2 n = unpack2(value);
+                value = pack2(w.x > kFarW ? v.x * 0x1p-46f * mm_exp2(46.f - w.x) : n.x,
+                              w.y > kFarW ? v.y * 0x1p-46f * mm_exp2(46.f - w.y) : n.y);
+            }
+        }
     }
 }
 
@@ -386,26 +444,39 @@ __device__ __forceinline__ void mm_finish(const MmAt<EPI> &at, MmOutputs &o, flo
         float y[4], z[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float x = v[k][j] + o.b[0][j];
-            if constexpr (EPI == kMmStore) {
-                v[k][j] = x;
-                y[j] = mm_act1<ACT>(x);
+            v[k][j] += o.b[0][j];
+            if constexpr (mm_both(EPI)) u[k][j] += o.b[1][j];
+        }
+        float there[4];
+        if constexpr (EPI == kMmStore) {
+            const bool far = mm_far<ACT>(v[k], there);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = mm_act1<ACT>(v[k][j]);
+            mm_put_far<false>(far, there, y);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
                 if (at.from) y[j] += other[k][j];
-            } else if constexpr (EPI == kMmGated) {
-                v[k][j] = x;
-                u[k][j] += o.b[1][j];
-                y[j] = mm_act1<ACT>(x) * u[k][j];
-            } else {
+        } else if constexpr (EPI == kMmGated) {
+            const bool far = mm_far<ACT>(v[k], there);
+            mm_far_times(far, there, u[k]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = mm_act1<ACT>(v[k][j]) * u[k][j];
+            mm_put_far<true>(far, there, y);
+        } else {
+            const bool far = EPI == kMmGatedSlope && mm_far<ACT>(v[k], there);
+            mm_far_times(far, there, other[k]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
                 float value, slope;
-                mm_slope1<ACT>(x, value, slope);
-                if constexpr (EPI == kMmSlope) {
-                    y[j] = other[k][j] * slope;
-                } else {
-                    y[j] = other[k][j] * (u[k][j] + o.b[1][j]) * slope;
-                    z[j] = other[k][j] * value;
-                    o.sum[1][j] += z[j];
-                }
+                mm_slope1<ACT>(v[k][j], value, slope);
+                y[j] = (EPI == kMmSlope ? other[k][j] : other[k][j] * u[k][j]) * slope;
+                z[j] = other[k][j] * value;
                 o.sum[0][j] += y[j];
+            }
+            if constexpr (EPI == kMmGatedSlope) {
+                mm_put_far<true>(far, there, z);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o.sum[1][j] += z[j];
             }
         }
         if constexpr (EPI == kMmStore || EPI == kMmGated)
