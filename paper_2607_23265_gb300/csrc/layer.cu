@@ -315,10 +315,19 @@ size_t shares_bytes(int64_t M, int N, int K, int both, int dx, int dw) {
 }
 constexpr size_t kMostSharesBytes = 48u << 20;
 
+// A weight gradient's terms are the rows, of which there may be any number, and a sum on the tensor cores comes out too
+// small by a part that grows with its terms (see kLongSteps): terms of one sign lose 1.3e-3 with a million, 4e-3, a bf16
+// rounding, with three.  So one sum takes 65,536 rows at most, as many as a forward product has terms, and loses
+// 2^-11 at the very most; the shares' sums are added in fp32.
+constexpr int64_t kMostSumSteps = 1024;
+int least_shares(int64_t M) { return (int)std::max<int64_t>(1, (steps_of(M) + kMostSumSteps - 1) / kMostSumSteps); }
+
 GradientSplit split_gradients(int64_t M, int N, int K, int both, bool dx, bool dw) {
     const int64_t sx = both * steps_of(N), sw = steps_of(M);
     const int64_t kx = (M + 255) / 256, kw = ((int64_t)N + 255) / 256;
-    GradientSplit best{1, 1, tile_of(M, kx), tile_of(N, kw)};
+    const int least_dw = dw ? least_shares(M) : 1;
+    const size_t most = std::max(kMostSharesBytes, shares_bytes(M, N, K, both, 1, least_dw));
+    GradientSplit best{1, least_dw, tile_of(M, kx), tile_of(N, kw)};
     int64_t least = INT64_MAX;
     const auto consider = [&](int tx, int tw, int a, int b) {
         if (!tx || !tw) return;
@@ -335,17 +344,19 @@ GradientSplit split_gradients(int64_t M, int N, int K, int both, bool dx, bool d
     };
     // as few row tiles as hold the rows, or one or two more
     for (int64_t i = kx; i <= kx + (dx && kx <= 8 ? 2 : 0); ++i)
-        for (int64_t j = kw; j <= kw + (dw && kw <= 8 ? 2 : 0); ++j) consider(tile_of(M, i), tile_of(N, j), 1, 1);
-    // and shares, unless the pairs have no less to do on the whole
-    const Units x = dx ? units(M, K, 1, sx, best.tile_x, 1) : Units{0, 0}, w = dw ? units(N, K, both, sw, best.tile_w, 1) : Units{0, 0};
+        for (int64_t j = kw; j <= kw + (dw && kw <= 8 ? 2 : 0); ++j) consider(tile_of(M, i), tile_of(N, j), 1, least_dw);
+    // and more shares, unless the pairs have no less to do on the whole
+    const Units x = dx ? units(M, K, 1, sx, best.tile_x, 1) : Units{0, 0},
+                w = dw ? units(N, K, both, sw, best.tile_w, least_dw) : Units{0, 0};
     if (least <= (x.n * x.cycles + w.n * w.cycles) / kPlanPairs * 9 / 8) return best;
     const int tiles[2][2] = {{best.tile_x, best.tile_w}, {tile_of(M, kx), tile_of(N, kw)}};
     constexpr int kShares[] = {1, 2, 3, 4, 6, 8};
     for (const auto &t : tiles)
         for (int a : kShares)
-            for (int b : kShares) {
+            for (int more : kShares) {
+                const int b = std::max(more, least_dw);
                 if ((a > 1 && (!dx || sx < 2 * a)) || (b > 1 && (!dw || sw < 2 * b)) || (a == 1 && b == 1)) continue;
-                if (shares_bytes(M, N, K, both, a, b) <= kMostSharesBytes) consider(t[0], t[1], a, b);
+                if (shares_bytes(M, N, K, both, a, b) <= most) consider(t[0], t[1], a, b);
             }
     return best;
 }
@@ -517,7 +528,10 @@ BackwardLayout layout_of(const wz_gated_backward_args &a) {
 
 // The most that a call of these sizes needs, whichever gradients it asks for.
 size_t most_bytes(int64_t M, int N, int K, int both) {
-    return both * (delta_bytes(M, N) + part_bytes(M, N)) + std::min(kMostSharesBytes, shares_bytes(M, N, K, both, 8, 8));
+    const int least = least_shares(M);
+    return both * (delta_bytes(M, N) + part_bytes(M, N)) +
+           std::max(std::min(kMostSharesBytes, shares_bytes(M, N, K, both, 8, std::max(8, least))),
+                    shares_bytes(M, N, K, both, 1, least));
 }
 
 }  // namespace

@@ -573,8 +573,8 @@ cudaError_t launch_mm_pair(MmEpilogue epi, MmArgs &p, int sms, cudaStream_t s, i
         }
         q.box_rows = q.tile_m / 2;   // a CTA's
         q.mt = (int)(((int64_t)q.M + q.tile_m - 1) / q.tile_m);
-        if ((int64_t)q.mt * q.nt > INT32_MAX / 32) return cudaErrorInvalidValue;
         q.split = q.sums ? q.split : 1;
+        if ((int64_t)q.mt * q.nt > INT32_MAX / 32 || (int64_t)q.mt * q.nt * q.split > INT32_MAX / 2) return cudaErrorInvalidValue;
         q.share = q.segments * q.steps / q.split;
         q.more = q.segments * q.steps % q.split;
         q.tiles = q.mt * q.nt * q.split;
