@@ -247,6 +247,8 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
     mm_outputs<kBoth>(p, q, o, out0 + 4 * own);
     // rows that are in shared memory at a time, of each share of K; a multiple of four
     const int chunk = shared_k ? (rows + 4 * q.split - 1) / (4 * q.split) * 4 : p.chunk;
+    // times that the lane's stage of the ring is used (here, while the products are under way)
+    const int uses = PAIR && warp == 0 && lane < p.stages ? (step1 - step0 + p.stages - 1 - lane) / p.stages : 0;
     // (a wait that gives up says so; the products under way are waited for all the same)
     if (!ptx::mbar_wait(&S->done, 0, p.wait_ns)) {
         give_up(p, abort_flag);
@@ -297,6 +299,10 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
         MmAt<EPI> at(p, q, (int64_t)row0 + first, o.i);
         float other[U][4];
         if (ok && o.left > 0) mm_fetch<EPI, U>(at, o.left, other, kRowsAll, (hi - first + kRowsAll - 1) / kRowsAll);
+        // (the last arrivals that free the stages came with the one on done, but nothing orders them before it; 333 x 3584 x
+        // 4608 took 0.2 us longer with this right behind that wait, 0.3 at the kernel's end)
+        if (c0 == 0 && uses > 0 && !ptx::mbar_wait(&S->empty[lane], (uint32_t)(uses - 1) & 1u, p.wait_ns)) give_up(p, abort_flag);
+        __syncwarp();
         if (shared_k) ptx::cluster_sync();
         else __syncthreads();
         if (ok && o.left > 0)
@@ -350,8 +356,8 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
             p.part[w][(size_t)((row0 / q.tile_m) * q.split + part) * q.N + out0 + i] = s;
         }
     }
-    // a pair's arrivals have all come: the last is the one that says that its products are done,
-    // unless a wait ran out
+    // a pair's arrivals have all come, to the CTA that has the barrier: full is waited for by the products, empty and done by
+    // the epilogue (a wait that ran out has been followed by the two milliseconds)
     if (PAIR) {
         cluster_arrive_relaxed();
         cluster_wait();

@@ -256,6 +256,15 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                     }
                 }
             }
+            // the products' last arrivals here: all stages are free again
+            for (int i = 0; ok && i < kStages; ++i) {
+                ok = ptx::mbar_wait(&S->empty[stage], phase, p.wait_ns);
+                if (!ok) give_up(p, abort_flag);
+                if (++stage == kStages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+            }
         }
     } else if (warp == 1 && rank == 0) {
         if (ptx::elect_one()) {
@@ -275,6 +284,7 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                 const int b = it & 1;
                 if (!ptx::mbar_wait(&S->tempty[b], ((uint32_t)(it >> 1) & 1u) ^ 1u, p.wait_ns)) {
                     give_up(p, abort_flag);
+                    ok = false;
                     break;
                 }
                 ptx::tc_fence_after();
@@ -306,6 +316,12 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
             }
             ptx::mma_commit_pair(&S->drain);
             ptx::mbar_wait(&S->drain, 0, kMmTimeoutNs);
+            // both epilogues' last arrivals here: the sums of all tiles are read
+            for (int b = 0; ok && b < 2; ++b) {
+                const int uses = (it + 1 - b) >> 1;
+                ok = uses == 0 || ptx::mbar_wait(&S->tempty[b], (uint32_t)(uses - 1) & 1u, p.wait_ns);
+                if (!ok) give_up(p, abort_flag);
+            }
         }
     } else if (warp == 1 && rank == 1 && ptx::elect_one()) {
         ptx::mbar_wait(&S->drain, 0, 2 * kMmTimeoutNs);   // the even CTA's last arrivals here
@@ -489,7 +505,9 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
         }
     }
     __syncthreads();
-    // no commit or arrival is under way to either CTA (the arrival waits for no store)
+    // No commit or arrival is under way to either CTA: each barrier's last phase has been waited for in the CTA that has
+    // it, full and tfull by the products and the epilogue, empty, tempty and drain above (a wait that ran out instead
+    // has been followed by the two milliseconds).  So the barrier has nothing to order, and waits for no store.
     asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
     if (warp == 1) {
         ptx::tc_fence_after();
