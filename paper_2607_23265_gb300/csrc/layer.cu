@@ -26,8 +26,9 @@ struct DeltaArgs {
     __nv_bfloat16 *d[2];
     float *part[2];                     // [ceil(M / 64)][N]; null: not wanted
     int64_t dy_stride, pre_stride[2], d_stride;
-    int64_t M;
+    int64_t M, room_rows, room_part;    // rows at d, floats at each part: see MmProblem
     int N, act;
+    int *status;
 };
 
 }  // namespace
@@ -67,7 +68,7 @@ __global__ void __launch_bounds__(32 * kDeltaWarps) mm_delta_kernel(const __grid
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
                     const int64_t m = m0 + r0 + k * kDeltaWarps;
-                    if (!wide && m >= p.M) break;
+                    if ((!wide && m >= p.M) || !wz_in_range(p.status, m < p.room_rows)) break;
                     f2_t dy[4], g[4], u[4];
                     const auto take = [&](int a, f2_t (&x)[4]) {
                         if (wide) {
@@ -132,7 +133,8 @@ __global__ void __launch_bounds__(32 * kDeltaWarps) mm_delta_kernel(const __grid
             float s = 0.f;
 #pragma unroll
             for (int w = 0; w < kDeltaWarps; ++w) s += sums[w][threadIdx.x];
-            p.part[i][(size_t)blockIdx.x * p.N + c] = s;
+            const size_t at = (size_t)blockIdx.x * p.N + c;
+            if (wz_in_range(p.status, at < (size_t)p.room_part)) p.part[i][at] = s;
         }
     }
 }
@@ -159,11 +161,12 @@ struct JoinArgs {
     struct {
         const float *sums;
         __nv_bfloat16 *out;
-        int64_t out_stride, M;
+        int64_t out_stride, M, room_rows;
         int cols, split;
         unsigned first;        // its first block
     } join[kMmProblems];
     int joins;
+    int *status;
 };
 
 }  // namespace
@@ -189,8 +192,9 @@ __global__ void __launch_bounds__(kSumThreads) mm_join_kernel(const __grid_const
     const int64_t m0 = (int64_t)(block / across) * (4 * kJoinRows) + (int)(threadIdx.x >> 7);
     if (left <= 0) return;
     const int64_t plane = j.M * j.cols;
+    if (!wz_in_range(p.status, m0 < j.room_rows)) return;
     const bool wide = left >= 4 && j.cols % 4 == 0;
-    if (wide && m0 + 4 * (kJoinRows - 1) < j.M) {
+    if (wide && m0 + 4 * (kJoinRows - 1) < j.M && wz_in_range(p.status, m0 + 4 * (kJoinRows - 1) < j.room_rows)) {
         float x[kJoinRows][4] = {};
         const float *from = j.sums + m0 * j.cols + n;
 #pragma unroll 2
@@ -207,7 +211,7 @@ __global__ void __launch_bounds__(kSumThreads) mm_join_kernel(const __grid_const
     }
     for (int r = 0; r < kJoinRows; ++r) {
         const int64_t m = m0 + 4 * r;
-        if (m >= j.M) break;
+        if (m >= j.M || !wz_in_range(p.status, m < j.room_rows)) break;
         const float *from = j.sums + m * j.cols + n;
         float x[4] = {};
         for (int k = 0; k < j.split; ++k, from += plane)
@@ -257,9 +261,22 @@ MmArgs mm_args(int act, int *status) {
 
 int64_t steps_of(int64_t k) { return (k + 63) / 64; }
 
-JoinArgs join_args(const float *part0, const float *part1, float *db0, float *db1, int64_t rows, int N) {
+// What there is room for, as the checked build's kernels are told (its test takes some away).
+#ifdef WZ_CHECKED
+int check_room = 0;   // bits: 1 the last row of outputs, 2 sums over rows but for the first, 4 shares' sums but for the first
+int64_t room_rows(int64_t rows) { return rows - (check_room & 1); }
+int64_t room_part(size_t bytes, int N) { return check_room & 2 ? N : (int64_t)(bytes / 4); }
+int64_t room_sums(size_t bytes, int64_t plane) { return check_room & 4 ? plane : (int64_t)(bytes / 4); }
+#else
+int64_t room_rows(int64_t rows) { return rows; }
+int64_t room_part(size_t bytes, int) { return (int64_t)(bytes / 4); }
+int64_t room_sums(size_t bytes, int64_t) { return (int64_t)(bytes / 4); }
+#endif
+
+JoinArgs join_args(const float *part0, const float *part1, float *db0, float *db1, int64_t rows, int N, int *status) {
     JoinArgs j;
     memset(&j, 0, sizeof(j));
+    j.status = status;
     MmSums &p = j.sums;
     p.part[0] = part0, p.part[1] = part1, p.db[0] = db0, p.db[1] = db1;
     p.part_rows = rows, p.N = N;
@@ -363,15 +380,16 @@ GradientSplit split_gradients(int64_t M, int N, int K, int both, bool dx, bool d
 
 // The products of both gradients in one launch, with the bias gradients of `join` where they are few enough; what
 // they leave to be joined goes into `join`.
-cudaError_t launch_gradients(const Gradients &g, const GradientSplit &split, bool beside, char *shares, JoinArgs &join,
-                             int *status, int sms, cudaStream_t s) {
+// (shares_end: where the workspace ends)
+cudaError_t launch_gradients(const Gradients &g, const GradientSplit &split, bool beside, char *shares,
+                             const char *shares_end, JoinArgs &join, int *status, int sms, cudaStream_t s) {
     MmArgs p = mm_args(WZ_ACT_NONE, status);
     MmProblem in, weight[2];
     memset(&in, 0, sizeof(in));
     memset(weight, 0, sizeof(weight));
     in.M = (int)g.M, in.N = g.K, in.segments = g.both, in.steps = (int)steps_of(g.N);
     in.b_mn = 1;
-    in.out = half(g.dx), in.out_stride = g.dx_stride;
+    in.out = half(g.dx), in.out_stride = g.dx_stride, in.room_rows = room_rows(g.M);
     for (int i = 0; i < g.both; ++i) {
         const MmOperand d{g.d[i], g.M, g.N, g.d_stride};
         in.from_a[i] = d;
@@ -379,7 +397,7 @@ cudaError_t launch_gradients(const Gradients &g, const GradientSplit &split, boo
         MmProblem &q = weight[i];
         q.M = g.N, q.N = g.K, q.segments = 1, q.steps = (int)steps_of(g.M);
         q.a_mn = q.b_mn = 1;
-        q.out = half(g.dw[i]), q.out_stride = g.dw_stride[i];
+        q.out = half(g.dw[i]), q.out_stride = g.dw_stride[i], q.room_rows = room_rows(g.N);
         q.from_a[0] = d;
         q.from_b[0] = MmOperand{g.x, g.M, g.K, g.x_stride};
     }
@@ -391,13 +409,17 @@ cudaError_t launch_gradients(const Gradients &g, const GradientSplit &split, boo
     }
     in.tile_m = split.tile_x;
     weight[0].tile_m = weight[1].tile_m = split.tile_w;
+    bool none_left = false;
     const auto add = [&](MmProblem &q, int shared) {
         q.split = shared;
         if (shared > 1) {
             q.sums = reinterpret_cast<float *>(shares);
+            q.room_sums = room_sums((size_t)(shares_end - shares), (int64_t)q.M * q.N);
             shares += pad256((size_t)shared * (size_t)q.M * (size_t)q.N * 4);
+            none_left = none_left || shares > shares_end;
             auto &j = join.join[join.joins++];
             j.sums = q.sums, j.out = q.out, j.out_stride = q.out_stride, j.M = q.M, j.cols = q.N, j.split = shared;
+            j.room_rows = q.room_rows;
         }
         p.prob[p.problems++] = q;
     };
@@ -409,6 +431,7 @@ cudaError_t launch_gradients(const Gradients &g, const GradientSplit &split, boo
         for (int i = 0; i < g.both; ++i) add(weight[i], split.dw);
     if (g.dx && weights_first) add(in, split.dx);
     if (!p.problems) return cudaSuccess;
+    if (none_left) return cudaErrorInvalidValue;
     if (beside || join.sums.blocks <= kSumBlocksEach * sms) {
         p.sums = join.sums;
         join.sums.blocks = 0;
@@ -432,6 +455,7 @@ void forward_product(MmArgs &p, int64_t M, int N, int K, const void *x, int64_t 
                      int64_t stride0, const void *w1, int64_t stride1) {
     MmProblem &q = p.prob[0];
     q.M = (int)M, q.N = N, q.segments = 1, q.steps = (int)steps_of(K);
+    q.room_rows = room_rows(M);
     q.from_a[0] = MmOperand{x, M, K, x_stride};
     q.from_b[0] = MmOperand{w0, N, K, stride0};
     q.from_b[1] = MmOperand{w1, N, K, stride1};
@@ -550,7 +574,7 @@ size_t gated_backward_need(const wz_gated_backward_args &a) { return a.M > 0 ? l
 cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, cudaStream_t s) {
     if (a.M == 0) {
         MM_TRY(zero_rows(a.dw, a.dw_stride, a.N, a.K, s));
-        JoinArgs join = join_args(nullptr, nullptr, a.db, nullptr, 0, a.N);
+        JoinArgs join = join_args(nullptr, nullptr, a.db, nullptr, 0, a.N, a.device_status);
         return launch_join(join, s);
     }
     const int sms = sm_count();
@@ -566,7 +590,7 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
         p.prob[0].out = d, p.prob[0].out_stride = d_stride;
         p.bias[0] = a.bias;
         p.dy = half(a.dy), p.dy_stride = a.dy_stride;
-        p.part[0] = part;
+        p.part[0] = part, p.room_part = room_part(part_bytes(a.M, a.N), a.N);
         MM_TRY(launch_mm(kMmSlope, p, sms, s, &part_rows));
     } else if (a.act != WZ_ACT_NONE || part) {
         DeltaArgs p;
@@ -575,7 +599,8 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
         p.pre[0] = half(a.pre), p.pre_stride[0] = a.pre_stride;
         p.d[0] = d, p.d_stride = d_stride;
         p.part[0] = part;
-        p.M = a.M, p.N = a.N, p.act = a.act;
+        p.M = a.M, p.N = a.N, p.act = a.act, p.status = a.device_status;
+        p.room_rows = room_rows(a.M), p.room_part = room_part(part_bytes(a.M, a.N), a.N);
         MM_TRY(launch_delta(a.act == WZ_ACT_NONE ? kDeltaSums : kDeltaSlope, p, s));
     }
     Gradients g;
@@ -588,12 +613,12 @@ cudaError_t launch_linear_backward(const wz_linear_backward_args &a, char *ws, c
     g.dx = a.dx, g.dx_stride = a.dx_stride;
     g.dw[0] = a.dw, g.dw_stride[0] = a.dw_stride;
     g.M = a.M, g.N = a.N, g.K = a.K;
-    JoinArgs join = join_args(part, nullptr, a.db, nullptr, part_rows, a.N);
+    JoinArgs join = join_args(part, nullptr, a.db, nullptr, part_rows, a.N, a.device_status);
     if (at.of_dy) {
         join.sums.part_rows = 0;
         join.sums.dy = half(a.dy), join.sums.dy_stride = a.dy_stride, join.sums.dy_rows = a.M;
     }
-    MM_TRY(launch_gradients(g, at.split, at.beside, ws + at.shares, join, a.device_status, sms, s));
+    MM_TRY(launch_gradients(g, at.split, at.beside, ws + at.shares, ws + at.total, join, a.device_status, sms, s));
     return launch_join(join, s);
 }
 
@@ -602,7 +627,7 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
     if (a.M == 0) {
         MM_TRY(zero_rows(a.dw_gate, a.dw_gate_stride, a.N, a.K, s));
         MM_TRY(zero_rows(a.dw_up, a.dw_up_stride, a.N, a.K, s));
-        JoinArgs join = join_args(nullptr, nullptr, db[0], db[1], 0, a.N);
+        JoinArgs join = join_args(nullptr, nullptr, db[0], db[1], 0, a.N, a.device_status);
         return launch_join(join, s);
     }
     const int sms = sm_count();
@@ -624,7 +649,8 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
         p.pre[1] = half(a.up), p.pre_stride[1] = a.up_stride;
         p.d[0] = d[0], p.d[1] = d[1], p.d_stride = d_stride;
         p.part[0] = part[0], p.part[1] = part[1];
-        p.M = a.M, p.N = a.N, p.act = a.act;
+        p.M = a.M, p.N = a.N, p.act = a.act, p.status = a.device_status;
+        p.room_rows = room_rows(a.M), p.room_part = room_part(part_bytes(a.M, a.N), a.N);
         MM_TRY(launch_delta(kDeltaGated, p, s));
     } else {
         MmArgs p = mm_args(a.act, a.device_status);
@@ -633,7 +659,7 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
         p.out2 = d[1], p.out2_stride = d_stride;
         p.bias[0] = a.b_gate, p.bias[1] = a.b_up;
         p.dy = half(a.dout), p.dy_stride = a.dout_stride;
-        p.part[0] = part[0], p.part[1] = part[1];
+        p.part[0] = part[0], p.part[1] = part[1], p.room_part = room_part(part_bytes(a.M, a.N), a.N);
         MM_TRY(launch_mm(kMmGatedSlope, p, sms, s, &part_rows));
     }
     Gradients g;
@@ -646,8 +672,8 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
     g.dw[0] = a.dw_gate, g.dw[1] = a.dw_up;
     g.dw_stride[0] = a.dw_gate_stride, g.dw_stride[1] = a.dw_up_stride;
     g.M = a.M, g.N = a.N, g.K = a.K;
-    JoinArgs join = join_args(part[0], part[1], db[0], db[1], part_rows, a.N);
-    MM_TRY(launch_gradients(g, at.split, at.beside, ws + at.shares, join, a.device_status, sms, s));
+    JoinArgs join = join_args(part[0], part[1], db[0], db[1], part_rows, a.N, a.device_status);
+    MM_TRY(launch_gradients(g, at.split, at.beside, ws + at.shares, ws + at.total, join, a.device_status, sms, s));
     return launch_join(join, s);
 }
 
@@ -658,4 +684,7 @@ cudaError_t launch_gated_backward(const wz_gated_backward_args &a, char *ws, cud
 extern "C" __attribute__((visibility("default"))) void wz_check_mm_wait(uint64_t ns) {
     wz::check_mm_wait_ns = ns ? ns : wz::kMmTimeoutNs;
 }
+
+// Test hook: what the kernels take for out of range although it is not (see check_room).
+extern "C" __attribute__((visibility("default"))) void wz_check_mm_room(int what) { wz::check_room = what; }
 #endif

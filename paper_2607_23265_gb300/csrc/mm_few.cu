@@ -295,17 +295,19 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
         // this CTA's rows
         const int lo = shared_k ? part * chunk : c0, hi = lo + chunk < rows ? lo + chunk : rows;
         const int first = lo + warp * kRowsWarp + sub;   // the lane's first row
+        const bool mine = ok && o.left > 0 &&
+                          wz_in_range(p.status, o.i >= 0 && row0 >= 0 && lo >= 0 && (int64_t)row0 + hi <= q.room_rows);
         constexpr int U = 2;                              // rows in flight
         MmAt<EPI> at(p, q, (int64_t)row0 + first, o.i);
         float other[U][4];
-        if (ok && o.left > 0) mm_fetch<EPI, U>(at, o.left, other, kRowsAll, (hi - first + kRowsAll - 1) / kRowsAll);
+        if (mine) mm_fetch<EPI, U>(at, o.left, other, kRowsAll, (hi - first + kRowsAll - 1) / kRowsAll);
         // (the last arrivals that free the stages came with the one on done, but nothing orders them before it; 333 x 3584 x
         // 4608 took 0.2 us longer with this right behind that wait, 0.3 at the kernel's end)
         if (c0 == 0 && uses > 0 && !ptx::mbar_wait(&S->empty[lane], (uint32_t)(uses - 1) & 1u, p.wait_ns)) give_up(p, abort_flag);
         __syncwarp();
         if (shared_k) ptx::cluster_sync();
         else __syncthreads();
-        if (ok && o.left > 0)
+        if (mine)
             mm_with_act(p.act, [&](auto act) {
                 constexpr int ACT = decltype(act)::value;
                 for (int c = first; c < hi; c += U * kRowsAll) {
@@ -353,7 +355,8 @@ __global__ void __launch_bounds__(kThreads, 2) mm_few_kernel(const __grid_consta
             float s = 0.f;
 #pragma unroll
             for (int k = 0; k < kEach; ++k) s += sums[(w * kEach + k) * kOwn + i];
-            p.part[w][(size_t)((row0 / q.tile_m) * q.split + part) * q.N + out0 + i] = s;
+            const size_t at = (size_t)((row0 / q.tile_m) * q.split + part) * q.N + out0 + i;
+            if (wz_in_range(p.status, at < (size_t)p.room_part)) p.part[w][at] = s;
         }
     }
     // a pair's arrivals have all come, to the CTA that has the barrier: full is waited for by the products, empty and done by

@@ -349,7 +349,8 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
             const int b = it & 1;
             const int rows = q.M - t.row0 < t.rows ? q.M - t.row0 : t.rows;
             const int i = (t.n * 2 + (int)rank) * kOwn + 32 * (kBoth ? quadrant & 1 : quadrant) + lane;
-            const int there = i < q.N ? rows : 0;               // of the lane's rows
+            const bool inside = i < q.N && wz_in_range(p.status, t.row0 >= 0 && i >= 0 && t.row0 + (int64_t)rows <= q.room_rows);
+            const int there = inside ? rows : 0;                // of the lane's rows
             const float bias = p.bias[kind] && i < q.N ? __ldg(p.bias[kind] + i) : 0.f;
             // from this warp's first row on, which it is in a gated product when it has finished the exchange
             const int first = side * (kStride / kSides), mine = first + kUnitRows * kind;
@@ -393,8 +394,11 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
                         sums(c, x);
                         read(c + kStride >= rows);
                         if (EPI == kMmStore && q.sums) {   // a share of K: the sums as they are
-                            float *to = q.sums + ((int64_t)t.part * q.M + t.row0 + c) * q.N + i;
-                            const int count = there - c;
+                            const int64_t first_sum = ((int64_t)t.part * q.M + t.row0 + c) * q.N + i;
+                            float *to = q.sums + first_sum;
+                            int count = there - c;
+                            if (count > 0 && !wz_in_range(p.status, first_sum + (int64_t)(min(count, kUnitRows) - 1) * q.N < q.room_sums))
+                                count = 0;
 #pragma unroll
                             for (int j = 0; j < kUnitRows; ++j)
                                 if (j < count) to[(int64_t)j * q.N] = x[j];
@@ -491,8 +495,10 @@ __global__ void __launch_bounds__(kThreads, 1) mm_pair_kernel(const __grid_const
             if constexpr (EPI == kMmSlope || EPI == kMmGatedSlope) {
                 // each warp's sums over its rows are a row of their own
                 const size_t at = (size_t)((t.row0 / q.tile_m) * kSides * (kBoth ? 2 : 1) + (kBoth ? 2 * side + kind : side)) * q.N + i;
-                if (i < q.N && p.part[0]) p.part[0][at] = sum0;
-                if (kBoth && i < q.N && p.part[1]) p.part[1][at] = sum1;
+                if (i < q.N && (p.part[0] || p.part[1]) && wz_in_range(p.status, at < (size_t)p.room_part)) {
+                    if (p.part[0]) p.part[0][at] = sum0;
+                    if (kBoth && p.part[1]) p.part[1][at] = sum1;
+                }
             }
             ++it;
         }

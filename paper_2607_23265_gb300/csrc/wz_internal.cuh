@@ -115,11 +115,11 @@ __host__ __device__ __forceinline__ int qhl_row(int q_row0, int v) { return 2 * 
 // ---- device helpers -------------------------------------------------------
 
 // Index checks of the bounds-checked build (WZ_CHECKED): a write whose index
-// is out of range records WZ_STATUS_BOUNDS in the status word and is skipped.
+// is out of range records WZ_STATUS_BOUNDS in the status word (if there is one) and is skipped.
 // In the normal build the check is a constant true and costs nothing.
 __device__ __forceinline__ bool wz_in_range(const int *status, bool ok) {
 #ifdef WZ_CHECKED
-    if (!ok) atomicOr(const_cast<int *>(status), WZ_STATUS_BOUNDS);
+    if (!ok && status) atomicOr(const_cast<int *>(status), WZ_STATUS_BOUNDS);
     return ok;
 #else
     (void)status;

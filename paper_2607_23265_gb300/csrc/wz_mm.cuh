@@ -73,6 +73,7 @@ struct MmProblem {
     __nv_bfloat16 *out;    // [M] rows of N
     int64_t out_stride;
     MmOperand from_a[2], from_b[2];   // host: the operands
+    int64_t room_rows, room_sums;     // rows at out and floats at sums that there is room for (the checked build's kernels look)
     // set by the launch
     int a[2], b[2];        // their tensor maps
     float *sums;           // pairs, K shared: [split][M][N] sums of the shares
@@ -108,6 +109,7 @@ struct MmArgs {
     __nv_bfloat16 *pre[2];                  // kept products; null: none
     __nv_bfloat16 *out2;                    // kMmGatedSlope
     float *part[2];                         // [some rows][N] sums over rows; null: none
+    int64_t room_part;                      // floats at each of them
     int64_t residual_stride, dy_stride, pre_stride[2], out2_stride;
     int maps;                               // tensor maps in use
     int second;                             // pairs: columns from the even steps' sums to the odd ones'; 0: one
