@@ -543,9 +543,9 @@ WZ_API int wz_attend(const wz_attend_args *a);
  * feed-forward block), and what trains those products and the projector P.
  * Rows x [M][K], weights [N][K] (torch.nn.Linear, out x in), results and weight
  * gradients are bf16; biases and their gradients f32.  Products run on the
- * tensor cores (tcgen05) with fp32 accumulation (which cuts off: terms of one sign may
- * lose 2^-11 of their sum over 65,536 of them, about 1e-4 on average; sums over more rows
- * are made of such parts, added in fp32); bias, activation and residual are
+ * tensor cores (tcgen05) with fp32 accumulation (which cuts off: 65,536 terms of one sign
+ * lose about 4e-4 of their sum, others less; sums over more rows are made of such parts,
+ * added in fp32); bias, activation and residual are
  * applied to the fp32 sums, which are rounded once, when they are stored.
  *   M >= 0, N and K from 1 to 65536, odd ones among them; a stride is the
  * elements from one row to the next, a multiple of 8 that is no less than the row;

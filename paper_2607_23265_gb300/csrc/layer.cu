@@ -333,9 +333,9 @@ size_t shares_bytes(int64_t M, int N, int K, int both, int dx, int dw) {
 constexpr size_t kMostSharesBytes = 48u << 20;
 
 // A weight gradient's terms are the rows, of which there may be any number, and a sum on the tensor cores comes out too
-// small by a part that grows with its terms (see kLongSteps): terms of one sign lose 1.3e-3 with a million, 4e-3, a bf16
-// rounding, with three.  So one sum takes 65,536 rows at most, as many as a forward product has terms, and loses
-// 2^-11 at the very most; the shares' sums are added in fp32.
+// small by a part that grows with its terms (see kLongSteps): 3,000,000 rows of one sign, in eight shares, lost
+// 3.1e-3, about a bf16 rounding (now 2e-4 to 4e-4).  So one sum takes 65,536 rows at most, as many as a forward product
+// has terms, and loses about 4e-4 of terms of one sign; the shares' sums are added in fp32.
 constexpr int64_t kMostSumSteps = 1024;
 int least_shares(int64_t M) { return (int)std::max<int64_t>(1, (steps_of(M) + kMostSumSteps - 1) / kMostSumSteps); }
 
