@@ -551,7 +551,7 @@ WZ_API int wz_attend(const wz_attend_args *a);
  * elements from one row to the next, a multiple of 8 that is no less than the row;
  * what lies between a row's end and the next row is neither read nor written.
  * Every bf16 array 16-byte aligned, f32 arrays 4-byte.  Results do not depend
- * on the order in which blocks run: equal calls give equal bits.
+ * on the order in which blocks run: equal calls give equal bits on the same device.
  *   Outputs must not overlap inputs or one another, but for `out` of wz_linear, which
  * may be `residual` itself (same address and stride).
  * Errors of all four: WZ_ERR_INVALID_ARG (null, misaligned, bad size or enum),

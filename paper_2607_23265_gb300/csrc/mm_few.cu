@@ -446,8 +446,8 @@ bool plan_mm_few(MmEpilogue epi, const MmArgs &p, int sms, MmFewPlan *plan) {
     }
 #endif
     // What a call takes, in cycles, fitted to 9 weights (512 x 512 to 14336 x 3584) of 1 to 2,048 rows, plain
-    // and gated, with up to 60 plans each: the plan that it chooses is 2 % slower than the fastest on
-    // average, 14 % at most.  A step of K is bound by what comes into an SM or by its issue, a pair's wide
+    // and gated, with up to 60 plans each: the plan that it chooses is 1.9 % slower than the fastest on
+    // average, 19 % at most (48 x 3584 x 4608).  A step of K is bound by what comes into an SM or by its issue, a pair's wide
     // ones by the products; all of them together by HBM (the weights once, up to 3,700 bytes a cycle
     // from two CTAs an SM, 3,200 from 84); clusters that find no place share SMs.  Examples, us, this
     // file's best / mm_pair.cu's: 80 x 14336 x 3584 (rows x K x outputs) 21 / 49, 512 x 14336 x 3584 41 / 66,

@@ -16,8 +16,8 @@
 // one launch, whose rounds of tiles even out together.
 //   What bounds it: a step of 64 along K is max(2 rows, 256 + rows) cycles, products against
 // the 64 bytes a cycle that come into an SM, so tiles of 256 rows are bound by the tensor
-// cores: 18,662 x 3584 x 3584 253 us (1,892 TFLOP/s), 18,699 x 14336 x 3584 1,155 to 1,196 under
-// the power limit, the pipe 96 % busy.  An epilogue takes 4,900 cycles, 64-byte stores at
+// cores: 18,662 x 3584 x 3584 253 us (1,892 TFLOP/s), 18,699 x 14336 x 3584 1,138 to 1,196 under
+// the power limit; the pipe is busy in 96 % of the active cycles of 6,151 x 3584 x 2 x 14336.  An epilogue takes 4,900 cycles, 64-byte stores at
 // 4.8 cycles, which fewer than ten steps do not hide; staging them in shared memory, by rows or for
 // TMA stores, was not faster, and TMA writes a whole word where a row ends inside one.
 // Warps: 0 copies, 1 products (the even CTA's), 2-17 epilogue, four a TMEM lane quadrant.  A

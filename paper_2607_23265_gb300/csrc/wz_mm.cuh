@@ -26,7 +26,8 @@ constexpr uint64_t kMmTimeoutNs = 2000000000ull;
 // slopes keep two in mm_pair.cu, in tiles of half the rows, when they have more steps than this or it costs next to
 // nothing, and have a share of K for each as many steps in mm_few.cu.
 constexpr int kLongSteps = 64;
-// Pairs of SMs that tiles are planned for: a constant, so that workspace sizes and results do not depend on the device.
+// Pairs of SMs that row tiles and both gradients are planned for: a constant, so that workspace sizes and the cut of
+// gradients do not depend on the device.  (Which kernel a product takes does: plan_mm_few asks for its SMs and places.)
 constexpr int kPlanPairs = 76;
 
 struct MmMaps {
